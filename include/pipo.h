@@ -239,6 +239,86 @@ int pipo_opd_targets_bf16(int32_t T, int32_t V, const uint16_t *d_logits_s, cons
                           const int32_t *d_teacher_rows, const int32_t *d_labels, float *d_kl, float *d_alpha,
                           double *d_sums, void *stream);
 
+/* ---- OPD losses with their gradients (App. C; no context needed) -----------
+ * Three operators on logit rows, fp32 or (_bf16) bf16 bit patterns: T rows of V
+ * logits, row t at d_logits + t * ld elements (V <= ld <= 2^31; rows need no alignment
+ * beyond their element's), V from 1 to 524288.  x = z / temperature (finite,
+ * > 0), p = softmax(x).  All sums are fp32 or wider, the arithmetic on single
+ * entries is fp64.  T = 0 is allowed (the arrays may then be NULL).  Logits may
+ * be -inf or the type's lowest value (masked tokens); a row without any token
+ * of positive probability, or with a NaN or +inf, gives NaN results (ids
+ * stay in range).  Outputs must not overlap inputs or each other, except that
+ * a gradient may be written over the logits themselves (same address and ld).
+ * d_work: device scratch of at least pipo_opd_work_bytes(T, V, k) bytes (k = 1
+ * for pipo_opd_policy), 16-byte aligned, whose contents matter neither before
+ * nor after; calls that may overlap need one each.  With NULL every row is
+ * worked on by one workgroup, which is slower for few long rows.
+ * Errors: PIPO_EINVAL (NULL pointers with T > 0, sizes, kind, beta,
+ * temperature, clip bounds or coefficient outside their ranges, misaligned
+ * rows, d_logits and d_grad that overlap in part, work_bytes too small for a
+ * non-NULL d_work), PIPO_EHIP (launch failure).
+ *
+ * pipo_opd_top_logits: the teacher's side.  Per row the k largest logits (k
+ * from 1 to 256, at most V) in descending order, equal ones by ascending id
+ * (-0 equals 0): d_ids [T][k], d_logp [T][k] = log p of each, d_tail [T] (may
+ * be NULL) = the log of the probability outside the k (-inf where it is 0).
+ *
+ * pipo_opd_distill: the divergence of position t's row from the teacher's list
+ * in row r = d_teacher_rows[t] (NULL: r = t) of d_ids, d_logp ([Tt][k], k from
+ * 1 to 256; an id < 0 is an empty slot) and d_tail.  Over the listed entries,
+ * and with d_tail non-NULL the tokens outside as one more entry, with teacher
+ * probability Q (Q = exp(d_logp), exp(d_tail)) and student probability P:
+ *   PIPO_OPD_FORWARD  sum Q (log Q - log P)
+ *   PIPO_OPD_REVERSE  sum P (log P - log Q)
+ *   PIPO_OPD_JSD      sum beta Q (log Q - log M) + (1 - beta) P (log P - log M),
+ *                     M = beta Q + (1 - beta) P, 0 < beta < 1 (beta is read for this kind only)
+ * (0 log 0 = 0).  Positions with a label < 0 are not scored (loss and gradient
+ * 0; the label's value is not used otherwise; NULL: every position is scored).
+ * A scored position whose teacher row is outside [0, Tt), or whose list has an
+ * id >= V or the same id twice, gets NaN.
+ *
+ * pipo_opd_policy: the clipped policy loss of label y = d_labels[t] with
+ * advantage A = d_adv[t] and, with logp = log p(y), ratio rho = exp(logp -
+ * d_old_logp[t]) (NULL: rho = 1, the on-policy gradient):
+ *   loss = -min(A rho, A clip(rho, 1 - clip_low, 1 + clip_high)) + kl_coef * kl
+ *   kl   = exp(u) - u - 1,  u = d_ref_logp[t] - logp
+ * with 0 <= clip_low <= 1, clip_high >= 0.  Without d_ref_logp kl_coef must be
+ * 0 and d_kl NULL.  d_logp and d_kl ([T]) may be NULL.  Positions with y < 0
+ * are not scored (all outputs 0), y >= V gets NaN.
+ *
+ * Both losses: d_loss [T]; with d_grad non-NULL its row t (stride ld_grad >= V,
+ * the logits' type) = d_scale[t] (NULL: 1) times the gradient of loss t with
+ * respect to the logits of row t (teacher rows, old and reference
+ * log-probabilities and advantages are constants). */
+#define PIPO_OPD_FORWARD  0
+#define PIPO_OPD_REVERSE  1
+#define PIPO_OPD_JSD      2
+int64_t pipo_opd_work_bytes(int32_t T, int32_t V, int32_t k);
+int pipo_opd_top_logits(int32_t T, int32_t V, const float *d_logits, int64_t ld, double temperature, int32_t k,
+                        int32_t *d_ids, float *d_logp, float *d_tail, void *d_work, int64_t work_bytes, void *stream);
+int pipo_opd_top_logits_bf16(int32_t T, int32_t V, const uint16_t *d_logits, int64_t ld, double temperature, int32_t k,
+                             int32_t *d_ids, float *d_logp, float *d_tail, void *d_work, int64_t work_bytes,
+                             void *stream);
+int pipo_opd_distill(int32_t T, int32_t V, const float *d_logits, int64_t ld, int32_t Tt, int32_t k,
+                     const int32_t *d_ids, const float *d_logp, const float *d_tail, const int32_t *d_teacher_rows,
+                     const int32_t *d_labels, int32_t kind, double beta, double temperature, const float *d_scale,
+                     float *d_loss, float *d_grad, int64_t ld_grad, void *d_work, int64_t work_bytes, void *stream);
+int pipo_opd_distill_bf16(int32_t T, int32_t V, const uint16_t *d_logits, int64_t ld, int32_t Tt, int32_t k,
+                          const int32_t *d_ids, const float *d_logp, const float *d_tail,
+                          const int32_t *d_teacher_rows, const int32_t *d_labels, int32_t kind, double beta,
+                          double temperature, const float *d_scale, float *d_loss, uint16_t *d_grad, int64_t ld_grad,
+                          void *d_work, int64_t work_bytes, void *stream);
+int pipo_opd_policy(int32_t T, int32_t V, const float *d_logits, int64_t ld, const int32_t *d_labels,
+                    const float *d_adv, const float *d_old_logp, const float *d_ref_logp, double clip_low,
+                    double clip_high, double kl_coef, double temperature, const float *d_scale, float *d_loss,
+                    float *d_logp, float *d_kl, float *d_grad, int64_t ld_grad, void *d_work, int64_t work_bytes,
+                    void *stream);
+int pipo_opd_policy_bf16(int32_t T, int32_t V, const uint16_t *d_logits, int64_t ld, const int32_t *d_labels,
+                         const float *d_adv, const float *d_old_logp, const float *d_ref_logp, double clip_low,
+                         double clip_high, double kl_coef, double temperature, const float *d_scale, float *d_loss,
+                         float *d_logp, float *d_kl, uint16_t *d_grad, int64_t ld_grad, void *d_work,
+                         int64_t work_bytes, void *stream);
+
 /* Release a context made by pipo_init_weights and all its device memory.
  * NULL is a no-op (returns 0). */
 int pipo_free(pipo_ctx *ctx);

@@ -329,6 +329,122 @@ def opd_loss_sums(d, labels):
     return out
 
 
+def _log_softmax_row(z, temperature):
+    x = np.asarray(z, F64) / temperature
+    with np.errstate(all="ignore"):
+        m = np.max(x)
+        return (x - m) - np.log(np.sum(np.exp(x - m)))
+
+
+def opd_top_logits(logits, k, temperature=1.0):
+    """Per row the k largest logits, descending and by ascending id among equal
+    ones: (ids, their log-probabilities, the log of the mass outside)."""
+    T = len(logits)
+    ids = np.zeros((T, k), np.int64)
+    logp, tail = np.zeros((T, k)), np.zeros(T)
+    for t in range(T):
+        z = np.asarray(logits[t], F64)
+        ids[t] = np.argsort(-z, kind="stable")[:k]
+        lp = _log_softmax_row(z, temperature)
+        logp[t] = lp[ids[t]]
+        with np.errstate(all="ignore"):
+            tail[t] = np.log(np.sum(np.exp(np.delete(lp, ids[t]))))
+    return ids, logp, tail
+
+
+def _divergence_terms(kind, beta, lp, lq):
+    """One entry's term f of a divergence of probabilities P = e^lp and Q =
+    e^lq, and a = P df/dP (0 log 0 = 0)."""
+    P, Q = np.exp(lp), np.exp(lq)
+    with np.errstate(all="ignore"):
+        if kind == "forward":
+            return np.where(Q == 0, 0.0, Q * (lq - lp)), -Q
+        if kind == "reverse":
+            f = np.where(P == 0, 0.0, P * (lp - lq))
+            return f, f + P
+        lm = np.log(beta * Q + (1 - beta) * P)
+        fp = np.where(P == 0, 0.0, P * (lp - lm))
+        return beta * np.where(Q == 0, 0.0, Q * (lq - lm)) + (1 - beta) * fp, (1 - beta) * fp
+
+
+def opd_distill(logits, ids, logp, tail=None, rows=None, labels=None, kind="reverse", beta=0.5, temperature=1.0,
+                scale=None):
+    """Divergence of each row from its teacher list (row rows[t] of ids, logp,
+    tail; ids < 0 are empty slots), and scale[t] times its gradient in the
+    logits.  Rows with a negative label: zeros; with a bad teacher row, an id
+    >= V or an id listed twice: NaN.  Returns (loss, grad, size): size bounds
+    the magnitude of the terms each gradient is a sum of."""
+    T, V = np.shape(logits)
+    loss, grad, size = np.zeros(T), np.zeros((T, V)), np.zeros((T, V))
+    for t in range(T):
+        if labels is not None and labels[t] < 0:
+            continue
+        r = t if rows is None else int(rows[t])
+        here = np.asarray(ids[r]) if 0 <= r < len(ids) else np.array([V])
+        slot = np.nonzero(here >= 0)[0]
+        here = here[slot]
+        if np.any(here >= V) or len(set(here.tolist())) < len(here):
+            loss[t], grad[t] = np.nan, np.nan
+            continue
+        lp = _log_softmax_row(logits[t], temperature)
+        p = np.exp(lp)
+        out = np.ones(V, bool)
+        out[here] = False
+        f, a = _divergence_terms(kind, beta, lp[here], np.asarray(logp[r], F64)[slot])
+        per, mag = np.zeros(V), np.zeros(V)
+        per[here], mag[here] = a, np.abs(a) + 2 * p[here]
+        total, A = np.sum(f), np.sum(a)
+        if tail is not None:
+            with np.errstate(all="ignore"):
+                lr = np.log(np.sum(p[out]))
+            fr, ar = _divergence_terms(kind, beta, lr, F64(tail[r]))
+            total, A = total + fr, A + ar
+            if np.any(p[out] > 0):
+                share = p[out] / np.sum(p[out])
+                per[out], mag[out] = ar * share, (np.abs(ar) + 2 * np.exp(lr)) * share
+        w = (1.0 if scale is None else float(scale[t])) / temperature
+        loss[t] = total
+        grad[t] = w * (per - p * A)
+        size[t] = abs(w) * (mag + p * (np.sum(np.abs(a)) + 2 + (abs(ar) if tail is not None else 0.0)))
+    return loss, grad, size
+
+
+def opd_policy(logits, labels, advantages, old_logp=None, ref_logp=None, clip=(0.2, 0.2), kl_coef=0.0,
+               temperature=1.0, scale=None):
+    """Clipped policy loss of each row's label with the KL term exp(u) - u - 1,
+    u = ref - logp, and scale[t] times its gradient in the logits.  Rows with a
+    negative label: zeros; label >= V: NaN.  Returns (loss, logp, kl, grad,
+    slope): slope bounds |dloss/dlogp| of each part."""
+    T, V = np.shape(logits)
+    loss, logp, kl, slope = (np.zeros(T) for _ in range(4))
+    grad = np.zeros((T, V))
+    for t in range(T):
+        y = int(labels[t])
+        if y < 0:
+            continue
+        if y >= V:
+            loss[t] = logp[t] = kl[t] = np.nan
+            grad[t] = np.nan
+            continue
+        lps = _log_softmax_row(logits[t], temperature)
+        lp, adv = lps[y], float(advantages[t])
+        ratio = np.exp(lp - (float(old_logp[t]) if old_logp is not None else lp))    # a row without a distribution: NaN
+        cut = min(max(ratio, 1 - clip[0]), 1 + clip[1])
+        loss[t] = -min(adv * ratio, adv * cut)
+        d = -adv * ratio if adv * ratio <= adv * cut else 0.0
+        slope[t] = abs(adv * ratio)
+        if ref_logp is not None:
+            u = float(ref_logp[t]) - lp
+            kl[t] = np.exp(u) - u - 1
+            loss[t] += kl_coef * kl[t]
+            d += kl_coef * (1 - np.exp(u))
+            slope[t] += abs(kl_coef) * (1 + np.exp(u))
+        logp[t] = lp
+        onehot = np.arange(V) == y
+        grad[t] = (1.0 if scale is None else float(scale[t])) / temperature * d * (onehot - np.exp(lps))
+    return loss, logp, kl, grad, slope
+
+
 # ------------------------------------------------------------------- weights
 
 class OracleWeights:

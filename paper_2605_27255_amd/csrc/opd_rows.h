@@ -1,0 +1,123 @@
+// Logit rows of the OPD operators: 16-byte pieces at any element alignment,
+// exponentials of differences at a temperature, and sums of them that carry
+// their own maximum.
+#pragma once
+#include "device_common.h"
+#include <math.h>
+
+namespace pipo {
+
+// ---- 16 bytes of a row --------------------------------------------------------
+// Rows start at any multiple of the element size (odd vocabularies, padded or
+// sliced rows): the pieces are loaded and stored as 16 bytes all the same,
+// which the hardware does at any alignment.
+
+template <typename L> struct Piece;
+template <> struct Piece<float> {
+    static constexpr int N = 4;
+    typedef u32x4 __attribute__((aligned(4))) raw_t;
+    static __device__ __forceinline__ float get(u32x4 w, int e) { return __uint_as_float(w[e]); }
+    static __device__ __forceinline__ u32x4 pack(const float *v) {
+        return u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    }
+    static __device__ __forceinline__ float one(const float *p) { return *p; }
+    static __device__ __forceinline__ void put(float *p, float v) { *p = v; }
+    static constexpr uint32_t kNegInf = 0xFF800000u;
+};
+template <> struct Piece<uint16_t> {
+    static constexpr int N = 8;
+    typedef u32x4 __attribute__((aligned(2))) raw_t;
+    static __device__ __forceinline__ float get(u32x4 w, int e) { return (e & 1) ? bf_hi(w[e >> 1]) : bf_lo(w[e >> 1]); }
+    static __device__ __forceinline__ u32x4 pack(const float *v) {
+        return u32x4{pack_bf2_hw(v[0], v[1]), pack_bf2_hw(v[2], v[3]), pack_bf2_hw(v[4], v[5]), pack_bf2_hw(v[6], v[7])};
+    }
+    static __device__ __forceinline__ float one(const uint16_t *p) { return bf2f(*p); }
+    static __device__ __forceinline__ void put(uint16_t *p, float v) { *p = (uint16_t)pack_bf2_hw(v, 0.f); }
+    static constexpr uint32_t kNegInf = 0xFF80FF80u;
+};
+
+// Piece i of a row of n elements; the elements behind the row's end read as -inf.
+template <typename L> __device__ __forceinline__ u32x4 load_piece(const L *row, int i, int n) {
+    typedef Piece<L> P;
+    if ((i + 1) * P::N <= n) return __builtin_nontemporal_load((const typename P::raw_t *)(row + (int64_t)i * P::N));
+    u32x4 w{P::kNegInf, P::kNegInf, P::kNegInf, P::kNegInf};
+    const int left = n - i * P::N;
+#pragma unroll
+    for (int e = 0; e < P::N; ++e) {
+        if (e >= left) continue;
+        if (sizeof(L) == 4) w[e] = ((const uint32_t *)row)[i * P::N + e];
+        else if (e & 1) w[e >> 1] = (w[e >> 1] & 0xFFFFu) | ((uint32_t)((const uint16_t *)row)[i * P::N + e] << 16);
+        else w[e >> 1] = (w[e >> 1] & 0xFFFF0000u) | ((const uint16_t *)row)[i * P::N + e];
+    }
+    return w;
+}
+template <typename L> __device__ __forceinline__ void store_piece(L *row, int i, int n, const float *v) {
+    typedef Piece<L> P;
+    if ((i + 1) * P::N <= n) {
+        __builtin_nontemporal_store(P::pack(v), (typename P::raw_t *)(row + (int64_t)i * P::N));
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < P::N; ++e)
+        if (i * P::N + e < n) P::put(row + i * P::N + e, v[e]);
+}
+
+// ---- exp((a - b) / temperature) --------------------------------------------------
+// 2^((a - b) c) with c = log2(e) / temperature in two floats, c rounded down and
+// the (positive) rest: one float of c would tilt every term the same way by up to
+// 2^-24 of its exponent, which sums do not average out.  The difference is taken
+// first, so that rows at the type's lowest value still give exp(0).  a = -inf
+// gives 0 (both products are -inf); a NaN stays one.
+struct ExpScale { float hi, lo; double inv; };
+inline ExpScale exp_scale(double temperature) {
+    const double c = 1.4426950408889634074 / temperature;
+    float hi = (float)c;
+    if ((double)hi > c) hi = nextafterf(hi, 0.f);
+    const float lo = (float)(c - (double)hi);
+    return ExpScale{hi, lo > 1e-30f ? lo : 1e-30f, 1.0 / temperature};
+}
+__device__ __forceinline__ float exp_diff(float a, float b, ExpScale c) {
+    const float d = a - b;
+    return __builtin_amdgcn_exp2f(fmaf(d, c.hi, d * c.lo));
+}
+
+// ---- (max, sum of exp((x - max) / temperature)) ------------------------------------
+struct MaxSum { float m, s; };
+// max as a reference: 0 while nothing finite was seen, so that -inf - ref is -inf
+__device__ __forceinline__ float ref_of(float m) { return m == -INFINITY ? 0.f : m; }
+__device__ __forceinline__ MaxSum merge(MaxSum a, MaxSum b, ExpScale c) {
+    const float m = fmaxf(a.m, b.m);
+    const float fa = a.m == m ? 1.f : exp_diff(a.m, m, c), fb = b.m == m ? 1.f : exp_diff(b.m, m, c);
+    return MaxSum{m, a.s * fa + b.s * fb};
+}
+template <int N> __device__ __forceinline__ void add_values(MaxSum &a, const float *v, ExpScale c) {
+    float m = v[0];
+#pragma unroll
+    for (int e = 1; e < N; ++e) m = fmaxf(m, v[e]);
+    if (m > a.m) {
+        if (a.m != -INFINITY) a.s *= exp_diff(a.m, m, c);
+        a.m = m;
+    }
+    const float r = ref_of(a.m);
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) s += exp_diff(v[e], r, c);
+    a.s += s;
+}
+// Over a workgroup of NT threads, in a fixed order; every thread gets the result.
+template <int NT> __device__ __forceinline__ MaxSum block_merge(MaxSum a, ExpScale c, MaxSum *s_red) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) a = merge(a, MaxSum{__shfl_xor(a.m, o), __shfl_xor(a.s, o)}, c);
+    if ((threadIdx.x & 63) == 0) s_red[threadIdx.x >> 6] = a;
+    __syncthreads();
+    MaxSum r = s_red[0];
+    for (int w = 1; w < NT / 64; ++w) r = merge(r, s_red[w], c);
+    return r;
+}
+__device__ __forceinline__ double wave_sum_f64(double v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+}  // namespace pipo

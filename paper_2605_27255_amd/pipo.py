@@ -18,6 +18,8 @@ EXPORTED = ("pipo_init_weights", "pipo_prefill", "pipo_prefill_ragged", "pipo_de
             "pipo_regular_prefill", "pipo_regular_prefill_ragged", "pipo_regular_step", "pipo_free",
             "pipo_last_error", "pipo_read_weight", "pipo_profile_enable", "pipo_profile_read",
             "pipo_opd_teacher_rows", "pipo_opd_targets", "pipo_opd_targets_bf16",
+            "pipo_opd_work_bytes", "pipo_opd_top_logits", "pipo_opd_top_logits_bf16", "pipo_opd_distill",
+            "pipo_opd_distill_bf16", "pipo_opd_policy", "pipo_opd_policy_bf16",
             "pipo_calibrate_stream", "pipo_calibrate_mfma")
 #: kernel classes of the profiling counters (PIPO_K_* in include/pipo.h)
 KERNEL_CLASSES = ("gemv_layer", "gemv_lmhead", "gemv_small", "attn_decode", "sample", "gate",
@@ -80,13 +82,24 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.pipo_opd_teacher_rows.argtypes = [vp, i32, i32, vp, vp]
     lib.pipo_opd_targets.argtypes = [i32, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp]
     lib.pipo_opd_targets_bf16.argtypes = [i32, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp]
+    f64 = ctypes.c_double
+    lib.pipo_opd_work_bytes.argtypes = [i32, i32, i32]
+    lib.pipo_opd_work_bytes.restype = i64
+    for dt in ("", "_bf16"):
+        getattr(lib, "pipo_opd_top_logits" + dt).argtypes = [i32, i32, vp, i64, f64, i32, vp, vp, vp, vp, i64, vp]
+        getattr(lib, "pipo_opd_distill" + dt).argtypes = [i32, i32, vp, i64, i32, i32, vp, vp, vp, vp, vp, i32, f64,
+                                                          f64, vp, vp, vp, i64, vp, i64, vp]
+        getattr(lib, "pipo_opd_policy" + dt).argtypes = [i32, i32, vp, i64, vp, vp, vp, vp, f64, f64, f64, f64, vp,
+                                                         vp, vp, vp, vp, i64, vp, i64, vp]
     lib.pipo_calibrate_stream.argtypes = [vp, i64, i64, i32, ctypes.POINTER(ctypes.c_double), vp]
     lib.pipo_calibrate_mfma.argtypes = [vp, i32, i32, i32, ctypes.POINTER(ctypes.c_double), vp]
     for fn in ("pipo_init_weights", "pipo_prefill", "pipo_prefill_ragged", "pipo_decode_step",
                "pipo_decode_step_noalloc", "pipo_regular_prefill",
                "pipo_regular_prefill_ragged", "pipo_regular_step", "pipo_free", "pipo_read_weight",
                "pipo_profile_enable", "pipo_profile_read", "pipo_opd_teacher_rows", "pipo_opd_targets",
-               "pipo_opd_targets_bf16", "pipo_calibrate_stream", "pipo_calibrate_mfma"):
+               "pipo_opd_targets_bf16", "pipo_opd_top_logits", "pipo_opd_top_logits_bf16", "pipo_opd_distill",
+               "pipo_opd_distill_bf16", "pipo_opd_policy", "pipo_opd_policy_bf16",
+               "pipo_calibrate_stream", "pipo_calibrate_mfma"):
         getattr(lib, fn).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -299,6 +312,150 @@ def opd_targets(logits_s, logits_t, labels, rows=None, sums: bool = True):
                                          _ptr(labels), _ptr(kl), _ptr(alpha), _ptr(sm),
                                          ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)))
     return kl, alpha, sm
+
+
+# ---- OPD losses with their gradients ------------------------------------------------------------------------------
+
+#: divergences of opd_distill (PIPO_OPD_* in include/pipo.h)
+OPD_KINDS = {"forward": 0, "reverse": 1, "jsd": 2}
+
+
+def _refuse(why):
+    raise PipoError(PIPO_EINVAL, why)
+
+
+def _opd_rows(logits, name="logits"):
+    """T, V, the row stride and the library's suffix for a [T, V] tensor of fp32 or bf16 rows."""
+    import torch
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or not logits.is_cuda:
+        _refuse(f"{name}: a two-dimensional CUDA tensor")
+    if logits.dtype not in (torch.float32, torch.bfloat16):
+        _refuse(f"{name}: float32 or bfloat16, not {logits.dtype}")
+    T, V = logits.shape
+    if V < 1 or (V > 1 and logits.stride(1) != 1) or (T > 1 and logits.stride(0) < V):
+        _refuse(f"{name}: rows of consecutive elements that do not overlap, not strides {tuple(logits.stride())}")
+    return T, V, logits.stride(0) if T > 1 else V, "" if logits.dtype == torch.float32 else "_bf16"
+
+
+def _opd_arg(x, name, dtype, shape, like, optional=True):
+    """One contiguous argument of a given type and shape on the logits' device."""
+    import torch
+    if x is None and optional:
+        return None
+    if not isinstance(x, torch.Tensor) or x.dtype != dtype or tuple(x.shape) != tuple(shape) or not x.is_contiguous():
+        _refuse(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)}")
+    if x.device != like.device:
+        _refuse(f"{name}: on {x.device}, the logits on {like.device}")
+    return x
+
+
+def _opd_grad(grad, logits, V):
+    """The gradient's tensor and row stride: None, a new tensor (True) or the caller's."""
+    import torch
+    if grad is None or grad is False:
+        return None, 0
+    if grad is True:
+        grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    elif (not isinstance(grad, torch.Tensor) or grad.shape != logits.shape or grad.dtype != logits.dtype
+          or grad.device != logits.device):
+        _refuse("grad: True, or a tensor of the logits' shape, type and device")
+    return grad, _opd_rows(grad, "grad")[2]
+
+
+def _opd_work(lib, T, V, k, logits):
+    import torch
+    n = lib.pipo_opd_work_bytes(T, V, k)
+    return (torch.empty(n, dtype=torch.uint8, device=logits.device) if n else None), n
+
+
+def _opd_stream(logits):
+    import torch
+    return ctypes.c_void_p(torch.cuda.current_stream(logits.device).cuda_stream)
+
+
+def opd_top_logits(logits, k: int, temperature: float = 1.0):
+    """The k largest logits of each row (fp32 or bf16 CUDA [T, V], any row
+    stride), descending, equal ones by ascending id.  Returns (ids [T, k]
+    int32, logp [T, k] float32, tail [T] float32: the log of the probability
+    outside the k)."""
+    import torch
+    lib = load_library()
+    T, V, ld, dt = _opd_rows(logits)
+    with torch.cuda.device(logits.device):
+        n = max(int(k), 0)
+        ids = torch.empty((T, n), dtype=torch.int32, device=logits.device)
+        logp = torch.empty((T, n), dtype=torch.float32, device=logits.device)
+        tail = torch.empty(T, dtype=torch.float32, device=logits.device)
+        work, nw = _opd_work(lib, T, V, n, logits)
+        _opd_check(lib, getattr(lib, "pipo_opd_top_logits" + dt)(T, V, _ptr(logits), ld, float(temperature), int(k),
+                                                                 _ptr(ids), _ptr(logp), _ptr(tail), _ptr(work), nw,
+                                                                 _opd_stream(logits)))
+    return ids, logp, tail
+
+
+def opd_distill(logits, ids, logp, tail=None, rows=None, labels=None, kind: str = "reverse", beta: float = 0.5,
+                temperature: float = 1.0, scale=None, grad=None):
+    """Divergence of student rows from a teacher's top logits, with its gradient.
+    logits: fp32 or bf16 CUDA [T, V], any row stride; ids int32, logp float32
+    [Tt, k] (an id < 0 is an empty slot) and tail float32 [Tt] (the tokens
+    outside as one more entry; None: listed entries only), as opd_top_logits
+    gives them; rows: int32 [T], each position's list (None: row t); labels:
+    int32 [T], negative: not scored; kind: "forward", "reverse" or "jsd" (with
+    beta); scale: float32 [T], each position's factor in the gradient; grad:
+    None, True, or a tensor to write it to (the logits themselves to replace
+    them).  Returns (loss [T] float32, grad or None); the caller goes on with
+    ``logits.backward(grad)``."""
+    import torch
+    lib = load_library()
+    T, V, ld, dt = _opd_rows(logits)
+    if kind not in OPD_KINDS:
+        _refuse(f"kind: one of {', '.join(OPD_KINDS)}, not {kind!r}")
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 2:
+        _refuse("ids: a tensor of shape [Tt, k]")
+    Tt, k = ids.shape
+    _opd_arg(ids, "ids", torch.int32, (Tt, k), logits, optional=False)
+    _opd_arg(logp, "logp", torch.float32, (Tt, k), logits, optional=False)
+    _opd_arg(tail, "tail", torch.float32, (Tt,), logits)
+    _opd_arg(rows, "rows", torch.int32, (T,), logits)
+    _opd_arg(labels, "labels", torch.int32, (T,), logits)
+    _opd_arg(scale, "scale", torch.float32, (T,), logits)
+    with torch.cuda.device(logits.device):
+        loss = torch.empty(T, dtype=torch.float32, device=logits.device)
+        grad, ldg = _opd_grad(grad, logits, V)
+        work, nw = _opd_work(lib, T, V, k, logits)
+        _opd_check(lib, getattr(lib, "pipo_opd_distill" + dt)(
+            T, V, _ptr(logits), ld, Tt, k, _ptr(ids), _ptr(logp), _ptr(tail), _ptr(rows), _ptr(labels),
+            OPD_KINDS[kind], float(beta), float(temperature), _ptr(scale), _ptr(loss), _ptr(grad), ldg, _ptr(work), nw,
+            _opd_stream(logits)))
+    return loss, grad
+
+
+def opd_policy(logits, labels, advantages, old_logp=None, ref_logp=None, clip=(0.2, 0.2), kl_coef: float = 0.0,
+               temperature: float = 1.0, scale=None, grad=None):
+    """Clipped policy loss of each row's label with a KL term, and its gradient.
+    logits: fp32 or bf16 CUDA [T, V], any row stride; labels: int32 [T],
+    negative: not scored; advantages, old_logp (None: on-policy, ratio 1),
+    ref_logp (None: no KL term): float32 [T]; clip: the ratio is clipped to
+    [1 - clip[0], 1 + clip[1]]; scale, grad: as in opd_distill.  Returns (loss
+    [T], logp [T], kl [T] or None, grad or None), float32 but for the gradient."""
+    import torch
+    lib = load_library()
+    T, V, ld, dt = _opd_rows(logits)
+    _opd_arg(labels, "labels", torch.int32, (T,), logits, optional=False)
+    _opd_arg(advantages, "advantages", torch.float32, (T,), logits, optional=False)
+    _opd_arg(old_logp, "old_logp", torch.float32, (T,), logits)
+    _opd_arg(ref_logp, "ref_logp", torch.float32, (T,), logits)
+    _opd_arg(scale, "scale", torch.float32, (T,), logits)
+    with torch.cuda.device(logits.device):
+        loss, logp = (torch.empty(T, dtype=torch.float32, device=logits.device) for _ in range(2))
+        kl = None if ref_logp is None else torch.empty(T, dtype=torch.float32, device=logits.device)
+        grad, ldg = _opd_grad(grad, logits, V)
+        work, nw = _opd_work(lib, T, V, 1, logits)
+        _opd_check(lib, getattr(lib, "pipo_opd_policy" + dt)(
+            T, V, _ptr(logits), ld, _ptr(labels), _ptr(advantages), _ptr(old_logp), _ptr(ref_logp), float(clip[0]),
+            float(clip[1]), float(kl_coef), float(temperature), _ptr(scale), _ptr(loss), _ptr(logp), _ptr(kl),
+            _ptr(grad), ldg, _ptr(work), nw, _opd_stream(logits)))
+    return loss, logp, kl, grad
 
 
 def calibrate_stream(buf, nbytes: int, reps: int = 20) -> float:

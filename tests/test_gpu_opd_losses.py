@@ -1,0 +1,508 @@
+"""GPU parity of the OPD losses (teacher's top logits, distillation, clipped
+policy loss) and their gradients against the float64 oracle.
+
+Tolerances.  A log-probability is a logit, exact in fp64, minus the log of a sum
+of exponentials of up to V terms.  Each term is 2^x of a difference with three
+fp32 roundings (difference, product, fma), each at most 2^-24 of an exponent of
+at most 30 (terms further down weigh less than e^-20 of the sum), plus the
+exponential's own 2^-23: 3 * 30 * 2^-24 + 2^-23 = 5.5e-6.  A sum of fp32 adds
+passes at most 512 terms in one thread (V = 524288 over 1024 threads) and 16
+merges: 528 * 2^-24 = 3.1e-5 in the worst order, 1.1e-5 for the rows of up to
+152000 tokens that most tests use.  So |error of log p| <= DELTA, and every
+output is at most its derivative in log p times DELTA off, plus the rounding of
+the output itself (half a step of its type)."""
+import numpy as np
+import pytest
+
+from oracle import pipo_oracle as O
+
+pytestmark = pytest.mark.gpu
+
+DELTA = 5.5e-6 + 1.1e-5
+DELTA_LONG = 5.5e-6 + 3.1e-5
+HALF = {"float32": 2.0 ** -24, "bfloat16": 2.0 ** -8}
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as t
+    assert t.cuda.is_available(), "GPU tests need a GPU"
+    return t
+
+
+def _rows(torch, T, V, dtype, seed, pad=0, raised=8):
+    """Logit rows with some tokens raised, as a view of padded storage (pad
+    columns hold a sentinel), and their values in float64."""
+    rng = np.random.default_rng(seed)
+    z = 2.0 * rng.standard_normal((T, V + pad), dtype=np.float32)
+    for t in range(T):
+        at = rng.integers(0, V, raised)
+        z[t, at] += 12.0 * rng.random(raised, dtype=np.float32)
+    z[:, V:] = 1e4
+    d = torch.from_numpy(z).cuda().to(getattr(torch, dtype))[:, :V]
+    return d, d.double().cpu().numpy()
+
+
+def _close(got, ref, tol, what=""):
+    got = got.double().cpu().numpy()
+    bad = np.isnan(ref) != np.isnan(got)
+    assert not bad.any(), (what, "NaN", np.argwhere(bad)[:4])
+    with np.errstate(invalid="ignore"):
+        over = (np.abs(got - ref) > tol) & (got != ref) & ~np.isnan(ref)
+    assert not over.any(), (what, np.argwhere(over)[:4], got[over][:4], ref[over][:4], np.broadcast_to(tol, ref.shape)[over][:4])
+
+
+# ---- top logits ------------------------------------------------------------------------------------------------
+
+def _check_top(torch, d, z, k, temperature=1.0, delta=DELTA):
+    from paper_2605_27255_amd import opd_top_logits
+    ids, logp, tail = opd_top_logits(d, k, temperature)
+    torch.cuda.synchronize()
+    r_ids, r_logp, r_tail = O.opd_top_logits(z, k, temperature)
+    np.testing.assert_array_equal(ids.cpu().numpy(), r_ids)
+    _close(logp, r_logp, delta + HALF["float32"] * np.abs(r_logp), "logp")
+    # the mass outside and the whole are two such sums; with nothing outside, -inf exactly
+    _close(tail, r_tail, 2 * delta + HALF["float32"] * np.abs(r_tail), "tail")
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("T,V,k,pad", [(1, 1, 1, 0), (3, 7, 7, 2), (2, 9, 1, 0), (5, 255, 128, 1), (2, 1000, 256, 0),
+                                       (4, 2041, 255, 3), (7, 4096, 32, 0), (3, 16384, 20, 0), (3, 16385, 20, 5),
+                                       (2, 50021, 100, 0), (3, 151936, 32, 0), (2, 151937, 256, 1)])
+def test_top_logits(torch, T, V, k, pad, dtype):
+    d, z = _rows(torch, T, V, dtype, seed=V + k, pad=pad)
+    _check_top(torch, d, z, k, temperature=1.0 if k % 2 else 1.6)
+
+
+def test_top_logits_longest_rows_and_many_rows(torch):
+    d, z = _rows(torch, 2, 1 << 19, "bfloat16", seed=1)
+    _check_top(torch, d, z, 64, delta=DELTA_LONG)
+    d, z = _rows(torch, 700, 1201, "float32", seed=2)
+    _check_top(torch, d, z, 17)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("V", [300, 4099, 70001])
+def test_top_logits_of_crowded_rows(torch, V, dtype):
+    """Constant rows, sorted rows, one value on more entries than are ranked,
+    zeros of either sign, masked rows with fewer tokens than k."""
+    k, rows = 50, []
+    ramp = np.arange(V, dtype=np.float32) / V * 20
+    rows += [np.full(V, 3.0, np.float32), ramp, ramp[::-1].copy(), np.zeros(V, np.float32)]
+    rows[-1][::2] = -0.0
+    crowd = np.random.default_rng(V).standard_normal(V).astype(np.float32)
+    crowd[V // 20:] = 2.5                                  # most of the row at one value
+    crowd[V // 3] = 9.0
+    rows.append(crowd)
+    lowest = np.full(V, float(torch.finfo(getattr(torch, dtype)).min), np.float32)
+    rows.append(lowest.copy())                             # everything masked with the lowest value: uniform
+    lowest[5:25] = 1.0
+    rows.append(lowest)
+    few = np.full(V, -np.inf, np.float32)
+    few[7:290:13] = np.arange(22, dtype=np.float32)        # 22 tokens, k of 50
+    rows.append(few)
+    d = torch.from_numpy(np.stack(rows)).cuda().to(getattr(torch, dtype))
+    _check_top(torch, d, d.double().cpu().numpy(), k)
+
+
+def test_top_logits_of_rows_without_a_distribution(torch):
+    """All -inf, a NaN, a +inf: NaN log-probabilities, ids different and in range; other rows as ever."""
+    from paper_2605_27255_amd import opd_top_logits
+    for V in (40, 40000):
+        d, z = _rows(torch, 6, V, "float32", seed=8)
+        d[1] = -float("inf")
+        d[2, 3] = float("nan")
+        d[3, V - 1] = float("inf")
+        d[4] = float("nan")
+        bad = torch.tensor([1, 2, 3, 4])
+        ids, logp, tail = opd_top_logits(d, 24)
+        torch.cuda.synchronize()
+        assert logp[bad].isnan().all() and tail[bad].isnan().all()
+        for r in ids.cpu().numpy():
+            assert len(set(r.tolist())) == 24 and r.min() >= 0 and r.max() < V
+        r_ids, r_logp, _ = O.opd_top_logits(z[[0, 5]], 24)
+        np.testing.assert_array_equal(ids[[0, 5]].cpu().numpy(), r_ids)
+        _close(logp[[0, 5]], r_logp, DELTA + HALF["float32"] * np.abs(r_logp))
+
+
+# ---- distillation ------------------------------------------------------------------------------------------------
+
+def _teacher(torch, z, k, temperature, seed, noise=0.7):
+    rng = np.random.default_rng(seed)
+    ids, logp, tail = O.opd_top_logits(z + noise * rng.standard_normal(z.shape), k, temperature)
+    dev = lambda a, t: torch.from_numpy(np.ascontiguousarray(a)).cuda().to(t)  # noqa: E731
+    ids, logp, tail = dev(ids, torch.int32), dev(logp, torch.float32), dev(tail, torch.float32)
+    return ids, logp, tail
+
+
+def _host(*ts):
+    return [None if t is None else t.cpu().numpy().astype(np.float64 if t.is_floating_point() else np.int64) for t in ts]
+
+
+def _check_distill(torch, d, z, ids, logp, tail=None, rows=None, labels=None, scale=None, grad=True, delta=DELTA, **kw):
+    from paper_2605_27255_amd import opd_distill
+    loss, g = opd_distill(d, ids, logp, tail, rows=rows, labels=labels, scale=scale, grad=grad, **kw)
+    torch.cuda.synchronize()
+    h_ids, h_logp, h_tail, h_rows, h_labels, h_scale = _host(ids, logp, tail, rows, labels, scale)
+    r_loss, r_grad, size = O.opd_distill(z, h_ids, h_logp, h_tail, h_rows, h_labels, scale=h_scale, **kw)
+    unit = O.opd_distill(z, h_ids, h_logp, h_tail, h_rows, h_labels, **kw)[2].sum(1) * kw.get("temperature", 1.0)
+    # each entry's term moves by at most (|a| + 2 P) DELTA (its a is P df/dP), and size sums just that
+    _close(loss, r_loss, delta * unit + HALF["float32"] * np.abs(r_loss), "loss")
+    if grad is not None:
+        name = str(d.dtype).split(".")[1]
+        # a product of an exponential of its own (DELTA again) and of sums that carry DELTA; 1e-38: denormals flush
+        _close(g, r_grad, 4 * delta * size + HALF[name] * np.abs(r_grad) + 1e-37, "grad")
+    return loss, g
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("kind", ["forward", "reverse", "jsd"])
+@pytest.mark.parametrize("T,V,k,pad,with_tail", [(1, 1, 1, 0, False), (2, 2, 1, 0, True), (3, 9, 9, 1, True),
+                                                 (4, 513, 100, 0, True), (5, 4096, 32, 0, False), (3, 16384, 3, 3, True),
+                                                 (2, 16387, 256, 0, True), (4, 50021, 20, 7, False), (2, 151936, 32, 0, True)])
+def test_distill(torch, T, V, k, pad, with_tail, kind, dtype):
+    d, z = _rows(torch, T, V, dtype, seed=V + k, pad=pad)
+    temperature = 1.0 if V % 2 else 1.7
+    ids, logp, tail = _teacher(torch, z, k, temperature, seed=5)
+    scale = torch.linspace(0.3, -1.2, T).cuda()
+    _check_distill(torch, d, z, ids, logp, tail if with_tail else None, scale=scale, kind=kind, beta=0.3,
+                   temperature=temperature)
+
+
+@pytest.mark.parametrize("V", [1000, 40001])
+def test_distill_rows_labels_and_slots(torch, V):
+    """A row map, unscored positions, empty slots in odd places, and flagged
+    positions (no teacher row, an id out of range, an id listed twice) that
+    leave the others alone."""
+    T, k = 12, 40
+    d, z = _rows(torch, T, V, "float32", seed=V)
+    ids, logp, tail = _teacher(torch, z[:8], k, 1.0, seed=6)
+    rows = torch.tensor([0, 1, 1, 2, 3, 8, -1, 4, 5, 6, 7, 7], dtype=torch.int32).cuda()     # 8 and -1: no such row
+    labels = torch.tensor([1, 1, -1, 1, 1, 1, 1, 1, 1, 1, -5, 2 ** 31 - 1], dtype=torch.int32).cuda()
+    ids[2, ::3] = -1
+    ids[3, :] = -7                       # nothing listed
+    ids[4, 5] = V
+    ids[5, 39] = ids[5, 0]
+    ids[6, 0] = 2 ** 31 - 1
+    for tl in (tail, None):
+        for kind in ("forward", "reverse", "jsd"):
+            loss, g = _check_distill(torch, d, z, ids, logp, tl, rows=rows, labels=labels, kind=kind)
+            flagged = [5, 6, 7, 8, 9]
+            assert loss[flagged].isnan().all() and g[flagged].isnan().all()
+            assert not loss[[2, 10]].any() and not g[[2, 10]].any()
+
+
+def test_distill_masked_logits(torch):
+    """Students with masked tokens (-inf, the lowest value), everything listed
+    but masked, tails without mass, and rows without any token."""
+    V = 3001
+    d, z = _rows(torch, 8, V, "float32", seed=2)
+    ids, logp, tail = _teacher(torch, z, 16, 1.0, seed=3)
+    out = torch.ones(V, dtype=torch.bool, device="cuda")
+    out[ids[1].long()] = False
+    d[0, ::2] = -float("inf")
+    d[1, out] = -float("inf")            # the student has nothing outside the list
+    d[2, ids[2].long()] = -float("inf")  # ... and nothing on it
+    d[3] = -float("inf")
+    d[4, 1::2] = float(torch.finfo(torch.float32).min)
+    d[5, 77] = float("nan")
+    d[6, 78] = float("inf")
+    d[7] = float(torch.finfo(torch.float32).min)
+    z = d.double().cpu().numpy()
+    for kind in ("reverse", "jsd"):
+        with np.errstate(all="ignore"):
+            loss, g = _check_distill(torch, d, z, ids, logp, tail, kind=kind)
+        assert loss[[3, 5, 6]].isnan().all() and g[[3, 5, 6]].isnan().all()
+        assert loss[[0, 1, 2, 4, 7]].isfinite().all() and g[[0, 1, 2, 4, 7]].isfinite().all()
+    from paper_2605_27255_amd import opd_distill
+    loss, _ = opd_distill(d, ids, logp, tail, kind="forward", grad=True)
+    assert torch.isposinf(loss[[0, 1, 2]]).all() and loss[[3, 5, 6]].isnan().all()   # teacher mass where there is none
+
+
+def test_distill_near_teacher_and_sharp_student(torch):
+    """A student that is its teacher (nothing left but rounding), and one with
+    all but 1e-9 of its mass on one listed token: the rest's mass is exact."""
+    V, k = 20011, 8
+    d, z = _rows(torch, 3, V, "float32", seed=4)
+    d[1] = 0
+    d[1, 17] = 30.0
+    d[2, :] = -50.0
+    d[2, 3] = 45.0                       # the rest holds e^-85 of the mass, below fp32 normals
+    z = d.double().cpu().numpy()
+    ids, logp, tail = _teacher(torch, z, k, 1.0, seed=9, noise=0.0)
+    for kind in ("forward", "reverse", "jsd"):
+        _check_distill(torch, d, z, ids, logp, tail, kind=kind)
+    ids, logp, tail = _teacher(torch, z, k, 1.0, seed=9, noise=0.5)
+    for kind in ("forward", "reverse", "jsd"):
+        _check_distill(torch, d, z, ids, logp, tail, kind=kind)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("T,V,pad", [(3, 777, 0), (40, 70003, 5), (300, 20001, 0)])
+def test_gradients_in_place_and_beside(torch, T, V, pad, dtype):
+    """The gradient over the logits, in a buffer of another stride and
+    alignment, and beside the logits in one buffer: the same values, and
+    nothing written outside the rows."""
+    from paper_2605_27255_amd import opd_distill, opd_policy
+    d, z = _rows(torch, T, V, dtype, seed=11, pad=pad)
+    ids, logp, tail = _teacher(torch, z[:3], 12, 1.0, seed=2)
+    rows = (torch.arange(T, dtype=torch.int32) % 3).cuda()
+    y = ids[rows.long(), 0].contiguous()
+    y[T // 2] = -1
+    adv = torch.linspace(-1, 1, T).cuda()
+    for call in (lambda x, g: opd_distill(x, ids, logp, tail, rows=rows, labels=y, grad=g)[-1],
+                 lambda x, g: opd_policy(x, y, adv, grad=g)[-1]):
+        want = call(d, True)
+        other = torch.full((T, V + 9), 7.0, device="cuda", dtype=d.dtype)
+        call(d, other[:, 3:3 + V])
+        assert torch.equal(other[:, 3:3 + V], want) and (other[:, :3] == 7).all() and (other[:, 3 + V:] == 7).all()
+        both = torch.full((T, 2 * V + 3), 7.0, device="cuda", dtype=d.dtype)
+        both[:, :V] = d
+        call(both[:, :V], both[:, V + 1:2 * V + 1])
+        assert torch.equal(both[:, V + 1:2 * V + 1], want) and torch.equal(both[:, :V], d)
+        assert (both[:, V] == 7).all() and (both[:, 2 * V + 1:] == 7).all()
+        store = torch.full((T, V + 6), 7.0, device="cuda", dtype=d.dtype)
+        store[:, 1:V + 1] = d
+        x = store[:, 1:V + 1]
+        assert call(x, x) is x
+        assert torch.equal(x, want) and (store[:, 0] == 7).all() and (store[:, V + 1:] == 7).all()
+
+
+def test_distill_gradient_against_differences(torch):
+    """Along random directions: (loss(z + h u) - loss(z - h u)) / 2h against the
+    gradient.  The two losses carry at most DELTA_SMALL (901 tokens: 4 terms a
+    thread and 10 merges, 14 * 2^-24 beside the exponentials' 5.5e-6) times
+    their terms' slopes each; the quotient's own error is h^2 / 6 times the third
+    derivative, which three powers of u's largest element and the terms bound."""
+    from paper_2605_27255_amd import opd_distill
+    delta, T, V, k, h = 5.5e-6 + 14 * 2.0 ** -24, 6, 901, 10, 2e-2
+    d, z = _rows(torch, T, V, "float32", seed=21)
+    ids, logp, tail = _teacher(torch, z, k, 1.0, seed=22)
+    for kind in ("forward", "reverse", "jsd"):
+        _, grad = opd_distill(d, ids, logp, tail, kind=kind, grad=True)
+        h_ids, h_logp, h_tail = _host(ids, logp, tail)
+        slopes = O.opd_distill(z, h_ids, h_logp, h_tail, kind=kind)[2].sum(1)
+        for seed in range(3):
+            u = torch.from_numpy(np.random.default_rng(seed).standard_normal((T, V)).astype(np.float32)).cuda()
+            u = u / u.abs().amax(1, keepdim=True)
+            up = opd_distill((d.double() + h * u.double()).float(), ids, logp, tail, kind=kind)[0].double()
+            down = opd_distill((d.double() - h * u.double()).float(), ids, logp, tail, kind=kind)[0].double()
+            got = ((up - down) / (2 * h)).cpu().numpy()
+            want = (grad.double() * u.double()).sum(1).cpu().numpy()
+            # inputs round too: 2^-24 of logits up to 20 moves each loss by 20 * 2^-24 of its slopes
+            tol = slopes * ((2 * delta + 40 * 2.0 ** -24) / (2 * h) + 8 * h * h / 6)
+            assert (np.abs(got - want) <= tol).all(), (kind, got, want, tol)
+
+
+# ---- policy loss ---------------------------------------------------------------------------------------------------
+
+def _check_policy(torch, d, z, y, adv, old=None, ref=None, scale=None, grad=True, delta=DELTA, **kw):
+    from paper_2605_27255_amd import opd_policy
+    loss, logp, kl, g = opd_policy(d, y, adv, old_logp=old, ref_logp=ref, scale=scale, grad=grad, **kw)
+    torch.cuda.synchronize()
+    h_y, h_adv, h_old, h_ref, h_scale = _host(y, adv, old, ref, scale)
+    r_loss, r_logp, r_kl, r_grad, slope = O.opd_policy(z, h_y, h_adv, h_old, h_ref, scale=h_scale, **kw)
+    eps = HALF["float32"]
+    _close(logp, r_logp, delta + eps * np.abs(r_logp), "logp")
+    _close(loss, r_loss, delta * slope + eps * np.abs(r_loss), "loss")
+    if ref is None:
+        assert kl is None
+    else:
+        u = np.where(h_y >= 0, h_ref - r_logp, 0)
+        _close(kl, r_kl, delta * np.abs(np.expm1(u)) + delta ** 2 + eps * np.abs(r_kl), "kl")
+    if grad is not None:
+        T, V = z.shape
+        name = str(d.dtype).split(".")[1]
+        w = np.abs(h_scale if h_scale is not None else np.ones(T)) / kw.get("temperature", 1.0)
+        p = np.stack([np.exp(O._log_softmax_row(r, kw.get("temperature", 1.0))) for r in z])
+        hot = np.zeros((T, V))
+        for t in range(T):
+            if 0 <= h_y[t] < V:
+                hot[t, int(h_y[t])] = 1
+        # the factor moves by slope * DELTA, each probability by itself * 2 DELTA (its own exponential and the sum)
+        tol = (w * slope)[:, None] * (p + hot * (1 - p)) * 4 * delta + HALF[name] * np.abs(r_grad) + 1e-37
+        _close(g, r_grad, tol, "grad")
+    return loss, logp, kl, g
+
+
+def _rollout(torch, z, temperature, seed):
+    """Labels the row likes, and old and reference log-probabilities whose
+    ratios stay 1e-3 from the clip's edges (the gradient jumps there)."""
+    rng = np.random.default_rng(seed)
+    T, V = z.shape
+    y = np.array([int(np.argsort(-z[t], kind="stable")[min(V - 1, rng.integers(0, 6))]) for t in range(T)])
+    lp = O.opd_policy(z, y, np.ones(T), temperature=temperature)[1]
+    ratio = np.exp(0.3 * rng.standard_normal(T))
+    for edge in (0.8, 1.3):
+        ratio = np.where(np.abs(ratio - edge) < 1e-3, edge + 2e-3, ratio)
+    dev = lambda a: torch.from_numpy(a.astype(np.float32)).cuda()  # noqa: E731
+    return (torch.from_numpy(y.astype(np.int32)).cuda(), dev(rng.standard_normal(T)), dev(lp - np.log(ratio)),
+            dev(lp + 0.3 * rng.standard_normal(T)))
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("T,V,pad", [(1, 1, 0), (3, 2, 1), (5, 777, 0), (9, 4096, 0), (4, 16384, 4), (6, 16385, 0),
+                                     (5, 50021, 3), (3, 151936, 0)])
+def test_policy(torch, T, V, pad, dtype):
+    d, z = _rows(torch, T, V, dtype, seed=V, pad=pad)
+    temperature = 1.0 if V % 2 else 0.7
+    y, adv, old, ref = _rollout(torch, z, temperature, seed=V)
+    scale = torch.linspace(1.0, 0.2, T).cuda()
+    if T > 3:
+        y[1] = -1
+        y[3] = V                        # no such token: flagged
+    kw = dict(clip=(0.2, 0.3), temperature=temperature)
+    loss, logp, _, g = _check_policy(torch, d, z, y, adv, old, ref, scale, kl_coef=0.1, **kw)
+    if T > 3:
+        assert loss[3].isnan() and g[3].isnan().all() and loss[1] == 0 and logp[1] == 0 and not g[1].any()
+    _check_policy(torch, d, z, y, adv, old, None, None, **kw)
+    _check_policy(torch, d, z, y, adv, None, ref, None, kl_coef=0.0, grad=None, **kw)
+    _check_policy(torch, d, z, y, adv, None, None, scale, **kw)
+
+
+def test_policy_sharp_rows_and_masks(torch):
+    """A label with all but 1e-12 of the mass keeps the gradient of that rest;
+    masked tokens get none; rows without a token, or with a NaN, are NaN."""
+    V = 9001
+    d, z = _rows(torch, 6, V, "float32", seed=3)
+    d[0] = 0
+    d[0, 5] = 37.0
+    d[1, ::2] = -float("inf")
+    d[2] = -float("inf")
+    d[3, 9] = float("nan")
+    d[4] = float(torch.finfo(torch.float32).min)
+    d[5, 100:] = float(torch.finfo(torch.float32).min)
+    z = d.double().cpu().numpy()
+    y = torch.tensor([5, 1, 0, 0, 7, 50], dtype=torch.int32).cuda()
+    adv = torch.tensor([1.0, -1, 1, 1, 2, 1]).cuda()
+    with np.errstate(all="ignore"):
+        loss, _, _, g = _check_policy(torch, d, z, y, adv)
+    assert g[0, 5] < 0 and abs(g[0, 5].item()) < 1e-10 and not g[1, ::2].any() and not g[5, 100:].any()
+    assert loss[[2, 3]].isnan().all() and g[[2, 3]].isnan().all()
+
+
+# ---- together, streams, graphs, far offsets --------------------------------------------------------------------------
+
+def test_training_chunk_end_to_end(torch):
+    """A chunk as a training loop runs it: PAD-compacted teacher rows, the
+    teacher's list, the OPD targets, distillation into the logits' place, and a
+    policy step whose advantages are the sampled KL terms."""
+    from paper_2605_27255_amd import opd_distill, opd_policy, opd_targets, opd_teacher_rows, opd_top_logits
+    rng = np.random.default_rng(31)
+    T, V, k = 96, 8192, 32
+    tok = rng.integers(0, V - 1, T).astype(np.int32)
+    tok[rng.random(T) < 0.25] = V - 1
+    tok[0] = 1
+    Tt = int(np.count_nonzero(tok != V - 1))
+    s, zs = _rows(torch, T, V, "bfloat16", seed=32)
+    te, zt = _rows(torch, Tt, V, "bfloat16", seed=33)
+    y = rng.integers(0, V - 1, T).astype(np.int32)
+    y[rng.random(T) < 0.1] = -1
+    labels = torch.from_numpy(y).cuda()
+    rows = opd_teacher_rows(torch.from_numpy(tok).cuda(), V - 1)
+    ids, logp, tail = opd_top_logits(te, k)
+    kl, _, _ = opd_targets(s.contiguous(), te.contiguous(), labels, rows)
+    loss, g = opd_distill(s, ids, logp, tail, rows=rows, labels=labels, kind="reverse", scale=torch.full((T,), 1 / T).cuda(),
+                          grad=True)
+    adv = -kl
+    p_loss, p_logp, _, p_grad = opd_policy(s, labels, adv, grad=s)
+    torch.cuda.synchronize()
+    assert p_grad is s
+    o_rows = O.opd_teacher_rows(tok, V - 1)
+    o_ids, o_logp, o_tail = O.opd_top_logits(zt, k)
+    np.testing.assert_array_equal(ids.cpu().numpy(), o_ids)
+    o_loss, o_grad, size = O.opd_distill(zs, o_ids, o_logp, o_tail, o_rows, y, scale=np.full(T, 1 / T))
+    unit = O.opd_distill(zs, o_ids, o_logp, o_tail, o_rows, y)[2].sum(1)
+    # the teacher's numbers carry DELTA as well
+    _close(loss, o_loss, 3 * DELTA * unit + 2.0 ** -24 * np.abs(o_loss), "loss")
+    _close(g, o_grad, 8 * DELTA * size + HALF["bfloat16"] * np.abs(o_grad) + 1e-37, "grad")
+    o = O.opd_policy(zs, y, adv.cpu().numpy())
+    _close(p_loss, o[0], DELTA * o[4] + 2.0 ** -24 * np.abs(o[0]), "policy loss")
+    p = np.stack([np.exp(O._log_softmax_row(r, 1.0)) for r in zs])
+    hot = (np.arange(V)[None] == y[:, None]) * 1.0
+    _close(p_grad, o[3], o[4][:, None] * (p + hot) * 4 * DELTA + HALF["bfloat16"] * np.abs(o[3]) + 1e-37, "policy grad")
+
+
+@pytest.mark.parametrize("T,V", [(3, 60001), (400, 20000)])
+def test_streams_and_graphs(torch, T, V):
+    """The calls on a side stream, and captured in two graphs whose replays
+    interleave with eager calls and new inputs, give the eager results."""
+    from paper_2605_27255_amd import opd_distill, opd_policy, opd_top_logits
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    fresh = lambda: 3 * torch.randn((T, V), generator=gen, device="cuda")  # noqa: E731
+    s, te = fresh(), fresh()
+    adv, y = torch.randn(T, generator=gen, device="cuda"), torch.randint(0, V, (T,), generator=gen, device="cuda").int()
+
+    def step():
+        ids, logp, tail = opd_top_logits(te, 16)
+        return (ids, logp, tail) + opd_distill(s, ids, logp, tail, labels=y, grad=True)
+
+    def policy():
+        loss, logp, _, g = opd_policy(s, y, adv, grad=True)
+        return loss, logp, g
+
+    side = torch.cuda.Stream()
+    want = [t.clone() for t in step() + policy()]
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = step() + policy()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graphs, outs = [], []
+    for fn in (step, policy):
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(fn())
+        graphs.append(g)
+    for i in range(4):
+        s.copy_(fresh())
+        te.copy_(fresh())
+        for g in graphs if i % 2 else graphs[::-1]:
+            g.replay()
+        want = step() + policy()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs[0] + outs[1], want)), i
+
+
+def test_rows_far_apart(torch):
+    """Row offsets beyond 2^32 bytes and 2^31 elements."""
+    V, ld, T = 5003, (1 << 30) + 3, 4
+    store = torch.empty(ld * (T - 1) + V, dtype=torch.bfloat16, device="cuda")
+    d = store.as_strided((T, V), (ld, 1))
+    src, z = _rows(torch, T, V, "bfloat16", seed=7)
+    d.copy_(src)
+    _check_top(torch, d, z, 30)
+    ids, logp, tail = _teacher(torch, z, 8, 1.0, seed=1)
+    want = _check_distill(torch, src, z, ids, logp, tail, kind="reverse")[1]
+    from paper_2605_27255_amd import opd_distill
+    opd_distill(d, ids, logp, tail, kind="reverse", grad=d)
+    assert torch.equal(d, want)
+
+
+def test_python_refusals(torch):
+    from paper_2605_27255_amd import PIPO_EINVAL, PipoError, opd_distill, opd_policy, opd_top_logits
+    d, z = _rows(torch, 4, 100, "float32", seed=1)
+    ids, logp, tail = _teacher(torch, z, 5, 1.0, seed=1)
+    y, adv = torch.zeros(4, dtype=torch.int32).cuda(), torch.zeros(4).cuda()
+    calls = [lambda: opd_top_logits(d, 0), lambda: opd_top_logits(d, 101), lambda: opd_top_logits(d[0], 1),
+             lambda: opd_top_logits(d.half(), 5), lambda: opd_top_logits(d.t(), 2), lambda: opd_top_logits(d, 5, 0.0),
+             lambda: opd_top_logits(d[:1].expand(4, 100), 5),
+             lambda: opd_distill(d, ids, logp, tail, kind="kl"), lambda: opd_distill(d, ids.long(), logp),
+             lambda: opd_distill(d, ids, logp[:, :3]), lambda: opd_distill(d, ids, logp.cpu()),
+             lambda: opd_distill(d, ids, logp, tail[:3]), lambda: opd_distill(d, ids, logp, rows=y[:3]),
+             lambda: opd_distill(d, ids, logp, grad=torch.empty(4, 99, device="cuda")),
+             lambda: opd_distill(d, ids, logp, grad=d.bfloat16()), lambda: opd_distill(d, ids, logp, kind="jsd", beta=1.0),
+             lambda: opd_distill(d[:, :50], ids, logp, grad=d[:, 25:75]),
+             lambda: opd_policy(d, y, adv[:2]), lambda: opd_policy(d, y.long(), adv), lambda: opd_policy(d, y, adv, kl_coef=0.1),
+             lambda: opd_policy(d, y, adv, clip=(1.5, 0.2)), lambda: opd_policy(d, y, adv, temperature=float("nan")),
+             lambda: opd_policy(d, y, adv, scale=torch.ones(4, 1, device="cuda"))]
+    for i, call in enumerate(calls):
+        with pytest.raises(PipoError) as e:
+            call()
+        assert e.value.code == PIPO_EINVAL, i
+    empty = d[:0]
+    assert opd_top_logits(empty, 5)[0].shape == (0, 5)
+    loss, g = opd_distill(empty, ids, logp, tail, grad=True)
+    assert loss.shape == (0,) and g.shape == (0, 100)
+    assert opd_policy(empty, y[:0], adv[:0], grad=True)[3].shape == (0, 100)
