@@ -18,6 +18,7 @@
 
 namespace pipo {
 
+constexpr double kLn2 = 0.69314718055994530942;
 constexpr int kEntries = 256;       // listed entries of a row
 constexpr int kOpdMaxVocab = 1 << 19;
 constexpr int64_t kOpdMaxStride = (int64_t)1 << 31;   // with T < 2^31, byte offsets stay far inside 64 bits
@@ -45,6 +46,7 @@ struct LossShared {
     MaxSum red[16];
     int id[kEntries];               // listed ids, -1: an empty slot
     float z[kEntries];              // their logits
+    double a[kEntries], p[kEntries];   // their a = p df/dp, and p
     float patch[kEntries];          // their gradients
     float coef;                     // the others' gradient over exp((z - m) / temperature)
     int bad;
@@ -53,31 +55,30 @@ struct LossShared {
 // What happens at position t: not scored, flagged (no such row, label or id), or scored with k entries.
 enum { kSkip, kFlag, kScore };
 
-// Reads position t's entries into LDS and marks them in the bitmap (bit id of
-// a row's ids); ends with a barrier.
-template <typename L, int NT>
-__device__ __forceinline__ int list_entries(const LossParams<L> &p, int t, LossShared &sh, uint32_t *bits, int &trow) {
-    const int tid = threadIdx.x;
-    const int y = p.labels ? p.labels[t] : 0;
-    if (y < 0) return kSkip;
+// What happens at position t (the same for the whole workgroup), and its teacher row.
+template <typename L> __device__ __forceinline__ int position_state(const LossParams<L> &p, int t, int &y, int &trow) {
+    y = p.labels ? p.labels[t] : 0;
     trow = p.rows ? p.rows[t] : t;
-    if (p.kind == kPolicy ? y >= p.V : (trow < 0 || trow >= p.Tt)) return kFlag;
-    for (int i = tid; i < (p.V + 31) / 32; i += NT) bits[i] = 0;
+    if (y < 0) return kSkip;
+    return (p.kind == kPolicy ? y >= p.V : (trow < 0 || trow >= p.Tt)) ? kFlag : kScore;
+}
+template <typename L> __device__ __forceinline__ int entry_id(const LossParams<L> &p, int j, int y, int trow) {
+    if (j >= p.k) return -1;
+    return p.kind == kPolicy ? y : p.ids[(int64_t)trow * p.k + j];
+}
+// Marks the listed ids in the bitmap (bit id) and keeps them in LDS; sh.bad is
+// set where one is out of range or listed twice.  Thread j brings entry j.
+// Ends with a barrier.
+template <int NT> __device__ __forceinline__ void mark_entries(int id, int k, int V, LossShared &sh, uint32_t *bits) {
+    const int tid = threadIdx.x;
+    for (int i = tid; i < (V + 31) / 32; i += NT) bits[i] = 0;
     if (tid == 0) sh.bad = 0;
     __syncthreads();
-    for (int j = tid; j < p.k; j += NT) {
-        const int id = p.kind == kPolicy ? y : p.ids[(int64_t)trow * p.k + j];
-        float z = 0.f;
-        if (id >= p.V) sh.bad = 1;
-        else if (id >= 0) {
-            z = Piece<L>::one(p.z + (int64_t)t * p.ld + id);
-            if (atomicOr(&bits[id >> 5], 1u << (id & 31)) >> (id & 31) & 1u) sh.bad = 1;   // listed twice
-        }
-        sh.id[j] = id;
-        sh.z[j] = z;
+    if (tid < k) {
+        sh.id[tid] = id;
+        if (id >= V || (id >= 0 && (atomicOr(&bits[id >> 5], 1u << (id & 31)) >> (id & 31) & 1u))) sh.bad = 1;
     }
     __syncthreads();
-    return sh.bad ? kFlag : kScore;
 }
 
 // The bitmap's bits of piece i (bit e: its element e is listed).
@@ -117,9 +118,10 @@ __device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, int tr
         double sum = 0.;
         for (int j = lane; j < p.k; j += 64) if (sh.id[j] >= 0) sum += exp(((double)sh.z[j] - m) * inv);
         sum = wave_sum_f64(sum);
-        const double rest_ref = ref_of(rest.m);
-        const double rest_at = rest.m == -INFINITY ? 0. : exp((rest_ref - m) * inv);   // exp((rest.m - m) / temperature)
-        sum += (double)rest.s * (rest.m == -INFINITY ? 1. : rest_at);
+        // log of the rest's unit (its sum counts multiples of it) over exp(m / temperature)
+        const double unit = is_far(rest.m) ? ((double)rest.m - m) * inv : (double)ref_of(rest.m, p.c) * kLn2 - m * inv;
+        const double rest_at = rest.m == -INFINITY ? 1. : exp(unit);
+        sum += (double)rest.s * rest_at;     // without a rest its sum is 0 (or NaN)
         // of x - m / temperature; a row without any mass has none
         const double lse = m == -INFINITY ? (double)__builtin_nanf("") : log(sum);
         const double g = (p.scale ? (double)p.scale[t] : 1.) * inv;
@@ -149,31 +151,26 @@ __device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, int tr
         } else {
             double f = 0.;
             const float *q = p.q + (int64_t)trow * p.k;
-            for (int j = lane; j < p.k; j += 64) {
-                if (sh.id[j] < 0) continue;
+            // entry k stands for the tokens outside the list
+            for (int j = lane; j < p.k + (p.q_rest ? 1 : 0); j += 64) {
+                const bool out = j == p.k;
+                if (!out && sh.id[j] < 0) continue;
+                double lp = out ? unit + log((double)rest.s) - lse : ((double)sh.z[j] - m) * inv - lse;
+                if (out && rest.s == 0.f) lp = lse == lse ? -INFINITY : lse;
                 double fj, aj;
-                divergence(p.kind, p.beta, ((double)sh.z[j] - m) * inv - lse, (double)q[j], fj, aj);
+                divergence(p.kind, p.beta, lp, out ? (double)p.q_rest[trow] : (double)q[j], fj, aj);
                 f += fj;
                 A += aj;
+                if (out) a_rest = aj;
+                else { sh.a[j] = aj; sh.p[j] = exp(lp); }
             }
             f = wave_sum_f64(f);
             A = wave_sum_f64(A);
-            if (p.q_rest) {
-                double fr;
-                const double lp = rest.s == 0.f ? -INFINITY + lse * 0. : (rest_ref - m) * inv + log((double)rest.s) - lse;
-                divergence(p.kind, p.beta, lp, (double)p.q_rest[trow], fr, a_rest);
-                f += fr;
-                A += a_rest;
-            }
+            a_rest = __shfl(a_rest, p.k & 63);
             if (!(lse == lse)) f = lse;
             if (lane == 0) p.loss[t] = (float)f;
-            for (int j = lane; j < p.k; j += 64) {
-                if (sh.id[j] < 0) continue;
-                double fj, aj;
-                const double lp = ((double)sh.z[j] - m) * inv - lse;
-                divergence(p.kind, p.beta, lp, (double)q[j], fj, aj);
-                sh.patch[j] = (float)(g * (aj - exp(lp) * A));
-            }
+            for (int j = lane; j < p.k; j += 64)
+                if (sh.id[j] >= 0) sh.patch[j] = (float)(g * (sh.a[j] - sh.p[j] * A));
         }
         if (lane == 0) {
             // with no mass outside the list there is nothing to spread there
@@ -189,7 +186,9 @@ __device__ __forceinline__ void fill_row(L *row, int V, float v) {
     float x[Piece<L>::N];
 #pragma unroll
     for (int e = 0; e < Piece<L>::N; ++e) x[e] = v;
-    for (int i = threadIdx.x; i * Piece<L>::N < V; i += NT) store_piece(row, i, V, x);
+    const int whole = V / Piece<L>::N;
+    for (int i = threadIdx.x; i < whole; i += NT) store_piece(row, i, x);
+    if ((int)threadIdx.x == whole % NT) store_last(row, whole, V, x);
 }
 
 // A position that is not scored (zeros) or flagged (NaN).
@@ -201,16 +200,25 @@ __device__ __forceinline__ void put_constant(const LossParams<L> &p, int t, floa
     if (p.kl) p.kl[t] = v;
 }
 
-// One workgroup per position.
-template <typename L, int NT, bool GRAD>
+// One workgroup per position.  Its first NV pieces a thread stay in registers
+// between the two passes; the rest of a longer row is read again.
+template <typename L, int NT, int NV, bool GRAD>
 __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
     constexpr int N = Piece<L>::N;
     extern __shared__ uint32_t bits[];
     __shared__ LossShared sh;
-    const int t = blockIdx.x, tid = threadIdx.x, V = p.V, n = (V + N - 1) / N;
+    const int t = blockIdx.x, tid = threadIdx.x, V = p.V, whole = V / N;
     const L *row = p.z + (int64_t)t * p.ld;
-    int trow = 0;
-    const int what = list_entries<L, NT>(p, t, sh, bits, trow);
+    int y, trow, what = position_state(p, t, y, trow);
+    u32x4 keep[NV ? NV : 1];
+    if (what == kScore) {
+        const int id = entry_id(p, tid, y, trow);
+#pragma unroll
+        for (int j = 0; j < NV; ++j)      // in flight while the entries are marked
+            if (tid + NT * j < whole) keep[j] = load_piece(row, tid + NT * j);
+        mark_entries<NT>(id, p.k, V, sh, bits);
+        if (sh.bad) what = kFlag;
+    }
     if (what != kScore) {
         const float v = what == kSkip ? 0.f : __builtin_nanf("");
         put_constant(p, t, v);
@@ -218,8 +226,7 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
         return;
     }
     MaxSum a{-INFINITY, 0.f};
-    for (int i = tid; i < n; i += NT) {
-        const u32x4 w = load_piece(row, i, V);
+    auto add_piece = [&](u32x4 w, int i) {
         const uint32_t b = listed_bits<N>(bits, i);
         float v[N];
 #pragma unroll
@@ -229,33 +236,73 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
             for (int e = 0; e < N; ++e) if (b >> e & 1u) v[e] = -INFINITY;
         }
         add_values<N>(a, v, p.c);
-    }
+    };
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+        if (tid + NT * j < whole) add_piece(keep[j], tid + NT * j);
+    each_piece<NT, 4>(row, tid + NT * NV, V, add_piece);
+    if (tid < p.k && sh.id[tid] >= 0) sh.z[tid] = Piece<L>::one(row + sh.id[tid]);
     a = block_merge<NT>(a, p.c, sh.red);
+    const bool far = is_far(a.m);
+    if (far) {
+        float s = 0.f;
+        each_piece<NT, 1>(row, tid, V, [&](u32x4 w, int i) {
+            const uint32_t b = listed_bits<N>(bits, i);
+#pragma unroll
+            for (int e = 0; e < N; ++e) if (!(b >> e & 1u)) s += exp_diff(Piece<L>::get(w, e), a.m, p.c);
+        });
+        a.s = (float)block_sum<NT>(s, sh.red);
+    }
     finish_row(p, t, trow, a, sh);
     if (!GRAD) return;
     L *out = p.grad + (int64_t)t * p.ldg;
-    const float coef = sh.coef, m = ref_of(a.m);
-    for (int i = tid; i < n; i += NT) {
-        const u32x4 w = load_piece(row, i, V);
+    const float coef = sh.coef, B = ref_of(a.m, p.c);
+    // c's second float matters to sums only: here it is less than one rounding of each exponent
+    auto put_piece = [&](u32x4 w, int i) {
         float v[N];
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = coef * exp_diff(Piece<L>::get(w, e), m, p.c);
-        store_piece(out, i, V, v);
+        for (int e = 0; e < N; ++e) v[e] = coef * __builtin_amdgcn_exp2f(fmaf(Piece<L>::get(w, e), p.c.hi, -B));
+        if (i < whole) store_piece(out, i, v);
+        else store_last(out, i, V, v);
+    };
+    if (far) {
+        each_piece<NT, 1>(row, tid, V, [&](u32x4 w, int i) {
+            float v[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] = coef * exp_diff(Piece<L>::get(w, e), a.m, p.c);
+            if (i < whole) store_piece(out, i, v);
+            else store_last(out, i, V, v);
+        });
+    } else {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        asm volatile("" : "+v"(keep[j]));   // unpacked again: the first pass' floats would take twice the registers
+        if (tid + NT * j < whole) put_piece(keep[j], tid + NT * j);
+    }
+    each_piece<NT, 4>(row, tid + NT * NV, V, put_piece);
     }
     __syncthreads();   // the listed entries over what the pass above wrote there
-    for (int j = tid; j < p.k; j += NT) if (sh.id[j] >= 0) Piece<L>::put(out + sh.id[j], sh.patch[j]);
+    if (tid < p.k && sh.id[tid] >= 0) Piece<L>::put(out + sh.id[tid], sh.patch[tid]);
 }
 
-template <typename L, int NT> static int launch_rows(const LossParams<L> &p, hipStream_t s) {
+template <typename L, int NT, int NV, bool GRAD> static int launch_rows(const LossParams<L> &p, hipStream_t s) {
     const size_t lds = (size_t)((p.V + 31) / 32) * 4;
-    if (p.grad) hipLaunchKernelGGL((k_opd_loss<L, NT, true>), dim3(p.T), dim3(NT), lds, s, p);
-    else hipLaunchKernelGGL((k_opd_loss<L, NT, false>), dim3(p.T), dim3(NT), lds, s, p);
+    hipLaunchKernelGGL((k_opd_loss<L, NT, NV, GRAD>), dim3(p.T), dim3(NT), lds, s, p);
     return hipGetLastError() == hipSuccess ? PIPO_OK : PIPO_EHIP;
 }
 
 template <typename L> static int launch_loss(const LossParams<L> &p, void *work, int64_t work_bytes, hipStream_t s) {
     (void)work; (void)work_bytes;
-    return p.V > 16384 ? launch_rows<L, 1024>(p, s) : launch_rows<L, 256>(p, s);
+    const int n = (p.V + Piece<L>::N - 1) / Piece<L>::N;
+    if (!p.grad) return p.V > 16384 ? launch_rows<L, 1024, 0, false>(p, s) : launch_rows<L, 256, 0, false>(p, s);
+    if (n <= 256 * 2) return launch_rows<L, 256, 2, true>(p, s);
+    if (n <= 256 * 4) return launch_rows<L, 256, 4, true>(p, s);
+    if (n <= 256 * 8) return launch_rows<L, 256, 8, true>(p, s);
+    if (n <= 512 * 8) return launch_rows<L, 512, 8, true>(p, s);
+    if (n <= 512 * 16) return launch_rows<L, 512, 16, true>(p, s);
+    if (n <= 512 * 24) return launch_rows<L, 512, 24, true>(p, s);
+    if (n <= 512 * 32) return launch_rows<L, 512, 32, true>(p, s);
+    return launch_rows<L, 512, 38, true>(p, s);
 }
 
 // ---- checks ---------------------------------------------------------------------
@@ -274,8 +321,7 @@ static bool same_or_apart(const void *a, int64_t lda, const void *b, int64_t ldb
 
 bool opd_rows_ok(int32_t T, int32_t V, const void *z, int64_t ld, double temperature, size_t es) {
     return T >= 0 && V >= 1 && V <= kOpdMaxVocab && (T <= 1 || (ld >= V && ld <= kOpdMaxStride)) && (T == 0 || (z && aligned(z, es))) &&
-           temperature > 0. && isfinite(temperature) && isfinite(1.4426950408889634 / temperature) &&
-           1.4426950408889634 / temperature < 1e30 && 1.4426950408889634 / temperature > 1e-30;
+           temperature >= 1e-5 && temperature <= 1e5;
 }
 
 template <typename L> static int check_common(const LossParams<L> &p, double temperature) {

@@ -36,38 +36,54 @@ template <> struct Piece<uint16_t> {
     static constexpr uint32_t kNegInf = 0xFF80FF80u;
 };
 
-// Piece i of a row of n elements; the elements behind the row's end read as -inf.
-template <typename L> __device__ __forceinline__ u32x4 load_piece(const L *row, int i, int n) {
+// Piece i of a row, whole; and the last, partial piece of a row of n elements,
+// whose elements behind the row's end read as -inf and are not written.
+template <typename L> __device__ __forceinline__ u32x4 load_piece(const L *row, int i) {
+    return __builtin_nontemporal_load((const typename Piece<L>::raw_t *)(row + (int64_t)i * Piece<L>::N));
+}
+template <typename L> __device__ __forceinline__ void store_piece(L *row, int i, const float *v) {
+    __builtin_nontemporal_store(Piece<L>::pack(v), (typename Piece<L>::raw_t *)(row + (int64_t)i * Piece<L>::N));
+}
+template <typename L> __device__ __forceinline__ u32x4 load_last(const L *row, int i, int n) {
     typedef Piece<L> P;
-    if ((i + 1) * P::N <= n) return __builtin_nontemporal_load((const typename P::raw_t *)(row + (int64_t)i * P::N));
     u32x4 w{P::kNegInf, P::kNegInf, P::kNegInf, P::kNegInf};
-    const int left = n - i * P::N;
 #pragma unroll
     for (int e = 0; e < P::N; ++e) {
-        if (e >= left) continue;
+        if (i * P::N + e >= n) continue;
         if (sizeof(L) == 4) w[e] = ((const uint32_t *)row)[i * P::N + e];
         else if (e & 1) w[e >> 1] = (w[e >> 1] & 0xFFFFu) | ((uint32_t)((const uint16_t *)row)[i * P::N + e] << 16);
         else w[e >> 1] = (w[e >> 1] & 0xFFFF0000u) | ((const uint16_t *)row)[i * P::N + e];
     }
     return w;
 }
-template <typename L> __device__ __forceinline__ void store_piece(L *row, int i, int n, const float *v) {
-    typedef Piece<L> P;
-    if ((i + 1) * P::N <= n) {
-        __builtin_nontemporal_store(P::pack(v), (typename P::raw_t *)(row + (int64_t)i * P::N));
-        return;
-    }
+template <typename L> __device__ __forceinline__ void store_last(L *row, int i, int n, const float *v) {
 #pragma unroll
-    for (int e = 0; e < P::N; ++e)
-        if (i * P::N + e < n) P::put(row + i * P::N + e, v[e]);
+    for (int e = 0; e < Piece<L>::N; ++e)
+        if (i * Piece<L>::N + e < n) Piece<L>::put(row + i * Piece<L>::N + e, v[e]);
+}
+// Calls f(piece, its index) for this thread's pieces from index first on, NT
+// apart and U of them in flight, and for the partial piece, which belongs to the
+// thread whose turn it is.
+template <int NT, int U, typename L, typename F>
+__device__ __forceinline__ void each_piece(const L *row, int first, int n, F f) {
+    const int whole = n / Piece<L>::N;
+    int i = first;
+    for (; i + (U - 1) * NT < whole; i += U * NT) {
+        u32x4 w[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) w[u] = load_piece(row, i + u * NT);
+#pragma unroll
+        for (int u = 0; u < U; ++u) f(w[u], i + u * NT);
+    }
+    for (; i < whole; i += NT) f(load_piece(row, i), i);
+    if (whole * Piece<L>::N < n && first % NT == whole % NT) f(load_last(row, whole, n), whole);
 }
 
-// ---- exp((a - b) / temperature) --------------------------------------------------
-// 2^((a - b) c) with c = log2(e) / temperature in two floats, c rounded down and
-// the (positive) rest: one float of c would tilt every term the same way by up to
-// 2^-24 of its exponent, which sums do not average out.  The difference is taken
-// first, so that rows at the type's lowest value still give exp(0).  a = -inf
-// gives 0 (both products are -inf); a NaN stays one.
+// ---- exp(z / temperature) over a reference -------------------------------------------
+// 2^(z c - B) with c = log2(e) / temperature in two floats, c rounded down and
+// the (positive) rest: one float of c would tilt every term of a sum the same way
+// by up to 2^-24 of its exponent, which does not average out.  B is a float known
+// exactly, so its own rounding costs nothing.  z = -inf gives 0, a NaN stays one.
 struct ExpScale { float hi, lo; double inv; };
 inline ExpScale exp_scale(double temperature) {
     const double c = 1.4426950408889634074 / temperature;
@@ -76,32 +92,41 @@ inline ExpScale exp_scale(double temperature) {
     const float lo = (float)(c - (double)hi);
     return ExpScale{hi, lo > 1e-30f ? lo : 1e-30f, 1.0 / temperature};
 }
+__device__ __forceinline__ float exp_at(float z, float B, ExpScale c) {
+    return __builtin_amdgcn_exp2f(fmaf(z, c.lo, fmaf(z, c.hi, -B)));
+}
+// Logits beyond this in magnitude (masks at the type's lowest value, as a rule)
+// weigh nothing beside smaller ones; a row of nothing else is summed by
+// differences (exp_diff), which its own maximum keeps from overflowing.
+constexpr float kFar = 1e30f;
+__device__ __forceinline__ float ref_of(float m, ExpScale c) {
+#pragma clang fp contract(off)      // the product as the one float that every use of it takes
+    return fmaxf(m, -kFar) * c.hi;
+}
+__device__ __forceinline__ bool is_far(float m) { return m != -INFINITY && !(fabsf(m) <= kFar); }
 __device__ __forceinline__ float exp_diff(float a, float b, ExpScale c) {
     const float d = a - b;
     return __builtin_amdgcn_exp2f(fmaf(d, c.hi, d * c.lo));
 }
 
-// ---- (max, sum of exp((x - max) / temperature)) ------------------------------------
+// ---- (max, sum of 2^(z c - ref_of(max))) ----------------------------------------------
 struct MaxSum { float m, s; };
-// max as a reference: 0 while nothing finite was seen, so that -inf - ref is -inf
-__device__ __forceinline__ float ref_of(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ MaxSum merge(MaxSum a, MaxSum b, ExpScale c) {
-    const float m = fmaxf(a.m, b.m);
-    const float fa = a.m == m ? 1.f : exp_diff(a.m, m, c), fb = b.m == m ? 1.f : exp_diff(b.m, m, c);
-    return MaxSum{m, a.s * fa + b.s * fb};
+    const float m = fmaxf(a.m, b.m), B = ref_of(m, c);
+    return MaxSum{m, a.s * __builtin_amdgcn_exp2f(ref_of(a.m, c) - B) + b.s * __builtin_amdgcn_exp2f(ref_of(b.m, c) - B)};
 }
 template <int N> __device__ __forceinline__ void add_values(MaxSum &a, const float *v, ExpScale c) {
     float m = v[0];
 #pragma unroll
     for (int e = 1; e < N; ++e) m = fmaxf(m, v[e]);
     if (m > a.m) {
-        if (a.m != -INFINITY) a.s *= exp_diff(a.m, m, c);
+        a.s *= __builtin_amdgcn_exp2f(ref_of(a.m, c) - ref_of(m, c));
         a.m = m;
     }
-    const float r = ref_of(a.m);
+    const float B = ref_of(a.m, c);
     float s = 0.f;
 #pragma unroll
-    for (int e = 0; e < N; ++e) s += exp_diff(v[e], r, c);
+    for (int e = 0; e < N; ++e) s += exp_at(v[e], B, c);
     a.s += s;
 }
 // Over a workgroup of NT threads, in a fixed order; every thread gets the result.
@@ -112,6 +137,17 @@ template <int NT> __device__ __forceinline__ MaxSum block_merge(MaxSum a, ExpSca
     __syncthreads();
     MaxSum r = s_red[0];
     for (int w = 1; w < NT / 64; ++w) r = merge(r, s_red[w], c);
+    return r;
+}
+// The sum over a workgroup of NT threads, in a fixed order and 64 bits across waves.
+template <int NT> __device__ __forceinline__ double block_sum(float v, MaxSum *s_red) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) s_red[threadIdx.x >> 6].s = v;
+    __syncthreads();
+    double r = 0.;
+    for (int w = 0; w < NT / 64; ++w) r += (double)s_red[w].s;
     return r;
 }
 __device__ __forceinline__ double wave_sum_f64(double v) {

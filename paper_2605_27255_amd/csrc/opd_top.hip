@@ -21,6 +21,8 @@ namespace pipo {
 constexpr int kTopMax = 256;        // k
 constexpr int kTopCand = 2048;      // candidates ranked
 
+constexpr double kLn2 = 0.69314718055994530942;
+
 bool opd_rows_ok(int32_t T, int32_t V, const void *z, int64_t ld, double temperature, size_t es);
 
 template <typename L> struct TopParams {
@@ -88,7 +90,7 @@ __device__ __forceinline__ uint32_t bound_of_kth(TopShared<NT> &sh, uint32_t lo,
 }
 
 template <typename L, int NT>
-__global__ __launch_bounds__(NT) void k_opd_top(TopParams<L> p) {
+__global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
     constexpr int N = Piece<L>::N, W = NT / 64;
     __shared__ TopShared<NT> sh;
     const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -96,13 +98,12 @@ __global__ __launch_bounds__(NT) void k_opd_top(TopParams<L> p) {
     const L *row = p.z + (int64_t)t * p.ld;
 
     MaxSum own{-INFINITY, 0.f};
-    for (int i = tid; i < n; i += NT) {
-        const u32x4 w = load_piece(row, i, V);
+    each_piece<NT, 4>(row, tid, V, [&](u32x4 w, int) {
         float v[N];
 #pragma unroll
         for (int e = 0; e < N; ++e) v[e] = Piece<L>::get(w, e);
         add_values<N>(own, v, p.c);
-    }
+    });
     const uint32_t mine = tid < n ? value_key(own.m) : 0u;
     sh.tmax[tid] = mine;
     uint32_t least = tid < n ? mine : 0xFFFFFFFFu;
@@ -111,7 +112,9 @@ __global__ __launch_bounds__(NT) void k_opd_top(TopParams<L> p) {
     if (lane == 0) sh.wmin[wave] = least;
     if (tid == 0) sh.n = 0;
     const MaxSum all = block_merge<NT>(own, p.c, sh.red);   // its barrier: tmax, wmin and n are set
-    const float m = ref_of(all.m);
+    const bool far = is_far(all.m);
+    const float B = ref_of(all.m, p.c);
+    auto term = [&](float v) { return far ? exp_diff(v, all.m, p.c) : exp_at(v, B, p.c); };
     for (int w = 0; w < W; ++w) least = min(least, sh.wmin[w]);
     // fewer pieces than k: everything is a candidate
     const uint32_t bound = n < k ? 0u : bound_of_kth<NT>(sh, least, value_key(all.m), k);
@@ -130,12 +133,12 @@ __global__ __launch_bounds__(NT) void k_opd_top(TopParams<L> p) {
     uint32_t *list = sh.tmax;       // every wave is past the search: its entries become the picked threads
     if (picked) list[at + __popcll(ball & ((1ull << lane) - 1))] = tid;
     __syncthreads();
-    float rest = picked ? 0.f : own.s * (own.m == -INFINITY ? 1.f : exp_diff(own.m, m, p.c));
+    float rest = picked ? 0.f : own.s * __builtin_amdgcn_exp2f(ref_of(own.m, p.c) - B);
     const int per = (n + NT - 1) / NT;
     for (int x = tid; x < total * per; x += NT) {
         const int i = (int)list[x / per] + NT * (x % per);
         if (i >= n) continue;
-        const u32x4 w = load_piece(row, i, V);
+        const u32x4 w = i < V / N ? load_piece(row, i) : load_last(row, i, V);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             const float v = Piece<L>::get(w, e);
@@ -144,13 +147,14 @@ __global__ __launch_bounds__(NT) void k_opd_top(TopParams<L> p) {
                 const int c = atomicAdd(&sh.n, 1);
                 if (c < kTopCand) sh.cand[c] = pair_key(key, i * N + e);
             } else {
-                rest += exp_diff(v, m, p.c);
+                rest += term(v);
             }
         }
     }
     __syncthreads();
     int nc = sh.n;
-    if (nc > kTopCand || nc < k) {  // too many (ties), or NaNs, which no maximum sees: select among all keys
+    if (nc > kTopCand || nc < k || far) {   // too many (ties), or NaNs, which no maximum sees, or sums that do not fit:
+                                            // select among all keys
         uint64_t thr = 0;           // keys at or above thr, of which the first `bits` bits are settled
         int need = k;
         for (int bits = 8; bits <= 64; bits += 8) {
@@ -158,8 +162,7 @@ __global__ __launch_bounds__(NT) void k_opd_top(TopParams<L> p) {
             __syncthreads();
             for (int i = tid; i < 256; i += NT) sh.hist[i] = 0;
             __syncthreads();
-            for (int i = tid; i < n; i += NT) {
-                const u32x4 w = load_piece(row, i, V);
+            each_piece<NT, 4>(row, tid, V, [&](u32x4 w, int i) {
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     if (i * N + e >= V) continue;
@@ -174,7 +177,7 @@ __global__ __launch_bounds__(NT) void k_opd_top(TopParams<L> p) {
                         atomicAdd(&sh.hist[bin], 1);
                     }
                 }
-            }
+            });
             __syncthreads();
             if (tid == 0) {
                 int b = 255, above = 0;
@@ -191,17 +194,16 @@ __global__ __launch_bounds__(NT) void k_opd_top(TopParams<L> p) {
         if (tid == 0) sh.n = 0;
         __syncthreads();
         rest = 0.f;
-        for (int i = tid; i < n; i += NT) {
-            const u32x4 w = load_piece(row, i, V);
+        each_piece<NT, 4>(row, tid, V, [&](u32x4 w, int i) {
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 if (i * N + e >= V) continue;
                 const float v = Piece<L>::get(w, e);
                 const uint64_t key = pair_key(value_key(v), i * N + e);
                 if (key >= thr) sh.cand[atomicAdd(&sh.n, 1)] = key;
-                else rest += exp_diff(v, m, p.c);
+                else rest += term(v);
             }
-        }
+        });
         __syncthreads();
         nc = sh.n;
     }
@@ -213,15 +215,12 @@ __global__ __launch_bounds__(NT) void k_opd_top(TopParams<L> p) {
         sh.sorted[rank] = key;
     }
     __syncthreads();
-    for (int j = k + tid; j < nc; j += NT) rest += exp_diff(key_value((uint32_t)(sh.sorted[j] >> 32)), m, p.c);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) rest += __shfl_xor(rest, o);
-    __syncthreads();
-    if (lane == 0) sh.red[wave].s = rest;
-    __syncthreads();
+    for (int j = k + tid; j < nc; j += NT) rest += term(key_value((uint32_t)(sh.sorted[j] >> 32)));
+    double outside = block_sum<NT>(rest, sh.red);
     if (wave != 0) return;
-    double outside = 0., sum = 0.;
-    for (int w = 0; w < W; ++w) outside += (double)sh.red[w].s;
+    // in multiples of exp(max / temperature)
+    if (!far && all.m != -INFINITY) outside *= exp((double)B * kLn2 - (double)all.m * p.c.inv);
+    double sum = 0.;
     for (int j = lane; j < k; j += 64)
         sum += exp(((double)key_value((uint32_t)(sh.sorted[j] >> 32)) - (double)all.m) * p.c.inv);
     const double lse = log(wave_sum_f64(sum) + outside);    // of x - max / temperature
