@@ -43,7 +43,6 @@ template <typename L> struct LossParams {
 constexpr int kPolicy = 3;
 
 struct LossShared {
-    MaxSum red[16];
     int id[kEntries];               // listed ids, -1: an empty slot
     float z[kEntries];              // their logits
     double a[kEntries], p[kEntries];   // their a = p df/dp, and p
@@ -112,9 +111,9 @@ __device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, int tr
     if (threadIdx.x < 64) {
         const int lane = threadIdx.x;
         const double inv = p.c.inv;
-        double m = rest.m;
-        for (int j = lane; j < p.k; j += 64) if (sh.id[j] >= 0) m = fmax(m, (double)sh.z[j]);
-        for (int o = 32; o > 0; o >>= 1) m = fmax(m, __shfl_xor(m, o));
+        float top = rest.m;
+        for (int j = lane; j < p.k; j += 64) if (sh.id[j] >= 0) top = fmaxf(top, sh.z[j]);
+        const double m = wave_max_dpp(top);
         double sum = 0.;
         for (int j = lane; j < p.k; j += 64) if (sh.id[j] >= 0) sum += exp(((double)sh.z[j] - m) * inv);
         sum = wave_sum_f64(sum);
@@ -166,7 +165,7 @@ __device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, int tr
             }
             f = wave_sum_f64(f);
             A = wave_sum_f64(A);
-            a_rest = __shfl(a_rest, p.k & 63);
+            a_rest = readlane_f64(a_rest, p.k & 63);
             if (!(lse == lse)) f = lse;
             if (lane == 0) p.loss[t] = (float)f;
             for (int j = lane; j < p.k; j += 64)
@@ -207,10 +206,12 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
     constexpr int N = Piece<L>::N;
     extern __shared__ uint32_t bits[];
     __shared__ LossShared sh;
+    __shared__ float red[3][NT / 64];
     const int t = blockIdx.x, tid = threadIdx.x, V = p.V, whole = V / N;
     const L *row = p.z + (int64_t)t * p.ld;
     int y, trow, what = position_state(p, t, y, trow);
     u32x4 keep[NV ? NV : 1];
+    float zj = 0.f;
     if (what == kScore) {
         const int id = entry_id(p, tid, y, trow);
 #pragma unroll
@@ -218,6 +219,7 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
             if (tid + NT * j < whole) keep[j] = load_piece(row, tid + NT * j);
         mark_entries<NT>(id, p.k, V, sh, bits);
         if (sh.bad) what = kFlag;
+        else if (id >= 0) zj = Piece<L>::one(row + id);
     }
     if (what != kScore) {
         const float v = what == kSkip ? 0.f : __builtin_nanf("");
@@ -241,8 +243,8 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
     for (int j = 0; j < NV; ++j)
         if (tid + NT * j < whole) add_piece(keep[j], tid + NT * j);
     each_piece<NT, 4>(row, tid + NT * NV, V, add_piece);
-    if (tid < p.k && sh.id[tid] >= 0) sh.z[tid] = Piece<L>::one(row + sh.id[tid]);
-    a = block_merge<NT>(a, p.c, sh.red);
+    if (tid < p.k) sh.z[tid] = zj;
+    a = block_merge<NT>(a, p.c, red);
     const bool far = is_far(a.m);
     if (far) {
         float s = 0.f;
@@ -251,7 +253,7 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
 #pragma unroll
             for (int e = 0; e < N; ++e) if (!(b >> e & 1u)) s += exp_diff(Piece<L>::get(w, e), a.m, p.c);
         });
-        a.s = (float)block_sum<NT>(s, sh.red);
+        a.s = (float)block_sum<NT>(s, red[2]);
     }
     finish_row(p, t, trow, a, sh);
     if (!GRAD) return;
@@ -294,7 +296,10 @@ template <typename L, int NT, int NV, bool GRAD> static int launch_rows(const Lo
 template <typename L> static int launch_loss(const LossParams<L> &p, void *work, int64_t work_bytes, hipStream_t s) {
     (void)work; (void)work_bytes;
     const int n = (p.V + Piece<L>::N - 1) / Piece<L>::N;
-    if (!p.grad) return p.V > 16384 ? launch_rows<L, 1024, 0, false>(p, s) : launch_rows<L, 256, 0, false>(p, s);
+    if (!p.grad) {
+        if (n <= 256 * 32) return launch_rows<L, 256, 0, false>(p, s);
+        return launch_rows<L, 512, 0, false>(p, s);
+    }
     if (n <= 256 * 2) return launch_rows<L, 256, 2, true>(p, s);
     if (n <= 256 * 4) return launch_rows<L, 256, 4, true>(p, s);
     if (n <= 256 * 8) return launch_rows<L, 256, 8, true>(p, s);

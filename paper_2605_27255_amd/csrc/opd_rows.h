@@ -111,10 +111,6 @@ __device__ __forceinline__ float exp_diff(float a, float b, ExpScale c) {
 
 // ---- (max, sum of 2^(z c - ref_of(max))) ----------------------------------------------
 struct MaxSum { float m, s; };
-__device__ __forceinline__ MaxSum merge(MaxSum a, MaxSum b, ExpScale c) {
-    const float m = fmaxf(a.m, b.m), B = ref_of(m, c);
-    return MaxSum{m, a.s * __builtin_amdgcn_exp2f(ref_of(a.m, c) - B) + b.s * __builtin_amdgcn_exp2f(ref_of(b.m, c) - B)};
-}
 template <int N> __device__ __forceinline__ void add_values(MaxSum &a, const float *v, ExpScale c) {
     float m = v[0];
 #pragma unroll
@@ -129,31 +125,64 @@ template <int N> __device__ __forceinline__ void add_values(MaxSum &a, const flo
     for (int e = 0; e < N; ++e) s += exp_at(v[e], B, c);
     a.s += s;
 }
-// Over a workgroup of NT threads, in a fixed order; every thread gets the result.
-template <int NT> __device__ __forceinline__ MaxSum block_merge(MaxSum a, ExpScale c, MaxSum *s_red) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) a = merge(a, MaxSum{__shfl_xor(a.m, o), __shfl_xor(a.s, o)}, c);
-    if ((threadIdx.x & 63) == 0) s_red[threadIdx.x >> 6] = a;
-    __syncthreads();
-    MaxSum r = s_red[0];
-    for (int w = 1; w < NT / 64; ++w) r = merge(r, s_red[w], c);
-    return r;
+// ---- reductions without LDS traffic inside a wave ------------------------------------------
+// DPP within each row of 16 lanes (pairs, quads, half rows, rows), then the four
+// rows' values through scalar registers; every lane gets the result, added in
+// the same order in every lane.
+__device__ __forceinline__ float wave_max_dpp(float v) {
+    v = fmaxf(v, PIPO_DPP(v, 0xB1));
+    v = fmaxf(v, PIPO_DPP(v, 0x4E));
+    v = fmaxf(v, PIPO_DPP(v, 0x141));
+    v = fmaxf(v, PIPO_DPP(v, 0x140));
+    const int u = __float_as_int(v);
+    return fmaxf(fmaxf(__int_as_float(__builtin_amdgcn_readlane(u, 0)), __int_as_float(__builtin_amdgcn_readlane(u, 16))),
+                 fmaxf(__int_as_float(__builtin_amdgcn_readlane(u, 32)), __int_as_float(__builtin_amdgcn_readlane(u, 48))));
 }
-// The sum over a workgroup of NT threads, in a fixed order and 64 bits across waves.
-template <int NT> __device__ __forceinline__ double block_sum(float v, MaxSum *s_red) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) s_red[threadIdx.x >> 6].s = v;
-    __syncthreads();
-    double r = 0.;
-    for (int w = 0; w < NT / 64; ++w) r += (double)s_red[w].s;
-    return r;
+template <int CTRL> __device__ __forceinline__ double dpp_f64(double v) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)u, CTRL, 0xF, 0xF, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)(u >> 32), CTRL, 0xF, 0xF, false);
+    return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+}
+__device__ __forceinline__ double readlane_f64(double v, int lane) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, lane);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), lane);
+    return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
 }
 __device__ __forceinline__ double wave_sum_f64(double v) {
+    v += dpp_f64<0xB1>(v);
+    v += dpp_f64<0x4E>(v);
+    v += dpp_f64<0x141>(v);
+    v += dpp_f64<0x140>(v);
+    return (readlane_f64(v, 0) + readlane_f64(v, 16)) + (readlane_f64(v, 32) + readlane_f64(v, 48));
+}
+
+// ---- over a workgroup of NT threads, in a fixed order; every thread gets the result ----------
+// (a value per wave in s_w[NT / 64]; ends with every wave past its reads of what it wrote before)
+template <int NT> __device__ __forceinline__ float block_max(float v, float *s_w) {
+    v = wave_max_dpp(v);
+    if ((threadIdx.x & 63) == 0) s_w[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = s_w[0];
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    for (int w = 1; w < NT / 64; ++w) v = fmaxf(v, s_w[w]);
     return v;
+}
+template <int NT> __device__ __forceinline__ double block_sum(float v, float *s_w) {
+    v = wave_sum_dpp(v);
+    if ((threadIdx.x & 63) == 0) s_w[threadIdx.x >> 6] = v;
+    __syncthreads();
+    double r = 0.;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) r += (double)s_w[w];
+    return r;
+}
+// The threads' (max, sum) as one: the sum in 64 bits across waves.  s_w: NT / 64 each for the maxima and the sums.
+template <int NT> __device__ __forceinline__ MaxSum block_merge(MaxSum a, ExpScale c, float (*s_w)[NT / 64]) {
+    const float m = block_max<NT>(a.m, s_w[0]);
+    const float s = a.s * __builtin_amdgcn_exp2f(ref_of(a.m, c) - ref_of(m, c));
+    return MaxSum{m, (float)block_sum<NT>(s, s_w[1])};
 }
 
 }  // namespace pipo

@@ -50,41 +50,41 @@ template <int NT> struct TopShared {
     uint32_t tmax[NT];              // each thread's largest value key, 0: no pieces
     uint64_t cand[kTopCand];
     uint64_t sorted[kTopCand];
-    MaxSum red[NT / 64];
+    float red[3][NT / 64];
     uint32_t wmin[NT / 64];
-    int count[NT / 64];
+    int count[2][NT / 64], wcount[NT / 64];
     int hist[256];
     int n, bin, above;
 };
 
-// The largest bound found for which at least k of the NT keys reach it: each
-// round every wave counts the keys at or above a pivot of its own, so a round
-// cuts the range by the number of waves plus one.  lo is reached by at least k.
+// A bound that at least k of the NT keys reach, and few more: each round every
+// wave counts the keys at or above a pivot of its own, so a round cuts the range
+// by the number of waves plus one.  lo is reached by at least k, none is above hi.
 template <int NT>
 __device__ __forceinline__ uint32_t bound_of_kth(TopShared<NT> &sh, uint32_t lo, uint32_t hi, int k) {
     constexpr int W = NT / 64;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    while (lo < hi) {
+    uint32_t key[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) key[i] = sh.tmax[i * 64 + lane];
+    for (int round = 0; lo < hi; ++round) {
         const uint64_t span = (uint64_t)(hi - lo) + 1;
         const uint32_t pivot = lo + (uint32_t)(span * (wave + 1) / (W + 1));
         int n = 0;
 #pragma unroll
-        for (int i = 0; i < NT / 64; ++i) n += __popcll(__ballot(sh.tmax[i * 64 + lane] >= pivot));
-        __syncthreads();            // the counts of the round before were read
-        if (lane == 0) sh.count[wave] = n;
+        for (int i = 0; i < W; ++i) n += __popcll(__ballot(key[i] >= pivot));
+        int *count = sh.count[round & 1];   // the other half is still read
+        if (lane == 0) count[wave] = n;
         __syncthreads();
-        uint32_t new_lo = lo, new_hi = hi;
-        int reach = NT;
-        for (int w = 0; w < W; ++w) {
-            const uint32_t pw = lo + (uint32_t)(span * (w + 1) / (W + 1));
-            if (sh.count[w] >= k) { new_lo = pw; reach = sh.count[w]; }
-            else { new_hi = pw - 1; break; }
+        // counts fall with the pivot: the last wave whose pivot k keys reach, and the one after it
+        const int c = count[lane & (W - 1)];
+        const int reach = __popcll(__ballot(lane < W && c >= k));
+        const uint32_t base = lo;
+        if (reach < W) hi = base + (uint32_t)(span * (reach + 1) / (W + 1)) - 1;
+        if (reach > 0) {
+            lo = base + (uint32_t)(span * reach / (W + 1));
+            if (__builtin_amdgcn_readlane(c, reach - 1) <= k + (k >> 2) + 8) break;
         }
-        // a span below the number of pivots repeats them; the last one always shrinks the range
-        if (new_lo == lo && new_hi == hi) break;
-        lo = new_lo;
-        hi = new_hi;
-        if (reach <= k + (k >> 2) + 8) break;
     }
     return lo;
 }
@@ -106,31 +106,33 @@ __global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
     });
     const uint32_t mine = tid < n ? value_key(own.m) : 0u;
     sh.tmax[tid] = mine;
-    uint32_t least = tid < n ? mine : 0xFFFFFFFFu;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) least = min(least, (uint32_t)__shfl_xor((int)least, o));
-    if (lane == 0) sh.wmin[wave] = least;
+    // the least of them, as the largest of the negated maxima (-0 and 0 have one key)
+    const float least_w = -wave_max_dpp(tid < n ? -own.m : -INFINITY);
+    if (lane == 0) sh.wmin[wave] = value_key(least_w);
     if (tid == 0) sh.n = 0;
     const MaxSum all = block_merge<NT>(own, p.c, sh.red);   // its barrier: tmax, wmin and n are set
     const bool far = is_far(all.m);
     const float B = ref_of(all.m, p.c);
     auto term = [&](float v) { return far ? exp_diff(v, all.m, p.c) : exp_at(v, B, p.c); };
-    for (int w = 0; w < W; ++w) least = min(least, sh.wmin[w]);
+    uint32_t least = sh.wmin[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) least = min(least, sh.wmin[w]);
     // fewer pieces than k: everything is a candidate
     const uint32_t bound = n < k ? 0u : bound_of_kth<NT>(sh, least, value_key(all.m), k);
 
     // the pieces of the threads that reach the bound, again
     const bool picked = mine >= bound && tid < n;
     const uint64_t ball = __ballot(picked);
-    __syncthreads();
-    if (lane == 0) sh.count[wave] = __popcll(ball);
-    __syncthreads();
+    if (lane == 0) sh.wcount[wave] = __popcll(ball);
+    __syncthreads();                // every wave is past the search: its keys become the picked threads
     int at = 0, total = 0;
+#pragma unroll
     for (int w = 0; w < W; ++w) {
-        if (w < wave) at += sh.count[w];
-        total += sh.count[w];
+        const int c = sh.wcount[w];
+        if (w < wave) at += c;
+        total += c;
     }
-    uint32_t *list = sh.tmax;       // every wave is past the search: its entries become the picked threads
+    uint32_t *list = sh.tmax;
     if (picked) list[at + __popcll(ball & ((1ull << lane) - 1))] = tid;
     __syncthreads();
     float rest = picked ? 0.f : own.s * __builtin_amdgcn_exp2f(ref_of(own.m, p.c) - B);
@@ -216,7 +218,7 @@ __global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
     }
     __syncthreads();
     for (int j = k + tid; j < nc; j += NT) rest += term(key_value((uint32_t)(sh.sorted[j] >> 32)));
-    double outside = block_sum<NT>(rest, sh.red);
+    double outside = block_sum<NT>(rest, sh.red[2]);
     if (wave != 0) return;
     // in multiples of exp(max / temperature)
     if (!far && all.m != -INFINITY) outside *= exp((double)B * kLn2 - (double)all.m * p.c.inv);
