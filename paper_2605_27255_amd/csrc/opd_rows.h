@@ -7,6 +7,16 @@
 
 namespace pipo {
 
+constexpr double kLn2 = 0.69314718055994530942;
+constexpr int kOpdMaxVocab = 1 << 19;
+constexpr int kMaxParts = 64;       // workgroups of a split row: a lane of a wave joins each
+struct Part { float m, s; int bad, pad; };      // what a segment of a row leaves for the others
+
+// ---- checks on the host, shared by the entry points ---------------------------------
+bool opd_rows_ok(int32_t T, int32_t V, const void *z, int64_t ld, double temperature, size_t es);
+bool opd_work_ok(const void *work, int64_t work_bytes, int64_t need);
+int64_t opd_loss_work_bytes(int T, int V, int k);
+
 // ---- 16 bytes of a row --------------------------------------------------------
 // Rows start at any multiple of the element size (odd vocabularies, padded or
 // sliced rows): the pieces are loaded and stored as 16 bytes all the same,
@@ -61,21 +71,26 @@ template <typename L> __device__ __forceinline__ void store_last(L *row, int i, 
     for (int e = 0; e < Piece<L>::N; ++e)
         if (i * Piece<L>::N + e < n) Piece<L>::put(row + i * Piece<L>::N + e, v[e]);
 }
-// Calls f(piece, its index) for this thread's pieces from index first on, NT
-// apart and U of them in flight, and for the partial piece, which belongs to the
-// thread whose turn it is.
+// Calls f(piece, its index) for this thread's whole pieces from index first up to
+// end, NT apart and U of them in flight.
 template <int NT, int U, typename L, typename F>
-__device__ __forceinline__ void each_piece(const L *row, int first, int n, F f) {
-    const int whole = n / Piece<L>::N;
+__device__ __forceinline__ void whole_pieces(const L *row, int first, int end, F f) {
     int i = first;
-    for (; i + (U - 1) * NT < whole; i += U * NT) {
+    for (; i + (U - 1) * NT < end; i += U * NT) {
         u32x4 w[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) w[u] = load_piece(row, i + u * NT);
 #pragma unroll
         for (int u = 0; u < U; ++u) f(w[u], i + u * NT);
     }
-    for (; i < whole; i += NT) f(load_piece(row, i), i);
+    for (; i < end; i += NT) f(load_piece(row, i), i);
+}
+// ... of a row of n elements, and the partial piece at its end, which belongs to
+// the thread whose turn it is.
+template <int NT, int U, typename L, typename F>
+__device__ __forceinline__ void each_piece(const L *row, int first, int n, F f) {
+    const int whole = n / Piece<L>::N;
+    whole_pieces<NT, U>(row, first, whole, f);
     if (whole * Piece<L>::N < n && first % NT == whole % NT) f(load_last(row, whole, n), whole);
 }
 
@@ -183,6 +198,20 @@ template <int NT> __device__ __forceinline__ MaxSum block_merge(MaxSum a, ExpSca
     const float m = block_max<NT>(a.m, s_w[0]);
     const float s = a.s * __builtin_amdgcn_exp2f(ref_of(a.m, c) - ref_of(m, c));
     return MaxSum{m, (float)block_sum<NT>(s, s_w[1])};
+}
+
+// A row's segments as one (max, sum), in every lane.
+__device__ __forceinline__ MaxSum join_parts(const Part *part, int S, ExpScale c, bool &bad) {
+    const int lane = threadIdx.x & 63;
+    Part x{-INFINITY, 0.f, 0, 0};
+    if (lane < S) x = part[lane];
+    bad = __ballot(x.bad != 0) != 0;
+    const float m = wave_max_dpp(x.m);
+    // beside a far maximum, and beside a near one where they are far, the other segments weigh nothing
+    const bool far = is_far(m);
+    float f = far ? (x.m == m ? 1.f : exp_diff(x.m, m, c)) : __builtin_amdgcn_exp2f(ref_of(x.m, c) - ref_of(m, c));
+    if (!far && is_far(x.m)) f = 0.f;
+    return MaxSum{m, (float)wave_sum_f64((double)x.s * (double)f)};
 }
 
 }  // namespace pipo

@@ -1,17 +1,19 @@
 // The k largest logits of each row, in the order of (value descending, id
 // ascending), with their log-probabilities and the log of the mass outside.
 //
-// One pass over the row: every thread keeps the maximum and the sum of
-// exponentials of its own pieces.  A value that at least k threads' maxima
-// reach is a lower bound of the k-th largest logit, so only those threads'
-// pieces can hold the k largest: they are read again (about k of 1024 threads,
-// from the caches), and what reaches the bound, usually little more than k
-// values, is ranked by counting.  Threads that hold none of the k keep their
-// sums; the others' are added up again without them, so that the mass outside
+// One pass over the row, which is dealt into units of pieces, two to a thread:
+// each has its maximum and its sum of exponentials.  A value that at least k
+// maxima reach is a lower bound of the k-th largest logit, so only those units
+// can hold the k largest: they are read again (about k of 1024, from the
+// caches), and what reaches the bound, usually little more than k values, is
+// ranked by counting.  Units that hold none of the k keep their sums; the
+// others' are added up again without them, so that the mass outside
 // the list is a sum of what is outside, not a difference.
 // Rows whose values crowd at the bound (constant rows, long ties) overflow the
 // candidate array; a radix select over (value, id) keys, which are all
 // different, then narrows the row to what fits.
+// Where there are too few rows for the chip, each is split over several
+// workgroups, and a last one picks the row's k among the segments' lists.
 // HBM-bound: V logits read per row.
 #include "opd_rows.h"
 #include "pipo.h"
@@ -19,17 +21,19 @@
 namespace pipo {
 
 constexpr int kTopMax = 256;        // k
-constexpr int kTopCand = 2048;      // candidates ranked
-
-constexpr double kLn2 = 0.69314718055994530942;
-
-bool opd_rows_ok(int32_t T, int32_t V, const void *z, int64_t ld, double temperature, size_t es);
+constexpr int kTopCand = 1024;      // candidates ranked
+constexpr int kUnits = 2;           // units of a row to a thread
+constexpr int kJoinThreads = 1024;
 
 template <typename L> struct TopParams {
     const L *z; int64_t ld;
     int T, V, k;
     ExpScale c;
     int32_t *ids; float *logp, *tail;
+    // of a split row: S segments of seg elements, each with a sorted list of k keys (0: none) and its other values' sum
+    int S, seg;
+    Part *part;                     // [T][S]
+    uint64_t *keys;                 // [T][S][k]
 };
 
 // Unsigned integers in the order of the values; -0 counts as 0.
@@ -46,8 +50,8 @@ __device__ __forceinline__ uint64_t pair_key(uint32_t vkey, int id) {
 }
 __device__ __forceinline__ int key_id(uint64_t k) { return (int)~(uint32_t)k; }
 
-template <int NT> struct TopShared {
-    uint32_t tmax[NT];              // each thread's largest value key, 0: no pieces
+template <int NT, int H> struct TopShared {
+    uint32_t umax[NT * H];          // each unit's largest value key, 0: no pieces
     uint64_t cand[kTopCand];
     uint64_t sorted[kTopCand];
     float red[3][NT / 64];
@@ -57,22 +61,22 @@ template <int NT> struct TopShared {
     int n, bin, above;
 };
 
-// A bound that at least k of the NT keys reach, and few more: each round every
+// A bound that at least k of the keys in sh.umax reach, and few more: each round every
 // wave counts the keys at or above a pivot of its own, so a round cuts the range
 // by the number of waves plus one.  lo is reached by at least k, none is above hi.
-template <int NT>
-__device__ __forceinline__ uint32_t bound_of_kth(TopShared<NT> &sh, uint32_t lo, uint32_t hi, int k) {
+template <int NT, int H>
+__device__ __forceinline__ uint32_t bound_of_kth(TopShared<NT, H> &sh, uint32_t lo, uint32_t hi, int k) {
     constexpr int W = NT / 64;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    uint32_t key[W];
+    uint32_t key[W * H];
 #pragma unroll
-    for (int i = 0; i < W; ++i) key[i] = sh.tmax[i * 64 + lane];
+    for (int i = 0; i < W * H; ++i) key[i] = sh.umax[i * 64 + lane];
     for (int round = 0; lo < hi; ++round) {
         const uint64_t span = (uint64_t)(hi - lo) + 1;
         const uint32_t pivot = lo + (uint32_t)(span * (wave + 1) / (W + 1));
         int n = 0;
 #pragma unroll
-        for (int i = 0; i < W; ++i) n += __popcll(__ballot(key[i] >= pivot));
+        for (int i = 0; i < W * H; ++i) n += __popcll(__ballot(key[i] >= pivot));
         int *count = sh.count[round & 1];   // the other half is still read
         if (lane == 0) count[wave] = n;
         __syncthreads();
@@ -89,25 +93,75 @@ __device__ __forceinline__ uint32_t bound_of_kth(TopShared<NT> &sh, uint32_t lo,
     return lo;
 }
 
-template <typename L, int NT>
-__global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
-    constexpr int N = Piece<L>::N, W = NT / 64;
-    __shared__ TopShared<NT> sh;
-    const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int V = p.V, k = p.k, n = (V + N - 1) / N;
-    const L *row = p.z + (int64_t)t * p.ld;
+// Sorts sh.cand[0, nc) into sh.sorted: ranked by counting the larger ones.
+template <int NT, int H> __device__ __forceinline__ void sort_candidates(TopShared<NT, H> &sh, int nc) {
+    for (int i = threadIdx.x; i < nc; i += NT) {
+        const uint64_t key = sh.cand[i];
+        int rank = 0;
+#pragma unroll 8
+        for (int j = 0; j < nc; ++j) rank += sh.cand[j] > key;
+        sh.sorted[rank] = key;
+    }
+    __syncthreads();
+}
+// The row's outputs, by its first wave: sorted[0, k) are the k largest, `outside` the sum of exp((z - m) / temperature) of all others.
+template <typename L>
+__device__ __forceinline__ void put_top(const TopParams<L> &p, int t, const uint64_t *sorted, float m, double outside) {
+    const int lane = threadIdx.x;
+    double sum = 0.;
+    for (int j = lane; j < p.k; j += 64)
+        sum += exp(((double)key_value((uint32_t)(sorted[j] >> 32)) - (double)m) * p.c.inv);
+    const double lse = log(wave_sum_f64(sum) + outside);    // of x - m / temperature
+    for (int j = lane; j < p.k; j += 64) {
+        const uint64_t key = sorted[j];
+        p.ids[(int64_t)t * p.k + j] = key_id(key);
+        p.logp[(int64_t)t * p.k + j] = (float)(((double)key_value((uint32_t)(key >> 32)) - (double)m) * p.c.inv - lse);
+    }
+    if (lane == 0 && p.tail) p.tail[t] = (float)(log(outside) - lse);
+}
+// A sum in units of 2^ref_of(m) (or, far, of exp(m / temperature)) in units of exp(m / temperature).
+__device__ __forceinline__ double unit_of_max(float m, ExpScale c) {
+    return is_far(m) || m == -INFINITY ? 1. : exp((double)ref_of(m, c) * kLn2 - (double)m * c.inv);
+}
 
-    MaxSum own{-INFINITY, 0.f};
-    each_piece<NT, 4>(row, tid, V, [&](u32x4 w, int) {
-        float v[N];
+// One workgroup per row, or (SPLIT) per segment of one.
+template <typename L, int NT, bool SPLIT>
+__global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
+    constexpr int N = Piece<L>::N, W = NT / 64, H = kUnits;
+    __shared__ TopShared<NT, H> sh;
+    const int t = SPLIT ? blockIdx.x / p.S : blockIdx.x, seg = SPLIT ? blockIdx.x % p.S : 0;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int lo = seg * p.seg, V = min(p.seg, p.V - lo), k = min(p.k, V), n = (V + N - 1) / N, whole = V / N;
+    const L *row = p.z + (int64_t)t * p.ld + lo;
+
+    // unit h NT + tid: the pieces tid + NT j for j from h per on, per of them
+    const int per = (n + NT * H - 1) / (NT * H);
+    MaxSum unit[H], own{-INFINITY, 0.f};
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = Piece<L>::get(w, e);
-        add_values<N>(own, v, p.c);
-    });
-    const uint32_t mine = tid < n ? value_key(own.m) : 0u;
-    sh.tmax[tid] = mine;
+    for (int h = 0; h < H; ++h) {
+        unit[h] = MaxSum{-INFINITY, 0.f};
+        const int first = tid + h * per * NT, end = (h + 1) * per * NT;
+        auto add = [&](u32x4 w, int) {
+            float v[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[e] = Piece<L>::get(w, e);
+            add_values<N>(unit[h], v, p.c);
+        };
+        whole_pieces<NT, 4>(row, first, min(end, whole), add);
+        if (whole < n && whole >= first && whole < end && (whole - first) % NT == 0) add(load_last(row, whole, V), whole);
+    }
+    float least_own = INFINITY;
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+        const bool used = tid + h * per * NT < n;
+        sh.umax[h * NT + tid] = used ? value_key(unit[h].m) : 0u;
+        if (used) least_own = fminf(least_own, unit[h].m);
+        own.m = fmaxf(own.m, unit[h].m);
+    }
+#pragma unroll
+    for (int h = 0; h < H; ++h) own.s += unit[h].s * __builtin_amdgcn_exp2f(ref_of(unit[h].m, p.c) - ref_of(own.m, p.c));
     // the least of them, as the largest of the negated maxima (-0 and 0 have one key)
-    const float least_w = -wave_max_dpp(tid < n ? -own.m : -INFINITY);
+    const float least_w = -wave_max_dpp(-least_own);
     if (lane == 0) sh.wmin[wave] = value_key(least_w);
     if (tid == 0) sh.n = 0;
     const MaxSum all = block_merge<NT>(own, p.c, sh.red);   // its barrier: tmax, wmin and n are set
@@ -118,13 +172,21 @@ __global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
 #pragma unroll
     for (int w = 1; w < W; ++w) least = min(least, sh.wmin[w]);
     // fewer pieces than k: everything is a candidate
-    const uint32_t bound = n < k ? 0u : bound_of_kth<NT>(sh, least, value_key(all.m), k);
+    const uint32_t bound = n < k ? 0u : bound_of_kth(sh, least, value_key(all.m), k);
 
-    // the pieces of the threads that reach the bound, again
-    const bool picked = mine >= bound && tid < n;
-    const uint64_t ball = __ballot(picked);
-    if (lane == 0) sh.wcount[wave] = __popcll(ball);
-    __syncthreads();                // every wave is past the search: its keys become the picked threads
+    // the units that reach the bound, again
+    float rest = 0.f;
+    uint64_t ball[H];
+    int mine = 0;
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+        const bool used = tid + h * per * NT < n, picked = used && value_key(unit[h].m) >= bound;
+        ball[h] = __ballot(picked);
+        if (!picked) rest += unit[h].s * __builtin_amdgcn_exp2f(ref_of(unit[h].m, p.c) - B);
+        mine += __popcll(ball[h]);
+    }
+    if (lane == 0) sh.wcount[wave] = mine;
+    __syncthreads();                // every wave is past the search: its keys become the picked units
     int at = 0, total = 0;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
@@ -132,24 +194,36 @@ __global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
         if (w < wave) at += c;
         total += c;
     }
-    uint32_t *list = sh.tmax;
-    if (picked) list[at + __popcll(ball & ((1ull << lane) - 1))] = tid;
-    __syncthreads();
-    float rest = picked ? 0.f : own.s * __builtin_amdgcn_exp2f(ref_of(own.m, p.c) - B);
-    const int per = (n + NT - 1) / NT;
-    for (int x = tid; x < total * per; x += NT) {
-        const int i = (int)list[x / per] + NT * (x % per);
-        if (i >= n) continue;
-        const u32x4 w = i < V / N ? load_piece(row, i) : load_last(row, i, V);
+    uint32_t *list = sh.umax;
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float v = Piece<L>::get(w, e);
-            const uint32_t key = value_key(v);
-            if (key >= bound && i * N + e < V) {
-                const int c = atomicAdd(&sh.n, 1);
-                if (c < kTopCand) sh.cand[c] = pair_key(key, i * N + e);
-            } else {
-                rest += term(v);
+    for (int h = 0; h < H; ++h) {
+        if (ball[h] >> lane & 1u) list[at + __popcll(ball[h] & ((1ull << lane) - 1))] = h * per * NT + tid;   // its first piece
+        at += __popcll(ball[h]);
+    }
+    __syncthreads();
+    for (int x0 = tid; x0 < total * per; x0 += 4 * NT) {
+        u32x4 w[4];
+        int at[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {       // four in flight: this is all latency
+            const int x = x0 + u * NT;
+            at[u] = x < total * per ? (int)list[x / per] + NT * (x % per) : n;
+            if (at[u] < V / N) w[u] = load_piece(row, at[u]);
+            else if (at[u] < n) w[u] = load_last(row, at[u], V);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (at[u] >= n) continue;
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float v = Piece<L>::get(w[u], e);
+                const uint32_t key = value_key(v);
+                if (key >= bound && at[u] * N + e < V) {
+                    const int c = atomicAdd(&sh.n, 1);
+                    if (c < kTopCand) sh.cand[c] = pair_key(key, at[u] * N + e);
+                } else {
+                    rest += term(v);
+                }
             }
         }
     }
@@ -209,41 +283,96 @@ __global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
         __syncthreads();
         nc = sh.n;
     }
-    // ranked by counting the larger ones
-    for (int i = tid; i < nc; i += NT) {
-        const uint64_t key = sh.cand[i];
-        int rank = 0;
-        for (int j = 0; j < nc; ++j) rank += sh.cand[j] > key;
-        sh.sorted[rank] = key;
-    }
-    __syncthreads();
+    sort_candidates(sh, nc);
     for (int j = k + tid; j < nc; j += NT) rest += term(key_value((uint32_t)(sh.sorted[j] >> 32)));
-    double outside = block_sum<NT>(rest, sh.red[2]);
-    if (wave != 0) return;
-    // in multiples of exp(max / temperature)
-    if (!far && all.m != -INFINITY) outside *= exp((double)B * kLn2 - (double)all.m * p.c.inv);
-    double sum = 0.;
-    for (int j = lane; j < k; j += 64)
-        sum += exp(((double)key_value((uint32_t)(sh.sorted[j] >> 32)) - (double)all.m) * p.c.inv);
-    const double lse = log(wave_sum_f64(sum) + outside);    // of x - max / temperature
-    for (int j = lane; j < k; j += 64) {
-        const uint64_t key = sh.sorted[j];
-        p.ids[(int64_t)t * k + j] = key_id(key);
-        p.logp[(int64_t)t * k + j] = (float)(((double)key_value((uint32_t)(key >> 32)) - (double)all.m) * p.c.inv - lse);
+    const double outside = block_sum<NT>(rest, sh.red[2]);
+    if (SPLIT) {
+        uint64_t *keys = p.keys + ((int64_t)t * p.S + seg) * p.k;
+        for (int j = tid; j < p.k; j += NT) {
+            const uint64_t key = j < k ? sh.sorted[j] : 0;
+            keys[j] = key ? pair_key((uint32_t)(key >> 32), key_id(key) + lo) : 0;
+        }
+        if (tid == 0) p.part[(int64_t)t * p.S + seg] = Part{all.m, (float)outside, 0, 0};
+    } else if (wave == 0) {
+        put_top(p, t, sh.sorted, all.m, outside * unit_of_max(all.m, p.c));
     }
-    if (lane == 0 && p.tail) p.tail[t] = (float)(log(outside) - lse);
+}
+
+// The k largest of a split row among its segments' lists: S k keys, at most one a thread.
+template <typename L> __global__ __launch_bounds__(kJoinThreads) void k_opd_top_join(TopParams<L> p) {
+    constexpr int NT = kJoinThreads;
+    __shared__ TopShared<NT, 1> sh;
+    const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, k = p.k;
+    const uint64_t *keys = p.keys + (int64_t)t * p.S * k;
+    bool bad;
+    const MaxSum rests = join_parts(p.part + (int64_t)t * p.S, p.S, p.c, bad);
+    const uint64_t mine = tid < p.S * k ? keys[tid] : 0;
+    // a whole list reaches its own last key: the largest of these is a bound that k keys reach
+    uint32_t lo = lane < p.S ? (uint32_t)(keys[(int64_t)lane * k + k - 1] >> 32) : 0;
+    uint32_t hi = lane < p.S ? (uint32_t)(keys[(int64_t)lane * k] >> 32) : 0;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        lo = max(lo, (uint32_t)__shfl_xor((int)lo, o));
+        hi = max(hi, (uint32_t)__shfl_xor((int)hi, o));
+    }
+    lo = max(lo, 1u);
+    sh.umax[tid] = (uint32_t)(mine >> 32);
+    if (tid == 0) sh.n = 0;
+    __syncthreads();
+    const uint32_t bound = bound_of_kth(sh, lo, hi, k);
+    float rest = 0.f;
+    if (mine && (uint32_t)(mine >> 32) >= bound) sh.cand[atomicAdd(&sh.n, 1)] = mine;
+    const bool far = is_far(rests.m);
+    const float B = ref_of(rests.m, p.c);
+    auto term = [&](uint64_t key) {
+        const float v = key_value((uint32_t)(key >> 32));
+        return far ? exp_diff(v, rests.m, p.c) : exp_at(v, B, p.c);
+    };
+    if (mine && (uint32_t)(mine >> 32) < bound) rest = term(mine);
+    __syncthreads();
+    const int nc = sh.n;
+    sort_candidates(sh, nc);
+    for (int j = k + tid; j < nc; j += NT) rest += term(sh.sorted[j]);
+    const double outside = block_sum<NT>(rest, sh.red[2]) + (double)rests.s;
+    if (tid < 64) put_top(p, t, sh.sorted, rests.m, outside * unit_of_max(rests.m, p.c));
+}
+
+// Segments of each row: about four workgroups a compute unit in all, at least
+// 4096 elements each, and no more keys than the joining workgroup has threads.
+static void top_split(int T, int V, int k, int &S, int &seg) {
+    S = T <= 96 ? 512 / T : 1;
+    if (S > kMaxParts) S = kMaxParts;
+    if (S > V / 4096) S = V / 4096;
+    if (S > kJoinThreads / k) S = kJoinThreads / k;
+    if (S < 2) { S = 1; seg = V; return; }
+    seg = ((V + S - 1) / S + 255) / 256 * 256;
+    S = (V + seg - 1) / seg;
+}
+static int64_t top_bytes(int T, int V, int k) {
+    int S, seg;
+    top_split(T, V, k, S, seg);
+    return S > 1 ? (int64_t)T * S * ((int64_t)sizeof(Part) + (int64_t)k * 8) : 0;
 }
 
 template <typename L>
 static int top_logits(int32_t T, int32_t V, const L *d_logits, int64_t ld, double temperature, int32_t k,
                       int32_t *d_ids, float *d_logp, float *d_tail, void *d_work, int64_t work_bytes, void *stream) {
-    (void)d_work; (void)work_bytes;
     if (!opd_rows_ok(T, V, d_logits, ld, temperature, sizeof(L)) || k < 1 || k > kTopMax || k > V) return PIPO_EINVAL;
     if (T == 0) return PIPO_OK;
-    if (!d_ids || !d_logp) return PIPO_EINVAL;
-    TopParams<L> p{d_logits, ld, T, V, k, exp_scale(temperature), d_ids, d_logp, d_tail};
-    if (V > 16384) hipLaunchKernelGGL((k_opd_top<L, 1024>), dim3(T), dim3(1024), 0, (hipStream_t)stream, p);
-    else hipLaunchKernelGGL((k_opd_top<L, 256>), dim3(T), dim3(256), 0, (hipStream_t)stream, p);
+    if (!d_ids || !d_logp || !opd_work_ok(d_work, work_bytes, top_bytes(T, V, k))) return PIPO_EINVAL;
+    TopParams<L> p{d_logits, ld, T, V, k, exp_scale(temperature), d_ids, d_logp, d_tail, 1, V, nullptr, nullptr};
+    hipStream_t s = (hipStream_t)stream;
+    if (d_work && top_bytes(T, V, k) > 0) {
+        top_split(T, V, k, p.S, p.seg);
+        p.part = (Part *)d_work;
+        p.keys = (uint64_t *)(p.part + (int64_t)T * p.S);
+        hipLaunchKernelGGL((k_opd_top<L, 256, true>), dim3(T * p.S), dim3(256), 0, s, p);
+        hipLaunchKernelGGL(k_opd_top_join<L>, dim3(T), dim3(kJoinThreads), 0, s, p);
+    } else if (V > 16384) {
+        hipLaunchKernelGGL((k_opd_top<L, 512, false>), dim3(T), dim3(512), 0, s, p);
+    } else {
+        hipLaunchKernelGGL((k_opd_top<L, 256, false>), dim3(T), dim3(256), 0, s, p);
+    }
     return hipGetLastError() == hipSuccess ? PIPO_OK : PIPO_EHIP;
 }
 
@@ -252,8 +381,9 @@ static int top_logits(int32_t T, int32_t V, const L *d_logits, int64_t ld, doubl
 using namespace pipo;
 
 extern "C" int64_t pipo_opd_work_bytes(int32_t T, int32_t V, int32_t k) {
-    (void)T; (void)V; (void)k;
-    return 0;
+    if (T < 1 || V < 1 || V > kOpdMaxVocab || k < 1) return 0;
+    const int64_t loss = opd_loss_work_bytes(T, V, k), top = k <= kTopMax && k <= V ? top_bytes(T, V, k) : 0;
+    return loss > top ? loss : top;
 }
 
 extern "C" int pipo_opd_top_logits(int32_t T, int32_t V, const float *d_logits, int64_t ld, double temperature,

@@ -329,48 +329,59 @@ def _opd_rows(logits, name="logits"):
     import torch
     if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or not logits.is_cuda:
         _refuse(f"{name}: a two-dimensional CUDA tensor")
-    if logits.dtype not in (torch.float32, torch.bfloat16):
+    if logits.dtype is not torch.float32 and logits.dtype is not torch.bfloat16:
         _refuse(f"{name}: float32 or bfloat16, not {logits.dtype}")
-    T, V = logits.shape
-    if V < 1 or (V > 1 and logits.stride(1) != 1) or (T > 1 and logits.stride(0) < V):
-        _refuse(f"{name}: rows of consecutive elements that do not overlap, not strides {tuple(logits.stride())}")
-    return T, V, logits.stride(0) if T > 1 else V, "" if logits.dtype == torch.float32 else "_bf16"
+    (T, V), (ld, step) = logits.shape, logits.stride()
+    if V < 1 or (V > 1 and step != 1) or (T > 1 and ld < V):
+        _refuse(f"{name}: rows of consecutive elements that do not overlap, not strides {(ld, step)}")
+    return T, V, ld if T > 1 else V, "" if logits.dtype is torch.float32 else "_bf16"
 
 
-def _opd_arg(x, name, dtype, shape, like, optional=True):
-    """One contiguous argument of a given type and shape on the logits' device."""
-    import torch
-    if x is None and optional:
+def _opd_arg(x, name, dtype, shape, device):
+    """The address of a contiguous argument of a given type and shape on the logits' device (None: none)."""
+    if x is None:
         return None
-    if not isinstance(x, torch.Tensor) or x.dtype != dtype or tuple(x.shape) != tuple(shape) or not x.is_contiguous():
-        _refuse(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)}")
-    if x.device != like.device:
-        _refuse(f"{name}: on {x.device}, the logits on {like.device}")
-    return x
+    try:
+        if x.dtype is dtype and x.shape == shape and x.device == device and x.is_contiguous():
+            return x.data_ptr()
+    except AttributeError:
+        pass
+    _refuse(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
 
 
-def _opd_grad(grad, logits, V):
-    """The gradient's tensor and row stride: None, a new tensor (True) or the caller's."""
+def _opd_grad(grad, logits, T, V, ld):
+    """The gradient's tensor, address and row stride: none, a new tensor (True) or the caller's."""
     import torch
     if grad is None or grad is False:
-        return None, 0
+        return None, None, 0
     if grad is True:
-        grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    elif (not isinstance(grad, torch.Tensor) or grad.shape != logits.shape or grad.dtype != logits.dtype
-          or grad.device != logits.device):
+        grad = torch.empty((T, V), dtype=logits.dtype, device=logits.device)
+        return grad, grad.data_ptr(), V
+    if grad is logits:
+        return grad, grad.data_ptr(), ld
+    if (not isinstance(grad, torch.Tensor) or grad.shape != logits.shape or grad.dtype != logits.dtype
+            or grad.device != logits.device):
         _refuse("grad: True, or a tensor of the logits' shape, type and device")
-    return grad, _opd_rows(grad, "grad")[2]
+    return grad, grad.data_ptr(), _opd_rows(grad, "grad")[2]
 
 
-def _opd_work(lib, T, V, k, logits):
+def _opd_call(name, logits, T, V, k, args):
+    """Calls a loss entry with the work array and the current stream of the logits' device behind its arguments."""
     import torch
+    lib = load_library()
     n = lib.pipo_opd_work_bytes(T, V, k)
-    return (torch.empty(n, dtype=torch.uint8, device=logits.device) if n else None), n
+    work = torch.empty(n, dtype=torch.uint8, device=logits.device).data_ptr() if n else None
+    # (the address of the current stream without an object around it: a third of a small call's time)
+    rc = getattr(lib, name)(T, V, logits.data_ptr(), *args, work, n, torch._C._cuda_getCurrentRawStream(logits.device.index))
+    if rc != PIPO_OK:
+        raise PipoError(rc, f"{name}: " + ("sizes, strides or coefficients outside the documented ranges"
+                                           if rc == PIPO_EINVAL else "launch failure"))
 
 
-def _opd_stream(logits):
+def _elsewhere(x):
+    """Whether x is on another CUDA device than the current one."""
     import torch
-    return ctypes.c_void_p(torch.cuda.current_stream(logits.device).cuda_stream)
+    return getattr(x, "is_cuda", False) and x.device.index != torch.cuda.current_device()
 
 
 def opd_top_logits(logits, k: int, temperature: float = 1.0):
@@ -379,17 +390,17 @@ def opd_top_logits(logits, k: int, temperature: float = 1.0):
     int32, logp [T, k] float32, tail [T] float32: the log of the probability
     outside the k)."""
     import torch
-    lib = load_library()
+    if _elsewhere(logits):
+        with torch.cuda.device(logits.device):
+            return opd_top_logits(logits, k, temperature)
     T, V, ld, dt = _opd_rows(logits)
-    with torch.cuda.device(logits.device):
-        n = max(int(k), 0)
-        ids = torch.empty((T, n), dtype=torch.int32, device=logits.device)
-        logp = torch.empty((T, n), dtype=torch.float32, device=logits.device)
-        tail = torch.empty(T, dtype=torch.float32, device=logits.device)
-        work, nw = _opd_work(lib, T, V, n, logits)
-        _opd_check(lib, getattr(lib, "pipo_opd_top_logits" + dt)(T, V, _ptr(logits), ld, float(temperature), int(k),
-                                                                 _ptr(ids), _ptr(logp), _ptr(tail), _ptr(work), nw,
-                                                                 _opd_stream(logits)))
+    if not 1 <= k <= min(V, 256):
+        _refuse(f"k: from 1 to 256 and at most {V}, not {k}")
+    ids = torch.empty((T, k), dtype=torch.int32, device=logits.device)
+    logp = torch.empty((T, k), dtype=torch.float32, device=logits.device)
+    tail = torch.empty(T, dtype=torch.float32, device=logits.device)
+    _opd_call("pipo_opd_top_logits" + dt, logits, T, V, k,
+              (ld, temperature, k, ids.data_ptr(), logp.data_ptr(), tail.data_ptr()))
     return ids, logp, tail
 
 
@@ -406,27 +417,24 @@ def opd_distill(logits, ids, logp, tail=None, rows=None, labels=None, kind: str 
     them).  Returns (loss [T] float32, grad or None); the caller goes on with
     ``logits.backward(grad)``."""
     import torch
-    lib = load_library()
+    if _elsewhere(logits):
+        with torch.cuda.device(logits.device):
+            return opd_distill(logits, ids, logp, tail, rows, labels, kind, beta, temperature, scale, grad)
+    i32, f32 = torch.int32, torch.float32
     T, V, ld, dt = _opd_rows(logits)
     if kind not in OPD_KINDS:
         _refuse(f"kind: one of {', '.join(OPD_KINDS)}, not {kind!r}")
-    if not isinstance(ids, torch.Tensor) or ids.dim() != 2:
-        _refuse("ids: a tensor of shape [Tt, k]")
-    Tt, k = ids.shape
-    _opd_arg(ids, "ids", torch.int32, (Tt, k), logits, optional=False)
-    _opd_arg(logp, "logp", torch.float32, (Tt, k), logits, optional=False)
-    _opd_arg(tail, "tail", torch.float32, (Tt,), logits)
-    _opd_arg(rows, "rows", torch.int32, (T,), logits)
-    _opd_arg(labels, "labels", torch.int32, (T,), logits)
-    _opd_arg(scale, "scale", torch.float32, (T,), logits)
-    with torch.cuda.device(logits.device):
-        loss = torch.empty(T, dtype=torch.float32, device=logits.device)
-        grad, ldg = _opd_grad(grad, logits, V)
-        work, nw = _opd_work(lib, T, V, k, logits)
-        _opd_check(lib, getattr(lib, "pipo_opd_distill" + dt)(
-            T, V, _ptr(logits), ld, Tt, k, _ptr(ids), _ptr(logp), _ptr(tail), _ptr(rows), _ptr(labels),
-            OPD_KINDS[kind], float(beta), float(temperature), _ptr(scale), _ptr(loss), _ptr(grad), ldg, _ptr(work), nw,
-            _opd_stream(logits)))
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 2 or logp is None:
+        _refuse("ids and logp: tensors of shape [Tt, k]")
+    lists, dev = ids.shape, logits.device
+    Tt, k = lists
+    args = (_opd_arg(ids, "ids", i32, lists, dev), _opd_arg(logp, "logp", f32, lists, dev),
+            _opd_arg(tail, "tail", f32, (Tt,), dev), _opd_arg(rows, "rows", i32, (T,), dev),
+            _opd_arg(labels, "labels", i32, (T,), dev), OPD_KINDS[kind], beta, temperature,
+            _opd_arg(scale, "scale", f32, (T,), dev))
+    loss = torch.empty(T, dtype=f32, device=dev)
+    grad, grad_ptr, ldg = _opd_grad(grad, logits, T, V, ld)
+    _opd_call("pipo_opd_distill" + dt, logits, T, V, k, (ld, Tt, k, *args, loss.data_ptr(), grad_ptr, ldg))
     return loss, grad
 
 
@@ -439,22 +447,22 @@ def opd_policy(logits, labels, advantages, old_logp=None, ref_logp=None, clip=(0
     [1 - clip[0], 1 + clip[1]]; scale, grad: as in opd_distill.  Returns (loss
     [T], logp [T], kl [T] or None, grad or None), float32 but for the gradient."""
     import torch
-    lib = load_library()
+    if _elsewhere(logits):
+        with torch.cuda.device(logits.device):
+            return opd_policy(logits, labels, advantages, old_logp, ref_logp, clip, kl_coef, temperature, scale, grad)
+    f32 = torch.float32
     T, V, ld, dt = _opd_rows(logits)
-    _opd_arg(labels, "labels", torch.int32, (T,), logits, optional=False)
-    _opd_arg(advantages, "advantages", torch.float32, (T,), logits, optional=False)
-    _opd_arg(old_logp, "old_logp", torch.float32, (T,), logits)
-    _opd_arg(ref_logp, "ref_logp", torch.float32, (T,), logits)
-    _opd_arg(scale, "scale", torch.float32, (T,), logits)
-    with torch.cuda.device(logits.device):
-        loss, logp = (torch.empty(T, dtype=torch.float32, device=logits.device) for _ in range(2))
-        kl = None if ref_logp is None else torch.empty(T, dtype=torch.float32, device=logits.device)
-        grad, ldg = _opd_grad(grad, logits, V)
-        work, nw = _opd_work(lib, T, V, 1, logits)
-        _opd_check(lib, getattr(lib, "pipo_opd_policy" + dt)(
-            T, V, _ptr(logits), ld, _ptr(labels), _ptr(advantages), _ptr(old_logp), _ptr(ref_logp), float(clip[0]),
-            float(clip[1]), float(kl_coef), float(temperature), _ptr(scale), _ptr(loss), _ptr(logp), _ptr(kl),
-            _ptr(grad), ldg, _ptr(work), nw, _opd_stream(logits)))
+    if labels is None or advantages is None:
+        _refuse("labels and advantages: tensors of shape [T]")
+    dev, shape = logits.device, (T,)
+    args = (_opd_arg(labels, "labels", torch.int32, shape, dev), _opd_arg(advantages, "advantages", f32, shape, dev),
+            _opd_arg(old_logp, "old_logp", f32, shape, dev), _opd_arg(ref_logp, "ref_logp", f32, shape, dev),
+            clip[0], clip[1], kl_coef, temperature, _opd_arg(scale, "scale", f32, shape, dev))
+    loss, logp = torch.empty(T, dtype=f32, device=dev), torch.empty(T, dtype=f32, device=dev)
+    kl = None if ref_logp is None else torch.empty(T, dtype=f32, device=dev)
+    grad, grad_ptr, ldg = _opd_grad(grad, logits, T, V, ld)
+    _opd_call("pipo_opd_policy" + dt, logits, T, V, 1,
+              (ld, *args, loss.data_ptr(), logp.data_ptr(), None if kl is None else kl.data_ptr(), grad_ptr, ldg))
     return loss, logp, kl, grad
 
 
