@@ -47,7 +47,7 @@ constexpr int kPolicy = 3;
 
 struct LossShared {
     int id[kEntries];               // listed ids, -1: an empty slot
-    float z[kEntries];              // their logits
+    float z[kEntries], q[kEntries];     // their logits, the teacher's log-probabilities
     double a[kEntries], p[kEntries];   // their a = p df/dp, and p
     float patch[kEntries];          // their gradients
     float coef;                     // the others' gradient over exp((z - m) / temperature)
@@ -57,32 +57,55 @@ struct LossShared {
 // What happens at position t: not scored, flagged (no such row, label or id), or scored with k entries.
 enum { kSkip, kFlag, kScore };
 
-// What happens at position t (the same for the whole workgroup), and its teacher row.
-template <typename L> __device__ __forceinline__ int position_state(const LossParams<L> &p, int t, int &y, int &trow) {
-    y = p.labels ? p.labels[t] : 0;
-    trow = p.rows ? p.rows[t] : t;
-    if (y < 0) return kSkip;
-    return (p.kind == kPolicy ? y >= p.V : (trow < 0 || trow >= p.Tt)) ? kFlag : kScore;
-}
-template <typename L> __device__ __forceinline__ int entry_id(const LossParams<L> &p, int j, int y, int trow) {
-    if (j >= p.k) return -1;
-    return p.kind == kPolicy ? y : p.ids[(int64_t)trow * p.k + j];
-}
-// Marks the listed ids of [lo, lo + len) in the bitmap (bit id - lo) and keeps
-// all of them in LDS; sh.bad is set where one is out of range, or twice in this
-// range.  Thread j brings entry j.  Ends with a barrier.
-template <int NT>
-__device__ __forceinline__ void mark_entries(int id, int k, int V, int lo, int len, LossShared &sh, uint32_t *bits) {
-    const int tid = threadIdx.x;
-    for (int i = tid; i < (len + 31) / 32; i += NT) bits[i] = 0;
-    if (tid == 0) sh.bad = 0;
-    __syncthreads();
-    if (tid < k) {
-        sh.id[tid] = id;
-        const int at = id - lo;
-        if (id >= V || (id >= lo && at < len && (atomicOr(&bits[at >> 5], 1u << (at & 31)) >> (at & 31) & 1u))) sh.bad = 1;
+// Position t's own numbers (the same for the whole workgroup: scalar loads).
+struct Position {
+    int what, y, trow;
+    float scale, q_rest, adv, old_lp, ref_lp;
+};
+template <typename L> __device__ __forceinline__ Position read_position(const LossParams<L> &p, int t) {
+    Position x;
+    x.y = p.labels ? p.labels[t] : 0;
+    x.trow = p.rows ? p.rows[t] : t;
+    x.scale = p.scale ? p.scale[t] : 1.f;
+    x.q_rest = x.adv = x.old_lp = x.ref_lp = 0.f;
+    if (p.kind == kPolicy) {
+        x.adv = p.adv[t];
+        if (p.old_lp) x.old_lp = p.old_lp[t];
+        if (p.ref_lp) x.ref_lp = p.ref_lp[t];
+        x.what = x.y < 0 ? kSkip : x.y >= p.V ? kFlag : kScore;
+    } else {
+        x.what = x.y < 0 ? kSkip : x.trow < 0 || x.trow >= p.Tt ? kFlag : kScore;
+        if (p.q_rest && x.what == kScore) x.q_rest = p.q_rest[x.trow];
     }
-    __syncthreads();
+    return x;
+}
+// Entry j of a scored position: its id and the teacher's log-probability.
+template <typename L>
+__device__ __forceinline__ void read_entry(const LossParams<L> &p, int j, const Position &x, int &id, float &q) {
+    id = -1;
+    q = 0.f;
+    if (j >= p.k || x.what != kScore) return;
+    if (p.kind == kPolicy) {
+        id = x.y;
+    } else {
+        id = p.ids[(int64_t)x.trow * p.k + j];
+        q = p.q[(int64_t)x.trow * p.k + j];
+    }
+}
+// Marks the listed ids of [lo, lo + len) in a cleared bitmap (bit id - lo) and
+// keeps all entries in LDS; sh.bad, cleared before, is set where one is out of
+// range, or twice in this range.  Thread j brings entry j.
+__device__ __forceinline__ void mark_entry(int id, float q, int k, int V, int lo, int len, LossShared &sh, uint32_t *bits) {
+    const int tid = threadIdx.x;
+    if (tid >= k) return;
+    sh.id[tid] = id;
+    sh.q[tid] = q;
+    const int at = id - lo;
+    if (id >= V || (id >= lo && at < len && (atomicOr(&bits[at >> 5], 1u << (at & 31)) >> (at & 31) & 1u))) sh.bad = 1;
+}
+template <int NT> __device__ __forceinline__ void clear_bits(uint32_t *bits, int len, LossShared &sh) {
+    for (int i = threadIdx.x; i < (len + 31) / 32; i += NT) bits[i] = 0;
+    if (threadIdx.x == 0) sh.bad = 0;
 }
 
 // The bitmap's bits of piece i (bit e: its element e is listed).
@@ -112,7 +135,7 @@ __device__ __forceinline__ void divergence(int kind, double beta, double lp, dou
 // The first wave turns the listed logits and the rest's (max, sum) into the
 // position's outputs (where `first`) and its gradient's numbers; ends with a barrier.
 template <typename L>
-__device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, int trow, MaxSum rest, LossShared &sh,
+__device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, const Position &x, MaxSum rest, LossShared &sh,
                                            bool first = true) {
     if (threadIdx.x < 64) {
         const int lane = threadIdx.x;
@@ -129,17 +152,17 @@ __device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, int tr
         sum += (double)rest.s * rest_at;     // without a rest its sum is 0 (or NaN)
         // of x - m / temperature; a row without any mass has none
         const double lse = m == -INFINITY ? (double)__builtin_nanf("") : log(sum);
-        const double g = (p.scale ? (double)p.scale[t] : 1.) * inv;
+        const double g = (double)x.scale * inv;
         double A = 0., a_rest = 0.;
         if (p.kind == kPolicy) {
-            const double lp = ((double)sh.z[0] - m) * inv - lse, py = exp(lp), adv = p.adv[t];
-            const double r = p.old_lp ? exp(lp - (double)p.old_lp[t]) : exp(lp - lp);
+            const double lp = ((double)sh.z[0] - m) * inv - lse, py = exp(lp), adv = x.adv;
+            const double r = exp(lp - (p.old_lp ? (double)x.old_lp : lp));
             const double cut = fmin(fmax(r, 1. - p.clip_lo), 1. + p.clip_hi);
             const bool inside = adv * r <= adv * cut;
             double loss = -(inside ? adv * r : adv * cut), d = inside ? -adv * r : 0., kl = 0.;
             if (r != r || adv != adv) loss = d = r + adv;
             if (p.ref_lp) {
-                const double far = (double)p.ref_lp[t] - lp;
+                const double far = (double)x.ref_lp - lp;
                 kl = expm1(far) - far;
                 if (p.kl_coef != 0.) {
                     loss += p.kl_coef * kl;
@@ -155,7 +178,6 @@ __device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, int tr
             }
         } else {
             double f = 0.;
-            const float *q = p.q + (int64_t)trow * p.k;
             // entry k stands for the tokens outside the list
             for (int j = lane; j < p.k + (p.q_rest ? 1 : 0); j += 64) {
                 const bool out = j == p.k;
@@ -163,7 +185,7 @@ __device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, int tr
                 double lp = out ? unit + log((double)rest.s) - lse : ((double)sh.z[j] - m) * inv - lse;
                 if (out && rest.s == 0.f) lp = lse == lse ? -INFINITY : lse;
                 double fj, aj;
-                divergence(p.kind, p.beta, lp, out ? (double)p.q_rest[trow] : (double)q[j], fj, aj);
+                divergence(p.kind, p.beta, lp, out ? (double)x.q_rest : (double)sh.q[j], fj, aj);
                 f += fj;
                 A += aj;
                 if (out) a_rest = aj;
@@ -232,14 +254,16 @@ __device__ __forceinline__ float sum_far(const L *row, int len, const uint32_t *
     return (float)block_sum<NT>(s, s_w);
 }
 // A piece's gradients away from the list; those of listed elements are written over them later.
+template <typename L> __device__ __forceinline__ void gradients(float *v, u32x4 w, float coef, float B, ExpScale c) {
+    // c's second float matters to sums only: here it is less than one rounding of each exponent
+#pragma unroll
+    for (int e = 0; e < Piece<L>::N; ++e) v[e] = coef * __builtin_amdgcn_exp2f(fmaf(Piece<L>::get(w, e), c.hi, -B));
+}
 template <typename L>
 __device__ __forceinline__ void put_piece(L *out, u32x4 w, int i, int len, float coef, MaxSum rest, ExpScale c) {
     constexpr int N = Piece<L>::N;
-    const float B = ref_of(rest.m, c);
     float v[N];
-    // c's second float matters to sums only: here it is less than one rounding of each exponent
-#pragma unroll
-    for (int e = 0; e < N; ++e) v[e] = coef * __builtin_amdgcn_exp2f(fmaf(Piece<L>::get(w, e), c.hi, -B));
+    gradients<L>(v, w, coef, ref_of(rest.m, c), c);
     if ((i + 1) * N <= len) store_piece(out, i, v);
     else store_last(out, i, len, v);
 }
@@ -255,58 +279,167 @@ __device__ __forceinline__ void put_far(L *out, const L *row, int len, float coe
     });
 }
 
-// One workgroup per position.  Its first NV pieces a thread stay in registers
-// between the two passes; the rest of a longer row is read again.
-template <typename L, int NT, int NV, bool GRAD>
+// A piece's sum of 2^(z c - B), without pieces that hold a listed element.
+template <typename L> __device__ __forceinline__ void sum_piece(float &s, u32x4 w, int i, const uint32_t *bits, float B, ExpScale c) {
+    constexpr int N = Piece<L>::N;
+    float x = 0.f;
+#pragma unroll
+    for (int e = 0; e < N; ++e) x += exp_at(Piece<L>::get(w, e), B, c);
+    s += listed_bits<N>(bits, i) ? 0.f : x;
+}
+template <typename L> __device__ __forceinline__ void max_piece(float &m, u32x4 w, int i, const uint32_t *bits) {
+    constexpr int N = Piece<L>::N;
+    float x = Piece<L>::get(w, 0);
+#pragma unroll
+    for (int e = 1; e < N; ++e) x = fmaxf(x, Piece<L>::get(w, e));
+    m = fmaxf(m, listed_bits<N>(bits, i) ? -INFINITY : x);
+}
+// (max, sum) of the unlisted elements of a row where the reference of the fast
+// pass did not fit, from two passes of their own.
+template <typename L, int NT>
+__device__ __forceinline__ MaxSum sum_slowly(const L *row, int V, const uint32_t *bits, ExpScale c, float (*red)[NT / 64]) {
+    constexpr int N = Piece<L>::N;
+    MaxSum a{-INFINITY, 0.f};
+    each_piece<NT, 1>(row, (int)threadIdx.x, V, [&](u32x4 w, int i) { add_piece<L>(a, w, i, bits, c); });
+    __syncthreads();
+    a = block_merge<NT>(a, c, red);
+    __syncthreads();
+    if (is_far(a.m)) a.s = sum_far<L, NT>(row, V, bits, a.m, c, red[0]);
+    __syncthreads();
+    return a;
+}
+
+// A workgroup takes positions blockIdx.x, + gridDim.x, ...  Of a row's whole
+// slabs (a piece for every thread) the first NV stay in registers between the two
+// passes; what lies behind them is read again.
+//   The sum's reference is the largest unlisted value of the first AHEAD slabs,
+// which a row's maximum does not pass by more than a float holds (2^127) unless
+// masks hide all of them: then the sum is inf, and taken again slowly.  So no
+// value needs a comparison, and no sum is rescaled.  Pieces with a listed element
+// are left out and added by the thread that brings the entry.
+//   Rows that run with NV slabs have at least NV - STEP of them.
+//   The AHEAD slabs are loaded while the position before is written, the others
+// AHEAD slabs before their sum, so that neither loads nor sums wait for all of
+// the other.
+template <int NT, int NV> constexpr bool kTakesSeveral = NT == 512 && NV >= 12;    // one workgroup fills a compute unit
+template <typename L, int NT, int NV, int STEP, bool GRAD>
 __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
+    constexpr bool LOOP = kTakesSeveral<NT, NV>;
+    constexpr int AHEAD = NV < 12 ? NV : 12, N = Piece<L>::N;
     extern __shared__ uint32_t bits[];
     __shared__ LossShared sh;
-    __shared__ float red[3][NT / 64];
-    const int t = blockIdx.x, tid = threadIdx.x, V = p.V, whole = V / Piece<L>::N;
+    __shared__ float red[2][NT / 64];
+    const int tid = threadIdx.x, V = p.V;
+    const int held = min(NV, V / (N * NT));
+    auto has = [&](int j) { return j < NV - STEP || j < held; };
+    // Slab j's piece.  One that is not wanted comes from the row's first bytes: a branch around each load would
+    // double the registers it is loaded into.  (Rows of less than a slab may not have those.)
+    auto slab = [&](const L *from, int j, uint32_t off, bool wanted) {
+        if (NV > STEP) return load_at(from, wanted && has(j) ? off : 0);
+        return wanted && has(j) ? load_at(from, off) : u32x4{0, 0, 0, 0};
+    };
+    u32x4 keep[NV];
+    int t = blockIdx.x, id;
+    float q;
+    Position x = read_position(p, t);
     const L *row = p.z + (int64_t)t * p.ld;
-    int y, trow, what = position_state(p, t, y, trow);
-    u32x4 keep[NV ? NV : 1];
-    float zj = 0.f;
-    if (what == kScore) {
-        const int id = entry_id(p, tid, y, trow);
+    read_entry(p, tid, x, id, q);
+    uint32_t off = tid * 16;
 #pragma unroll
-        for (int j = 0; j < NV; ++j)      // in flight while the entries are marked
-            if (tid + NT * j < whole) keep[j] = load_piece(row, tid + NT * j);
-        mark_entries<NT>(id, p.k, V, 0, V, sh, bits);
-        if (sh.bad) what = kFlag;
-        else if (id >= 0) zj = Piece<L>::one(row + id);
-    }
-    if (what != kScore) {
-        const float v = what == kSkip ? 0.f : __builtin_nanf("");
-        put_constant(p, t, v);
-        if (GRAD) fill_row<L, NT>(p.grad + (int64_t)t * p.ldg, V, v);
-        return;
-    }
-    MaxSum a{-INFINITY, 0.f};
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-        if (tid + NT * j < whole) add_piece<L>(a, keep[j], tid + NT * j, bits, p.c);
-    each_piece<NT, 4>(row, tid + NT * NV, V, [&](u32x4 w, int i) { add_piece<L>(a, w, i, bits, p.c); });
-    if (tid < p.k) sh.z[tid] = zj;
-    a = block_merge<NT>(a, p.c, red);
-    const bool far = is_far(a.m);
-    if (far) a.s = sum_far<L, NT>(row, V, bits, a.m, p.c, red[2]);
-    finish_row(p, t, trow, a, sh);
-    if (!GRAD) return;
-    L *out = p.grad + (int64_t)t * p.ldg;
-    const float coef = sh.coef;
-    if (far) {
-        put_far<L, NT>(out, row, V, coef, a.m, p.c);
-    } else {
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            asm volatile("" : "+v"(keep[j]));   // unpacked again: the first pass' floats would take twice the registers
-            if (tid + NT * j < whole) put_piece(out, keep[j], tid + NT * j, V, coef, a, p.c);
+    for (int j = 0; j < AHEAD; ++j, next_slab<NT>(off)) keep[j] = slab(row, j, off, x.what == kScore);
+    clear_bits<NT>(bits, V, sh);
+    __syncthreads();
+    for (;;) {
+        const int next = t + gridDim.x;
+        Position nx;
+        nx.what = kSkip;
+        if (LOOP && next < p.T) nx = read_position(p, next);
+        L *out = GRAD ? p.grad + (int64_t)t * p.ldg : nullptr;
+        bool scored = x.what == kScore, far = false;
+        if (scored) {
+            mark_entry(id, q, p.k, V, 0, V, sh, bits);
+            __syncthreads();
+            scored = sh.bad == 0;
         }
-        each_piece<NT, 4>(row, tid + NT * NV, V, [&](u32x4 w, int i) { put_piece(out, w, i, V, coef, a, p.c); });
+        MaxSum a{-INFINITY, 0.f};
+        if (scored) {
+            // this thread's entry: its logit and, if it is the first listed one of its piece, the piece's others
+            float zj = 0.f, s = 0.f;
+            u32x4 shared_piece;
+            uint32_t others = 0;
+            if (id >= 0) {
+                zj = Piece<L>::one(row + id);
+                const uint32_t listed = listed_bits<N>(bits, id / N);
+                if ((listed & ((1u << (id % N)) - 1)) == 0) {
+                    others = ~listed;
+                    shared_piece = (id / N + 1) * N <= V ? load_piece(row, id / N) : load_last(row, id / N, V);
+                }
+            }
+            float m = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) {
+                if (has(j)) max_piece<L>(m, keep[j], tid + NT * j, bits);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (NV <= STEP && held == 0) each_piece<NT, 1>(row, tid, V, [&](u32x4 w, int i) { max_piece<L>(m, w, i, bits); });
+            m = block_max<NT>(m, red[0]);
+            const float B = ref_of(m, p.c);
+            off = (tid + NT * AHEAD) * 16;
+#pragma unroll
+            for (int j = 0; j < NV; ++j, next_slab<NT>(off)) {
+                if (j + AHEAD < NV) keep[j + AHEAD] = slab(row, j + AHEAD, off, true);
+                asm volatile("" : "+v"(keep[j]));   // unpacked again: the floats would take twice the registers
+                if (has(j)) sum_piece<L>(s, keep[j], tid + NT * j, bits, B, p.c);
+            }
+            each_piece<NT, 4>(row, tid + NT * held, V, [&](u32x4 w, int i) { sum_piece<L>(s, w, i, bits, B, p.c); });
+            if (others) {
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if (others >> e & 1u) s += exp_at(Piece<L>::get(shared_piece, e), B, p.c);
+            }
+            if (tid < p.k) sh.z[tid] = zj;
+            a = MaxSum{m, (float)block_sum<NT>(s, red[1])};
+            if (!(a.s < INFINITY) || is_far(m)) a = sum_slowly<L, NT>(row, V, bits, p.c, red);
+            far = is_far(a.m);
+            if (id >= 0) bits[id >> 5] = 0;      // every wave is past its sums: ready for the next position
+            finish_row(p, t, x, a, sh);
+        } else {
+            const float v = x.what == kSkip ? 0.f : __builtin_nanf("");
+            put_constant(p, t, v);
+            if (GRAD) fill_row<L, NT>(out, V, v);
+            if (LOOP && x.what == kScore) {      // flagged by its list
+                __syncthreads();
+                clear_bits<NT>(bits, V, sh);
+            }
+        }
+        const int mine = scored ? id : -1;
+        const L *next_row = p.z + (int64_t)(nx.what == kScore ? next : t) * p.ld;
+        read_entry(p, tid, nx, id, q);
+        if (GRAD) {
+            const float coef = sh.coef, B = ref_of(a.m, p.c);
+            const bool put = scored && !far;
+            off = tid * 16;
+#pragma unroll
+            for (int j = 0; j < NV; ++j, next_slab<NT>(off)) {
+                asm volatile("" : "+v"(keep[j]));
+                if (put && has(j)) {
+                    float v[N];
+                    gradients<L>(v, keep[j], coef, B, p.c);
+                    store_at(out, off, v);
+                }
+                if (LOOP && j < AHEAD) keep[j] = slab(next_row, j, off, nx.what == kScore);
+            }
+            if (put) each_piece<NT, 4>(row, tid + NT * held, V, [&](u32x4 w, int i) { put_piece(out, w, i, V, coef, a, p.c); });
+            if (far) put_far<L, NT>(out, row, V, coef, a.m, p.c);
+        }
+        if (!GRAD) return;
+        __syncthreads();   // the listed entries over what the pass above wrote there
+        if (mine >= 0) Piece<L>::put(out + mine, sh.patch[tid]);
+        if (!LOOP || next >= p.T) return;
+        t = next;
+        row = next_row;
+        x = nx;
     }
-    __syncthreads();   // the listed entries over what the pass above wrote there
-    if (tid < p.k && sh.id[tid] >= 0) Piece<L>::put(out + sh.id[tid], sh.patch[tid]);
 }
 
 // ---- few rows: several workgroups each ----------------------------------------------
@@ -325,11 +458,16 @@ template <typename L> __global__ __launch_bounds__(kPartThreads) void k_opd_part
     __shared__ float red[3][NT / 64];
     const int t = blockIdx.x / q.S, seg = blockIdx.x % q.S, tid = threadIdx.x;
     const int lo = seg * q.seg, len = min(q.seg, p.V - lo);
-    int y, trow;
-    if (position_state(p, t, y, trow) != kScore) return;
+    const Position x = read_position(p, t);
+    if (x.what != kScore) return;
     const L *row = p.z + (int64_t)t * p.ld + lo;
-    const int id = entry_id(p, tid, y, trow);
-    mark_entries<NT>(id, p.k, p.V, lo, len, sh, bits);
+    int id;
+    float tq;
+    read_entry(p, tid, x, id, tq);
+    clear_bits<NT>(bits, len, sh);
+    __syncthreads();
+    mark_entry(id, tq, p.k, p.V, lo, len, sh, bits);
+    __syncthreads();
     if (id >= lo && id < lo + len) q.z[(int64_t)t * p.k + tid] = Piece<L>::one(row + (id - lo));
     MaxSum a{-INFINITY, 0.f};
     each_piece<NT, 4>(row, tid, len, [&](u32x4 w, int i) { add_piece<L>(a, w, i, bits, p.c); });
@@ -346,7 +484,8 @@ __global__ __launch_bounds__(kPartThreads) void k_opd_apply(LossParams<L> p, Spl
     const int t = blockIdx.x / S, seg = blockIdx.x % S, tid = threadIdx.x;
     const int lo = GRAD ? seg * q.seg : 0, len = GRAD ? min(q.seg, p.V - lo) : 0;
     L *out = GRAD ? p.grad + (int64_t)t * p.ldg + lo : nullptr;
-    int y, trow, what = position_state(p, t, y, trow), id = -1;
+    const Position x = read_position(p, t);
+    int what = x.what, id = -1;
     MaxSum a{-INFINITY, 0.f};
     if (what == kScore) {
         bool bad;
@@ -359,13 +498,15 @@ __global__ __launch_bounds__(kPartThreads) void k_opd_apply(LossParams<L> p, Spl
         if (GRAD) fill_row<L, NT>(out, len, v);
         return;
     }
+    float tq;
+    read_entry(p, tid, x, id, tq);
     if (tid < p.k) {
-        id = entry_id(p, tid, y, trow);
         sh.id[tid] = id;
+        sh.q[tid] = tq;
         sh.z[tid] = id >= 0 ? q.z[(int64_t)t * p.k + tid] : 0.f;
     }
     __syncthreads();
-    finish_row(p, t, trow, a, sh, seg == 0);
+    finish_row(p, t, x, a, sh, seg == 0);
     if (!GRAD) return;
     const L *row = p.z + (int64_t)t * p.ld + lo;
     const float coef = sh.coef;
@@ -391,9 +532,21 @@ static int64_t split_bytes(int T, int V, int k) {
 }
 int64_t opd_loss_work_bytes(int T, int V, int k) { return split_bytes(T, V, k); }
 
-template <typename L, int NT, int NV, bool GRAD> static int launch_rows(const LossParams<L> &p, hipStream_t s) {
+// Workgroups of a launch: one a row, or where a workgroup fills a compute unit
+// (its registers hold a long row) one a compute unit, which takes several rows.
+static int compute_units() {
+    int dev = 0, n = 0;
+    if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return 256;
+    return n;
+}
+template <typename L, int NT, int NV, int STEP, bool GRAD> static int launch_rows(const LossParams<L> &p, hipStream_t s) {
     const size_t lds = (size_t)((p.V + 31) / 32) * 4;
-    hipLaunchKernelGGL((k_opd_loss<L, NT, NV, GRAD>), dim3(p.T), dim3(NT), lds, s, p);
+    int grid = p.T;
+    if (kTakesSeveral<NT, NV>) {
+        const int cus = compute_units();
+        if (grid > cus) grid = cus;
+    }
+    hipLaunchKernelGGL((k_opd_loss<L, NT, NV, STEP, GRAD>), dim3(grid), dim3(NT), lds, s, p);
     return hipGetLastError() == hipSuccess ? PIPO_OK : PIPO_EHIP;
 }
 
@@ -406,7 +559,6 @@ template <typename L> static int launch_split(const LossParams<L> &p, SplitParam
 }
 
 template <typename L> static int launch_loss(const LossParams<L> &p, void *work, hipStream_t s) {
-    const int n = (p.V + Piece<L>::N - 1) / Piece<L>::N;
     if (work && split_bytes(p.T, p.V, p.k) > 0) {
         SplitParams q;
         split_of(p.T, p.V, q.S, q.seg);
@@ -414,18 +566,23 @@ template <typename L> static int launch_loss(const LossParams<L> &p, void *work,
         q.z = (float *)(q.part + (int64_t)p.T * q.S);
         return launch_split(p, q, s);
     }
+    const int n = p.V / Piece<L>::N;
     if (!p.grad) {
-        if (n <= 256 * 32) return launch_rows<L, 256, 0, false>(p, s);
-        return launch_rows<L, 512, 0, false>(p, s);
+        if (n <= 256 * 32) return launch_rows<L, 256, 4, 4, false>(p, s);
+        return launch_rows<L, 512, 4, 4, false>(p, s);
     }
-    if (n <= 256 * 2) return launch_rows<L, 256, 2, true>(p, s);
-    if (n <= 256 * 4) return launch_rows<L, 256, 4, true>(p, s);
-    if (n <= 256 * 8) return launch_rows<L, 256, 8, true>(p, s);
-    if (n <= 512 * 8) return launch_rows<L, 512, 8, true>(p, s);
-    if (n <= 512 * 16) return launch_rows<L, 512, 16, true>(p, s);
-    if (n <= 512 * 24) return launch_rows<L, 512, 24, true>(p, s);
-    if (n <= 512 * 32) return launch_rows<L, 512, 32, true>(p, s);
-    return launch_rows<L, 512, 38, true>(p, s);
+    if (n < 256 * 3) return launch_rows<L, 256, 2, 2, true>(p, s);
+    if (n < 256 * 5) return launch_rows<L, 256, 4, 2, true>(p, s);
+    if (n < 256 * 7) return launch_rows<L, 256, 6, 2, true>(p, s);
+    if (n < 512 * 4) return launch_rows<L, 256, 8, 2, true>(p, s);
+    if (n < 512 * 9) return launch_rows<L, 512, 8, 4, true>(p, s);
+    if (n < 512 * 13) return launch_rows<L, 512, 12, 4, true>(p, s);
+    if (n < 512 * 17) return launch_rows<L, 512, 16, 4, true>(p, s);
+    if (n < 512 * 21) return launch_rows<L, 512, 20, 4, true>(p, s);
+    if (n < 512 * 25) return launch_rows<L, 512, 24, 4, true>(p, s);
+    if (n < 512 * 29) return launch_rows<L, 512, 28, 4, true>(p, s);
+    if (n < 512 * 33) return launch_rows<L, 512, 32, 4, true>(p, s);
+    return launch_rows<L, 512, sizeof(L) == 4 ? 35 : 37, 5, true>(p, s);   // (what fits beside the other values)
 }
 
 // ---- checks ---------------------------------------------------------------------

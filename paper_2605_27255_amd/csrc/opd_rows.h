@@ -54,6 +54,20 @@ template <typename L> __device__ __forceinline__ u32x4 load_piece(const L *row, 
 template <typename L> __device__ __forceinline__ void store_piece(L *row, int i, const float *v) {
     __builtin_nontemporal_store(Piece<L>::pack(v), (typename Piece<L>::raw_t *)(row + (int64_t)i * Piece<L>::N));
 }
+// The same by byte offset from the row's start, for unrolled walks: with the
+// offset in a register that the compiler cannot see through (next_slab), it does
+// not keep an address for every step.
+template <typename L> __device__ __forceinline__ u32x4 load_at(const L *row, uint32_t off) {
+    return __builtin_nontemporal_load((const typename Piece<L>::raw_t *)((const char *)row + off));
+}
+template <typename L> __device__ __forceinline__ void store_at(L *row, uint32_t off, const float *v) {
+    __builtin_nontemporal_store(Piece<L>::pack(v), (typename Piece<L>::raw_t *)((char *)row + off));
+}
+template <int NT> __device__ __forceinline__ void next_slab(uint32_t &off) {
+    off += NT * 16;
+    asm volatile("" : "+v"(off));
+    __builtin_amdgcn_sched_barrier(0);  // nor mixes the steps, whose temporaries would not fit beside the row
+}
 template <typename L> __device__ __forceinline__ u32x4 load_last(const L *row, int i, int n) {
     typedef Piece<L> P;
     u32x4 w{P::kNegInf, P::kNegInf, P::kNegInf, P::kNegInf};
