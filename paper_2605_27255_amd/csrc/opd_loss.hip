@@ -24,6 +24,7 @@
 namespace pipo {
 
 constexpr int kEntries = 256;       // listed entries of a row
+constexpr size_t kLdsBytes = 160 * 1024;
 constexpr int64_t kOpdMaxStride = (int64_t)1 << 31;   // with T < 2^31, byte offsets stay far inside 64 bits
 
 template <typename L> struct LossParams {
@@ -42,6 +43,7 @@ template <typename L> struct LossParams {
     const float *scale;
     float *loss, *logp, *kl;
     L *grad; int64_t ldg;
+    int spill;                      // slabs of a row in LDS, behind those in registers
 };
 constexpr int kPolicy = 3;
 
@@ -317,6 +319,7 @@ __device__ __forceinline__ MaxSum sum_slowly(const L *row, int V, const uint32_t
 // masks hide all of them: then the sum is inf, and taken again slowly.  So no
 // value needs a comparison, and no sum is rescaled.  Pieces with a listed element
 // are left out and added by the thread that brings the entry.
+// (A row longer than the most slabs that registers hold keeps some in LDS.)
 //   Rows that run with NV slabs have at least NV - STEP of them.
 //   The AHEAD slabs are loaded while the position before is written, the others
 // AHEAD slabs before their sum, so that neither loads nor sums wait for all of
@@ -330,7 +333,8 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
     __shared__ LossShared sh;
     __shared__ float red[2][NT / 64];
     const int tid = threadIdx.x, V = p.V;
-    const int held = min(NV, V / (N * NT));
+    const int held = min(NV, V / (N * NT)), lower = LOOP ? held + p.spill : held;
+    u32x4 *more = (u32x4 *)(bits + (V + 127) / 128 * 4);
     auto has = [&](int j) { return j < NV - STEP || j < held; };
     // Slab j's piece.  One that is not wanted comes from the row's first bytes: a branch around each load would
     // double the registers it is loaded into.  (Rows of less than a slab may not have those.)
@@ -391,7 +395,12 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
                 asm volatile("" : "+v"(keep[j]));   // unpacked again: the floats would take twice the registers
                 if (has(j)) sum_piece<L>(s, keep[j], tid + NT * j, bits, B, p.c);
             }
-            each_piece<NT, 4>(row, tid + NT * held, V, [&](u32x4 w, int i) { sum_piece<L>(s, w, i, bits, B, p.c); });
+            if (LOOP)
+                whole_pieces<NT, 4>(row, tid + NT * held, NT * lower, [&](u32x4 w, int i) {
+                    more[i - NT * held] = w;
+                    sum_piece<L>(s, w, i, bits, B, p.c);
+                });
+            each_piece<NT, 4, GRAD>(row, tid + NT * lower, V, [&](u32x4 w, int i) { sum_piece<L>(s, w, i, bits, B, p.c); });
             if (others) {
 #pragma unroll
                 for (int e = 0; e < N; ++e)
@@ -429,7 +438,14 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
                 }
                 if (LOOP && j < AHEAD) keep[j] = slab(next_row, j, off, nx.what == kScore);
             }
-            if (put) each_piece<NT, 4>(row, tid + NT * held, V, [&](u32x4 w, int i) { put_piece(out, w, i, V, coef, a, p.c); });
+            if (LOOP && put) {
+                for (int i = tid + NT * held; i < NT * lower; i += NT) {
+                    float v[N];
+                    gradients<L>(v, more[i - NT * held], coef, B, p.c);
+                    store_at(out, (uint32_t)i * 16, v);
+                }
+            }
+            if (put) each_piece<NT, 4, GRAD>(row, tid + NT * lower, V, [&](u32x4 w, int i) { put_piece(out, w, i, V, coef, a, p.c); });
             if (far) put_far<L, NT>(out, row, V, coef, a.m, p.c);
         }
         if (!GRAD) return;
@@ -470,7 +486,7 @@ template <typename L> __global__ __launch_bounds__(kPartThreads) void k_opd_part
     __syncthreads();
     if (id >= lo && id < lo + len) q.z[(int64_t)t * p.k + tid] = Piece<L>::one(row + (id - lo));
     MaxSum a{-INFINITY, 0.f};
-    each_piece<NT, 4>(row, tid, len, [&](u32x4 w, int i) { add_piece<L>(a, w, i, bits, p.c); });
+    each_piece<NT, 4, true>(row, tid, len, [&](u32x4 w, int i) { add_piece<L>(a, w, i, bits, p.c); });
     a = block_merge<NT>(a, p.c, red);
     if (is_far(a.m)) a.s = sum_far<L, NT>(row, len, bits, a.m, p.c, red[2]);
     if (tid == 0) q.part[(int64_t)t * q.S + seg] = Part{a.m, a.s, sh.bad, 0};
@@ -511,7 +527,7 @@ __global__ __launch_bounds__(kPartThreads) void k_opd_apply(LossParams<L> p, Spl
     const L *row = p.z + (int64_t)t * p.ld + lo;
     const float coef = sh.coef;
     if (is_far(a.m)) put_far<L, NT>(out, row, len, coef, a.m, p.c);
-    else each_piece<NT, 4>(row, tid, len, [&](u32x4 w, int i) { put_piece(out, w, i, len, coef, a, p.c); });
+    else each_piece<NT, 4, true>(row, tid, len, [&](u32x4 w, int i) { put_piece(out, w, i, len, coef, a, p.c); });
     __syncthreads();
     if (id >= lo && id < lo + len) Piece<L>::put(out + (id - lo), sh.patch[tid]);
 }
@@ -539,12 +555,16 @@ static int compute_units() {
     if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return 256;
     return n;
 }
-template <typename L, int NT, int NV, int STEP, bool GRAD> static int launch_rows(const LossParams<L> &p, hipStream_t s) {
-    const size_t lds = (size_t)((p.V + 31) / 32) * 4;
+template <typename L, int NT, int NV, int STEP, bool GRAD> static int launch_rows(LossParams<L> p, hipStream_t s) {
+    size_t lds = (size_t)((p.V + 127) / 128) * 16;
     int grid = p.T;
     if (kTakesSeveral<NT, NV>) {
         const int cus = compute_units();
         if (grid > cus) grid = cus;
+        // beside the bitmap and the entries, a compute unit's 160 KB hold more slabs
+        const int left = p.V / (Piece<L>::N * NT) - NV, room = (int)((kLdsBytes - sizeof(LossShared) - 1024 - lds) / (NT * 16));
+        p.spill = left < 0 ? 0 : left < room ? left : room;
+        lds += (size_t)p.spill * NT * 16;
     }
     hipLaunchKernelGGL((k_opd_loss<L, NT, NV, STEP, GRAD>), dim3(grid), dim3(NT), lds, s, p);
     return hipGetLastError() == hipSuccess ? PIPO_OK : PIPO_EHIP;
@@ -581,8 +601,8 @@ template <typename L> static int launch_loss(const LossParams<L> &p, void *work,
     if (n < 512 * 21) return launch_rows<L, 512, 20, 4, true>(p, s);
     if (n < 512 * 25) return launch_rows<L, 512, 24, 4, true>(p, s);
     if (n < 512 * 29) return launch_rows<L, 512, 28, 4, true>(p, s);
-    if (n < 512 * 33) return launch_rows<L, 512, 32, 4, true>(p, s);
-    return launch_rows<L, 512, sizeof(L) == 4 ? 35 : 37, 5, true>(p, s);   // (what fits beside the other values)
+    if (n < 512 * (sizeof(L) == 4 ? 31 : 33)) return launch_rows<L, 512, 32, 4, true>(p, s);
+    return launch_rows<L, 512, sizeof(L) == 4 ? 34 : 36, 4, true>(p, s);   // (what fits beside the other values)
 }
 
 // ---- checks ---------------------------------------------------------------------

@@ -48,8 +48,11 @@ template <> struct Piece<uint16_t> {
 
 // Piece i of a row, whole; and the last, partial piece of a row of n elements,
 // whose elements behind the row's end read as -inf and are not written.
-template <typename L> __device__ __forceinline__ u32x4 load_piece(const L *row, int i) {
-    return __builtin_nontemporal_load((const typename Piece<L>::raw_t *)(row + (int64_t)i * Piece<L>::N));
+// AGAIN: the piece is read twice, and may stay in the caches.
+template <typename L, bool AGAIN = false> __device__ __forceinline__ u32x4 load_piece(const L *row, int i) {
+    const typename Piece<L>::raw_t *at = (const typename Piece<L>::raw_t *)(row + (int64_t)i * Piece<L>::N);
+    if (AGAIN) return *at;
+    return __builtin_nontemporal_load(at);
 }
 template <typename L> __device__ __forceinline__ void store_piece(L *row, int i, const float *v) {
     __builtin_nontemporal_store(Piece<L>::pack(v), (typename Piece<L>::raw_t *)(row + (int64_t)i * Piece<L>::N));
@@ -87,24 +90,24 @@ template <typename L> __device__ __forceinline__ void store_last(L *row, int i, 
 }
 // Calls f(piece, its index) for this thread's whole pieces from index first up to
 // end, NT apart and U of them in flight.
-template <int NT, int U, typename L, typename F>
+template <int NT, int U, bool AGAIN = false, typename L, typename F>
 __device__ __forceinline__ void whole_pieces(const L *row, int first, int end, F f) {
     int i = first;
     for (; i + (U - 1) * NT < end; i += U * NT) {
         u32x4 w[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) w[u] = load_piece(row, i + u * NT);
+        for (int u = 0; u < U; ++u) w[u] = load_piece<L, AGAIN>(row, i + u * NT);
 #pragma unroll
         for (int u = 0; u < U; ++u) f(w[u], i + u * NT);
     }
-    for (; i < end; i += NT) f(load_piece(row, i), i);
+    for (; i < end; i += NT) f(load_piece<L, AGAIN>(row, i), i);
 }
 // ... of a row of n elements, and the partial piece at its end, which belongs to
 // the thread whose turn it is.
-template <int NT, int U, typename L, typename F>
+template <int NT, int U, bool AGAIN = false, typename L, typename F>
 __device__ __forceinline__ void each_piece(const L *row, int first, int n, F f) {
     const int whole = n / Piece<L>::N;
-    whole_pieces<NT, U>(row, first, whole, f);
+    whole_pieces<NT, U, AGAIN>(row, first, whole, f);
     if (whole * Piece<L>::N < n && first % NT == whole % NT) f(load_last(row, whole, n), whole);
 }
 
