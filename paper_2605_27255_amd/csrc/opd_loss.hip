@@ -594,9 +594,11 @@ template <typename L> static int launch_loss(const LossParams<L> &p, void *work,
     if (n < 256 * 3) return launch_rows<L, 256, 2, 2, true>(p, s);
     if (n < 256 * 5) return launch_rows<L, 256, 4, 2, true>(p, s);
     if (n < 256 * 7) return launch_rows<L, 256, 6, 2, true>(p, s);
-    if (n < 512 * 4) return launch_rows<L, 256, 8, 2, true>(p, s);
-    if (n < 512 * 9) return launch_rows<L, 512, 8, 4, true>(p, s);
-    if (n < 512 * 13) return launch_rows<L, 512, 12, 4, true>(p, s);
+    if (n < 256 * 9) return launch_rows<L, 256, 8, 2, true>(p, s);
+    if (n < 256 * 13) return launch_rows<L, 256, 12, 4, true>(p, s);
+    if (n < 256 * 17) return launch_rows<L, 256, 16, 4, true>(p, s);
+    if (n < 256 * 21) return launch_rows<L, 256, 20, 4, true>(p, s);
+    if (n < 256 * 26) return launch_rows<L, 256, 24, 4, true>(p, s);
     if (n < 512 * 17) return launch_rows<L, 512, 16, 4, true>(p, s);
     if (n < 512 * 21) return launch_rows<L, 512, 20, 4, true>(p, s);
     if (n < 512 * 25) return launch_rows<L, 512, 24, 4, true>(p, s);
