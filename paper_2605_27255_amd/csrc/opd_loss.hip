@@ -43,6 +43,7 @@ template <typename L> struct LossParams {
     const float *scale;
     float *loss, *logp, *kl;
     L *grad; int64_t ldg;
+    int pieces;                     // whole pieces that every row has
     int spill;                      // slabs of a row in LDS, behind those in registers
 };
 constexpr int kPolicy = 3;
@@ -94,26 +95,30 @@ __device__ __forceinline__ void read_entry(const LossParams<L> &p, int j, const 
         q = p.q[(int64_t)x.trow * p.k + j];
     }
 }
-// Marks the listed ids of [lo, lo + len) in a cleared bitmap (bit id - lo) and
+// A bit of the bitmap for each element of a row's (or segment's) pieces, the
+// partial piece -1 first: element `at` has bit at - head + N.
+template <typename L> __host__ __device__ __forceinline__ int bitmap_words(int n) { return (n + 2 * Piece<L>::N + 127) / 128 * 4; }
+// Marks the listed ids of the segment [lo, lo + row.n) in a cleared bitmap and
 // keeps all entries in LDS; sh.bad, cleared before, is set where one is out of
-// range, or twice in this range.  Thread j brings entry j.
-__device__ __forceinline__ void mark_entry(int id, float q, int k, int V, int lo, int len, LossShared &sh, uint32_t *bits) {
+// range, or twice in this segment.  Thread j brings entry j.
+template <typename L>
+__device__ __forceinline__ void mark_entry(int id, float q, int k, int V, int lo, const Span<L> &row, LossShared &sh, uint32_t *bits) {
     const int tid = threadIdx.x;
     if (tid >= k) return;
     sh.id[tid] = id;
     sh.q[tid] = q;
-    const int at = id - lo;
-    if (id >= V || (id >= lo && at < len && (atomicOr(&bits[at >> 5], 1u << (at & 31)) >> (at & 31) & 1u))) sh.bad = 1;
+    const int at = id - lo, bit = at - row.head + 16 / (int)sizeof(L);
+    if (id >= V || (id >= lo && at < row.n && (atomicOr(&bits[bit >> 5], 1u << (bit & 31)) >> (bit & 31) & 1u))) sh.bad = 1;
 }
-template <int NT> __device__ __forceinline__ void clear_bits(uint32_t *bits, int len, LossShared &sh) {
-    for (int i = threadIdx.x; i < (len + 31) / 32; i += NT) bits[i] = 0;
+template <int NT> __device__ __forceinline__ void clear_bits(uint32_t *bits, int words, LossShared &sh) {
+    for (int i = threadIdx.x; i < words; i += NT) bits[i] = 0;
     if (threadIdx.x == 0) sh.bad = 0;
 }
 
 // The bitmap's bits of piece i (bit e: its element e is listed).
 template <int N> __device__ __forceinline__ uint32_t listed_bits(const uint32_t *bits, int i) {
-    const uint32_t b = ((const uint8_t *)bits)[i * N >> 3];
-    return N == 8 ? b : (b >> ((i & 1) * 4)) & 15u;
+    const uint32_t b = ((const uint8_t *)bits)[(i + 1) * N >> 3];
+    return N == 8 ? b : (b >> (((i + 1) & 1) * 4)) & 15u;
 }
 
 // One entry's share of a divergence and a = p df/dp, from the student's and the teacher's log-probabilities.
@@ -211,13 +216,13 @@ __device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, const 
 }
 
 template <typename L, int NT>
-__device__ __forceinline__ void fill_row(L *row, int V, float v) {
+__device__ __forceinline__ void fill_row(L *row, int n, float v) {
+    const Span<L> to(row, n);
     float x[Piece<L>::N];
 #pragma unroll
     for (int e = 0; e < Piece<L>::N; ++e) x[e] = v;
-    const int whole = V / Piece<L>::N;
-    for (int i = threadIdx.x; i < whole; i += NT) store_piece(row, i, x);
-    if ((int)threadIdx.x == whole % NT) store_last(row, whole, V, x);
+    for (int i = threadIdx.x; i < to.whole; i += NT) store_piece(to.body, i, x);
+    if (!to.exact() && (int)threadIdx.x >= NT - 2) store_edge(to.body, to, (int)threadIdx.x == NT - 1 ? -1 : to.whole, x);
 }
 
 // A position that is not scored (zeros) or flagged (NaN).
@@ -245,10 +250,10 @@ __device__ __forceinline__ void add_piece(MaxSum &a, u32x4 w, int i, const uint3
 }
 // The sum of a row (or segment) of far values, by differences from its maximum m.
 template <typename L, int NT>
-__device__ __forceinline__ float sum_far(const L *row, int len, const uint32_t *bits, float m, ExpScale c, float *s_w) {
+__device__ __forceinline__ float sum_far(const Span<const L> &row, const uint32_t *bits, float m, ExpScale c, float *s_w) {
     constexpr int N = Piece<L>::N;
     float s = 0.f;
-    each_piece<NT, 1>(row, (int)threadIdx.x, len, [&](u32x4 w, int i) {
+    each_piece<NT, 1>(row, (int)threadIdx.x, [&](u32x4 w, int i) {
         const uint32_t b = listed_bits<N>(bits, i);
 #pragma unroll
         for (int e = 0; e < N; ++e) if (!(b >> e & 1u)) s += exp_diff(Piece<L>::get(w, e), m, c);
@@ -261,52 +266,57 @@ template <typename L> __device__ __forceinline__ void gradients(float *v, u32x4 
 #pragma unroll
     for (int e = 0; e < Piece<L>::N; ++e) v[e] = coef * __builtin_amdgcn_exp2f(fmaf(Piece<L>::get(w, e), c.hi, -B));
 }
-template <typename L>
-__device__ __forceinline__ void put_piece(L *out, u32x4 w, int i, int len, float coef, MaxSum rest, ExpScale c) {
-    constexpr int N = Piece<L>::N;
-    float v[N];
-    gradients<L>(v, w, coef, ref_of(rest.m, c), c);
-    if ((i + 1) * N <= len) store_piece(out, i, v);
-    else store_last(out, i, len, v);
+// ... of this thread's pieces from index first on, and the partial ones (out: where the gradient's piece 0 lies).
+template <typename L, int NT>
+__device__ __forceinline__ void put_pieces(L *out, const Span<const L> &row, int first, float coef, float B, ExpScale c) {
+    whole_pieces<NT, 4, true>(row.body, first, row.whole, [&](u32x4 w, int i) {
+        float v[Piece<L>::N];
+        gradients<L>(v, w, coef, B, c);
+        store_piece(out, i, v);
+    });
+    edges<NT>(row, [&](u32x4 w, int i) {
+        float v[Piece<L>::N];
+        gradients<L>(v, w, coef, B, c);
+        store_edge(out, row, i, v);
+    });
 }
 template <typename L, int NT>
-__device__ __forceinline__ void put_far(L *out, const L *row, int len, float coef, float m, ExpScale c) {
+__device__ __forceinline__ void put_far(L *out, const Span<const L> &row, float coef, float m, ExpScale c) {
     constexpr int N = Piece<L>::N;
-    each_piece<NT, 1>(row, (int)threadIdx.x, len, [&](u32x4 w, int i) {
+    each_piece<NT, 1>(row, (int)threadIdx.x, [&](u32x4 w, int i) {
         float v[N];
 #pragma unroll
         for (int e = 0; e < N; ++e) v[e] = coef * exp_diff(Piece<L>::get(w, e), m, c);
-        if ((i + 1) * N <= len) store_piece(out, i, v);
-        else store_last(out, i, len, v);
+        if (i >= 0 && i < row.whole) store_piece(out, i, v);
+        else store_edge(out, row, i, v);
     });
 }
 
 // A piece's sum of 2^(z c - B), without pieces that hold a listed element.
-template <typename L> __device__ __forceinline__ void sum_piece(float &s, u32x4 w, int i, const uint32_t *bits, float B, ExpScale c) {
+template <typename L> __device__ __forceinline__ void sum_piece(float &s, u32x4 w, uint32_t listed, float B, ExpScale c) {
     constexpr int N = Piece<L>::N;
     float x = 0.f;
 #pragma unroll
     for (int e = 0; e < N; ++e) x += exp_at(Piece<L>::get(w, e), B, c);
-    s += listed_bits<N>(bits, i) ? 0.f : x;
+    s += listed ? 0.f : x;
 }
-template <typename L> __device__ __forceinline__ void max_piece(float &m, u32x4 w, int i, const uint32_t *bits) {
+template <typename L> __device__ __forceinline__ void max_piece(float &m, u32x4 w, uint32_t listed) {
     constexpr int N = Piece<L>::N;
     float x = Piece<L>::get(w, 0);
 #pragma unroll
     for (int e = 1; e < N; ++e) x = fmaxf(x, Piece<L>::get(w, e));
-    m = fmaxf(m, listed_bits<N>(bits, i) ? -INFINITY : x);
+    m = fmaxf(m, listed ? -INFINITY : x);
 }
 // (max, sum) of the unlisted elements of a row where the reference of the fast
 // pass did not fit, from two passes of their own.
 template <typename L, int NT>
-__device__ __forceinline__ MaxSum sum_slowly(const L *row, int V, const uint32_t *bits, ExpScale c, float (*red)[NT / 64]) {
-    constexpr int N = Piece<L>::N;
+__device__ __forceinline__ MaxSum sum_slowly(const Span<const L> &row, const uint32_t *bits, ExpScale c, float (*red)[NT / 64]) {
     MaxSum a{-INFINITY, 0.f};
-    each_piece<NT, 1>(row, (int)threadIdx.x, V, [&](u32x4 w, int i) { add_piece<L>(a, w, i, bits, c); });
+    each_piece<NT, 1>(row, (int)threadIdx.x, [&](u32x4 w, int i) { add_piece<L>(a, w, i, bits, c); });
     __syncthreads();
     a = block_merge<NT>(a, c, red);
     __syncthreads();
-    if (is_far(a.m)) a.s = sum_far<L, NT>(row, V, bits, a.m, c, red[0]);
+    if (is_far(a.m)) a.s = sum_far<L, NT>(row, bits, a.m, c, red[0]);
     __syncthreads();
     return a;
 }
@@ -333,9 +343,13 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
     __shared__ LossShared sh;
     __shared__ float red[2][NT / 64];
     const int tid = threadIdx.x, V = p.V;
-    const int held = min(NV, V / (N * NT)), lower = LOOP ? held + p.spill : held;
-    u32x4 *more = (u32x4 *)(bits + (V + 127) / 128 * 4);
+    const int held = min(NV, p.pieces / NT), lower = LOOP ? held + p.spill : held;
+    u32x4 *more = (u32x4 *)(bits + bitmap_words<L>(V));
     auto has = [&](int j) { return j < NV - STEP || j < held; };
+    // the bitmap's bits of this thread's piece in slab j: a constant number of bytes further for each slab
+    const uint8_t *bits0 = (const uint8_t *)bits + ((tid + 1) * N >> 3);
+    const int shift0 = N == 8 ? 0 : ((tid + 1) & 1) * 4;
+    auto listed = [&](int j) { return ((uint32_t)bits0[j * (NT * N / 8)] >> shift0) & (N == 8 ? 255u : 15u); };
     // Slab j's piece.  One that is not wanted comes from the row's first bytes: a branch around each load would
     // double the registers it is loaded into.  (Rows of less than a slab may not have those.)
     auto slab = [&](const L *from, int j, uint32_t off, bool wanted) {
@@ -346,12 +360,12 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
     int t = blockIdx.x, id;
     float q;
     Position x = read_position(p, t);
-    const L *row = p.z + (int64_t)t * p.ld;
+    Span<const L> row(p.z + (int64_t)t * p.ld, V);
     read_entry(p, tid, x, id, q);
     uint32_t off = tid * 16;
 #pragma unroll
-    for (int j = 0; j < AHEAD; ++j, next_slab<NT>(off)) keep[j] = slab(row, j, off, x.what == kScore);
-    clear_bits<NT>(bits, V, sh);
+    for (int j = 0; j < AHEAD; ++j, next_slab<NT>(off)) keep[j] = slab(row.body, j, off, x.what == kScore);
+    clear_bits<NT>(bits, bitmap_words<L>(V), sh);
     __syncthreads();
     for (;;) {
         const int next = t + gridDim.x;
@@ -361,7 +375,7 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
         L *out = GRAD ? p.grad + (int64_t)t * p.ldg : nullptr;
         bool scored = x.what == kScore, far = false;
         if (scored) {
-            mark_entry(id, q, p.k, V, 0, V, sh, bits);
+            mark_entry(id, q, p.k, V, 0, row, sh, bits);
             __syncthreads();
             scored = sh.bad == 0;
         }
@@ -372,35 +386,36 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
             u32x4 shared_piece;
             uint32_t others = 0;
             if (id >= 0) {
-                zj = Piece<L>::one(row + id);
-                const uint32_t listed = listed_bits<N>(bits, id / N);
-                if ((listed & ((1u << (id % N)) - 1)) == 0) {
-                    others = ~listed;
-                    shared_piece = (id / N + 1) * N <= V ? load_piece(row, id / N) : load_last(row, id / N, V);
+                zj = Piece<L>::one(row.body + (id - row.head));
+                const int i = (id - row.head + N) / N - 1, e = (id - row.head + N) % N;
+                const uint32_t here = listed_bits<N>(bits, i);
+                if ((here & ((1u << e) - 1)) == 0) {
+                    others = ~here;
+                    shared_piece = i >= 0 && i < row.whole ? load_piece(row.body, i) : load_edge(row, i);
                 }
             }
             float m = -INFINITY;
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
-                if (has(j)) max_piece<L>(m, keep[j], tid + NT * j, bits);
+                if (has(j)) max_piece<L>(m, keep[j], listed(j));
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (NV <= STEP && held == 0) each_piece<NT, 1>(row, tid, V, [&](u32x4 w, int i) { max_piece<L>(m, w, i, bits); });
+            if (NV <= STEP && held == 0) each_piece<NT, 1>(row, tid, [&](u32x4 w, int i) { max_piece<L>(m, w, listed_bits<N>(bits, i)); });
             m = block_max<NT>(m, red[0]);
             const float B = ref_of(m, p.c);
             off = (tid + NT * AHEAD) * 16;
 #pragma unroll
             for (int j = 0; j < NV; ++j, next_slab<NT>(off)) {
-                if (j + AHEAD < NV) keep[j + AHEAD] = slab(row, j + AHEAD, off, true);
+                if (j + AHEAD < NV) keep[j + AHEAD] = slab(row.body, j + AHEAD, off, true);
                 asm volatile("" : "+v"(keep[j]));   // unpacked again: the floats would take twice the registers
-                if (has(j)) sum_piece<L>(s, keep[j], tid + NT * j, bits, B, p.c);
+                if (has(j)) sum_piece<L>(s, keep[j], listed(j), B, p.c);
             }
             if (LOOP)
-                whole_pieces<NT, 4>(row, tid + NT * held, NT * lower, [&](u32x4 w, int i) {
+                whole_pieces<NT, 4>(row.body, tid + NT * held, NT * lower, [&](u32x4 w, int i) {
                     more[i - NT * held] = w;
-                    sum_piece<L>(s, w, i, bits, B, p.c);
+                    sum_piece<L>(s, w, listed_bits<N>(bits, i), B, p.c);
                 });
-            each_piece<NT, 4, GRAD>(row, tid + NT * lower, V, [&](u32x4 w, int i) { sum_piece<L>(s, w, i, bits, B, p.c); });
+            each_piece<NT, 4, GRAD>(row, tid + NT * lower, [&](u32x4 w, int i) { sum_piece<L>(s, w, listed_bits<N>(bits, i), B, p.c); });
             if (others) {
 #pragma unroll
                 for (int e = 0; e < N; ++e)
@@ -408,9 +423,9 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
             }
             if (tid < p.k) sh.z[tid] = zj;
             a = MaxSum{m, (float)block_sum<NT>(s, red[1])};
-            if (!(a.s < INFINITY) || is_far(m)) a = sum_slowly<L, NT>(row, V, bits, p.c, red);
+            if (!(a.s < INFINITY) || is_far(m)) a = sum_slowly<L, NT>(row, bits, p.c, red);
             far = is_far(a.m);
-            if (id >= 0) bits[id >> 5] = 0;      // every wave is past its sums: ready for the next position
+            if (id >= 0) bits[(id - row.head + N) >> 5] = 0;     // every wave is past its sums: ready for the next position
             finish_row(p, t, x, a, sh);
         } else {
             const float v = x.what == kSkip ? 0.f : __builtin_nanf("");
@@ -418,15 +433,16 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
             if (GRAD) fill_row<L, NT>(out, V, v);
             if (LOOP && x.what == kScore) {      // flagged by its list
                 __syncthreads();
-                clear_bits<NT>(bits, V, sh);
+                clear_bits<NT>(bits, bitmap_words<L>(V), sh);
             }
         }
         const int mine = scored ? id : -1;
-        const L *next_row = p.z + (int64_t)(nx.what == kScore ? next : t) * p.ld;
+        const Span<const L> next_row(p.z + (int64_t)(nx.what == kScore ? next : t) * p.ld, V);
         read_entry(p, tid, nx, id, q);
         if (GRAD) {
             const float coef = sh.coef, B = ref_of(a.m, p.c);
             const bool put = scored && !far;
+            L *body = out + row.head;
             off = tid * 16;
 #pragma unroll
             for (int j = 0; j < NV; ++j, next_slab<NT>(off)) {
@@ -434,19 +450,19 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
                 if (put && has(j)) {
                     float v[N];
                     gradients<L>(v, keep[j], coef, B, p.c);
-                    store_at(out, off, v);
+                    store_at(body, off, v);
                 }
-                if (LOOP && j < AHEAD) keep[j] = slab(next_row, j, off, nx.what == kScore);
+                if (LOOP && j < AHEAD) keep[j] = slab(next_row.body, j, off, nx.what == kScore);
             }
             if (LOOP && put) {
                 for (int i = tid + NT * held; i < NT * lower; i += NT) {
                     float v[N];
                     gradients<L>(v, more[i - NT * held], coef, B, p.c);
-                    store_at(out, (uint32_t)i * 16, v);
+                    store_at(body, (uint32_t)i * 16, v);
                 }
             }
-            if (put) each_piece<NT, 4, GRAD>(row, tid + NT * lower, V, [&](u32x4 w, int i) { put_piece(out, w, i, V, coef, a, p.c); });
-            if (far) put_far<L, NT>(out, row, V, coef, a.m, p.c);
+            if (put) put_pieces<L, NT>(body, row, tid + NT * lower, coef, B, p.c);
+            if (far) put_far<L, NT>(body, row, coef, a.m, p.c);
         }
         if (!GRAD) return;
         __syncthreads();   // the listed entries over what the pass above wrote there
@@ -476,19 +492,19 @@ template <typename L> __global__ __launch_bounds__(kPartThreads) void k_opd_part
     const int lo = seg * q.seg, len = min(q.seg, p.V - lo);
     const Position x = read_position(p, t);
     if (x.what != kScore) return;
-    const L *row = p.z + (int64_t)t * p.ld + lo;
+    const Span<const L> row(p.z + (int64_t)t * p.ld + lo, len);
     int id;
     float tq;
     read_entry(p, tid, x, id, tq);
-    clear_bits<NT>(bits, len, sh);
+    clear_bits<NT>(bits, bitmap_words<L>(len), sh);
     __syncthreads();
-    mark_entry(id, tq, p.k, p.V, lo, len, sh, bits);
+    mark_entry(id, tq, p.k, p.V, lo, row, sh, bits);
     __syncthreads();
-    if (id >= lo && id < lo + len) q.z[(int64_t)t * p.k + tid] = Piece<L>::one(row + (id - lo));
+    if (id >= lo && id < lo + len) q.z[(int64_t)t * p.k + tid] = Piece<L>::one(row.body + (id - lo - row.head));
     MaxSum a{-INFINITY, 0.f};
-    each_piece<NT, 4, true>(row, tid, len, [&](u32x4 w, int i) { add_piece<L>(a, w, i, bits, p.c); });
+    each_piece<NT, 4, true>(row, tid, [&](u32x4 w, int i) { add_piece<L>(a, w, i, bits, p.c); });
     a = block_merge<NT>(a, p.c, red);
-    if (is_far(a.m)) a.s = sum_far<L, NT>(row, len, bits, a.m, p.c, red[2]);
+    if (is_far(a.m)) a.s = sum_far<L, NT>(row, bits, a.m, p.c, red[2]);
     if (tid == 0) q.part[(int64_t)t * q.S + seg] = Part{a.m, a.s, sh.bad, 0};
 }
 
@@ -524,10 +540,9 @@ __global__ __launch_bounds__(kPartThreads) void k_opd_apply(LossParams<L> p, Spl
     __syncthreads();
     finish_row(p, t, x, a, sh, seg == 0);
     if (!GRAD) return;
-    const L *row = p.z + (int64_t)t * p.ld + lo;
-    const float coef = sh.coef;
-    if (is_far(a.m)) put_far<L, NT>(out, row, len, coef, a.m, p.c);
-    else each_piece<NT, 4, true>(row, tid, len, [&](u32x4 w, int i) { put_piece(out, w, i, len, coef, a, p.c); });
+    const Span<const L> row(p.z + (int64_t)t * p.ld + lo, len);
+    if (is_far(a.m)) put_far<L, NT>(out + row.head, row, sh.coef, a.m, p.c);
+    else put_pieces<L, NT>(out + row.head, row, tid, sh.coef, ref_of(a.m, p.c), p.c);
     __syncthreads();
     if (id >= lo && id < lo + len) Piece<L>::put(out + (id - lo), sh.patch[tid]);
 }
@@ -556,13 +571,13 @@ static int compute_units() {
     return n;
 }
 template <typename L, int NT, int NV, int STEP, bool GRAD> static int launch_rows(LossParams<L> p, hipStream_t s) {
-    size_t lds = (size_t)((p.V + 127) / 128) * 16;
+    size_t lds = (size_t)bitmap_words<L>(p.V) * 4;
     int grid = p.T;
     if (kTakesSeveral<NT, NV>) {
         const int cus = compute_units();
         if (grid > cus) grid = cus;
         // beside the bitmap and the entries, a compute unit's 160 KB hold more slabs
-        const int left = p.V / (Piece<L>::N * NT) - NV, room = (int)((kLdsBytes - sizeof(LossShared) - 1024 - lds) / (NT * 16));
+        const int left = p.pieces / NT - NV, room = (int)((kLdsBytes - sizeof(LossShared) - 1024 - lds) / (NT * 16));
         p.spill = left < 0 ? 0 : left < room ? left : room;
         lds += (size_t)p.spill * NT * 16;
     }
@@ -572,13 +587,13 @@ template <typename L, int NT, int NV, int STEP, bool GRAD> static int launch_row
 
 template <typename L> static int launch_split(const LossParams<L> &p, SplitParams q, hipStream_t s) {
     const dim3 grid((unsigned)(p.T * q.S)), block(kPartThreads);
-    hipLaunchKernelGGL(k_opd_part<L>, grid, block, (size_t)((q.seg + 31) / 32) * 4, s, p, q);
+    hipLaunchKernelGGL(k_opd_part<L>, grid, block, (size_t)bitmap_words<L>(q.seg) * 4, s, p, q);
     if (p.grad) hipLaunchKernelGGL((k_opd_apply<L, true>), grid, block, 0, s, p, q);
     else hipLaunchKernelGGL((k_opd_apply<L, false>), dim3(p.T), block, 0, s, p, q);
     return hipGetLastError() == hipSuccess ? PIPO_OK : PIPO_EHIP;
 }
 
-template <typename L> static int launch_loss(const LossParams<L> &p, void *work, hipStream_t s) {
+template <typename L> static int launch_loss(LossParams<L> p, void *work, hipStream_t s) {
     if (work && split_bytes(p.T, p.V, p.k) > 0) {
         SplitParams q;
         split_of(p.T, p.V, q.S, q.seg);
@@ -586,7 +601,7 @@ template <typename L> static int launch_loss(const LossParams<L> &p, void *work,
         q.z = (float *)(q.part + (int64_t)p.T * q.S);
         return launch_split(p, q, s);
     }
-    const int n = p.V / Piece<L>::N;
+    const int n = p.pieces = least_whole(p.z, p.ld, p.T, p.V);
     if (!p.grad) {
         if (n <= 256 * 32) return launch_rows<L, 256, 4, 4, false>(p, s);
         return launch_rows<L, 512, 4, 4, false>(p, s);
@@ -604,7 +619,7 @@ template <typename L> static int launch_loss(const LossParams<L> &p, void *work,
     if (n < 512 * 25) return launch_rows<L, 512, 24, 4, true>(p, s);
     if (n < 512 * 29) return launch_rows<L, 512, 28, 4, true>(p, s);
     if (n < 512 * (sizeof(L) == 4 ? 31 : 33)) return launch_rows<L, 512, 32, 4, true>(p, s);
-    return launch_rows<L, 512, sizeof(L) == 4 ? 34 : 36, 4, true>(p, s);   // (what fits beside the other values)
+    return launch_rows<L, 512, sizeof(L) == 4 ? 33 : 35, 4, true>(p, s);   // (what fits beside the other values)
 }
 
 // ---- checks ---------------------------------------------------------------------

@@ -17,15 +17,17 @@ bool opd_rows_ok(int32_t T, int32_t V, const void *z, int64_t ld, double tempera
 bool opd_work_ok(const void *work, int64_t work_bytes, int64_t need);
 int64_t opd_loss_work_bytes(int T, int V, int k);
 
-// ---- 16 bytes of a row --------------------------------------------------------
-// Rows start at any multiple of the element size (odd vocabularies, padded or
-// sliced rows): the pieces are loaded and stored as 16 bytes all the same,
-// which the hardware does at any alignment.
-
+// ---- pieces of 16 bytes of a row ------------------------------------------------
+// A row may start at any multiple of its element (odd vocabularies, padded or
+// sliced rows); 16-byte accesses across the grid of 16 are slow (512 x 50021 bf16
+// rows with their gradient: 35 us, from aligned pieces 24).  So its pieces lie on
+// the grid: piece 0 starts `head` elements into the row, and what is before it
+// (piece -1) and behind the last whole one are partial pieces, taken element by
+// element.
 template <typename L> struct Piece;
 template <> struct Piece<float> {
     static constexpr int N = 4;
-    typedef u32x4 __attribute__((aligned(4))) raw_t;
+    typedef u32x4 __attribute__((aligned(4))) raw_t;     // (a gradient's rows need not lie like the logits')
     static __device__ __forceinline__ float get(u32x4 w, int e) { return __uint_as_float(w[e]); }
     static __device__ __forceinline__ u32x4 pack(const float *v) {
         return u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
@@ -46,16 +48,37 @@ template <> struct Piece<uint16_t> {
     static constexpr uint32_t kNegInf = 0xFF80FF80u;
 };
 
-// Piece i of a row, whole; and the last, partial piece of a row of n elements,
-// whose elements behind the row's end read as -inf and are not written.
-// AGAIN: the piece is read twice, and may stay in the caches.
-template <typename L, bool AGAIN = false> __device__ __forceinline__ u32x4 load_piece(const L *row, int i) {
-    const typename Piece<L>::raw_t *at = (const typename Piece<L>::raw_t *)(row + (int64_t)i * Piece<L>::N);
+template <typename L> struct Span {
+    L *body;                        // piece 0
+    int head, n, whole;             // elements before piece 0, elements in all, whole pieces
+    __device__ __forceinline__ Span(L *row, int n_) : n(n_) {
+        constexpr int es = sizeof(L);
+        head = min((int)((16 - ((uintptr_t)row & 15)) & 15) / es, n);
+        body = row + head;
+        whole = (n - head) / (16 / es);
+    }
+    // no partial pieces (the same for the whole workgroup)
+    __device__ __forceinline__ bool exact() const { return head == 0 && whole * (int)(16 / sizeof(L)) == n; }
+    __device__ __forceinline__ bool has(int i, int e) const {   // element e of piece i
+        const int at = i * (int)(16 / sizeof(L)) + e;
+        return at >= -head && at < n - head;
+    }
+};
+// The fewest whole pieces that one of the rows has.
+template <typename L> inline int least_whole(const L *z, int64_t ld, int T, int n) {
+    constexpr int N = 16 / sizeof(L);
+    if (((uintptr_t)z & 15) == 0 && (T == 1 || ld % N == 0)) return n / N;
+    return n < N ? 0 : (n - N + 1) / N;
+}
+
+// Piece i, whole.  AGAIN: it is read twice, and may stay in the caches.
+template <typename L, bool AGAIN = false> __device__ __forceinline__ u32x4 load_piece(const L *body, int i) {
+    const typename Piece<L>::raw_t *at = (const typename Piece<L>::raw_t *)(body + (int64_t)i * Piece<L>::N);
     if (AGAIN) return *at;
     return __builtin_nontemporal_load(at);
 }
-template <typename L> __device__ __forceinline__ void store_piece(L *row, int i, const float *v) {
-    __builtin_nontemporal_store(Piece<L>::pack(v), (typename Piece<L>::raw_t *)(row + (int64_t)i * Piece<L>::N));
+template <typename L> __device__ __forceinline__ void store_piece(L *body, int i, const float *v) {
+    __builtin_nontemporal_store(Piece<L>::pack(v), (typename Piece<L>::raw_t *)(body + (int64_t)i * Piece<L>::N));
 }
 // The same by byte offset from the row's start, for unrolled walks: with the
 // offset in a register that the compiler cannot see through (next_slab), it does
@@ -71,44 +94,50 @@ template <int NT> __device__ __forceinline__ void next_slab(uint32_t &off) {
     asm volatile("" : "+v"(off));
     __builtin_amdgcn_sched_barrier(0);  // nor mixes the steps, whose temporaries would not fit beside the row
 }
-template <typename L> __device__ __forceinline__ u32x4 load_last(const L *row, int i, int n) {
+// A partial piece: elements outside the row read as -inf and are not written.
+// (out: where a gradient's piece 0 lies.)
+template <typename L> __device__ __forceinline__ u32x4 load_edge(const Span<const L> &row, int i) {
     typedef Piece<L> P;
     u32x4 w{P::kNegInf, P::kNegInf, P::kNegInf, P::kNegInf};
 #pragma unroll
     for (int e = 0; e < P::N; ++e) {
-        if (i * P::N + e >= n) continue;
-        if (sizeof(L) == 4) w[e] = ((const uint32_t *)row)[i * P::N + e];
-        else if (e & 1) w[e >> 1] = (w[e >> 1] & 0xFFFFu) | ((uint32_t)((const uint16_t *)row)[i * P::N + e] << 16);
-        else w[e >> 1] = (w[e >> 1] & 0xFFFF0000u) | ((const uint16_t *)row)[i * P::N + e];
+        if (!row.has(i, e)) continue;
+        const int at = i * P::N + e;
+        if (sizeof(L) == 4) w[e] = ((const uint32_t *)row.body)[at];
+        else if (e & 1) w[e >> 1] = (w[e >> 1] & 0xFFFFu) | ((uint32_t)((const uint16_t *)row.body)[at] << 16);
+        else w[e >> 1] = (w[e >> 1] & 0xFFFF0000u) | ((const uint16_t *)row.body)[at];
     }
     return w;
 }
-template <typename L> __device__ __forceinline__ void store_last(L *row, int i, int n, const float *v) {
+template <typename L, typename S> __device__ __forceinline__ void store_edge(L *out, const Span<S> &row, int i, const float *v) {
 #pragma unroll
     for (int e = 0; e < Piece<L>::N; ++e)
-        if (i * Piece<L>::N + e < n) Piece<L>::put(row + i * Piece<L>::N + e, v[e]);
+        if (row.has(i, e)) Piece<L>::put(out + i * Piece<L>::N + e, v[e]);
 }
 // Calls f(piece, its index) for this thread's whole pieces from index first up to
 // end, NT apart and U of them in flight.
 template <int NT, int U, bool AGAIN = false, typename L, typename F>
-__device__ __forceinline__ void whole_pieces(const L *row, int first, int end, F f) {
+__device__ __forceinline__ void whole_pieces(const L *body, int first, int end, F f) {
     int i = first;
     for (; i + (U - 1) * NT < end; i += U * NT) {
         u32x4 w[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) w[u] = load_piece<L, AGAIN>(row, i + u * NT);
+        for (int u = 0; u < U; ++u) w[u] = load_piece<L, AGAIN>(body, i + u * NT);
 #pragma unroll
         for (int u = 0; u < U; ++u) f(w[u], i + u * NT);
     }
-    for (; i < end; i += NT) f(load_piece<L, AGAIN>(row, i), i);
+    for (; i < end; i += NT) f(load_piece<L, AGAIN>(body, i), i);
 }
-// ... of a row of n elements, and the partial piece at its end, which belongs to
-// the thread whose turn it is.
+// ... and calls edge(piece, its index) for the partial ones, which belong to the last two threads.
+template <int NT, typename L, typename F> __device__ __forceinline__ void edges(const Span<const L> &row, F edge) {
+    if (row.exact() || (int)threadIdx.x < NT - 2) return;
+    const int i = (int)threadIdx.x == NT - 1 ? -1 : row.whole;
+    edge(load_edge(row, i), i);     // (empty where only the other one is there)
+}
 template <int NT, int U, bool AGAIN = false, typename L, typename F>
-__device__ __forceinline__ void each_piece(const L *row, int first, int n, F f) {
-    const int whole = n / Piece<L>::N;
-    whole_pieces<NT, U, AGAIN>(row, first, whole, f);
-    if (whole * Piece<L>::N < n && first % NT == whole % NT) f(load_last(row, whole, n), whole);
+__device__ __forceinline__ void each_piece(const Span<const L> &row, int first, F f) {
+    whole_pieces<NT, U, AGAIN>(row.body, first, row.whole, f);
+    edges<NT>(row, f);
 }
 
 // ---- exp(z / temperature) over a reference -------------------------------------------

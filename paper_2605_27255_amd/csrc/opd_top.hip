@@ -131,12 +131,13 @@ __global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
     __shared__ TopShared<NT, H> sh;
     const int t = SPLIT ? blockIdx.x / p.S : blockIdx.x, seg = SPLIT ? blockIdx.x % p.S : 0;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int lo = seg * p.seg, V = min(p.seg, p.V - lo), k = min(p.k, V), n = (V + N - 1) / N, whole = V / N;
-    const L *row = p.z + (int64_t)t * p.ld + lo;
+    const int lo = seg * p.seg, V = min(p.seg, p.V - lo), k = min(p.k, V);
+    const Span<const L> row(p.z + (int64_t)t * p.ld + lo, V);
+    const int n = row.whole;        // (the partial pieces, at most 14 values, are candidates in any case)
 
     // unit h NT + tid: the pieces tid + NT j for j from h per on, per of them
     const int per = (n + NT * H - 1) / (NT * H);
-    MaxSum unit[H], own{-INFINITY, 0.f};
+    MaxSum unit[H];
 #pragma unroll
     for (int h = 0; h < H; ++h) {
         unit[h] = MaxSum{-INFINITY, 0.f};
@@ -147,32 +148,33 @@ __global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
             for (int e = 0; e < N; ++e) v[e] = Piece<L>::get(w, e);
             add_values<N>(unit[h], v, p.c);
         };
-        whole_pieces<NT, 4>(row, first, min(end, whole), add);
-        if (whole < n && whole >= first && whole < end && (whole - first) % NT == 0) add(load_last(row, whole, V), whole);
+        whole_pieces<NT, 4>(row.body, first, min(end, n), add);
     }
-    float least_own = INFINITY;
+    float least_own = INFINITY, most_own = -INFINITY;
 #pragma unroll
     for (int h = 0; h < H; ++h) {
         const bool used = tid + h * per * NT < n;
         sh.umax[h * NT + tid] = used ? value_key(unit[h].m) : 0u;
         if (used) least_own = fminf(least_own, unit[h].m);
-        own.m = fmaxf(own.m, unit[h].m);
+        most_own = fmaxf(most_own, unit[h].m);
     }
+    edges<NT>(row, [&](u32x4 w, int) {
 #pragma unroll
-    for (int h = 0; h < H; ++h) own.s += unit[h].s * __builtin_amdgcn_exp2f(ref_of(unit[h].m, p.c) - ref_of(own.m, p.c));
+        for (int e = 0; e < N; ++e) most_own = fmaxf(most_own, Piece<L>::get(w, e));
+    });
     // the least of them, as the largest of the negated maxima (-0 and 0 have one key)
     const float least_w = -wave_max_dpp(-least_own);
     if (lane == 0) sh.wmin[wave] = value_key(least_w);
     if (tid == 0) sh.n = 0;
-    const MaxSum all = block_merge<NT>(own, p.c, sh.red);   // its barrier: tmax, wmin and n are set
-    const bool far = is_far(all.m);
-    const float B = ref_of(all.m, p.c);
-    auto term = [&](float v) { return far ? exp_diff(v, all.m, p.c) : exp_at(v, B, p.c); };
+    const float m = block_max<NT>(most_own, sh.red[0]);     // its barrier: umax, wmin and n are set
+    const bool far = is_far(m);
+    const float B = ref_of(m, p.c);
+    auto term = [&](float v) { return far ? exp_diff(v, m, p.c) : exp_at(v, B, p.c); };
     uint32_t least = sh.wmin[0];
 #pragma unroll
     for (int w = 1; w < W; ++w) least = min(least, sh.wmin[w]);
     // fewer pieces than k: everything is a candidate
-    const uint32_t bound = n < k ? 0u : bound_of_kth(sh, least, value_key(all.m), k);
+    const uint32_t bound = n < k ? 0u : bound_of_kth(sh, least, value_key(m), k);
 
     // the units that reach the bound, again
     float rest = 0.f;
@@ -201,6 +203,19 @@ __global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
         at += __popcll(ball[h]);
     }
     __syncthreads();
+    auto take = [&](u32x4 w, int i) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float v = Piece<L>::get(w, e);
+            const uint32_t key = value_key(v);
+            if (key >= bound && row.has(i, e)) {
+                const int c = atomicAdd(&sh.n, 1);
+                if (c < kTopCand) sh.cand[c] = pair_key(key, row.head + i * N + e);
+            } else {
+                rest += term(v);
+            }
+        }
+    };
     for (int x0 = tid; x0 < total * per; x0 += 4 * NT) {
         u32x4 w[4];
         int at[4];
@@ -208,25 +223,14 @@ __global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
         for (int u = 0; u < 4; ++u) {       // four in flight: this is all latency
             const int x = x0 + u * NT;
             at[u] = x < total * per ? (int)list[x / per] + NT * (x % per) : n;
-            if (at[u] < V / N) w[u] = load_piece(row, at[u]);
-            else if (at[u] < n) w[u] = load_last(row, at[u], V);
+            if (at[u] < n) w[u] = load_piece(row.body, at[u]);
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            if (at[u] >= n) continue;
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const float v = Piece<L>::get(w[u], e);
-                const uint32_t key = value_key(v);
-                if (key >= bound && at[u] * N + e < V) {
-                    const int c = atomicAdd(&sh.n, 1);
-                    if (c < kTopCand) sh.cand[c] = pair_key(key, at[u] * N + e);
-                } else {
-                    rest += term(v);
-                }
-            }
+            if (at[u] < n) take(w[u], at[u]);
         }
     }
+    edges<NT>(row, take);
     __syncthreads();
     int nc = sh.n;
     if (nc > kTopCand || nc < k || far) {   // too many (ties), or NaNs, which no maximum sees, or sums that do not fit:
@@ -238,11 +242,11 @@ __global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
             __syncthreads();
             for (int i = tid; i < 256; i += NT) sh.hist[i] = 0;
             __syncthreads();
-            each_piece<NT, 4>(row, tid, V, [&](u32x4 w, int i) {
+            each_piece<NT, 4>(row, tid, [&](u32x4 w, int i) {
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    if (i * N + e >= V) continue;
-                    const uint64_t key = pair_key(value_key(Piece<L>::get(w, e)), i * N + e);
+                    if (!row.has(i, e)) continue;
+                    const uint64_t key = pair_key(value_key(Piece<L>::get(w, e)), row.head + i * N + e);
                     if (bits > 8 && (key >> (sh_bits + 8)) != (thr >> (sh_bits + 8))) continue;
                     const int bin = (int)(key >> sh_bits) & 255;
                     // values of a crowded row share their bins: one addition for a wave of equal ones
@@ -270,12 +274,12 @@ __global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
         if (tid == 0) sh.n = 0;
         __syncthreads();
         rest = 0.f;
-        each_piece<NT, 4>(row, tid, V, [&](u32x4 w, int i) {
+        each_piece<NT, 4>(row, tid, [&](u32x4 w, int i) {
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                if (i * N + e >= V) continue;
+                if (!row.has(i, e)) continue;
                 const float v = Piece<L>::get(w, e);
-                const uint64_t key = pair_key(value_key(v), i * N + e);
+                const uint64_t key = pair_key(value_key(v), row.head + i * N + e);
                 if (key >= thr) sh.cand[atomicAdd(&sh.n, 1)] = key;
                 else rest += term(v);
             }
@@ -292,9 +296,9 @@ __global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
             const uint64_t key = j < k ? sh.sorted[j] : 0;
             keys[j] = key ? pair_key((uint32_t)(key >> 32), key_id(key) + lo) : 0;
         }
-        if (tid == 0) p.part[(int64_t)t * p.S + seg] = Part{all.m, (float)outside, 0, 0};
+        if (tid == 0) p.part[(int64_t)t * p.S + seg] = Part{m, (float)outside, 0, 0};
     } else if (wave == 0) {
-        put_top(p, t, sh.sorted, all.m, outside * unit_of_max(all.m, p.c));
+        put_top(p, t, sh.sorted, m, outside * unit_of_max(m, p.c));
     }
 }
 
