@@ -335,15 +335,16 @@ __device__ __forceinline__ MaxSum sum_slowly(const Span<const L> &row, const uin
 // AHEAD slabs before their sum, so that neither loads nor sums wait for all of
 // the other.
 template <int NT, int NV> constexpr bool kTakesSeveral = NT == 512 && NV >= 12;    // one workgroup fills a compute unit
+template <int NT, int NV> constexpr bool kSpills = NV >= (NT == 512 ? 33 : 44);     // the longest rows' variants
 template <typename L, int NT, int NV, int STEP, bool GRAD>
 __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
-    constexpr bool LOOP = kTakesSeveral<NT, NV>;
+    constexpr bool LOOP = kTakesSeveral<NT, NV>, DEEP = kSpills<NT, NV>;
     constexpr int AHEAD = NV < 12 ? NV : 12, N = Piece<L>::N;
     extern __shared__ uint32_t bits[];
     __shared__ LossShared sh;
     __shared__ float red[2][NT / 64];
     const int tid = threadIdx.x, V = p.V;
-    const int held = min(NV, p.pieces / NT), lower = LOOP ? held + p.spill : held;
+    const int held = min(NV, p.pieces / NT), lower = DEEP ? held + p.spill : held;
     u32x4 *more = (u32x4 *)(bits + bitmap_words<L>(V));
     auto has = [&](int j) { return j < NV - STEP || j < held; };
     // the bitmap's bits of this thread's piece in slab j: a constant number of bytes further for each slab
@@ -410,7 +411,7 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
                 asm volatile("" : "+v"(keep[j]));   // unpacked again: the floats would take twice the registers
                 if (has(j)) sum_piece<L>(s, keep[j], listed(j), B, p.c);
             }
-            if (LOOP)
+            if (DEEP)
                 whole_pieces<NT, 4>(row.body, tid + NT * held, NT * lower, [&](u32x4 w, int i) {
                     more[i - NT * held] = w;
                     sum_piece<L>(s, w, listed_bits<N>(bits, i), B, p.c);
@@ -454,7 +455,7 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
                 }
                 if (LOOP && j < AHEAD) keep[j] = slab(next_row.body, j, off, nx.what == kScore);
             }
-            if (LOOP && put) {
+            if (DEEP && put) {
                 for (int i = tid + NT * held; i < NT * lower; i += NT) {
                     float v[N];
                     gradients<L>(v, more[i - NT * held], coef, B, p.c);
@@ -576,8 +577,11 @@ template <typename L, int NT, int NV, int STEP, bool GRAD> static int launch_row
     if (kTakesSeveral<NT, NV>) {
         const int cus = compute_units();
         if (grid > cus) grid = cus;
-        // beside the bitmap and the entries, a compute unit's 160 KB hold more slabs
-        const int left = p.pieces / NT - NV, room = (int)((kLdsBytes - sizeof(LossShared) - 1024 - lds) / (NT * 16));
+    }
+    if (kSpills<NT, NV>) {
+        // beside the bitmap and the entries, a compute unit's 160 KB (for one workgroup of 512 or two of 256) hold more slabs
+        const int left = p.pieces / NT - NV;
+        const int room = (int)((kLdsBytes / (NT == 512 ? 1 : 2) - sizeof(LossShared) - 1024 - lds) / (NT * 16));
         p.spill = left < 0 ? 0 : left < room ? left : room;
         lds += (size_t)p.spill * NT * 16;
     }
@@ -606,6 +610,11 @@ template <typename L> static int launch_loss(LossParams<L> p, void *work, hipStr
         if (n <= 256 * 32) return launch_rows<L, 256, 4, 4, false>(p, s);
         return launch_rows<L, 512, 4, 4, false>(p, s);
     }
+    // Workgroups of four waves, as many to a compute unit as their registers allow (two with 44 slabs): while one sums
+    // or finishes a row, others load and write.  Only rows of which two leave most to be read again go to one workgroup
+    // of eight waves a compute unit, which holds twice as much.  With the gradient, two of four waves / one of eight,
+    // in us: 2048 x 100000 bf16 159 / 170, 2048 x 151936 bf16 231 / 253, 1187 x 262144 bf16 267 / 248; fp32 1944 x 80000
+    // 233 / 245, 2048 x 100000 321 / 316, 2048 x 151936 534 / 515.
     if (n < 256 * 3) return launch_rows<L, 256, 2, 2, true>(p, s);
     if (n < 256 * 5) return launch_rows<L, 256, 4, 2, true>(p, s);
     if (n < 256 * 7) return launch_rows<L, 256, 6, 2, true>(p, s);
@@ -614,12 +623,11 @@ template <typename L> static int launch_loss(LossParams<L> p, void *work, hipStr
     if (n < 256 * 17) return launch_rows<L, 256, 16, 4, true>(p, s);
     if (n < 256 * 21) return launch_rows<L, 256, 20, 4, true>(p, s);
     if (n < 256 * 26) return launch_rows<L, 256, 24, 4, true>(p, s);
-    if (n < 512 * 17) return launch_rows<L, 512, 16, 4, true>(p, s);
-    if (n < 512 * 21) return launch_rows<L, 512, 20, 4, true>(p, s);
-    if (n < 512 * 25) return launch_rows<L, 512, 24, 4, true>(p, s);
-    if (n < 512 * 29) return launch_rows<L, 512, 28, 4, true>(p, s);
-    if (n < 512 * (sizeof(L) == 4 ? 31 : 33)) return launch_rows<L, 512, 32, 4, true>(p, s);
-    return launch_rows<L, 512, sizeof(L) == 4 ? 33 : 35, 4, true>(p, s);   // (what fits beside the other values)
+    if (n < 256 * 30) return launch_rows<L, 256, 29, 4, true>(p, s);
+    if (n < 256 * 35) return launch_rows<L, 256, 34, 5, true>(p, s);
+    if (n < 256 * 40) return launch_rows<L, 256, 39, 5, true>(p, s);
+    if (n < 256 * 82) return launch_rows<L, 256, 44, 5, true>(p, s);
+    return launch_rows<L, 512, sizeof(L) == 4 ? 33 : 35, 4, true>(p, s);    // (slabs that fit beside the other values)
 }
 
 // ---- checks ---------------------------------------------------------------------
