@@ -249,10 +249,11 @@ int pipo_opd_targets_bf16(int32_t T, int32_t V, const uint16_t *d_logits_s, cons
  * of positive probability, or with a NaN or +inf, gives NaN results (ids
  * stay in range).  Outputs must not overlap inputs or each other, except that
  * a gradient may be written over the logits themselves (same address and ld).
- * d_work: device scratch of at least pipo_opd_work_bytes(T, V, k) bytes (k = 1
- * for pipo_opd_policy), 16-byte aligned, whose contents matter neither before
- * nor after; calls that may overlap need one each.  With NULL every row is
- * worked on by one workgroup, which is slower for few long rows.
+ * d_work: device scratch of at least pipo_opd_work_bytes(call, T, V, k, bf16)
+ * bytes (call: PIPO_OPD_CALL_*, k = 1 for pipo_opd_policy; 0 where none is
+ * needed), 16-byte aligned, whose contents matter neither before nor after;
+ * calls that may overlap need one each.  With NULL every row is worked on by
+ * one workgroup, which is slower for few long rows.
  * Errors: PIPO_EINVAL (NULL pointers with T > 0, sizes, kind, beta,
  * temperature, clip bounds or coefficient outside their ranges, misaligned
  * rows, d_logits and d_grad that overlap in part, work_bytes too small for a
@@ -293,7 +294,10 @@ int pipo_opd_targets_bf16(int32_t T, int32_t V, const uint16_t *d_logits_s, cons
 #define PIPO_OPD_FORWARD  0
 #define PIPO_OPD_REVERSE  1
 #define PIPO_OPD_JSD      2
-int64_t pipo_opd_work_bytes(int32_t T, int32_t V, int32_t k);
+#define PIPO_OPD_CALL_TOP   0   /* pipo_opd_top_logits                        */
+#define PIPO_OPD_CALL_LOSS  1   /* a loss without its gradient (d_grad NULL)  */
+#define PIPO_OPD_CALL_GRAD  2   /* a loss with its gradient                   */
+int64_t pipo_opd_work_bytes(int32_t call, int32_t T, int32_t V, int32_t k, int32_t bf16);
 int pipo_opd_top_logits(int32_t T, int32_t V, const float *d_logits, int64_t ld, double temperature, int32_t k,
                         int32_t *d_ids, float *d_logp, float *d_tail, void *d_work, int64_t work_bytes, void *stream);
 int pipo_opd_top_logits_bf16(int32_t T, int32_t V, const uint16_t *d_logits, int64_t ld, double temperature, int32_t k,

@@ -477,7 +477,8 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
 
 // ---- few rows: several workgroups each ----------------------------------------------
 constexpr int kPartThreads = 256;
-constexpr int kSplitRows = 160;     // more rows than this go one workgroup each
+constexpr int kSplitRows = 96;                  // more rows than this go one workgroup each
+constexpr int64_t kSplitGrad = 192 << 10, kSplitSum = 400 << 10;     // ... and shorter ones (bytes)
 struct SplitParams {
     Part *part;                     // [T][S]
     float *z;                       // [T][k] the listed logits
@@ -548,21 +549,25 @@ __global__ __launch_bounds__(kPartThreads) void k_opd_apply(LossParams<L> p, Spl
     if (id >= lo && id < lo + len) Piece<L>::put(out + (id - lo), sh.patch[tid]);
 }
 
-// Segments of each row: about two workgroups a compute unit in all, at least 4096 elements each.
-static void split_of(int T, int V, int &S, int &seg) {
+// Segments of each row: about two workgroups a compute unit in all, at least
+// 4096 elements each.  The second launch takes 4 us of the host's time, so a row
+// is split only where one workgroup would take longer than that over it: with
+// the gradient (bf16, us for split / whole) 8 x 65536 15.5 / 13.5, 8 x 151936
+// 15.6 / 20, 64 x 151936 16 / 22, 128 x 151936 27 / 25; without it 8 x 151936
+// bf16 14.5 / 12.6.
+static void split_of(int T, int V, int es, bool grad, int &S, int &seg) {
     S = 512 / (T > 0 ? T : 1);
     if (S > kMaxParts) S = kMaxParts;
     if (S > V / 4096) S = V / 4096;
-    if (S < 2 || T > kSplitRows) { S = 1; seg = V; return; }
+    if (S < 2 || T > kSplitRows || (int64_t)V * es < (grad ? kSplitGrad : kSplitSum)) { S = 1; seg = V; return; }
     seg = ((V + S - 1) / S + 255) / 256 * 256;
     S = (V + seg - 1) / seg;
 }
-static int64_t split_bytes(int T, int V, int k) {
+int64_t opd_loss_work_bytes(int T, int V, int k, int es, bool grad) {
     int S, seg;
-    split_of(T, V, S, seg);
+    split_of(T, V, es, grad, S, seg);
     return S > 1 ? (int64_t)T * S * (int64_t)sizeof(Part) + (int64_t)T * k * 4 : 0;
 }
-int64_t opd_loss_work_bytes(int T, int V, int k) { return split_bytes(T, V, k); }
 
 // Workgroups of a launch: one a row, or where a workgroup fills a compute unit
 // (its registers hold a long row) one a compute unit, which takes several rows.
@@ -598,16 +603,20 @@ template <typename L> static int launch_split(const LossParams<L> &p, SplitParam
 }
 
 template <typename L> static int launch_loss(LossParams<L> p, void *work, hipStream_t s) {
-    if (work && split_bytes(p.T, p.V, p.k) > 0) {
+    if (work && opd_loss_work_bytes(p.T, p.V, p.k, sizeof(L), p.grad != nullptr) > 0) {
         SplitParams q;
-        split_of(p.T, p.V, q.S, q.seg);
+        split_of(p.T, p.V, sizeof(L), p.grad != nullptr, q.S, q.seg);
         q.part = (Part *)work;
         q.z = (float *)(q.part + (int64_t)p.T * q.S);
         return launch_split(p, q, s);
     }
     const int n = p.pieces = least_whole(p.z, p.ld, p.T, p.V);
     if (!p.grad) {
-        if (n <= 256 * 32) return launch_rows<L, 256, 4, 4, false>(p, s);
+        // Few rows: all of a compute unit's waves on each; many short ones: several rows to a compute unit.  Four / eight /
+        // sixteen waves, us: 128 x 151936 fp32 34 / 22 / 18, 256 x 32003 bf16 10.8 / 9.2 / 8.3, 512 x 32003 bf16
+        // 13.1 / 11.8 / 15.6, 2048 x 8192 bf16 13.5 / 16.6 / 35, 2048 x 151936 bf16 104 / 98 / 120.
+        if (p.T <= 256 && n >= 4000) return launch_rows<L, 1024, 4, 4, false>(p, s);
+        if (p.T > 1024 && n <= 256 * 32) return launch_rows<L, 256, 4, 4, false>(p, s);
         return launch_rows<L, 512, 4, 4, false>(p, s);
     }
     // Workgroups of four waves, as many to a compute unit as their registers allow (two with 44 slabs): while one sums
@@ -661,7 +670,7 @@ static int check_common(const LossParams<L> &p, double temperature, const void *
     if (p.grad && (!aligned(p.grad, sizeof(L)) || (p.T > 1 && (p.ldg < p.V || p.ldg > kOpdMaxStride)) ||
                    !same_or_apart(p.z, p.ld, p.grad, p.ldg, p.T, p.V, sizeof(L))))
         return PIPO_EINVAL;
-    return opd_work_ok(work, work_bytes, split_bytes(p.T, p.V, p.k)) ? PIPO_OK : PIPO_EINVAL;
+    return opd_work_ok(work, work_bytes, opd_loss_work_bytes(p.T, p.V, p.k, sizeof(L), p.grad != nullptr)) ? PIPO_OK : PIPO_EINVAL;
 }
 
 template <typename L>

@@ -15,7 +15,7 @@ struct Part { float m, s; int bad, pad; };      // what a segment of a row leave
 // ---- checks on the host, shared by the entry points ---------------------------------
 bool opd_rows_ok(int32_t T, int32_t V, const void *z, int64_t ld, double temperature, size_t es);
 bool opd_work_ok(const void *work, int64_t work_bytes, int64_t need);
-int64_t opd_loss_work_bytes(int T, int V, int k);
+int64_t opd_loss_work_bytes(int T, int V, int k, int es, bool grad);
 
 // ---- pieces of 16 bytes of a row ------------------------------------------------
 // A row may start at any multiple of its element (odd vocabularies, padded or

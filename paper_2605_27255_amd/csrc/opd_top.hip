@@ -341,20 +341,23 @@ template <typename L> __global__ __launch_bounds__(kJoinThreads) void k_opd_top_
     if (tid < 64) put_top(p, t, sh.sorted, rests.m, outside * unit_of_max(rests.m, p.c));
 }
 
-// Segments of each row: about four workgroups a compute unit in all, at least
+// Segments of each row: about two workgroups a compute unit in all, at least
 // 4096 elements each, and no more keys than the joining workgroup has threads.
-static void top_split(int T, int V, int k, int &S, int &seg) {
-    S = T <= 96 ? 512 / T : 1;
+// Two launches pay for few long rows (bf16, top 20, us for split / whole): 8 x
+// 65536 15.1 / 11.6, 8 x 151936 15.1 / 17.4, 64 x 151936 18 / 22, 128 x 151936
+// 23 / 22.
+static void top_split(int T, int V, int k, int es, int &S, int &seg) {
+    S = 512 / T;
     if (S > kMaxParts) S = kMaxParts;
     if (S > V / 4096) S = V / 4096;
     if (S > kJoinThreads / k) S = kJoinThreads / k;
-    if (S < 2) { S = 1; seg = V; return; }
+    if (S < 2 || T > 96 || (int64_t)V * es < 256 << 10) { S = 1; seg = V; return; }
     seg = ((V + S - 1) / S + 255) / 256 * 256;
     S = (V + seg - 1) / seg;
 }
-static int64_t top_bytes(int T, int V, int k) {
+static int64_t top_bytes(int T, int V, int k, int es) {
     int S, seg;
-    top_split(T, V, k, S, seg);
+    top_split(T, V, k, es, S, seg);
     return S > 1 ? (int64_t)T * S * ((int64_t)sizeof(Part) + (int64_t)k * 8) : 0;
 }
 
@@ -363,11 +366,11 @@ static int top_logits(int32_t T, int32_t V, const L *d_logits, int64_t ld, doubl
                       int32_t *d_ids, float *d_logp, float *d_tail, void *d_work, int64_t work_bytes, void *stream) {
     if (!opd_rows_ok(T, V, d_logits, ld, temperature, sizeof(L)) || k < 1 || k > kTopMax || k > V) return PIPO_EINVAL;
     if (T == 0) return PIPO_OK;
-    if (!d_ids || !d_logp || !opd_work_ok(d_work, work_bytes, top_bytes(T, V, k))) return PIPO_EINVAL;
+    if (!d_ids || !d_logp || !opd_work_ok(d_work, work_bytes, top_bytes(T, V, k, sizeof(L)))) return PIPO_EINVAL;
     TopParams<L> p{d_logits, ld, T, V, k, exp_scale(temperature), d_ids, d_logp, d_tail, 1, V, nullptr, nullptr};
     hipStream_t s = (hipStream_t)stream;
-    if (d_work && top_bytes(T, V, k) > 0) {
-        top_split(T, V, k, p.S, p.seg);
+    if (d_work && top_bytes(T, V, k, sizeof(L)) > 0) {
+        top_split(T, V, k, sizeof(L), p.S, p.seg);
         p.part = (Part *)d_work;
         p.keys = (uint64_t *)(p.part + (int64_t)T * p.S);
         hipLaunchKernelGGL((k_opd_top<L, 256, true>), dim3(T * p.S), dim3(256), 0, s, p);
@@ -384,10 +387,10 @@ static int top_logits(int32_t T, int32_t V, const L *d_logits, int64_t ld, doubl
 
 using namespace pipo;
 
-extern "C" int64_t pipo_opd_work_bytes(int32_t T, int32_t V, int32_t k) {
-    if (T < 1 || V < 1 || V > kOpdMaxVocab || k < 1) return 0;
-    const int64_t loss = opd_loss_work_bytes(T, V, k), top = k <= kTopMax && k <= V ? top_bytes(T, V, k) : 0;
-    return loss > top ? loss : top;
+extern "C" int64_t pipo_opd_work_bytes(int32_t call, int32_t T, int32_t V, int32_t k, int32_t bf16) {
+    const int es = bf16 ? 2 : 4;
+    if (T < 1 || V < 1 || V > kOpdMaxVocab || k < 1 || k > kTopMax) return 0;
+    return call == PIPO_OPD_CALL_TOP ? top_bytes(T, V, k, es) : opd_loss_work_bytes(T, V, k, es, call == PIPO_OPD_CALL_GRAD);
 }
 
 extern "C" int pipo_opd_top_logits(int32_t T, int32_t V, const float *d_logits, int64_t ld, double temperature,

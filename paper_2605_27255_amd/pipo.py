@@ -83,7 +83,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.pipo_opd_targets.argtypes = [i32, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp]
     lib.pipo_opd_targets_bf16.argtypes = [i32, i32, vp, vp, i32, vp, vp, vp, vp, vp, vp]
     f64 = ctypes.c_double
-    lib.pipo_opd_work_bytes.argtypes = [i32, i32, i32]
+    lib.pipo_opd_work_bytes.argtypes = [i32, i32, i32, i32, i32]
     lib.pipo_opd_work_bytes.restype = i64
     for dt in ("", "_bf16"):
         getattr(lib, "pipo_opd_top_logits" + dt).argtypes = [i32, i32, vp, i64, f64, i32, vp, vp, vp, vp, i64, vp]
@@ -324,29 +324,29 @@ def _refuse(why):
     raise PipoError(PIPO_EINVAL, why)
 
 
-def _opd_rows(logits, name="logits"):
+def _opd_rows(x, name="logits"):
     """T, V, the row stride and the library's suffix for a [T, V] tensor of fp32 or bf16 rows."""
     import torch
-    if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or not logits.is_cuda:
-        _refuse(f"{name}: a two-dimensional CUDA tensor")
-    if logits.dtype is not torch.float32 and logits.dtype is not torch.bfloat16:
-        _refuse(f"{name}: float32 or bfloat16, not {logits.dtype}")
-    (T, V), (ld, step) = logits.shape, logits.stride()
+    dt = x.dtype if isinstance(x, torch.Tensor) else None
+    if dt is not torch.float32 and dt is not torch.bfloat16 or x.dim() != 2 or not x.is_cuda:
+        _refuse(f"{name}: a two-dimensional CUDA tensor of float32 or bfloat16, not {dt}")
+    (T, V), (ld, step) = x.shape, x.stride()
     if V < 1 or (V > 1 and step != 1) or (T > 1 and ld < V):
         _refuse(f"{name}: rows of consecutive elements that do not overlap, not strides {(ld, step)}")
-    return T, V, ld if T > 1 else V, "" if logits.dtype is torch.float32 else "_bf16"
+    return T, V, ld if T > 1 else V, "" if dt is torch.float32 else "_bf16"
 
 
-def _opd_arg(x, name, dtype, shape, device):
-    """The address of a contiguous argument of a given type and shape on the logits' device (None: none)."""
-    if x is None:
-        return None
-    try:
-        if x.dtype is dtype and x.shape == shape and x.device == device and x.is_contiguous():
-            return x.data_ptr()
-    except AttributeError:
-        pass
-    _refuse(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+def _opd_args(device, *args):
+    """The addresses of contiguous arguments on the logits' device, each given as (tensor or None, name, type, shape)."""
+    ptrs = []
+    for x, name, dtype, shape in args:
+        if x is None:
+            ptrs.append(None)
+        elif (getattr(x, "dtype", None) is dtype and x.shape == shape and x.device == device and x.is_contiguous()):
+            ptrs.append(x.data_ptr())
+        else:
+            _refuse(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+    return ptrs
 
 
 def _opd_grad(grad, logits, T, V, ld):
@@ -365,14 +365,18 @@ def _opd_grad(grad, logits, T, V, ld):
     return grad, grad.data_ptr(), _opd_rows(grad, "grad")[2]
 
 
-def _opd_call(name, logits, T, V, k, args):
+def _opd_call(name, call, logits, device, T, V, k, args):
     """Calls a loss entry with the work array and the current stream of the logits' device behind its arguments."""
     import torch
-    lib = load_library()
-    n = lib.pipo_opd_work_bytes(T, V, k)
-    work = torch.empty(n, dtype=torch.uint8, device=logits.device).data_ptr() if n else None
-    # (the address of the current stream without an object around it: a third of a small call's time)
-    rc = getattr(lib, name)(T, V, logits.data_ptr(), *args, work, n, torch._C._cuda_getCurrentRawStream(logits.device.index))
+    lib, work = _lib or load_library(), None
+    n = lib.pipo_opd_work_bytes(call, T, V, k, name[-1] == "6")
+    if n:
+        work = torch.empty(n, dtype=torch.uint8, device=device)     # held until the call returns: later work on
+        args = (*args, work.data_ptr())                             # the stream may have it then
+    else:
+        args = (*args, None)
+    # (the address of the current stream without an object around it, which takes 2 us)
+    rc = getattr(lib, name)(T, V, logits.data_ptr(), *args, n, torch._C._cuda_getCurrentRawStream(device.index))
     if rc != PIPO_OK:
         raise PipoError(rc, f"{name}: " + ("sizes, strides or coefficients outside the documented ranges"
                                            if rc == PIPO_EINVAL else "launch failure"))
@@ -381,7 +385,7 @@ def _opd_call(name, logits, T, V, k, args):
 def _elsewhere(x):
     """Whether x is on another CUDA device than the current one."""
     import torch
-    return getattr(x, "is_cuda", False) and x.device.index != torch.cuda.current_device()
+    return getattr(x, "is_cuda", False) and x.device.index != torch._C._cuda_getDevice()
 
 
 def opd_top_logits(logits, k: int, temperature: float = 1.0):
@@ -396,10 +400,11 @@ def opd_top_logits(logits, k: int, temperature: float = 1.0):
     T, V, ld, dt = _opd_rows(logits)
     if not 1 <= k <= min(V, 256):
         _refuse(f"k: from 1 to 256 and at most {V}, not {k}")
-    ids = torch.empty((T, k), dtype=torch.int32, device=logits.device)
-    logp = torch.empty((T, k), dtype=torch.float32, device=logits.device)
-    tail = torch.empty(T, dtype=torch.float32, device=logits.device)
-    _opd_call("pipo_opd_top_logits" + dt, logits, T, V, k,
+    dev = logits.device
+    ids = torch.empty((T, k), dtype=torch.int32, device=dev)
+    logp = torch.empty((T, k), dtype=torch.float32, device=dev)
+    tail = torch.empty(T, dtype=torch.float32, device=dev)
+    _opd_call("pipo_opd_top_logits" + dt, 0, logits, dev, T, V, k,
               (ld, temperature, k, ids.data_ptr(), logp.data_ptr(), tail.data_ptr()))
     return ids, logp, tail
 
@@ -428,13 +433,13 @@ def opd_distill(logits, ids, logp, tail=None, rows=None, labels=None, kind: str 
         _refuse("ids and logp: tensors of shape [Tt, k]")
     lists, dev = ids.shape, logits.device
     Tt, k = lists
-    args = (_opd_arg(ids, "ids", i32, lists, dev), _opd_arg(logp, "logp", f32, lists, dev),
-            _opd_arg(tail, "tail", f32, (Tt,), dev), _opd_arg(rows, "rows", i32, (T,), dev),
-            _opd_arg(labels, "labels", i32, (T,), dev), OPD_KINDS[kind], beta, temperature,
-            _opd_arg(scale, "scale", f32, (T,), dev))
+    shape = (T,)
+    *ptrs, scale_ptr = _opd_args(dev, (ids, "ids", i32, lists), (logp, "logp", f32, lists), (tail, "tail", f32, (Tt,)),
+                                 (rows, "rows", i32, shape), (labels, "labels", i32, shape), (scale, "scale", f32, shape))
     loss = torch.empty(T, dtype=f32, device=dev)
     grad, grad_ptr, ldg = _opd_grad(grad, logits, T, V, ld)
-    _opd_call("pipo_opd_distill" + dt, logits, T, V, k, (ld, Tt, k, *args, loss.data_ptr(), grad_ptr, ldg))
+    _opd_call("pipo_opd_distill" + dt, 1 if grad is None else 2, logits, dev, T, V, k,
+              (ld, Tt, k, *ptrs, OPD_KINDS[kind], beta, temperature, scale_ptr, loss.data_ptr(), grad_ptr, ldg))
     return loss, grad
 
 
@@ -455,14 +460,15 @@ def opd_policy(logits, labels, advantages, old_logp=None, ref_logp=None, clip=(0
     if labels is None or advantages is None:
         _refuse("labels and advantages: tensors of shape [T]")
     dev, shape = logits.device, (T,)
-    args = (_opd_arg(labels, "labels", torch.int32, shape, dev), _opd_arg(advantages, "advantages", f32, shape, dev),
-            _opd_arg(old_logp, "old_logp", f32, shape, dev), _opd_arg(ref_logp, "ref_logp", f32, shape, dev),
-            clip[0], clip[1], kl_coef, temperature, _opd_arg(scale, "scale", f32, shape, dev))
+    *ptrs, scale_ptr = _opd_args(dev, (labels, "labels", torch.int32, shape), (advantages, "advantages", f32, shape),
+                                 (old_logp, "old_logp", f32, shape), (ref_logp, "ref_logp", f32, shape),
+                                 (scale, "scale", f32, shape))
     loss, logp = torch.empty(T, dtype=f32, device=dev), torch.empty(T, dtype=f32, device=dev)
     kl = None if ref_logp is None else torch.empty(T, dtype=f32, device=dev)
     grad, grad_ptr, ldg = _opd_grad(grad, logits, T, V, ld)
-    _opd_call("pipo_opd_policy" + dt, logits, T, V, 1,
-              (ld, *args, loss.data_ptr(), logp.data_ptr(), None if kl is None else kl.data_ptr(), grad_ptr, ldg))
+    _opd_call("pipo_opd_policy" + dt, 1 if grad is None else 2, logits, dev, T, V, 1,
+              (ld, *ptrs, clip[0], clip[1], kl_coef, temperature, scale_ptr, loss.data_ptr(), logp.data_ptr(),
+               None if kl is None else kl.data_ptr(), grad_ptr, ldg))
     return loss, logp, kl, grad
 
 
