@@ -590,16 +590,14 @@ template <typename L, int NT, int NV, int STEP, bool GRAD> static int launch_row
         p.spill = left < 0 ? 0 : left < room ? left : room;
         lds += (size_t)p.spill * NT * 16;
     }
-    hipLaunchKernelGGL((k_opd_loss<L, NT, NV, STEP, GRAD>), dim3(grid), dim3(NT), lds, s, p);
-    return hipGetLastError() == hipSuccess ? PIPO_OK : PIPO_EHIP;
+    return launch(k_opd_loss<L, NT, NV, STEP, GRAD>, grid, NT, lds, s, p) ? PIPO_OK : PIPO_EHIP;
 }
 
 template <typename L> static int launch_split(const LossParams<L> &p, SplitParams q, hipStream_t s) {
-    const dim3 grid((unsigned)(p.T * q.S)), block(kPartThreads);
-    hipLaunchKernelGGL(k_opd_part<L>, grid, block, (size_t)bitmap_words<L>(q.seg) * 4, s, p, q);
-    if (p.grad) hipLaunchKernelGGL((k_opd_apply<L, true>), grid, block, 0, s, p, q);
-    else hipLaunchKernelGGL((k_opd_apply<L, false>), dim3(p.T), block, 0, s, p, q);
-    return hipGetLastError() == hipSuccess ? PIPO_OK : PIPO_EHIP;
+    bool ok = launch(k_opd_part<L>, p.T * q.S, kPartThreads, (size_t)bitmap_words<L>(q.seg) * 4, s, p, q);
+    if (p.grad) ok = ok && launch(k_opd_apply<L, true>, p.T * q.S, kPartThreads, 0, s, p, q);
+    else ok = ok && launch(k_opd_apply<L, false>, p.T, kPartThreads, 0, s, p, q);
+    return ok ? PIPO_OK : PIPO_EHIP;
 }
 
 template <typename L> static int launch_loss(LossParams<L> p, void *work, hipStream_t s) {

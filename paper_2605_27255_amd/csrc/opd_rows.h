@@ -12,7 +12,13 @@ constexpr int kOpdMaxVocab = 1 << 19;
 constexpr int kMaxParts = 64;       // workgroups of a split row: a lane of a wave joins each
 struct Part { float m, s; int bad, pad; };      // what a segment of a row leaves for the others
 
-// ---- checks on the host, shared by the entry points ---------------------------------
+// ---- launches and checks on the host, shared by the entry points ---------------------
+// (the launch's own status: asking for the last error takes another microsecond)
+template <typename... A, typename... B>
+inline bool launch(void (*kernel)(A...), unsigned grid, unsigned block, size_t lds, hipStream_t s, B... args) {
+    void *ptrs[] = {(void *)&args...};
+    return hipLaunchKernel((const void *)kernel, dim3(grid), dim3(block), ptrs, lds, s) == hipSuccess;
+}
 bool opd_rows_ok(int32_t T, int32_t V, const void *z, int64_t ld, double temperature, size_t es);
 bool opd_work_ok(const void *work, int64_t work_bytes, int64_t need);
 int64_t opd_loss_work_bytes(int T, int V, int k, int es, bool grad);

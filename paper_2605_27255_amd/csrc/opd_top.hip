@@ -1,7 +1,7 @@
 // The k largest logits of each row, in the order of (value descending, id
 // ascending), with their log-probabilities and the log of the mass outside.
 //
-// One pass over the row, which is dealt into units of pieces, two to a thread:
+// One pass over the row, which is dealt into units of pieces, some to a thread:
 // each has its maximum and its sum of exponentials.  A value that at least k
 // maxima reach is a lower bound of the k-th largest logit, so only those units
 // can hold the k largest: they are read again (about k of 1024, from the
@@ -22,7 +22,6 @@ namespace pipo {
 
 constexpr int kTopMax = 256;        // k
 constexpr int kTopCand = 1024;      // candidates ranked
-constexpr int kUnits = 2;           // units of a row to a thread
 constexpr int kJoinThreads = 1024;
 
 template <typename L> struct TopParams {
@@ -93,14 +92,32 @@ __device__ __forceinline__ uint32_t bound_of_kth(TopShared<NT, H> &sh, uint32_t 
     return lo;
 }
 
-// Sorts sh.cand[0, nc) into sh.sorted: ranked by counting the larger ones.
+// Sorts sh.cand[0, nc) into sh.sorted: each ranked by counting the larger ones,
+// where there are many by several threads each.
 template <int NT, int H> __device__ __forceinline__ void sort_candidates(TopShared<NT, H> &sh, int nc) {
-    for (int i = threadIdx.x; i < nc; i += NT) {
-        const uint64_t key = sh.cand[i];
-        int rank = 0;
+    if (nc > 64 && 2 * nc <= NT) {
+        int *ranks = (int *)sh.umax;            // (whose keys nobody reads any more)
+        const int share = NT / nc, len = (nc + share - 1) / share;
+        for (int i = threadIdx.x; i < nc; i += NT) ranks[i] = 0;
+        __syncthreads();
+        if ((int)threadIdx.x < nc * share) {
+            const int i = threadIdx.x % nc, from = threadIdx.x / nc * len, to = min(from + len, nc);
+            const uint64_t key = sh.cand[i];
+            int rank = 0;
+#pragma unroll 4
+            for (int j = from; j < to; ++j) rank += sh.cand[j] > key;
+            atomicAdd(&ranks[i], rank);
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < nc; i += NT) sh.sorted[ranks[i]] = sh.cand[i];
+    } else {
+        for (int i = threadIdx.x; i < nc; i += NT) {
+            const uint64_t key = sh.cand[i];
+            int rank = 0;
 #pragma unroll 8
-        for (int j = 0; j < nc; ++j) rank += sh.cand[j] > key;
-        sh.sorted[rank] = key;
+            for (int j = 0; j < nc; ++j) rank += sh.cand[j] > key;
+            sh.sorted[rank] = key;
+        }
     }
     __syncthreads();
 }
@@ -125,9 +142,9 @@ __device__ __forceinline__ double unit_of_max(float m, ExpScale c) {
 }
 
 // One workgroup per row, or (SPLIT) per segment of one.
-template <typename L, int NT, bool SPLIT>
+template <typename L, int NT, int H, bool SPLIT>
 __global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
-    constexpr int N = Piece<L>::N, W = NT / 64, H = kUnits;
+    constexpr int N = Piece<L>::N, W = NT / 64;
     __shared__ TopShared<NT, H> sh;
     const int t = SPLIT ? blockIdx.x / p.S : blockIdx.x, seg = SPLIT ? blockIdx.x % p.S : 0;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -373,14 +390,18 @@ static int top_logits(int32_t T, int32_t V, const L *d_logits, int64_t ld, doubl
         top_split(T, V, k, sizeof(L), p.S, p.seg);
         p.part = (Part *)d_work;
         p.keys = (uint64_t *)(p.part + (int64_t)T * p.S);
-        hipLaunchKernelGGL((k_opd_top<L, 256, true>), dim3(T * p.S), dim3(256), 0, s, p);
-        hipLaunchKernelGGL(k_opd_top_join<L>, dim3(T), dim3(kJoinThreads), 0, s, p);
-    } else if (V > 16384) {
-        hipLaunchKernelGGL((k_opd_top<L, 512, false>), dim3(T), dim3(512), 0, s, p);
-    } else {
-        hipLaunchKernelGGL((k_opd_top<L, 256, false>), dim3(T), dim3(256), 0, s, p);
+        return launch(k_opd_top<L, 256, 2, true>, T * p.S, 256, 0, s, p) && launch(k_opd_top_join<L>, T, kJoinThreads, 0, s, p)
+                   ? PIPO_OK : PIPO_EHIP;
     }
-    return hipGetLastError() == hipSuccess ? PIPO_OK : PIPO_EHIP;
+    // Threads and units a thread: enough units to leave little to read again, few to search.  Two / four units, us:
+    // 2048 x 151936 fp32 240 / 221, 2048 x 100003 fp32 top 100 213 / 184, 301 x 151936 bf16 33 / 36; one / two: 16384 x
+    // 4096 fp32 86 / 105, 4000 x 12003 fp32 91 / 74.
+    const int pieces = V / (16 / (int)sizeof(L));
+    const bool ok = pieces >= 20480 ? launch(k_opd_top<L, 512, 4, false>, T, 512, 0, s, p)
+                    : V > 16384      ? launch(k_opd_top<L, 512, 2, false>, T, 512, 0, s, p)
+                    : pieces <= 1024 ? launch(k_opd_top<L, 256, 1, false>, T, 256, 0, s, p)
+                                     : launch(k_opd_top<L, 256, 2, false>, T, 256, 0, s, p);
+    return ok ? PIPO_OK : PIPO_EHIP;
 }
 
 }  // namespace pipo
