@@ -53,7 +53,7 @@ struct LossShared {
     float z[kEntries], q[kEntries];     // their logits, the teacher's log-probabilities
     double a[kEntries], p[kEntries];   // their a = p df/dp, and p
     float patch[kEntries];          // their gradients
-    float coef;                     // the others' gradient over exp((z - m) / temperature)
+    float coef, B;                  // the others' gradient over 2^(z c - B)
     int bad;
 };
 
@@ -142,7 +142,7 @@ __device__ __forceinline__ void divergence(int kind, double beta, double lp, dou
 // The first wave turns the listed logits and the rest's (max, sum) into the
 // position's outputs (where `first`) and its gradient's numbers; ends with a barrier.
 template <typename L>
-__device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, const Position &x, MaxSum rest, LossShared &sh,
+__device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, const Position &x, RowSum rest, LossShared &sh,
                                            bool first = true) {
     if (threadIdx.x < 64) {
         const int lane = threadIdx.x;
@@ -154,9 +154,9 @@ __device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, const 
         for (int j = lane; j < p.k; j += 64) if (sh.id[j] >= 0) sum += exp(((double)sh.z[j] - m) * inv);
         sum = wave_sum_f64(sum);
         // log of the rest's unit (its sum counts multiples of it) over exp(m / temperature)
-        const double unit = is_far(rest.m) ? ((double)rest.m - m) * inv : (double)ref_of(rest.m, p.c) * kLn2 - m * inv;
+        const double unit = is_far(rest.m) ? ((double)rest.m - m) * inv : (double)rest.B * kLn2 - m * inv;
         const double rest_at = rest.m == -INFINITY ? 1. : exp(unit);
-        sum += (double)rest.s * rest_at;     // without a rest its sum is 0 (or NaN)
+        sum += rest.s * rest_at;     // without a rest its sum is 0 (or NaN)
         // of x - m / temperature; a row without any mass has none
         const double lse = m == -INFINITY ? (double)__builtin_nanf("") : log(sum);
         const double g = (double)x.scale * inv;
@@ -189,8 +189,8 @@ __device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, const 
             for (int j = lane; j < p.k + (p.q_rest ? 1 : 0); j += 64) {
                 const bool out = j == p.k;
                 if (!out && sh.id[j] < 0) continue;
-                double lp = out ? unit + log((double)rest.s) - lse : ((double)sh.z[j] - m) * inv - lse;
-                if (out && rest.s == 0.f) lp = lse == lse ? -INFINITY : lse;
+                double lp = out ? unit + log(rest.s) - lse : ((double)sh.z[j] - m) * inv - lse;
+                if (out && rest.s == 0.) lp = lse == lse ? -INFINITY : lse;
                 double fj, aj;
                 divergence(p.kind, p.beta, lp, out ? (double)x.q_rest : (double)sh.q[j], fj, aj);
                 f += fj;
@@ -208,8 +208,11 @@ __device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, const 
         }
         if (lane == 0) {
             // with no mass outside the list there is nothing to spread there
-            const double k = lse != lse ? lse : rest.s == 0.f ? 0. : g * (a_rest / (double)rest.s - A * rest_at * exp(-lse));
-            sh.coef = (float)k;
+            const double k = lse != lse ? lse : rest.s == 0. ? 0. : g * (a_rest / rest.s - A * rest_at * exp(-lse));
+            // against a reference near the values that weigh most: their exponents are small, and so their roundings
+            const int shift = is_far(rest.m) || !(rest.s > 0.) ? 0 : min(max(ilogb(rest.s), -120), 120);
+            sh.coef = (float)ldexp(k, shift);
+            sh.B = rest.B + (float)shift;
         }
     }
     __syncthreads();
@@ -250,7 +253,7 @@ __device__ __forceinline__ void add_piece(MaxSum &a, u32x4 w, int i, const uint3
 }
 // The sum of a row (or segment) of far values, by differences from its maximum m.
 template <typename L, int NT>
-__device__ __forceinline__ float sum_far(const Span<const L> &row, const uint32_t *bits, float m, ExpScale c, float *s_w) {
+__device__ __forceinline__ double sum_far(const Span<const L> &row, const uint32_t *bits, float m, ExpScale c, float *s_w) {
     constexpr int N = Piece<L>::N;
     float s = 0.f;
     each_piece<NT, 1>(row, (int)threadIdx.x, [&](u32x4 w, int i) {
@@ -258,7 +261,7 @@ __device__ __forceinline__ float sum_far(const Span<const L> &row, const uint32_
 #pragma unroll
         for (int e = 0; e < N; ++e) if (!(b >> e & 1u)) s += exp_diff(Piece<L>::get(w, e), m, c);
     });
-    return (float)block_sum<NT>(s, s_w);
+    return block_sum<NT>(s, s_w);
 }
 // A piece's gradients away from the list; those of listed elements are written over them later.
 template <typename L> __device__ __forceinline__ void gradients(float *v, u32x4 w, float coef, float B, ExpScale c) {
@@ -292,13 +295,29 @@ __device__ __forceinline__ void put_far(L *out, const Span<const L> &row, float 
     });
 }
 
-// A piece's sum of 2^(z c - B), without pieces that hold a listed element.
-template <typename L> __device__ __forceinline__ void sum_piece(float &s, u32x4 w, uint32_t listed, float B, ExpScale c) {
+// A thread's sum of 2^(z c - B), and its largest piece's share and slab.
+struct PieceSum { float s, most; int slab; };
+// Adds a piece, unless it holds a listed element.
+template <typename L> __device__ __forceinline__ void sum_piece(PieceSum &a, u32x4 w, int slab, uint32_t listed, float B, ExpScale c) {
     constexpr int N = Piece<L>::N;
     float x = 0.f;
 #pragma unroll
     for (int e = 0; e < N; ++e) x += exp_at(Piece<L>::get(w, e), B, c);
-    s += listed ? 0.f : x;
+    x = listed ? 0.f : x;
+    a.s += x;
+    if (x > a.most) { a.most = x; a.slab = slab; }
+}
+// Values far above the reference have large exponents, whose rounding the sum
+// would show: what it cost in this piece.
+template <typename L> __device__ __forceinline__ float rounding_of(u32x4 w, float B, ExpScale c) {
+    float x = 0.f;
+#pragma unroll
+    for (int e = 0; e < Piece<L>::N; ++e) {
+        const float z = Piece<L>::get(w, e), r = fmaf(z, c.lo, fmaf(z, c.hi, -B)), term = __builtin_amdgcn_exp2f(r);
+        const double off = fma((double)z, (double)c.lo, fma((double)z, (double)c.hi, -(double)B)) - (double)r;
+        if (term > 0.f) x = fmaf(term * (float)kLn2, (float)off, x);
+    }
+    return x;
 }
 template <typename L> __device__ __forceinline__ void max_piece(float &m, u32x4 w, uint32_t listed) {
     constexpr int N = Piece<L>::N;
@@ -310,11 +329,11 @@ template <typename L> __device__ __forceinline__ void max_piece(float &m, u32x4 
 // (max, sum) of the unlisted elements of a row where the reference of the fast
 // pass did not fit, from two passes of their own.
 template <typename L, int NT>
-__device__ __forceinline__ MaxSum sum_slowly(const Span<const L> &row, const uint32_t *bits, ExpScale c, float (*red)[NT / 64]) {
-    MaxSum a{-INFINITY, 0.f};
-    each_piece<NT, 1>(row, (int)threadIdx.x, [&](u32x4 w, int i) { add_piece<L>(a, w, i, bits, c); });
+__device__ __forceinline__ RowSum sum_slowly(const Span<const L> &row, const uint32_t *bits, ExpScale c, float (*red)[NT / 64]) {
+    MaxSum own{-INFINITY, 0.f};
+    each_piece<NT, 1>(row, (int)threadIdx.x, [&](u32x4 w, int i) { add_piece<L>(own, w, i, bits, c); });
     __syncthreads();
-    a = block_merge<NT>(a, c, red);
+    RowSum a = block_merge<NT>(own, c, red);
     __syncthreads();
     if (is_far(a.m)) a.s = sum_far<L, NT>(row, bits, a.m, c, red[0]);
     __syncthreads();
@@ -337,7 +356,7 @@ __device__ __forceinline__ MaxSum sum_slowly(const Span<const L> &row, const uin
 template <int NT, int NV> constexpr bool kTakesSeveral = NT == 512 && NV >= 12;    // one workgroup fills a compute unit
 template <int NT, int NV> constexpr bool kSpills = NV >= (NT == 512 ? 33 : 44);     // the longest rows' variants
 template <typename L, int NT, int NV, int STEP, bool GRAD>
-__global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
+__global__ __launch_bounds__(NT, GRAD ? NT / 256 : 8) void k_opd_loss(LossParams<L> p) {
     constexpr bool LOOP = kTakesSeveral<NT, NV>, DEEP = kSpills<NT, NV>;
     constexpr int AHEAD = NV < 12 ? NV : 12, N = Piece<L>::N;
     extern __shared__ uint32_t bits[];
@@ -380,10 +399,11 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
             __syncthreads();
             scored = sh.bad == 0;
         }
-        MaxSum a{-INFINITY, 0.f};
+        RowSum a{-INFINITY, 0.f, 0.};
         if (scored) {
             // this thread's entry: its logit and, if it is the first listed one of its piece, the piece's others
-            float zj = 0.f, s = 0.f;
+            float zj = 0.f;
+            PieceSum sum{0.f, 8.f, -1};
             u32x4 shared_piece;
             uint32_t others = 0;
             if (id >= 0) {
@@ -403,27 +423,36 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
             }
             if (NV <= STEP && held == 0) each_piece<NT, 1>(row, tid, [&](u32x4 w, int i) { max_piece<L>(m, w, listed_bits<N>(bits, i)); });
             m = block_max<NT>(m, red[0]);
-            const float B = ref_of(m, p.c);
+            const float B = round_ref(ref_of(m, p.c));
             off = (tid + NT * AHEAD) * 16;
 #pragma unroll
             for (int j = 0; j < NV; ++j, next_slab<NT>(off)) {
                 if (j + AHEAD < NV) keep[j + AHEAD] = slab(row.body, j + AHEAD, off, true);
                 asm volatile("" : "+v"(keep[j]));   // unpacked again: the floats would take twice the registers
-                if (has(j)) sum_piece<L>(s, keep[j], listed(j), B, p.c);
+                if (has(j)) sum_piece<L>(sum, keep[j], j, listed(j), B, p.c);
             }
             if (DEEP)
                 whole_pieces<NT, 4>(row.body, tid + NT * held, NT * lower, [&](u32x4 w, int i) {
                     more[i - NT * held] = w;
-                    sum_piece<L>(s, w, listed_bits<N>(bits, i), B, p.c);
+                    sum_piece<L>(sum, w, i / NT, listed_bits<N>(bits, i), B, p.c);
                 });
-            each_piece<NT, 4, GRAD>(row, tid + NT * lower, [&](u32x4 w, int i) { sum_piece<L>(s, w, listed_bits<N>(bits, i), B, p.c); });
+            whole_pieces<NT, 4, GRAD>(row.body, tid + NT * lower, row.whole, [&](u32x4 w, int i) {
+                sum_piece<L>(sum, w, i / NT, listed_bits<N>(bits, i), B, p.c);
+            });
+            float s = sum.s;
+            if (sum.slab >= 0) s += rounding_of<L>(load_piece(row.body, tid + NT * sum.slab), B, p.c);
+            edges<NT>(row, [&](u32x4 w, int i) {
+                PieceSum edge{0.f, 8.f, -1};
+                sum_piece<L>(edge, w, 0, listed_bits<N>(bits, i), B, p.c);
+                s += edge.s;
+            });
             if (others) {
 #pragma unroll
                 for (int e = 0; e < N; ++e)
                     if (others >> e & 1u) s += exp_at(Piece<L>::get(shared_piece, e), B, p.c);
             }
             if (tid < p.k) sh.z[tid] = zj;
-            a = MaxSum{m, (float)block_sum<NT>(s, red[1])};
+            a = RowSum{m, B, block_sum<NT>(s, red[1])};
             if (!(a.s < INFINITY) || is_far(m)) a = sum_slowly<L, NT>(row, bits, p.c, red);
             far = is_far(a.m);
             if (id >= 0) bits[(id - row.head + N) >> 5] = 0;     // every wave is past its sums: ready for the next position
@@ -441,7 +470,7 @@ __global__ __launch_bounds__(NT) void k_opd_loss(LossParams<L> p) {
         const Span<const L> next_row(p.z + (int64_t)(nx.what == kScore ? next : t) * p.ld, V);
         read_entry(p, tid, nx, id, q);
         if (GRAD) {
-            const float coef = sh.coef, B = ref_of(a.m, p.c);
+            const float coef = sh.coef, B = sh.B;
             const bool put = scored && !far;
             L *body = out + row.head;
             off = tid * 16;
@@ -503,11 +532,11 @@ template <typename L> __global__ __launch_bounds__(kPartThreads) void k_opd_part
     mark_entry(id, tq, p.k, p.V, lo, row, sh, bits);
     __syncthreads();
     if (id >= lo && id < lo + len) q.z[(int64_t)t * p.k + tid] = Piece<L>::one(row.body + (id - lo - row.head));
-    MaxSum a{-INFINITY, 0.f};
-    each_piece<NT, 4, true>(row, tid, [&](u32x4 w, int i) { add_piece<L>(a, w, i, bits, p.c); });
-    a = block_merge<NT>(a, p.c, red);
+    MaxSum own{-INFINITY, 0.f};
+    each_piece<NT, 4, true>(row, tid, [&](u32x4 w, int i) { add_piece<L>(own, w, i, bits, p.c); });
+    RowSum a = block_merge<NT>(own, p.c, red);
     if (is_far(a.m)) a.s = sum_far<L, NT>(row, bits, a.m, p.c, red[2]);
-    if (tid == 0) q.part[(int64_t)t * q.S + seg] = Part{a.m, a.s, sh.bad, 0};
+    if (tid == 0) q.part[(int64_t)t * q.S + seg] = Part{a.m, a.B, a.s, sh.bad, 0};
 }
 
 template <typename L, bool GRAD>
@@ -520,7 +549,7 @@ __global__ __launch_bounds__(kPartThreads) void k_opd_apply(LossParams<L> p, Spl
     L *out = GRAD ? p.grad + (int64_t)t * p.ldg + lo : nullptr;
     const Position x = read_position(p, t);
     int what = x.what, id = -1;
-    MaxSum a{-INFINITY, 0.f};
+    RowSum a{-INFINITY, 0.f, 0.};
     if (what == kScore) {
         bool bad;
         a = join_parts(q.part + (int64_t)t * q.S, q.S, p.c, bad);
@@ -544,7 +573,7 @@ __global__ __launch_bounds__(kPartThreads) void k_opd_apply(LossParams<L> p, Spl
     if (!GRAD) return;
     const Span<const L> row(p.z + (int64_t)t * p.ld + lo, len);
     if (is_far(a.m)) put_far<L, NT>(out + row.head, row, sh.coef, a.m, p.c);
-    else put_pieces<L, NT>(out + row.head, row, tid, sh.coef, ref_of(a.m, p.c), p.c);
+    else put_pieces<L, NT>(out + row.head, row, tid, sh.coef, sh.B, p.c);
     __syncthreads();
     if (id >= lo && id < lo + len) Piece<L>::put(out + (id - lo), sh.patch[tid]);
 }

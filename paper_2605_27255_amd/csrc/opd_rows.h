@@ -10,7 +10,7 @@ namespace pipo {
 constexpr double kLn2 = 0.69314718055994530942;
 constexpr int kOpdMaxVocab = 1 << 19;
 constexpr int kMaxParts = 64;       // workgroups of a split row: a lane of a wave joins each
-struct Part { float m, s; int bad, pad; };      // what a segment of a row leaves for the others
+struct Part { float m, B; double s; int bad, pad; };     // what a segment of a row leaves for the others (a RowSum)
 
 // ---- launches and checks on the host, shared by the entry points ---------------------
 // (the launch's own status: asking for the last error takes another microsecond)
@@ -245,25 +245,32 @@ template <int NT> __device__ __forceinline__ double block_sum(float v, float *s_
     for (int w = 0; w < NT / 64; ++w) r += (double)s_w[w];
     return r;
 }
+// A row's unlisted values: their sum in multiples of 2^B (where m is far, of
+// exp(m / temperature)); m is their maximum, or near it.
+struct RowSum { float m, B; double s; };
+// A reference that whole numbers can be added to exactly.
+__device__ __forceinline__ float round_ref(float B) { return rintf(B * 1024.f) * (1.f / 1024.f); }
+
 // The threads' (max, sum) as one: the sum in 64 bits across waves.  s_w: NT / 64 each for the maxima and the sums.
-template <int NT> __device__ __forceinline__ MaxSum block_merge(MaxSum a, ExpScale c, float (*s_w)[NT / 64]) {
+template <int NT> __device__ __forceinline__ RowSum block_merge(MaxSum a, ExpScale c, float (*s_w)[NT / 64]) {
     const float m = block_max<NT>(a.m, s_w[0]);
-    const float s = a.s * __builtin_amdgcn_exp2f(ref_of(a.m, c) - ref_of(m, c));
-    return MaxSum{m, (float)block_sum<NT>(s, s_w[1])};
+    const float B = round_ref(ref_of(m, c)), s = a.s * __builtin_amdgcn_exp2f(ref_of(a.m, c) - B);
+    return RowSum{m, B, block_sum<NT>(s, s_w[1])};
 }
 
 // A row's segments as one (max, sum), in every lane.
-__device__ __forceinline__ MaxSum join_parts(const Part *part, int S, ExpScale c, bool &bad) {
+__device__ __forceinline__ RowSum join_parts(const Part *part, int S, ExpScale c, bool &bad) {
     const int lane = threadIdx.x & 63;
-    Part x{-INFINITY, 0.f, 0, 0};
+    Part x{-INFINITY, -kFar, 0., 0, 0};
     if (lane < S) x = part[lane];
     bad = __ballot(x.bad != 0) != 0;
     const float m = wave_max_dpp(x.m);
     // beside a far maximum, and beside a near one where they are far, the other segments weigh nothing
     const bool far = is_far(m);
-    float f = far ? (x.m == m ? 1.f : exp_diff(x.m, m, c)) : __builtin_amdgcn_exp2f(ref_of(x.m, c) - ref_of(m, c));
-    if (!far && is_far(x.m)) f = 0.f;
-    return MaxSum{m, (float)wave_sum_f64((double)x.s * (double)f)};
+    const float B = round_ref(ref_of(m, c));
+    double f = far ? (x.m == m ? 1. : (double)exp_diff(x.m, m, c)) : exp(((double)x.B - (double)B) * kLn2);
+    if (!far && is_far(x.m)) f = 0.;
+    return RowSum{m, B, wave_sum_f64(x.s * f)};
 }
 
 }  // namespace pipo

@@ -136,9 +136,9 @@ __device__ __forceinline__ void put_top(const TopParams<L> &p, int t, const uint
     }
     if (lane == 0 && p.tail) p.tail[t] = (float)(log(outside) - lse);
 }
-// A sum in units of 2^ref_of(m) (or, far, of exp(m / temperature)) in units of exp(m / temperature).
-__device__ __forceinline__ double unit_of_max(float m, ExpScale c) {
-    return is_far(m) || m == -INFINITY ? 1. : exp((double)ref_of(m, c) * kLn2 - (double)m * c.inv);
+// What a row's sum counts (multiples of 2^B, or far of exp(m / temperature)) in multiples of exp(m / temperature).
+__device__ __forceinline__ double unit_of_max(float m, float B, ExpScale c) {
+    return is_far(m) || m == -INFINITY ? 1. : exp((double)B * kLn2 - (double)m * c.inv);
 }
 
 // One workgroup per row, or (SPLIT) per segment of one.
@@ -313,9 +313,9 @@ __global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
             const uint64_t key = j < k ? sh.sorted[j] : 0;
             keys[j] = key ? pair_key((uint32_t)(key >> 32), key_id(key) + lo) : 0;
         }
-        if (tid == 0) p.part[(int64_t)t * p.S + seg] = Part{m, (float)outside, 0, 0};
+        if (tid == 0) p.part[(int64_t)t * p.S + seg] = Part{m, B, outside, 0, 0};
     } else if (wave == 0) {
-        put_top(p, t, sh.sorted, m, outside * unit_of_max(m, p.c));
+        put_top(p, t, sh.sorted, m, outside * unit_of_max(m, B, p.c));
     }
 }
 
@@ -326,7 +326,7 @@ template <typename L> __global__ __launch_bounds__(kJoinThreads) void k_opd_top_
     const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, k = p.k;
     const uint64_t *keys = p.keys + (int64_t)t * p.S * k;
     bool bad;
-    const MaxSum rests = join_parts(p.part + (int64_t)t * p.S, p.S, p.c, bad);
+    const RowSum rests = join_parts(p.part + (int64_t)t * p.S, p.S, p.c, bad);
     const uint64_t mine = tid < p.S * k ? keys[tid] : 0;
     // a whole list reaches its own last key: the largest of these is a bound that k keys reach
     uint32_t lo = lane < p.S ? (uint32_t)(keys[(int64_t)lane * k + k - 1] >> 32) : 0;
@@ -344,7 +344,7 @@ template <typename L> __global__ __launch_bounds__(kJoinThreads) void k_opd_top_
     float rest = 0.f;
     if (mine && (uint32_t)(mine >> 32) >= bound) sh.cand[atomicAdd(&sh.n, 1)] = mine;
     const bool far = is_far(rests.m);
-    const float B = ref_of(rests.m, p.c);
+    const float B = rests.B;
     auto term = [&](uint64_t key) {
         const float v = key_value((uint32_t)(key >> 32));
         return far ? exp_diff(v, rests.m, p.c) : exp_at(v, B, p.c);
@@ -354,8 +354,8 @@ template <typename L> __global__ __launch_bounds__(kJoinThreads) void k_opd_top_
     const int nc = sh.n;
     sort_candidates(sh, nc);
     for (int j = k + tid; j < nc; j += NT) rest += term(sh.sorted[j]);
-    const double outside = block_sum<NT>(rest, sh.red[2]) + (double)rests.s;
-    if (tid < 64) put_top(p, t, sh.sorted, rests.m, outside * unit_of_max(rests.m, p.c));
+    const double outside = block_sum<NT>(rest, sh.red[2]) + rests.s;
+    if (tid < 64) put_top(p, t, sh.sorted, rests.m, outside * unit_of_max(rests.m, B, p.c));
 }
 
 // Segments of each row: about two workgroups a compute unit in all, at least
