@@ -125,6 +125,57 @@ def test_top_logits_of_rows_without_a_distribution(torch):
         _close(logp[[0, 5]], r_logp, DELTA + HALF["float32"] * np.abs(r_logp))
 
 
+@pytest.mark.parametrize("dtype,V", [("float32", 90001), ("bfloat16", 170003), ("float32", 4097), ("bfloat16", 20011)])
+def test_top_logits_of_many_crowded_rows(torch, dtype, V):
+    """Rows enough that none is split: ties, masks and NaNs among ordinary
+    rows, whole-row kernels of every size; the copies of a row agree."""
+    from paper_2605_27255_amd import opd_top_logits
+    pad = -V % 8                              # every row lies alike
+    d, z = _rows(torch, 8, V, dtype, seed=V, pad=pad)
+    d[1] = 2.0
+    d[2, V // 2:] = d[2].max()
+    d[3, 30:] = -float("inf")
+    d[4, 5] = float("nan")
+    d[5, ::2] = float(torch.finfo(d.dtype).min)
+    z = d.double().cpu().numpy()
+    many = d._base.repeat(13, 1)[:, :V]
+    ids, logp, tail = opd_top_logits(many, 40)
+    torch.cuda.synchronize()
+    for i in range(1, 13):
+        assert torch.equal(ids[:8], ids[8 * i:8 * i + 8])
+        assert torch.equal(logp[:8].nan_to_num(7), logp[8 * i:8 * i + 8].nan_to_num(7))
+    keep = [0, 1, 2, 3, 5, 6, 7]
+    r_ids, r_logp, r_tail = O.opd_top_logits(z[keep], 40)
+    np.testing.assert_array_equal(ids[:8][keep].cpu().numpy(), r_ids)
+    _close(logp[:8][keep], r_logp, DELTA + HALF["float32"] * np.abs(r_logp), "logp")
+    _close(tail[:8][keep], r_tail, 2 * DELTA + HALF["float32"] * np.abs(r_tail), "tail")
+    assert logp[4].isnan().all() and tail[4].isnan()
+    row = ids[4].cpu().numpy()
+    assert len(set(row.tolist())) == 40 and row.min() >= 0 and row.max() < V
+
+
+def test_top_logits_split_rows_without_a_distribution(torch):
+    """NaN, +inf and -inf rows, and ties across segments, in rows that are split."""
+    from paper_2605_27255_amd import opd_top_logits
+    V = 100003
+    d, z = _rows(torch, 6, V, "float32", seed=8)
+    d[1] = -float("inf")
+    d[2, 90000] = float("nan")
+    d[3, 3] = float("inf")
+    d[4, 1::5] = 50.0                         # 20001 equal values in every segment
+    ids, logp, tail = opd_top_logits(d, 24)
+    torch.cuda.synchronize()
+    for t in (1, 2, 3):
+        assert logp[t].isnan().all() and tail[t].isnan()
+        r = ids[t].cpu().numpy()
+        assert len(set(r.tolist())) == 24 and r.min() >= 0 and r.max() < V
+    keep = [0, 4, 5]
+    r_ids, r_logp, r_tail = O.opd_top_logits(d.double().cpu().numpy()[keep], 24)
+    np.testing.assert_array_equal(ids[keep].cpu().numpy(), r_ids)
+    _close(logp[keep], r_logp, DELTA + HALF["float32"] * np.abs(r_logp), "logp")
+    _close(tail[keep], r_tail, 2 * DELTA + HALF["float32"] * np.abs(r_tail), "tail")
+
+
 # ---- distillation ------------------------------------------------------------------------------------------------
 
 def _teacher(torch, z, k, temperature, seed, noise=0.7):
@@ -297,6 +348,102 @@ def test_distill_gradient_against_differences(torch):
             assert (np.abs(got - want) <= tol).all(), (kind, got, want, tol)
 
 
+# rows of 16-byte pieces on both sides of each size at which another kernel variant takes over (256 pieces a slab)
+SLABS = [0.01, 1, 3, 5, 7, 9, 13, 17, 21, 26, 30, 35, 40, 46, 82, 110]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("slabs", SLABS)
+@pytest.mark.parametrize("side", [-1, 1])
+def test_distill_row_lengths(torch, slabs, side, dtype):
+    """Enough rows that none is split (and, for the longest, that a workgroup
+    takes several): copies of six, among them unscored and flagged ones."""
+    from paper_2605_27255_amd import opd_distill
+    N = 4 if dtype == "float32" else 8
+    V = max(13, int(slabs * 256) * N + side * 3)
+    pad, copies = -V % N, 50 if slabs < 82 else 51
+    d, z = _rows(torch, 6, V, dtype, seed=V, pad=pad)
+    ids, logp, tail = _teacher(torch, z, 7, 1.0, seed=3)
+    ids[4, 1] = ids[4, 0]                     # flagged by its list
+    y = torch.tensor([1, -1, 1, 1, 1, 1], dtype=torch.int32).cuda()
+    rows = torch.tensor([0, 1, 2, 9, 4, 5], dtype=torch.int32).cuda()      # position 3: no such teacher row
+    scale = torch.linspace(0.5, 2, 6).cuda()
+    many = lambda a: a.repeat(copies, *[1] * (a.dim() - 1))  # noqa: E731
+    x = many(d._base)[:, :V]
+    loss, g = opd_distill(x, ids, logp, tail, rows=many(rows), labels=many(y), scale=many(scale), grad=True)
+    only, none = opd_distill(x, ids, logp, tail, rows=many(rows), labels=many(y))
+    torch.cuda.synchronize()
+    assert none is None
+    for i in range(1, copies):
+        part = slice(6 * i, 6 * i + 6)
+        assert torch.equal(loss[:6].nan_to_num(7), loss[part].nan_to_num(7)), i
+        assert torch.equal(g[:6].nan_to_num(7), g[part].nan_to_num(7)), i
+    h = _host(ids, logp, tail, rows, y, scale)
+    r_loss, r_grad, size = O.opd_distill(z, *h[:5], scale=h[5])
+    unit = O.opd_distill(z, *h[:5])[2].sum(1)
+    delta = DELTA_LONG
+    for got in (loss[:6], only[:6], only[-6:]):
+        _close(got, r_loss, delta * unit + HALF["float32"] * np.abs(r_loss), "loss")
+    _close(g[:6], r_grad, 4 * delta * size + HALF[dtype] * np.abs(r_grad) + 1e-37, "grad")
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("T,V", [(2, 3001), (2, 20011), (100, 70001), (2, 151936)])
+def test_rows_whose_beginning_is_masked(torch, T, V, dtype):
+    """Rows that start with masked tokens, or with tokens far below the others:
+    no sum may depend on where a row's large values stand."""
+    from paper_2605_27255_amd import opd_distill
+    d, z = _rows(torch, 6, V, dtype, seed=V, pad=-V % 8)
+    d[0, :V - V // 50] = -float("inf")
+    d[1, :V - V // 50] -= 300.0
+    d[2, :V // 2] = float(torch.finfo(d.dtype).min)
+    d[3, : V - 1] = -float("inf")
+    d[4, V - 5] = 200.0
+    z = d.double().cpu().numpy()
+    ids, logp, tail = _teacher(torch, np.where(np.isfinite(z) & (np.abs(z) < 1e30), z, 0.0), 9, 1.0, seed=1)
+    many = lambda a: a.repeat((T + 5) // 6, *[1] * (a.dim() - 1))[:T]  # noqa: E731
+    x = many(d._base)[:, :V]
+    zz = z[np.arange(T) % 6][:6]
+    loss, g = opd_distill(x, many(ids), many(logp), many(tail), kind="jsd", grad=True)
+    only, _ = opd_distill(x, many(ids), many(logp), many(tail), kind="jsd")
+    torch.cuda.synchronize()
+    n = len(zz)
+    h = _host(ids[:n], logp[:n], tail[:n])
+    with np.errstate(all="ignore"):
+        r_loss, r_grad, size = O.opd_distill(zz, *h, kind="jsd")
+    for got in (loss[:n], only[:n]):
+        _close(got, r_loss, DELTA * size.sum(1) + HALF["float32"] * np.abs(r_loss), "loss")
+    _close(g[:n], r_grad, 4 * DELTA * size + HALF[dtype] * np.abs(r_grad) + 1e-37, "grad")
+
+
+def test_calls_without_a_work_array(torch):
+    """The C entries with d_work NULL: one workgroup a row, the same results to rounding."""
+    import ctypes
+    from paper_2605_27255_amd import load_library, opd_distill, opd_top_logits
+    lib, V, T, k = load_library(), 151936, 3, 20
+    d, z = _rows(torch, T, V, "float32", seed=5)
+    ids, logp, tail = opd_top_logits(d, k)
+    i2, l2, t2 = torch.empty_like(ids), torch.empty_like(logp), torch.empty_like(tail)
+    stream = torch.cuda.current_stream().cuda_stream
+    p = lambda t: ctypes.c_void_p(t.data_ptr())  # noqa: E731
+    assert lib.pipo_opd_top_logits(T, V, p(d), V, 1.0, k, p(i2), p(l2), p(t2), None, 0, stream) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(ids, i2)
+    r = O.opd_top_logits(z, k)
+    _close(l2, r[1], DELTA + HALF["float32"] * np.abs(r[1]))
+    _close(t2, r[2], 2 * DELTA + HALF["float32"] * np.abs(r[2]))
+    t_ids, t_logp, t_tail = _teacher(torch, z, k, 1.0, seed=2)
+    loss, g = torch.empty(T, device="cuda"), torch.empty_like(d)
+    assert lib.pipo_opd_distill(T, V, p(d), V, T, k, p(t_ids), p(t_logp), p(t_tail), None, None, 1, 0.5, 1.0, None, p(loss),
+                                p(g), V, None, 0, stream) == 0
+    torch.cuda.synchronize()
+    r_loss, r_grad, size = O.opd_distill(z, *_host(t_ids, t_logp, t_tail))
+    _close(loss, r_loss, DELTA * size.sum(1) + HALF["float32"] * np.abs(r_loss), "loss")
+    _close(g, r_grad, 4 * DELTA * size + HALF["float32"] * np.abs(r_grad) + 1e-37, "grad")
+    again = opd_distill(d, t_ids, t_logp, t_tail, grad=True)
+    assert all(torch.equal(a, b) for a, b in zip(again, opd_distill(d, t_ids, t_logp, t_tail, grad=True)))
+
+
 # ---- policy loss ---------------------------------------------------------------------------------------------------
 
 def _check_policy(torch, d, z, y, adv, old=None, ref=None, scale=None, grad=True, delta=DELTA, **kw):
@@ -361,6 +508,16 @@ def test_policy(torch, T, V, pad, dtype):
     _check_policy(torch, d, z, y, adv, old, None, None, **kw)
     _check_policy(torch, d, z, y, adv, None, ref, None, kl_coef=0.0, grad=None, **kw)
     _check_policy(torch, d, z, y, adv, None, None, scale, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("T,V", [(1, 33333), (257, 20011), (1100, 9001), (1100, 40003)])
+def test_policy_without_a_gradient(torch, T, V, dtype):
+    """Rows from workgroups of four, eight and sixteen waves."""
+    d, z = _rows(torch, T, V, dtype, seed=V)
+    rng = np.random.default_rng(1)
+    y = torch.from_numpy(rng.integers(0, V, T).astype(np.int32)).cuda()
+    _check_policy(torch, d, z, y, torch.from_numpy(rng.standard_normal(T).astype(np.float32)).cuda(), grad=None)
 
 
 def test_policy_sharp_rows_and_masks(torch):

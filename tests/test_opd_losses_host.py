@@ -141,6 +141,23 @@ def test_bad_arguments_are_refused_before_device_work(lib, dt):
         assert _policy(lib, dt, **kw) == PIPO_EINVAL, kw
 
 
+def test_work_arrays_are_checked(lib):
+    """Calls that use a work array say how large; a smaller or misaligned one is refused."""
+    from paper_2605_27255_amd import PIPO_EINVAL
+    long = dict(T=4, V=151936, ld=151936)
+    for bf16, dt in enumerate(("", "_bf16")):
+        for call, fn, extra in ((0, _top, {}), (1, _distill, {}), (2, _distill, dict(grad=ctypes.c_void_p(1 << 30), ldg=151936)),
+                                (2, _policy, dict(grad=ctypes.c_void_p(1 << 30), ldg=151936))):
+            need = lib.pipo_opd_work_bytes(call, 4, 151936, 1 if fn is _policy else 2, bf16)
+            if need == 0:
+                continue
+            assert fn(lib, dt, work=B, nw=need - 1, **long, **extra) == PIPO_EINVAL
+            assert fn(lib, dt, work=ctypes.c_void_p((1 << 24) + 8), nw=need, **long, **extra) == PIPO_EINVAL
+        assert lib.pipo_opd_work_bytes(0, 4, 151936, 2, bf16) > 0 and lib.pipo_opd_work_bytes(2, 4, 151936, 2, bf16) > 0
+    for bad in ((0, 0, 100, 1, 0), (0, 4, 0, 1, 0), (0, 4, (1 << 19) + 1, 1, 0), (0, 4, 100, 0, 0), (2, 4, 100, 257, 0)):
+        assert lib.pipo_opd_work_bytes(*bad) == 0
+
+
 def test_empty_calls_need_no_arrays(lib):
     from paper_2605_27255_amd import PIPO_OK
     for dt in ("", "_bf16"):
