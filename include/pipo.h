@@ -240,8 +240,8 @@ int pipo_opd_targets_bf16(int32_t T, int32_t V, const uint16_t *d_logits_s, cons
                           double *d_sums, void *stream);
 
 /* ---- OPD losses with their gradients (App. C; no context needed) -----------
- * Three operators on logit rows, fp32 or (_bf16) bf16 bit patterns: T rows of V
- * logits, row t at d_logits + t * ld elements (V <= ld <= 2^31; rows need no alignment
+ * Three operators on logit rows, fp32 or (_bf16) bf16 bit patterns, on the
+ * current device: T rows (up to 4194303) of V logits, row t at d_logits + t * ld elements (V <= ld <= 2^31; rows need no alignment
  * beyond their element's), V from 1 to 524288.  x = z / temperature (1e-5 to
  * 1e5), p = softmax(x).  All sums are fp32 or wider, the arithmetic on single
  * entries is fp64.  T = 0 is allowed (the arrays may then be NULL).  Logits may

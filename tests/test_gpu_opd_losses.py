@@ -416,6 +416,29 @@ def test_rows_whose_beginning_is_masked(torch, T, V, dtype):
     _close(g[:n], r_grad, 4 * DELTA * size + HALF[dtype] * np.abs(r_grad) + 1e-37, "grad")
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("T", [3, 98])
+def test_longest_rows(torch, T, dtype):
+    """524288 tokens, split over workgroups and not, with 256 entries."""
+    from paper_2605_27255_amd import opd_distill
+    V = 1 << 19
+    d, z = _rows(torch, 3, V, dtype, seed=V)
+    ids, logp, tail = _teacher(torch, z, 256, 1.3, seed=4)
+    rows = (torch.arange(T, dtype=torch.int32) % 3).cuda()
+    x = d.repeat(33, 1)[:T]
+    kw = dict(rows=rows, kind="reverse", temperature=1.3)
+    loss, g = opd_distill(x, ids, logp, tail, grad=True, **kw)
+    only, _ = opd_distill(x, ids, logp, tail, **kw)
+    torch.cuda.synchronize()
+    r_loss, r_grad, size = O.opd_distill(z, *_host(ids, logp, tail), temperature=1.3)
+    unit = size.sum(1) * 1.3
+    for got in (loss[:3], only[:3], loss[-1:]):
+        at = (T - 1) % 3 if len(got) == 1 else slice(0, 3)
+        _close(got, np.atleast_1d(r_loss[at]), DELTA_LONG * np.atleast_1d(unit[at]) + HALF["float32"] * np.abs(np.atleast_1d(r_loss[at])))
+    _close(g[:3], r_grad, 4 * DELTA_LONG * size + HALF[dtype] * np.abs(r_grad) + 1e-37, "grad")
+    _close(g[-1], r_grad[(T - 1) % 3], (4 * DELTA_LONG * size + HALF[dtype] * np.abs(r_grad) + 1e-37)[(T - 1) % 3], "grad")
+
+
 def test_calls_without_a_work_array(torch):
     """The C entries with d_work NULL: one workgroup a row, the same results to rounding."""
     import ctypes

@@ -120,7 +120,7 @@ def _policy(lib, dt, **kw):
     return getattr(lib, "pipo_opd_policy" + dt)(*a.values())
 
 
-ROWS = [dict(T=-1), dict(V=0), dict(V=(1 << 19) + 1), dict(ld=7), dict(ld=1 << 40), dict(z=None), dict(z=ctypes.c_void_p((1 << 20) + 1)),
+ROWS = [dict(T=-1), dict(T=1 << 22), dict(V=0), dict(V=(1 << 19) + 1), dict(ld=7), dict(ld=1 << 40), dict(z=None), dict(z=ctypes.c_void_p((1 << 20) + 1)),
         dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=NAN), dict(temperature=float("inf")),
         dict(temperature=1e-200)]
 LOSS = ROWS + [dict(loss=None), dict(grad=ctypes.c_void_p((1 << 21) + 1), ldg=8), dict(grad=ctypes.c_void_p(1 << 21), ldg=7),
