@@ -38,10 +38,11 @@ template <typename L> struct TopParams {
     uint64_t *keys;                 // [T][S][k]
 };
 
-// Unsigned integers in the order of the values; -0 counts as 0.
+// Unsigned integers in the order of the values; -0 counts as 0.  0 stands for no
+// value: the NaN of all ones, which would have it, shares the next NaN's.
 __device__ __forceinline__ uint32_t value_key(float v) {
     const uint32_t u = __float_as_uint(v + 0.f);
-    return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+    return max((u & 0x80000000u) ? ~u : u | 0x80000000u, 1u);
 }
 __device__ __forceinline__ float key_value(uint32_t k) {
     return __uint_as_float((k & 0x80000000u) ? k & 0x7FFFFFFFu : ~k);

@@ -105,6 +105,23 @@ def test_top_logits_of_crowded_rows(torch, V, dtype):
     _check_top(torch, d, d.double().cpu().numpy(), k)
 
 
+@pytest.mark.parametrize("V", [300, 4099, 70001])
+def test_top_logits_of_rows_of_all_ones_bits(torch, V):
+    """Memory filled with ones is NaNs whose bits come last in any order: NaN
+    log-probabilities, ids different and in range, split rows or not."""
+    from paper_2605_27255_amd import opd_top_logits
+    k = 50
+    for bits, dtype in ((torch.int32, torch.float32), (torch.int16, torch.bfloat16)):
+        d = torch.full((3, V), -1, dtype=bits, device="cuda").view(dtype)
+        d[1, 5:25] = 1.0                                    # fewer than k others
+        d[2, 100:200] = torch.arange(100, device="cuda").to(dtype)
+        ids, logp, tail = opd_top_logits(d, k)
+        torch.cuda.synchronize()
+        assert logp.isnan().all() and tail.isnan().all()
+        for row in ids.tolist():
+            assert len(set(row)) == k and 0 <= min(row) and max(row) < V
+
+
 def test_top_logits_of_rows_without_a_distribution(torch):
     """All -inf, a NaN, a +inf: NaN log-probabilities, ids different and in range; other rows as ever."""
     from paper_2605_27255_amd import opd_top_logits
