@@ -647,8 +647,9 @@ template <typename L> static int launch_loss(LossParams<L> p, void *work, hipStr
     const int n = p.pieces = least_whole(p.z, p.ld, p.T, p.V);
     if (!p.grad) {
         // Few rows: all of a compute unit's waves on each; many short ones: several rows to a compute unit.  Four / eight /
-        // sixteen waves, us: 128 x 151936 fp32 34 / 22 / 18, 256 x 32003 bf16 10.8 / 9.2 / 8.3, 512 x 32003 bf16
-        // 13.1 / 11.8 / 15.6, 2048 x 8192 bf16 13.5 / 16.6 / 35, 2048 x 151936 bf16 104 / 98 / 120.
+        // sixteen waves, logits from memory, us: 128 x 151936 fp32 36 / 24 / 20, 256 x 32003 bf16 11.7 / 10.6 / 9.7,
+        // 512 x 32003 bf16 14.1 / 13.2 / 13.5, 2048 x 8192 bf16 14 / 16 / 24, 2048 x 32003 bf16 30 / 37 / 43,
+        // 2048 x 151936 bf16 109 / 103 / 104.
         if (p.T <= 256 && n >= 4000) return launch_rows<L, 1024, 4, 4, false>(p, s);
         if (p.T > 1024 && n <= 256 * 32) return launch_rows<L, 256, 4, 4, false>(p, s);
         return launch_rows<L, 512, 4, 4, false>(p, s);
@@ -656,8 +657,8 @@ template <typename L> static int launch_loss(LossParams<L> p, void *work, hipStr
     // Workgroups of four waves, as many to a compute unit as their registers allow (two with 44 slabs): while one sums
     // or finishes a row, others load and write.  Only rows of which two leave most to be read again go to one workgroup
     // of eight waves a compute unit, which holds twice as much.  With the gradient, two of four waves / one of eight,
-    // in us: 2048 x 100000 bf16 159 / 170, 2048 x 151936 bf16 231 / 253, 1187 x 262144 bf16 267 / 248; fp32 1944 x 80000
-    // 233 / 245, 2048 x 100000 321 / 316, 2048 x 151936 534 / 515.
+    // logits from memory, in us: bf16 2048 x 151936 255 / 256, 2048 x 168000 283 / 283, 1187 x 262144 287 / 275; fp32
+    // 1944 x 80000 254 / 253, 2048 x 100000 336 / 322, 2048 x 151936 538 / 519: the same up to some 80 slabs.
     if (n < 256 * 3) return launch_rows<L, 256, 2, 2, true>(p, s);
     if (n < 256 * 5) return launch_rows<L, 256, 4, 2, true>(p, s);
     if (n < 256 * 7) return launch_rows<L, 256, 6, 2, true>(p, s);
