@@ -270,6 +270,8 @@ __device__ __forceinline__ RowSum join_parts(const Part *part, int S, ExpScale c
     const float B = round_ref(ref_of(m, c));
     double f = far ? (x.m == m ? 1. : (double)exp_diff(x.m, m, c)) : exp(((double)x.B - (double)B) * kLn2);
     if (!far && is_far(x.m)) f = 0.;
+    // nothing there (s is 0, or a NaN that stays): its reference may be far below the others', or above them where all are empty
+    if (x.m == -INFINITY) f = 1.;
     return RowSum{m, B, wave_sum_f64(x.s * f)};
 }
 

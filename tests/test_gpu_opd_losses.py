@@ -703,3 +703,34 @@ def test_python_refusals(torch):
     loss, g = opd_distill(empty, ids, logp, tail, grad=True)
     assert loss.shape == (0,) and g.shape == (0, 100)
     assert opd_policy(empty, y[:0], adv[:0], grad=True)[3].shape == (0, 100)
+
+
+# ---- split rows, masks and magnitudes ----------------------------------------------------------------------------------
+
+def _is_split(call, T, V, k, dtype):
+    from paper_2605_27255_amd import load_library
+    return load_library().pipo_opd_work_bytes(call, T, V, k, dtype == "bfloat16") > 0
+
+
+@pytest.mark.parametrize("temperature", [0.7, 1.0, 2.0])
+@pytest.mark.parametrize("T,V,dtype,grad", [(3, 60001, "float32", True), (2, 151936, "bfloat16", True),
+                                            (16, 151936, "float32", None)])
+def test_split_rows_with_nothing_outside(torch, T, V, dtype, grad, temperature):
+    """Everything but the list (or the label) masked with -inf, in rows that are
+    split: the tokens outside have no mass, and nothing is NaN."""
+    d, z = _rows(torch, T, V, dtype, seed=V)
+    ids, logp, tail = _teacher(torch, z, 9, temperature, seed=1)
+    for x in (ids.long(), ids[:, :1].long()):
+        assert _is_split(2 if grad else 1, T, V, x.shape[1], dtype)
+        only = torch.full_like(d, -float("inf")).scatter_(1, x, d.gather(1, x))
+        oz = only.double().cpu().numpy()
+        if x.shape[1] == 1:
+            y, adv, ref = ids[:, 0].contiguous(), torch.linspace(-1, 1, T).cuda(), torch.full((T,), -0.3).cuda()
+            out = _check_policy(torch, only, oz, y, adv, None, ref, grad=grad, kl_coef=0.1, temperature=temperature)
+            assert all(t is None or t.isfinite().all() for t in out)
+            continue
+        for kind in ("reverse", "jsd", "forward"):
+            loss, g = _check_distill(torch, only, oz, ids, logp, tail, grad=grad, kind=kind, temperature=temperature)
+            # (a teacher with mass where the student has none is infinitely far in the forward direction)
+            assert torch.isposinf(loss).all() if kind == "forward" else loss.isfinite().all()
+            assert grad is None or g.isfinite().all()
