@@ -269,9 +269,10 @@ __device__ __forceinline__ double sum_far(const Span<const L> &row, const uint32
 }
 // A piece's gradients away from the list; those of listed elements are written over them later.
 template <typename L> __device__ __forceinline__ void gradients(float *v, u32x4 w, float coef, float B, ExpScale c) {
-    // c's second float matters to sums only: here it is less than one rounding of each exponent
+    // with c's second float, as in the sum: z times it is no rounding, but a tilt of the whole row (1e-4 at z = 1000 and
+    // temperature 0.7), which the exponents, differences that they are, would not show
 #pragma unroll
-    for (int e = 0; e < Piece<L>::N; ++e) v[e] = coef * __builtin_amdgcn_exp2f(fmaf(Piece<L>::get(w, e), c.hi, -B));
+    for (int e = 0; e < Piece<L>::N; ++e) v[e] = coef * exp_at(Piece<L>::get(w, e), B, c);
 }
 // ... of this thread's pieces from index first on, and the partial ones (out: where the gradient's piece 0 lies).
 template <typename L, int NT>
@@ -360,8 +361,11 @@ __device__ __forceinline__ RowSum sum_slowly(const Span<const L> &row, const uin
 // the other.
 template <int NT, int NV> constexpr bool kTakesSeveral = NT == 512 && NV >= 12;    // one workgroup fills a compute unit
 template <int NT, int NV> constexpr bool kSpills = NV >= (NT == 512 ? 33 : 44);     // the longest rows' variants
+// Waves of a SIMD that the registers leave room for: short rows live by their number (16384 x 8192 bf16 with the gradient
+// from five 108 us, from six 99).
+constexpr int waves_of(int nt, int nv, bool grad) { return !grad ? 8 : nv <= 2 ? 7 : nv <= 4 ? 6 : nv <= 8 ? 5 : nt / 256; }
 template <typename L, int NT, int NV, int STEP, bool GRAD>
-__global__ __launch_bounds__(NT, GRAD ? NT / 256 : 8) void k_opd_loss(LossParams<L> p) {
+__global__ __launch_bounds__(NT, waves_of(NT, NV, GRAD)) void k_opd_loss(LossParams<L> p) {
     constexpr bool LOOP = kTakesSeveral<NT, NV>, DEEP = kSpills<NT, NV>;
     constexpr int AHEAD = NV < 12 ? NV : 12, N = Piece<L>::N;
     extern __shared__ uint32_t bits[];

@@ -734,3 +734,28 @@ def test_split_rows_with_nothing_outside(torch, T, V, dtype, grad, temperature):
             # (a teacher with mass where the student has none is infinitely far in the forward direction)
             assert torch.isposinf(loss).all() if kind == "forward" else loss.isfinite().all()
             assert grad is None or g.isfinite().all()
+
+
+# A row's gradient sums to zero.  An unlisted one's exponent is at most 30 (less weighs under 2^-30) and rounded once, 21 *
+# 2^-24 of the value; its exponential 2^-23, coefficient and product 2^-24 each: 25 * 2^-24.  The sum behind the coefficient
+# has exponentials as exact, once more where threads are merged (46 * 2^-24), and adds: up to 20 in a thread, 16 in merges.
+ZERO_SUM = 107 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("offset,temperature", [(1000.0, 0.7), (-1000.0, 0.7), (10000.0, 1.0), (20.0, 0.05), (20.0, 1e-3),
+                                                (0.0, 1e-5), (3.0, 1e-5)])
+@pytest.mark.parametrize("T,V", [(4, 2001), (3, 70001), (100, 5003)])
+def test_gradients_of_rows_with_an_offset(torch, T, V, offset, temperature):
+    """softmax does not change with an offset of the row, nor with logits and
+    temperature scaled together: nor does the gradient's accuracy."""
+    rng = np.random.default_rng(V)
+    z = (offset + temperature * 3.0 * rng.standard_normal((T, V))).astype(np.float32)
+    d, z = torch.from_numpy(z).cuda(), z.astype(np.float64)
+    ids, logp, tail = O.opd_top_logits(z + temperature * rng.standard_normal(z.shape), 9, temperature)
+    ids, logp, tail = (torch.from_numpy(a).cuda().to(t) for a, t in ((ids, torch.int32), (logp, torch.float32), (tail, torch.float32)))
+    y = torch.from_numpy(rng.integers(0, V, T).astype(np.int32)).cuda()
+    grads = [_check_distill(torch, d, z, ids, logp, tail, kind=kind, temperature=temperature)[1] for kind in ("forward", "jsd")]
+    grads.append(_check_policy(torch, d, z, y, torch.linspace(0.5, 1.5, T).cuda(), temperature=temperature)[3])
+    for g in grads:
+        off = (g.double().sum(1).abs() / g.double().abs().sum(1)).cpu().numpy()
+        assert (off <= ZERO_SUM).all(), off
