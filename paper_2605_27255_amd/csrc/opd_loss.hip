@@ -214,9 +214,11 @@ __device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, const 
             // with no mass outside the list there is nothing to spread there
             const double k = lse != lse ? lse : rest.s == 0. ? 0. : g * (a_rest / rest.s - A * rest_at * exp(-lse));
             // against a reference near the values that weigh most: their exponents are small, and so their roundings
+            // (k counts from the one that a float holds, which far from 0 is not the sum's plus a whole number)
             const int shift = is_far(rest.m) || !(rest.s > 0.) ? 0 : min(max(ilogb(rest.s), -120), 120);
-            sh.coef = (float)ldexp(k, shift);
-            sh.B = rest.B + (float)shift;
+            const float B = rest.B + (float)shift;
+            sh.coef = (float)(shift ? k * exp2((double)B - (double)rest.B) : k);
+            sh.B = B;
         }
     }
     __syncthreads();
@@ -434,7 +436,7 @@ __global__ __launch_bounds__(NT, waves_of(NT, NV, GRAD)) void k_opd_loss(LossPar
             m = block_max<NT>(m, red[0]);
             const bool borrowed = !(m > -kFar);
             if (borrowed) m = block_max<NT>(id >= 0 ? zj : -INFINITY, red[2]);
-            const float B = round_ref(ref_of(m, p.c));
+            const float B = ref_of(m, p.c);
             off = (tid + NT * AHEAD) * 16;
 #pragma unroll
             for (int j = 0; j < NV; ++j, next_slab<NT>(off)) {

@@ -248,13 +248,11 @@ template <int NT> __device__ __forceinline__ double block_sum(float v, float *s_
 // A row's unlisted values: their sum in multiples of 2^B (where m is far, of
 // exp(m / temperature)); m is their maximum, or near it.
 struct RowSum { float m, B; double s; };
-// A reference that whole numbers can be added to exactly.
-__device__ __forceinline__ float round_ref(float B) { return rintf(B * 1024.f) * (1.f / 1024.f); }
 
 // The threads' (max, sum) as one: the sum in 64 bits across waves.  s_w: NT / 64 each for the maxima and the sums.
 template <int NT> __device__ __forceinline__ RowSum block_merge(MaxSum a, ExpScale c, float (*s_w)[NT / 64]) {
     const float m = block_max<NT>(a.m, s_w[0]);
-    const float B = round_ref(ref_of(m, c)), s = a.s * __builtin_amdgcn_exp2f(ref_of(a.m, c) - B);
+    const float B = ref_of(m, c), s = a.s * __builtin_amdgcn_exp2f(ref_of(a.m, c) - B);
     return RowSum{m, B, block_sum<NT>(s, s_w[1])};
 }
 
@@ -267,7 +265,7 @@ __device__ __forceinline__ RowSum join_parts(const Part *part, int S, ExpScale c
     const float m = wave_max_dpp(x.m);
     // beside a far maximum, and beside a near one where they are far, the other segments weigh nothing
     const bool far = is_far(m);
-    const float B = round_ref(ref_of(m, c));
+    const float B = ref_of(m, c);
     double f = far ? (x.m == m ? 1. : (double)exp_diff(x.m, m, c)) : exp(((double)x.B - (double)B) * kLn2);
     if (!far && is_far(x.m)) f = 0.;
     // nothing there (s is 0, or a NaN that stays): its reference may be far below the others', or above them where all are empty

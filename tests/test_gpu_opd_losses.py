@@ -759,3 +759,18 @@ def test_gradients_of_rows_with_an_offset(torch, T, V, offset, temperature):
     for g in grads:
         off = (g.double().sum(1).abs() / g.double().abs().sum(1)).cpu().numpy()
         assert (off <= ZERO_SUM).all(), off
+
+
+@pytest.mark.parametrize("level,temperature", [(14.5361, 1e-5), (20.0, 1e-5), (50.0, 1e-5), (200.0, 1e-5), (1000.0, 1e-5),
+                                               (1000.0, 1e-3), (-200.0, 1e-5)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("T,V", [(3, 3001), (2, 130001), (100, 20011)])
+def test_gradients_of_level_rows_at_small_temperatures(torch, T, V, dtype, level, temperature):
+    """Thousands of equal tokens far from 0 in units of the temperature: what a
+    reference of the exponentials cannot hold is not left out of the gradient."""
+    d = torch.full((T, V), level, device="cuda", dtype=getattr(torch, dtype))
+    d[:, 1::7] -= 1.5 * temperature             # (another level, where the type can tell it)
+    z = d.double().cpu().numpy()
+    ids, logp, tail = _teacher(torch, z, 9, temperature, seed=1, noise=temperature)
+    _check_distill(torch, d, z, ids, logp, tail, kind="jsd", temperature=temperature)
+    _check_policy(torch, d, z, ids[:, 0].contiguous(), torch.ones(T).cuda(), temperature=temperature)
