@@ -395,12 +395,15 @@ def opd_distill(logits, ids, logp, tail=None, rows=None, labels=None, kind="reve
         per[here], mag[here] = a, np.abs(a) + 2 * p[here]
         total, A = np.sum(f), np.sum(a)
         if tail is not None:
+            # as far below the list as masks put it: e^lr itself may be 0
+            near = np.max(lp[out], initial=-np.inf)
             with np.errstate(all="ignore"):
-                lr = np.log(np.sum(p[out]))
+                e = np.exp(lp[out] - near)
+                lr = near if np.isneginf(near) else near + np.log(np.sum(e))
             fr, ar = _divergence_terms(kind, beta, lr, F64(tail[r]))
             total, A = total + fr, A + ar
-            if np.any(p[out] > 0):
-                share = p[out] / np.sum(p[out])
+            if lr > -np.inf:
+                share = e / np.sum(e)
                 per[out], mag[out] = ar * share, (np.abs(ar) + 2 * np.exp(lr)) * share
         w = (1.0 if scale is None else float(scale[t])) / temperature
         loss[t] = total

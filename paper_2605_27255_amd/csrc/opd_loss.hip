@@ -158,7 +158,7 @@ __device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, const 
         for (int j = lane; j < p.k; j += 64) if (sh.id[j] >= 0) sum += exp(((double)sh.z[j] - m) * inv);
         sum = wave_sum_f64(sum);
         // log of the rest's unit (its sum counts multiples of it) over exp(m / temperature)
-        const double unit = is_far(rest.m) ? ((double)rest.m - m) * inv : (double)rest.B * kLn2 - m * inv;
+        const double unit = is_far(rest.m, p.c) ? ((double)rest.m - m) * inv : (double)rest.B * kLn2 - m * inv;
         const double rest_at = rest.m == -INFINITY ? 1. : exp(unit);
         sum += rest.s * rest_at;     // without a rest its sum is 0 (or NaN)
         // of x - m / temperature; a row without any mass has none
@@ -215,7 +215,7 @@ __device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, const 
             const double k = lse != lse ? lse : rest.s == 0. ? 0. : g * (a_rest / rest.s - A * rest_at * exp(-lse));
             // against a reference near the values that weigh most: their exponents are small, and so their roundings
             // (k counts from the one that a float holds, which far from 0 is not the sum's plus a whole number)
-            const int shift = is_far(rest.m) || !(rest.s > 0.) ? 0 : min(max(ilogb(rest.s), -120), 120);
+            const int shift = is_far(rest.m, p.c) || !(rest.s > 0.) ? 0 : min(max(ilogb(rest.s), -120), 120);
             const float B = rest.B + (float)shift;
             sh.coef = (float)(shift ? k * exp2((double)B - (double)rest.B) : k);
             sh.B = B;
@@ -342,7 +342,7 @@ __device__ __forceinline__ RowSum sum_slowly(const Span<const L> &row, const uin
     __syncthreads();
     RowSum a = block_merge<NT>(own, c, red);
     __syncthreads();
-    if (is_far(a.m)) a.s = sum_far<L, NT>(row, bits, a.m, c, red[0]);
+    if (is_far(a.m, c)) a.s = sum_far<L, NT>(row, bits, a.m, c, red[0]);
     __syncthreads();
     return a;
 }
@@ -434,7 +434,7 @@ __global__ __launch_bounds__(NT, waves_of(NT, NV, GRAD)) void k_opd_loss(LossPar
             }
             if (NV <= STEP && held == 0) each_piece<NT, 1>(row, tid, [&](u32x4 w, int i) { max_piece<L>(m, w, listed_bits<N>(bits, i)); });
             m = block_max<NT>(m, red[0]);
-            const bool borrowed = !(m > -kFar);
+            const bool borrowed = !(m * p.c.hi > -kFar);
             if (borrowed) m = block_max<NT>(id >= 0 ? zj : -INFINITY, red[2]);
             const float B = ref_of(m, p.c);
             off = (tid + NT * AHEAD) * 16;
@@ -466,8 +466,8 @@ __global__ __launch_bounds__(NT, waves_of(NT, NV, GRAD)) void k_opd_loss(LossPar
             }
             if (tid < p.k) sh.z[tid] = zj;
             a = RowSum{m, B, block_sum<NT>(s, red[1])};
-            if (!(a.s < INFINITY) || is_far(m) || (borrowed && a.s < 1e-30)) a = sum_slowly<L, NT>(row, bits, p.c, red);
-            far = is_far(a.m);
+            if (!(a.s < INFINITY) || is_far(m, p.c) || (borrowed && (a.s < 1e-30 || m == -INFINITY))) a = sum_slowly<L, NT>(row, bits, p.c, red);
+            far = is_far(a.m, p.c);
             if (id >= 0) bits[(id - row.head + N) >> 5] = 0;     // every wave is past its sums: ready for the next position
             finish_row(p, t, x, a, sh);
         } else {
@@ -548,7 +548,7 @@ template <typename L> __global__ __launch_bounds__(kPartThreads) void k_opd_part
     MaxSum own{-INFINITY, 0.f};
     each_piece<NT, 4, true>(row, tid, [&](u32x4 w, int i) { add_piece<L>(own, w, i, bits, p.c); });
     RowSum a = block_merge<NT>(own, p.c, red);
-    if (is_far(a.m)) a.s = sum_far<L, NT>(row, bits, a.m, p.c, red[2]);
+    if (is_far(a.m, p.c)) a.s = sum_far<L, NT>(row, bits, a.m, p.c, red[2]);
     if (tid == 0) q.part[(int64_t)t * q.S + seg] = Part{a.m, a.B, a.s, sh.bad, 0};
 }
 
@@ -585,7 +585,7 @@ __global__ __launch_bounds__(kPartThreads) void k_opd_apply(LossParams<L> p, Spl
     finish_row(p, t, x, a, sh, seg == 0);
     if (!GRAD) return;
     const Span<const L> row(p.z + (int64_t)t * p.ld + lo, len);
-    if (is_far(a.m)) put_far<L, NT>(out + row.head, row, sh.coef, a.m, p.c);
+    if (is_far(a.m, p.c)) put_far<L, NT>(out + row.head, row, sh.coef, a.m, p.c);
     else put_pieces<L, NT>(out + row.head, row, tid, sh.coef, sh.B, p.c);
     __syncthreads();
     if (id >= lo && id < lo + len) Piece<L>::put(out + (id - lo), sh.patch[tid]);

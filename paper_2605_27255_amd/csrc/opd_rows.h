@@ -162,15 +162,17 @@ inline ExpScale exp_scale(double temperature) {
 __device__ __forceinline__ float exp_at(float z, float B, ExpScale c) {
     return __builtin_amdgcn_exp2f(fmaf(z, c.lo, fmaf(z, c.hi, -B)));
 }
-// Logits beyond this in magnitude (masks at the type's lowest value, as a rule)
-// weigh nothing beside smaller ones; a row of nothing else is summed by
-// differences (exp_diff), which its own maximum keeps from overflowing.
-constexpr float kFar = 1e30f;
+// Exponents z c beyond this in magnitude are far: there the reference m c.hi is
+// rounded by up to a quarter, and further out by as many binades as a sum of floats
+// cannot hold.  Far values below near ones (masks, as a rule) weigh nothing; a row of
+// nothing nearer, or of far large ones, is summed by differences of its logits
+// (exp_diff), which are exact wherever its zero is.
+constexpr float kFar = 4194304.f;
 __device__ __forceinline__ float ref_of(float m, ExpScale c) {
 #pragma clang fp contract(off)      // the product as the one float that every use of it takes
-    return fmaxf(m, -kFar) * c.hi;
+    return fmaxf(m * c.hi, -kFar);
 }
-__device__ __forceinline__ bool is_far(float m) { return m != -INFINITY && !(fabsf(m) <= kFar); }
+__device__ __forceinline__ bool is_far(float m, ExpScale c) { return m != -INFINITY && !(fabsf(m * c.hi) <= kFar); }
 __device__ __forceinline__ float exp_diff(float a, float b, ExpScale c) {
     const float d = a - b;
     return __builtin_amdgcn_exp2f(fmaf(d, c.hi, d * c.lo));
@@ -263,13 +265,13 @@ __device__ __forceinline__ RowSum join_parts(const Part *part, int S, ExpScale c
     if (lane < S) x = part[lane];
     bad = __ballot(x.bad != 0) != 0;
     const float m = wave_max_dpp(x.m);
-    // beside a far maximum, and beside a near one where they are far, the other segments weigh nothing
-    const bool far = is_far(m);
+    const bool far = is_far(m, c), x_far = is_far(x.m, c);
     const float B = ref_of(m, c);
-    double f = far ? (x.m == m ? 1. : (double)exp_diff(x.m, m, c)) : exp(((double)x.B - (double)B) * kLn2);
-    if (!far && is_far(x.m)) f = 0.;
+    // log of the segment's unit over the row's: a far one counts multiples of exp(m / temperature), a near one of 2^B
+    const double at = x_far ? (double)x.m * c.inv : (double)x.B * kLn2, to = far ? (double)m * c.inv : (double)B * kLn2;
+    double f = exp(x_far && far ? ((double)x.m - (double)m) * c.inv : at - to);
     // nothing there (s is 0, or a NaN that stays): its reference may be far below the others', or above them where all are empty
-    if (x.m == -INFINITY) f = 1.;
+    if (x.m == -INFINITY || x.m == m) f = 1.;
     return RowSum{m, B, wave_sum_f64(x.s * f)};
 }
 

@@ -142,7 +142,7 @@ __device__ __forceinline__ void put_top(const TopParams<L> &p, int t, const uint
 }
 // What a row's sum counts (multiples of 2^B, or far of exp(m / temperature)) in multiples of exp(m / temperature).
 __device__ __forceinline__ double unit_of_max(float m, float B, ExpScale c) {
-    return is_far(m) || m == -INFINITY ? 1. : exp((double)B * kLn2 - (double)m * c.inv);
+    return is_far(m, c) || m == -INFINITY ? 1. : exp((double)B * kLn2 - (double)m * c.inv);
 }
 
 // One workgroup per row, or (SPLIT) per segment of one.
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
     if (lane == 0) sh.wmin[wave] = value_key(least_w);
     if (tid == 0) sh.n = 0;
     const float m = block_max<NT>(most_own, sh.red[0]);     // its barrier: umax, wmin and n are set
-    const bool far = is_far(m);
+    const bool far = is_far(m, p.c);
     const float B = ref_of(m, p.c);
     auto term = [&](float v) { return far ? exp_diff(v, m, p.c) : exp_at(v, B, p.c); };
     uint32_t least = sh.wmin[0];
@@ -347,7 +347,7 @@ template <typename L> __global__ __launch_bounds__(kJoinThreads) void k_opd_top_
     const uint32_t bound = bound_of_kth(sh, lo, hi, k);
     float rest = 0.f;
     if (mine && (uint32_t)(mine >> 32) >= bound) sh.cand[atomicAdd(&sh.n, 1)] = mine;
-    const bool far = is_far(rests.m);
+    const bool far = is_far(rests.m, p.c);
     const float B = rests.B;
     auto term = [&](uint64_t key) {
         const float v = key_value((uint32_t)(key >> 32));

@@ -774,3 +774,47 @@ def test_gradients_of_level_rows_at_small_temperatures(torch, T, V, dtype, level
     ids, logp, tail = _teacher(torch, z, 9, temperature, seed=1, noise=temperature)
     _check_distill(torch, d, z, ids, logp, tail, kind="jsd", temperature=temperature)
     _check_policy(torch, d, z, ids[:, 0].contiguous(), torch.ones(T).cuda(), temperature=temperature)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("mask,temperature", [(-1e4, 1.0), (-1e9, 0.7), (-1e9, 1.1), (-1e10, 1.0), (-1e10, 0.5), (-3e20, 1.0),
+                                              (-1e30, 1.4), (-1e32, 1.0), (-1e9, 1e-3)])
+@pytest.mark.parametrize("T,V", [(6, 3001), (6, 140001), (102, 20011)])
+def test_tokens_masked_with_finite_values(torch, T, V, dtype, mask, temperature):
+    """Masks of every magnitude weigh nothing beside a token that is not masked,
+    and alike where all are, or where all tokens outside the list are."""
+    d, z = _rows(torch, 6, V, dtype, seed=V)
+    ids, logp, tail = _teacher(torch, z, 9, temperature, seed=2)
+    d[0, 1::2] = mask
+    d[1, : V - V // 10] = mask
+    d[2, V // 10:] = mask
+    listed = ids[3:4].long()
+    d[3:4] = torch.full_like(d[3:4], mask).scatter_(1, listed, d[3:4].gather(1, listed))
+    d[4] = mask
+    z = d.double().cpu().numpy()
+    for k in (1, 9, 40) if temperature >= 0.5 else ():
+        _check_top(torch, d, z, k, temperature)
+    many = lambda a: a.repeat((T + 5) // 6, *[1] * (a.dim() - 1))[:T]  # noqa: E731
+    zz = np.tile(z, ((T + 5) // 6, 1))[:T]
+    for kind in ("forward", "jsd"):
+        _check_distill(torch, many(d), zz, many(ids), many(logp), many(tail), kind=kind, temperature=temperature)
+        _check_distill(torch, many(d), zz, many(ids), many(logp), None, kind=kind, temperature=temperature, grad=None)
+    y = torch.tensor([2, V - 1, 0, int(listed[0, 0]), 5, 1], dtype=torch.int32).cuda()
+    _check_policy(torch, many(d), zz, many(y), torch.linspace(0.5, 1.5, T).cuda(), temperature=temperature)
+
+
+# exponents on both sides of 2^22, where rows are summed by differences instead, in one row and apart
+@pytest.mark.parametrize("offset,temperature", [(1e6, 1.0), (-1e6, 1.0), (2907270.0, 1.0), (-2907270.0, 1.0), (2e7, 3.0),
+                                                (1e10, 500.0), (-1e10, 500.0), (29.0727, 1e-5), (-30.0, 1e-5), (3e12, 1e5)])
+@pytest.mark.parametrize("T,V", [(3, 3001), (3, 70001), (100, 5003)])
+def test_rows_far_from_zero(torch, T, V, offset, temperature):
+    """Finite logits of any magnitude: only their differences count."""
+    rng = np.random.default_rng(V)
+    z = (offset + temperature * 3.0 * rng.standard_normal((T, V))).astype(np.float32)
+    d, z = torch.from_numpy(z).cuda(), z.astype(np.float64)
+    for k in (9, 150):
+        _check_top(torch, d, z, k, temperature)
+    ids, logp, tail = _teacher(torch, z, 9, temperature, seed=2, noise=temperature)
+    for kind in ("forward", "reverse", "jsd"):
+        _check_distill(torch, d, z, ids, logp, tail, kind=kind, temperature=temperature)
+    _check_policy(torch, d, z, ids[:, 3].contiguous(), torch.linspace(0.5, 1.5, T).cuda(), temperature=temperature)
