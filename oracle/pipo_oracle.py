@@ -347,8 +347,10 @@ def opd_top_logits(logits, k, temperature=1.0):
         ids[t] = np.argsort(-z, kind="stable")[:k]
         lp = _log_softmax_row(z, temperature)
         logp[t] = lp[ids[t]]
+        outside = np.delete(lp, ids[t])
+        near = np.max(outside, initial=-np.inf)
         with np.errstate(all="ignore"):
-            tail[t] = np.log(np.sum(np.exp(np.delete(lp, ids[t]))))
+            tail[t] = near if np.isneginf(near) else near + np.log(np.sum(np.exp(outside - near)))
     return ids, logp, tail
 
 

@@ -157,8 +157,7 @@ __device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, const 
         double sum = 0.;
         for (int j = lane; j < p.k; j += 64) if (sh.id[j] >= 0) sum += exp(((double)sh.z[j] - m) * inv);
         sum = wave_sum_f64(sum);
-        // log of the rest's unit (its sum counts multiples of it) over exp(m / temperature)
-        const double unit = is_far(rest.m, p.c) ? ((double)rest.m - m) * inv : (double)rest.B * kLn2 - m * inv;
+        const double unit = log_unit(rest.m, rest.B, m, p.c);
         const double rest_at = rest.m == -INFINITY ? 1. : exp(unit);
         sum += rest.s * rest_at;     // without a rest its sum is 0 (or NaN)
         // of x - m / temperature; a row without any mass has none

@@ -248,8 +248,12 @@ template <int NT> __device__ __forceinline__ double block_sum(float v, float *s_
     return r;
 }
 // A row's unlisted values: their sum in multiples of 2^B (where m is far, of
-// exp(m / temperature)); m is their maximum, or near it.
+// exp(m / temperature)); m is their maximum, or near it (-inf: there are none).
 struct RowSum { float m, B; double s; };
+// The log of what such a sum counts in over exp(at / temperature).
+__device__ __forceinline__ double log_unit(float m, float B, double at, ExpScale c) {
+    return is_far(m, c) ? ((double)m - at) * c.inv : (double)B * kLn2 - at * c.inv;
+}
 
 // The threads' (max, sum) as one: the sum in 64 bits across waves.  s_w: NT / 64 each for the maxima and the sums.
 template <int NT> __device__ __forceinline__ RowSum block_merge(MaxSum a, ExpScale c, float (*s_w)[NT / 64]) {
@@ -265,11 +269,9 @@ __device__ __forceinline__ RowSum join_parts(const Part *part, int S, ExpScale c
     if (lane < S) x = part[lane];
     bad = __ballot(x.bad != 0) != 0;
     const float m = wave_max_dpp(x.m);
-    const bool far = is_far(m, c), x_far = is_far(x.m, c);
     const float B = ref_of(m, c);
-    // log of the segment's unit over the row's: a far one counts multiples of exp(m / temperature), a near one of 2^B
-    const double at = x_far ? (double)x.m * c.inv : (double)x.B * kLn2, to = far ? (double)m * c.inv : (double)B * kLn2;
-    double f = exp(x_far && far ? ((double)x.m - (double)m) * c.inv : at - to);
+    // a segment's unit over the row's
+    double f = exp(log_unit(x.m, x.B, m, c) - (is_far(m, c) ? 0. : log_unit(m, B, m, c)));
     // nothing there (s is 0, or a NaN that stays): its reference may be far below the others', or above them where all are empty
     if (x.m == -INFINITY || x.m == m) f = 1.;
     return RowSum{m, B, wave_sum_f64(x.s * f)};

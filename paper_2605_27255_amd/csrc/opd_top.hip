@@ -125,24 +125,51 @@ template <int NT, int H> __device__ __forceinline__ void sort_candidates(TopShar
     }
     __syncthreads();
 }
-// The row's outputs, by its first wave: sorted[0, k) are the k largest, `outside` the sum of exp((z - m) / temperature) of all others.
+// The row's outputs, by its first wave: sorted[0, k) are the k largest, m the largest, `out` the sum of all others.
 template <typename L>
-__device__ __forceinline__ void put_top(const TopParams<L> &p, int t, const uint64_t *sorted, float m, double outside) {
+__device__ __forceinline__ void put_top(const TopParams<L> &p, int t, const uint64_t *sorted, float m, RowSum out) {
     const int lane = threadIdx.x;
     double sum = 0.;
     for (int j = lane; j < p.k; j += 64)
         sum += exp(((double)key_value((uint32_t)(sorted[j] >> 32)) - (double)m) * p.c.inv);
-    const double lse = log(wave_sum_f64(sum) + outside);    // of x - m / temperature
+    const double unit = log_unit(out.m, out.B, m, p.c);
+    const double lse = log(wave_sum_f64(sum) + (out.m == -INFINITY ? out.s : out.s * exp(unit)));   // of x - m / temperature
     for (int j = lane; j < p.k; j += 64) {
         const uint64_t key = sorted[j];
         p.ids[(int64_t)t * p.k + j] = key_id(key);
         p.logp[(int64_t)t * p.k + j] = (float)(((double)key_value((uint32_t)(key >> 32)) - (double)m) * p.c.inv - lse);
     }
-    if (lane == 0 && p.tail) p.tail[t] = (float)(log(outside) - lse);
+    if (lane == 0 && p.tail) p.tail[t] = (float)(!(lse == lse) ? lse : out.s == 0. ? -INFINITY : unit + log(out.s) - lse);
 }
-// What a row's sum counts (multiples of 2^B, or far of exp(m / temperature)) in multiples of exp(m / temperature).
-__device__ __forceinline__ double unit_of_max(float m, float B, ExpScale c) {
-    return is_far(m, c) || m == -INFINITY ? 1. : exp((double)B * kLn2 - (double)m * c.inv);
+// A sum of exponentials under this share of its reference may have lost some that no float holds (2^-126, of 2^19 at most).
+constexpr double kThin = 1e-25;
+// The sum of a row's values whose keys are below `last`, over a reference of their own.
+template <typename L, int NT>
+__device__ __forceinline__ RowSum sum_below(const Span<const L> &row, uint64_t last, ExpScale c, float (*red)[NT / 64]) {
+    constexpr int N = Piece<L>::N;
+    float m = -INFINITY, s = 0.f;
+    auto below = [&](float v, int i, int e) { return row.has(i, e) && pair_key(value_key(v), row.head + i * N + e) < last; };
+    each_piece<NT, 1>(row, (int)threadIdx.x, [&](u32x4 w, int i) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float v = Piece<L>::get(w, e);
+            if (below(v, i, e)) m = fmaxf(m, v);
+        }
+    });
+    __syncthreads();
+    m = block_max<NT>(m, red[0]);
+    const bool far = is_far(m, c);
+    const float B = ref_of(m, c);
+    if (m != -INFINITY) {
+        each_piece<NT, 1>(row, (int)threadIdx.x, [&](u32x4 w, int i) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float v = Piece<L>::get(w, e);
+                if (below(v, i, e)) s += far ? exp_diff(v, m, c) : exp_at(v, B, c);
+            }
+        });
+    }
+    return RowSum{m, B, block_sum<NT>(s, red[1])};
 }
 
 // One workgroup per row, or (SPLIT) per segment of one.
@@ -310,16 +337,21 @@ __global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
     }
     sort_candidates(sh, nc);
     for (int j = k + tid; j < nc; j += NT) rest += term(key_value((uint32_t)(sh.sorted[j] >> 32)));
-    const double outside = block_sum<NT>(rest, sh.red[2]);
+    RowSum out{m, B, block_sum<NT>(rest, sh.red[2])};
+    if (out.s < kThin) {
+        const uint64_t last = sh.sorted[k - 1];     // (below a last one of -inf, or where all are on the list, there is nothing)
+        if (k < V && (uint32_t)(last >> 32) > value_key(-INFINITY)) out = sum_below<L, NT>(row, last, p.c, sh.red);
+        else out.m = -INFINITY;
+    }
     if (SPLIT) {
         uint64_t *keys = p.keys + ((int64_t)t * p.S + seg) * p.k;
         for (int j = tid; j < p.k; j += NT) {
             const uint64_t key = j < k ? sh.sorted[j] : 0;
             keys[j] = key ? pair_key((uint32_t)(key >> 32), key_id(key) + lo) : 0;
         }
-        if (tid == 0) p.part[(int64_t)t * p.S + seg] = Part{m, B, outside, 0, 0};
+        if (tid == 0) p.part[(int64_t)t * p.S + seg] = Part{out.m, out.B, out.s, 0, 0};
     } else if (wave == 0) {
-        put_top(p, t, sh.sorted, m, outside * unit_of_max(m, B, p.c));
+        put_top(p, t, sh.sorted, m, out);
     }
 }
 
@@ -345,21 +377,18 @@ template <typename L> __global__ __launch_bounds__(kJoinThreads) void k_opd_top_
     if (tid == 0) sh.n = 0;
     __syncthreads();
     const uint32_t bound = bound_of_kth(sh, lo, hi, k);
-    float rest = 0.f;
     if (mine && (uint32_t)(mine >> 32) >= bound) sh.cand[atomicAdd(&sh.n, 1)] = mine;
-    const bool far = is_far(rests.m, p.c);
-    const float B = rests.B;
-    auto term = [&](uint64_t key) {
-        const float v = key_value((uint32_t)(key >> 32));
-        return far ? exp_diff(v, rests.m, p.c) : exp_at(v, B, p.c);
-    };
-    if (mine && (uint32_t)(mine >> 32) < bound) rest = term(mine);
     __syncthreads();
-    const int nc = sh.n;
-    sort_candidates(sh, nc);
-    for (int j = k + tid; j < nc; j += NT) rest += term(sh.sorted[j]);
-    const double outside = block_sum<NT>(rest, sh.red[2]) + rests.s;
-    if (tid < 64) put_top(p, t, sh.sorted, rests.m, outside * unit_of_max(rests.m, B, p.c));
+    sort_candidates(sh, sh.n);
+    // the lists' other keys and the segments' other values, over the largest of them
+    const bool other = mine && mine < sh.sorted[k - 1];
+    const float v = key_value((uint32_t)(mine >> 32));
+    const float m = fmaxf(block_max<NT>(other ? v : -INFINITY, sh.red[0]), rests.m), B = ref_of(m, p.c);
+    const float term = !other ? 0.f : is_far(m, p.c) ? exp_diff(v, m, p.c) : exp_at(v, B, p.c);
+    RowSum out{m, B, block_sum<NT>(term, sh.red[1])};
+    const double f = exp(log_unit(rests.m, rests.B, m, p.c) - (is_far(m, p.c) ? 0. : log_unit(m, B, m, p.c)));
+    out.s += rests.m == -INFINITY || rests.m == m ? rests.s : rests.s * f;
+    if (tid < 64) put_top(p, t, sh.sorted, key_value((uint32_t)(sh.sorted[0] >> 32)), out);
 }
 
 // Segments of each row: about two workgroups a compute unit in all, at least

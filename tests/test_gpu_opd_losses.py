@@ -818,3 +818,39 @@ def test_rows_far_from_zero(torch, T, V, offset, temperature):
     for kind in ("forward", "reverse", "jsd"):
         _check_distill(torch, d, z, ids, logp, tail, kind=kind, temperature=temperature)
     _check_policy(torch, d, z, ids[:, 3].contiguous(), torch.linspace(0.5, 1.5, T).cuda(), temperature=temperature)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("T,V,k", [(9, 3001, 9), (9, 140001, 9), (9, 140001, 100), (99, 20011, 9), (3, 40, 40), (9, 257, 256)])
+def test_top_logits_with_little_outside(torch, T, V, k, dtype):
+    """The mass outside the list to its own precision however small it is, also
+    where no float holds it: sharp rows, small temperatures, masks."""
+    d, _ = _rows(torch, 9, V, dtype, seed=V + k)
+    at = torch.randperm(V, generator=torch.Generator().manual_seed(k))[:k].cuda()
+    top = torch.linspace(0, 5, k).cuda().to(d.dtype)
+    d[1] -= 150.0
+    d[2] -= 500.0
+    d[3] = -1e4
+    d[4] = -1e9
+    d[5] = float(torch.finfo(d.dtype).min)
+    d[6] = -float("inf")
+    d[7] = -float("inf")
+    d[7, V // 3] = -700.0                      # one segment has something outside, or it is on the list
+    for t in range(1, 8):
+        d[t, at] = top + (3000.0 if t == 2 else 0.0)
+    z = d.double().cpu().numpy()
+    many = lambda a: a.repeat((T + 8) // 9, *[1] * (a.dim() - 1))[:T]  # noqa: E731
+    from paper_2605_27255_amd import opd_distill, opd_top_logits
+    for temperature in (1.0, 1e-3, 30.0):
+        ids, logp, tail = opd_top_logits(many(d), k, temperature)
+        r_ids, r_logp, r_tail = (np.tile(r, ((T + 8) // 9,) + (1,) * (r.ndim - 1))[:T] for r in O.opd_top_logits(z, k, temperature))
+        np.testing.assert_array_equal(ids.cpu().numpy(), r_ids)
+        # what is below the least float32 (masks over 1e-3) is -inf in float32
+        r_logp, r_tail = (np.where(r < -3.4028235e38, -np.inf, r) for r in (r_logp, r_tail))
+        _close(logp, r_logp, DELTA + HALF["float32"] * np.abs(r_logp), "logp")
+        _close(tail, r_tail, 2 * DELTA + HALF["float32"] * np.abs(r_tail), "tail")
+    if V > k:
+        # a student that has that mass is finitely far from such a teacher
+        ids, logp, tail = opd_top_logits(d[:5], k)
+        loss, _ = opd_distill(torch.zeros_like(d[:5]), ids, logp, tail, kind="reverse")
+        assert loss.isfinite().all() and tail.isfinite().all()
