@@ -216,7 +216,8 @@ __device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, const 
             // (k counts from the one that a float holds, which far from 0 is not the sum's plus a whole number)
             const int shift = is_far(rest.m, p.c) || !(rest.s > 0.) ? 0 : min(max(ilogb(rest.s), -120), 120);
             const float B = rest.B + (float)shift;
-            sh.coef = (float)(shift ? k * exp2((double)B - (double)rest.B) : k);
+            const double off = (double)B - (double)rest.B;
+            sh.coef = (float)(off == (double)shift ? ldexp(k, shift) : k * exp2(off));
             sh.B = B;
         }
     }
