@@ -433,17 +433,19 @@ def opd_policy(logits, labels, advantages, old_logp=None, ref_logp=None, clip=(0
             continue
         lps = _log_softmax_row(logits[t], temperature)
         lp, adv = lps[y], float(advantages[t])
-        ratio = np.exp(lp - (float(old_logp[t]) if old_logp is not None else lp))    # a row without a distribution: NaN
+        # on-policy: 1, for a label of probability 0 too, but NaN in a row without a distribution
+        ratio = np.exp(lp - float(old_logp[t])) if old_logp is not None else 1.0 if lp == lp else lp
         cut = min(max(ratio, 1 - clip[0]), 1 + clip[1])
         loss[t] = -min(adv * ratio, adv * cut)
         d = -adv * ratio if adv * ratio <= adv * cut else 0.0
         slope[t] = abs(adv * ratio)
         if ref_logp is not None:
             u = float(ref_logp[t]) - lp
-            kl[t] = np.exp(u) - u - 1
-            loss[t] += kl_coef * kl[t]
-            d += kl_coef * (1 - np.exp(u))
-            slope[t] += abs(kl_coef) * (1 + np.exp(u))
+            kl[t] = np.inf if np.isposinf(u) else np.exp(u) - u - 1
+            if kl_coef:
+                loss[t] += kl_coef * kl[t]
+                d += kl_coef * (1 - np.exp(u))
+                slope[t] += abs(kl_coef) * (1 + np.exp(u))
         logp[t] = lp
         onehot = np.arange(V) == y
         grad[t] = (1.0 if scale is None else float(scale[t])) / temperature * d * (onehot - np.exp(lps))

@@ -166,14 +166,14 @@ __device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, const 
         double A = 0., a_rest = 0.;
         if (p.kind == kPolicy) {
             const double lp = ((double)sh.z[0] - m) * inv - lse, py = exp(lp), adv = x.adv;
-            const double r = exp(lp - (p.old_lp ? (double)x.old_lp : lp));
+            const double r = p.old_lp ? exp(lp - (double)x.old_lp) : lp == lp ? 1. : lp;     // on-policy: 1 for a masked label too
             const double cut = fmin(fmax(r, 1. - p.clip_lo), 1. + p.clip_hi);
             const bool inside = adv * r <= adv * cut;
             double loss = -(inside ? adv * r : adv * cut), d = inside ? -adv * r : 0., kl = 0.;
             if (r != r || adv != adv) loss = d = r + adv;
             if (p.ref_lp) {
                 const double far = (double)x.ref_lp - lp;
-                kl = expm1(far) - far;
+                kl = far == INFINITY ? far : expm1(far) - far;
                 if (p.kl_coef != 0.) {
                     loss += p.kl_coef * kl;
                     d -= p.kl_coef * expm1(far);

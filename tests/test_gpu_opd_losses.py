@@ -854,3 +854,26 @@ def test_top_logits_with_little_outside(torch, T, V, k, dtype):
         ids, logp, tail = opd_top_logits(d[:5], k)
         loss, _ = opd_distill(torch.zeros_like(d[:5]), ids, logp, tail, kind="reverse")
         assert loss.isfinite().all() and tail.isfinite().all()
+
+
+@pytest.mark.parametrize("V", [777, 140001])
+def test_policy_of_a_masked_label(torch, V):
+    """A label of probability 0: the ratio of an on-policy call is 1 all the
+    same, and a KL estimate of a token that the reference can draw is infinite."""
+    from paper_2605_27255_amd import opd_policy
+    d, _ = _rows(torch, 3, V, "float32", seed=V)
+    y = torch.tensor([4, V - 1, 9], dtype=torch.int32).cuda()
+    d[torch.arange(3), y.long()] = -float("inf")
+    z, adv = d.double().cpu().numpy(), torch.tensor([1.5, -0.5, 2.0]).cuda()
+    for grad in (True, None):
+        loss, logp, _, g = _check_policy(torch, d, z, y, adv, grad=grad)
+        assert torch.equal(loss, -adv) and torch.isneginf(logp).all()
+        assert grad is None or torch.equal(g[torch.arange(3), y.long()], -adv)
+        ref = torch.full((3,), -4.0).cuda()
+        loss, _, kl, _ = opd_policy(d, y, adv, ref_logp=ref, grad=grad)
+        assert torch.equal(loss, -adv) and torch.isposinf(kl).all()
+        loss, _, kl, _ = opd_policy(d, y, adv, ref_logp=ref, kl_coef=0.1, grad=grad)
+        assert torch.isposinf(loss).all() and torch.isposinf(kl).all()
+        # ... of rollouts that another policy drew: ratio 0, clipped where the advantage is negative
+        loss, _, _, _ = opd_policy(d, y, adv, old_logp=ref, grad=grad)
+        assert torch.equal(loss, torch.where(adv < 0, -adv * 0.8, 0.0))
