@@ -159,13 +159,15 @@ __device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, const 
         sum = wave_sum_f64(sum);
         const double unit = log_unit(rest.m, rest.B, m, p.c);
         const double rest_at = rest.m == -INFINITY ? 1. : exp(unit);
-        sum += rest.s * rest_at;     // without a rest its sum is 0 (or NaN)
+        // without a rest its sum is 0 (or NaN); one that nearly vanishes beside the list: what the sum's rounding takes goes
+        // into the log
+        const double x_rest = rest.s * rest_at, whole = sum + x_rest, lost = x_rest <= sum ? x_rest - (whole - sum) : 0.;
         // of x - m / temperature; a row without any mass has none
-        const double lse = m == -INFINITY ? (double)__builtin_nanf("") : log(sum);
+        const double lse = m == -INFINITY ? (double)__builtin_nanf("") : log(whole) + lost;
         const double g = (double)x.scale * inv;
         double A = 0., a_rest = 0.;
         if (p.kind == kPolicy) {
-            const double lp = ((double)sh.z[0] - m) * inv - lse, py = exp(lp), adv = x.adv;
+            const double lp = ((double)sh.z[0] - m) * inv - lse, adv = x.adv;
             const double r = p.old_lp ? exp(lp - (double)x.old_lp) : lp == lp ? 1. : lp;     // on-policy: 1 for a masked label too
             const double cut = fmin(fmax(r, 1. - p.clip_lo), 1. + p.clip_hi);
             const bool inside = adv * r <= adv * cut;
@@ -180,7 +182,6 @@ __device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, const 
                 }
             }
             A = d;
-            if (lane == 0) sh.patch[0] = (float)(g * (d - py * d));
             if (lane == 0 && first) {
                 p.loss[t] = (float)loss;
                 if (p.logp) p.logp[t] = (float)lp;
@@ -210,8 +211,10 @@ __device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, const 
                 if (sh.id[j] >= 0) sh.patch[j] = (float)(g * (sh.a[j] - sh.p[j] * A));
         }
         if (lane == 0) {
+            const double unit_p = rest_at * exp(-lse);      // the probability of one of the rest's units
+            if (p.kind == kPolicy) sh.patch[0] = (float)(g * A * (rest.s * unit_p));    // (1 - p of the label without cancellation)
             // with no mass outside the list there is nothing to spread there
-            const double k = lse != lse ? lse : rest.s == 0. ? 0. : g * (a_rest / rest.s - A * rest_at * exp(-lse));
+            const double k = lse != lse ? lse : rest.s == 0. ? 0. : g * (a_rest / rest.s - A * unit_p);
             // against a reference near the values that weigh most: their exponents are small, and so their roundings
             // (k counts from the one that a float holds, which far from 0 is not the sum's plus a whole number)
             const int shift = is_far(rest.m, p.c) || !(rest.s > 0.) ? 0 : min(max(ilogb(rest.s), -120), 120);
