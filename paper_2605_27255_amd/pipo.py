@@ -357,12 +357,21 @@ def _opd_grad(grad, logits, T, V, ld):
     if grad is True:
         grad = torch.empty((T, V), dtype=logits.dtype, device=logits.device)
         return grad, grad.data_ptr(), V
-    if grad is logits:
-        return grad, grad.data_ptr(), ld
-    if (not isinstance(grad, torch.Tensor) or grad.shape != logits.shape or grad.dtype != logits.dtype
-            or grad.device != logits.device):
-        _refuse("grad: True, or a tensor of the logits' shape, type and device")
-    return grad, grad.data_ptr(), _opd_rows(grad, "grad")[2]
+    if grad is not logits:
+        if (not isinstance(grad, torch.Tensor) or grad.shape != logits.shape or grad.dtype != logits.dtype
+                or grad.device != logits.device):
+            _refuse("grad: True, or a tensor of the logits' shape, type and device")
+        ld = _opd_rows(grad, "grad")[2]
+    if torch.is_grad_enabled() and grad.requires_grad and (grad if grad._base is None else grad._base).is_leaf:
+        _refuse("grad: not a leaf that requires a gradient (but under torch.no_grad())")     # as torch's own writes
+    return grad, grad.data_ptr(), ld
+
+
+def _opd_written(grad):
+    """Tells autograd that the caller's tensor was written: a backward pass that had saved its values raises."""
+    import torch
+    if not grad.is_inference():
+        torch.autograd.graph.increment_version(grad)
 
 
 def _opd_call(name, call, logits, device, T, V, k, args):
@@ -419,8 +428,9 @@ def opd_distill(logits, ids, logp, tail=None, rows=None, labels=None, kind: str 
     int32 [T], negative: not scored; kind: "forward", "reverse" or "jsd" (with
     beta); scale: float32 [T], each position's factor in the gradient; grad:
     None, True, or a tensor to write it to (the logits themselves to replace
-    them).  Returns (loss [T] float32, grad or None); the caller goes on with
-    ``logits.backward(grad)``."""
+    them; autograd counts it as a write in place, so a step that saved them for
+    its own backward pass, as a tanh does, raises there).  Returns (loss [T]
+    float32, grad or None); the caller goes on with ``logits.backward(grad)``."""
     import torch
     if _elsewhere(logits):
         with torch.cuda.device(logits.device):
@@ -437,9 +447,12 @@ def opd_distill(logits, ids, logp, tail=None, rows=None, labels=None, kind: str 
     *ptrs, scale_ptr = _opd_args(dev, (ids, "ids", i32, lists), (logp, "logp", f32, lists), (tail, "tail", f32, (Tt,)),
                                  (rows, "rows", i32, shape), (labels, "labels", i32, shape), (scale, "scale", f32, shape))
     loss = torch.empty(T, dtype=f32, device=dev)
-    grad, grad_ptr, ldg = _opd_grad(grad, logits, T, V, ld)
+    wanted = grad
+    grad, grad_ptr, ldg = _opd_grad(wanted, logits, T, V, ld)
     _opd_call("pipo_opd_distill" + dt, 1 if grad is None else 2, logits, dev, T, V, k,
               (ld, Tt, k, *ptrs, OPD_KINDS[kind], beta, temperature, scale_ptr, loss.data_ptr(), grad_ptr, ldg))
+    if grad is not None and wanted is not True:
+        _opd_written(grad)
     return loss, grad
 
 
@@ -465,10 +478,13 @@ def opd_policy(logits, labels, advantages, old_logp=None, ref_logp=None, clip=(0
                                  (scale, "scale", f32, shape))
     loss, logp = torch.empty(T, dtype=f32, device=dev), torch.empty(T, dtype=f32, device=dev)
     kl = None if ref_logp is None else torch.empty(T, dtype=f32, device=dev)
-    grad, grad_ptr, ldg = _opd_grad(grad, logits, T, V, ld)
+    wanted = grad
+    grad, grad_ptr, ldg = _opd_grad(wanted, logits, T, V, ld)
     _opd_call("pipo_opd_policy" + dt, 1 if grad is None else 2, logits, dev, T, V, 1,
               (ld, *ptrs, clip[0], clip[1], kl_coef, temperature, scale_ptr, loss.data_ptr(), logp.data_ptr(),
                None if kl is None else kl.data_ptr(), grad_ptr, ldg))
+    if grad is not None and wanted is not True:
+        _opd_written(grad)
     return loss, logp, kl, grad
 
 

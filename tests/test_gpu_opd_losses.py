@@ -897,3 +897,45 @@ def test_policy_label_with_almost_all_mass(torch, T, V):
     assert ((logp.double() - lp).abs() <= (DELTA + 2.0 ** -24) * lp.abs()).all(), (logp, lp)
     others = g.double().sum(1) - g[:, 5].double()
     assert ((g[:, 5].double() + others).abs() <= 2 * DELTA * want.abs()).all()
+
+
+def test_gradient_over_the_logits_and_autograd(torch):
+    """Writing the gradient over logits that a backward pass still needs is seen
+    by autograd, as any other write is; over a leaf it is refused like one."""
+    from paper_2605_27255_amd import PipoError, opd_distill, opd_policy
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    h = torch.randn((6, 32), generator=gen, device="cuda")
+    w = torch.randn((32, 700), generator=gen, device="cuda", requires_grad=True)
+    y, adv = torch.arange(6, dtype=torch.int32).cuda(), torch.ones(6).cuda()
+    ids, logp = torch.arange(24, dtype=torch.int32).cuda().view(6, 4), torch.full((6, 4), -1.5).cuda()
+    for call in (lambda x, g: opd_distill(x, ids, logp, grad=g), lambda x, g: opd_policy(x, y, adv, grad=g)):
+        x = h @ w                           # whose backward pass does not need its result
+        x.backward(call(x, True)[-1])
+        want, w.grad = w.grad, None
+        x = h @ w
+        x.backward(call(x, x)[-1])
+        assert torch.equal(w.grad, want)
+        w.grad = None
+        x = 5 * torch.tanh(h @ w)
+        capped = torch.tanh(h @ w)          # whose backward pass reads its result
+        call(x, x)                          # (the factor's backward pass does not)
+        g = call(capped, capped)[-1]
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            capped.backward(g)
+        w.grad = None
+        part = torch.tanh(h @ w)
+        call(part.detach(), part.detach())  # the same memory by another tensor
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            part.sum().backward()
+        w.grad = None
+        leaf = (h @ w).detach().requires_grad_()
+        before = leaf.detach().clone()
+        for target in (leaf, leaf[:]):
+            with pytest.raises(PipoError):
+                call(leaf, target)
+        assert torch.equal(leaf, before)
+        with torch.no_grad():
+            assert call(leaf, leaf)[-1] is leaf and not torch.equal(leaf, before)
+        with torch.inference_mode():
+            x = h @ w
+            assert call(x, x)[-1] is x
