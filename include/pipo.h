@@ -265,8 +265,9 @@ int pipo_opd_targets_bf16(int32_t T, int32_t V, const uint16_t *d_logits_s, cons
  * be NULL) = the log of the probability outside the k (-inf where it is 0).
  *
  * pipo_opd_distill: the divergence of position t's row from the teacher's list
- * in row r = d_teacher_rows[t] (NULL: r = t) of d_ids, d_logp ([Tt][k], k from
- * 1 to 256; an id < 0 is an empty slot) and d_tail.  Over the listed entries,
+ * in row r = d_teacher_rows[t] (NULL: r = t) of d_ids, d_logp ([Tt][k], Tt from
+ * 1 or, where T is 0, from 0; k from 1 to 256; an id < 0 is an empty slot) and
+ * d_tail.  Over the listed entries,
  * and with d_tail non-NULL the tokens outside as one more entry, with teacher
  * probability Q (Q = exp(d_logp), exp(d_tail)) and student probability P:
  *   PIPO_OPD_FORWARD  sum Q (log Q - log P)

@@ -728,7 +728,7 @@ static int distill(int32_t T, int32_t V, const L *d_logits, int64_t ld, int32_t 
     p.labels = d_labels; p.scale = d_scale; p.loss = d_loss; p.grad = d_grad; p.ldg = ld_grad;
     const int rc = check_common(p, temperature, d_work, work_bytes);
     if (rc != PIPO_OK) return rc;
-    if (Tt < 1 || k < 1 || k > kEntries || kind < PIPO_OPD_FORWARD || kind > PIPO_OPD_JSD) return PIPO_EINVAL;
+    if (Tt < (T > 0 ? 1 : 0) || k < 1 || k > kEntries || kind < PIPO_OPD_FORWARD || kind > PIPO_OPD_JSD) return PIPO_EINVAL;
     if (kind == PIPO_OPD_JSD && !(beta > 0. && beta < 1.)) return PIPO_EINVAL;
     if (T == 0) return PIPO_OK;
     if (!d_ids || !d_logp) return PIPO_EINVAL;

@@ -939,3 +939,15 @@ def test_gradient_over_the_logits_and_autograd(torch):
         with torch.inference_mode():
             x = h @ w
             assert call(x, x)[-1] is x
+
+
+def test_empty_chunk_with_an_empty_list(torch):
+    """A chunk of nothing: no positions, no teacher rows."""
+    from paper_2605_27255_amd import PipoError, opd_distill, opd_top_logits
+    for dtype in (torch.float32, torch.bfloat16):
+        z = torch.empty((0, 100), dtype=dtype, device="cuda")
+        ids, logp, tail = opd_top_logits(z, 5)
+        loss, g = opd_distill(z, ids, logp, tail, grad=True)
+        assert loss.shape == (0,) and g.shape == (0, 100)
+        with pytest.raises(PipoError):
+            opd_distill(torch.zeros((2, 100), dtype=dtype, device="cuda"), ids, logp, tail)

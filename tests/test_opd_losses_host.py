@@ -175,3 +175,14 @@ def test_python_calls_refuse_host_tensors(lib):
                  lambda: opd_policy(z, i, f)):
         with pytest.raises(PipoError):
             call()
+
+
+def test_empty_calls_with_empty_lists(lib):
+    """No positions and no teacher rows: a chunk of nothing but prompt."""
+    from paper_2605_27255_amd import PIPO_EINVAL, PIPO_OK
+    for dt in ("", "_bf16"):
+        nothing = dict(T=0, z=None, ids=None, logp=None, loss=None)
+        assert _distill(lib, dt, Tt=0, **nothing) == PIPO_OK
+        assert _distill(lib, dt, Tt=-1, **nothing) == PIPO_EINVAL
+        assert _distill(lib, dt, Tt=0, k=0, **nothing) == PIPO_EINVAL
+        assert _distill(lib, dt, Tt=0) == PIPO_EINVAL
