@@ -951,3 +951,148 @@ def test_empty_chunk_with_an_empty_list(torch):
         assert loss.shape == (0,) and g.shape == (0, 100)
         with pytest.raises(PipoError):
             opd_distill(torch.zeros((2, 100), dtype=dtype, device="cuda"), ids, logp, tail)
+
+
+# Rows that are split, by type and call: with the gradient, the loss alone, the top logits.
+SPLIT = [("float32", 70001, True), ("bfloat16", 110001, True), ("float32", 151936, None), ("bfloat16", 210001, None)]
+
+
+@pytest.mark.parametrize("dtype,V,grad", SPLIT)
+def test_split_rows_labels_and_slots(torch, dtype, V, grad):
+    """A row map, unscored positions, empty slots and flagged positions in split rows."""
+    T, k = 12, 40
+    assert _is_split(2 if grad else 1, T, V, k, dtype)
+    d, z = _rows(torch, T, V, dtype, seed=V)
+    ids, logp, tail = _teacher(torch, z[:8], k, 1.0, seed=6)
+    rows = torch.tensor([0, 1, 1, 2, 3, 8, -1, 4, 5, 6, 7, 7], dtype=torch.int32).cuda()     # 8 and -1: no such row
+    labels = torch.tensor([1, 1, -1, 1, 1, 1, 1, 1, 1, 1, -5, 2 ** 31 - 1], dtype=torch.int32).cuda()
+    ids[2, ::3] = -1
+    ids[3, :] = -7                       # nothing listed
+    ids[4, 5] = V
+    ids[5, 39] = ids[5, 0]
+    ids[6, 0] = 2 ** 31 - 1
+    flagged = [5, 6, 7, 8, 9]
+    for tl in (tail, None):
+        for kind in ("forward", "reverse", "jsd"):
+            loss, g = _check_distill(torch, d, z, ids, logp, tl, rows=rows, labels=labels, kind=kind, grad=grad)
+            assert loss[flagged].isnan().all() and not loss[[2, 10]].any()
+            assert grad is None or (g[flagged].isnan().all() and not g[[2, 10]].any())
+    y = torch.arange(T, dtype=torch.int32).cuda()
+    y[1], y[3], y[5] = -1, V, V - 1
+    adv, old, ref = torch.linspace(-1, 1, T).cuda(), torch.full((T,), -9.0).cuda(), torch.full((T,), -8.0).cuda()
+    out = _check_policy(torch, d, z, y, adv, old, ref, torch.linspace(1, 2, T).cuda(), grad=grad, kl_coef=0.1)
+    assert all(t is None or (t[3].isnan().all() and not t[1].any()) for t in out)
+
+
+@pytest.mark.parametrize("dtype,V,grad", SPLIT)
+def test_split_rows_with_masks_and_without_a_distribution(torch, dtype, V, grad):
+    """Masked segments, a rest or a list without mass, lowest values, NaN and infinities in split rows."""
+    assert _is_split(2 if grad else 1, 9, V, 16, dtype)
+    d, z = _rows(torch, 9, V, dtype, seed=2)
+    ids, logp, tail = _teacher(torch, z, 16, 1.0, seed=3)
+    out = torch.ones(V, dtype=torch.bool, device="cuda")
+    out[ids[1].long()] = False
+    low = float(torch.finfo(d.dtype).min)
+    d[0, ::2] = -float("inf")
+    d[1, out] = -float("inf")            # the student has nothing outside the list
+    d[2, ids[2].long()] = -float("inf")  # ... and nothing on it
+    d[3] = -float("inf")
+    d[4, V // 3: V - V // 3] = low       # whole segments of the lowest value
+    d[5, 77] = float("nan")
+    d[6, V - 78] = float("inf")
+    d[7] = low
+    d[8, : V // 2] = -float("inf")       # whole segments of nothing
+    z = d.double().cpu().numpy()
+    for kind in ("reverse", "jsd"):
+        for tl in (tail, None):
+            with np.errstate(all="ignore"):
+                loss, g = _check_distill(torch, d, z, ids, logp, tl, kind=kind, grad=grad)
+            assert loss[[3, 5, 6]].isnan().all() and loss[[0, 1, 2, 4, 7, 8]].isfinite().all()
+            if grad:
+                assert g[[3, 5, 6]].isnan().all() and g[[0, 1, 2, 4, 7, 8]].isfinite().all()
+    y = torch.tensor([1, int(ids[1, 3]), 0, 0, 7, 5, 5, 9, V - 1], dtype=torch.int32).cuda()
+    with np.errstate(all="ignore"):
+        loss, logp, _, g = _check_policy(torch, d, z, y, torch.linspace(0.5, 1.5, 9).cuda(), torch.full((9,), -5.0).cuda(), grad=grad)
+    assert loss[[3, 5, 6]].isnan().all() and loss[[0, 1, 2, 4, 7, 8]].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype,V", [("float32", 70001), ("bfloat16", 110001)])
+def test_split_near_teacher_and_sharp_student(torch, dtype, V):
+    k = 8
+    assert _is_split(2, 3, V, k, dtype)
+    d, z = _rows(torch, 3, V, dtype, seed=4)
+    d[1] = 0
+    d[1, 17] = 30.0
+    d[2, :] = -50.0
+    d[2, 3] = 45.0
+    z = d.double().cpu().numpy()
+    for noise in (0.0, 0.5):
+        ids, logp, tail = _teacher(torch, z, k, 1.0, seed=9, noise=noise)
+        for kind in ("forward", "reverse", "jsd"):
+            _check_distill(torch, d, z, ids, logp, tail, kind=kind)
+            _check_distill(torch, d, z, ids, logp, None, kind=kind, temperature=0.8)
+
+
+@pytest.mark.parametrize("T", [95, 96, 97])
+def test_rows_on_both_sides_of_the_split(torch, T):
+    """The same rows in calls that split them and that do not: the same results to rounding, masked or not."""
+    from paper_2605_27255_amd import opd_distill
+    V = 50001
+    assert _is_split(2, T, V, 9, "float32") == (T <= 96)
+    d, z = _rows(torch, 5, V, "float32", seed=7)
+    ids, logp, tail = _teacher(torch, z, 9, 1.0, seed=8)
+    d[1, V // 2:] = -float("inf")
+    only = ids[2:3].long()
+    d[2:3] = torch.full_like(d[2:3], -float("inf")).scatter_(1, only, d[2:3].gather(1, only))
+    d[3] = float(torch.finfo(torch.float32).min)
+    z = d.double().cpu().numpy()
+    pick = torch.arange(T).cuda() % 5
+    loss, g = opd_distill(d[pick], ids[pick], logp[pick], tail[pick], kind="jsd", grad=True)
+    torch.cuda.synchronize()
+    r_loss, r_grad, size = O.opd_distill(z, *_host(ids, logp, tail), kind="jsd")
+    for t in (0, 5, T - 5):
+        at = (np.arange(5) + t) % 5
+        _close(loss[t:t + 5], r_loss[at], (DELTA * size.sum(1) + HALF["float32"] * np.abs(r_loss))[at], "loss")
+        _close(g[t:t + 5], r_grad[at], (4 * DELTA * size + HALF["float32"] * np.abs(r_grad) + 1e-37)[at], "grad")
+
+
+def test_split_streams_and_graphs(torch):
+    """Split top logits and losses on a side stream, and captured in two graphs replayed between eager calls."""
+    from paper_2605_27255_amd import opd_distill, opd_policy, opd_top_logits
+    T, V = 3, 70001
+    assert all(_is_split(call, T, V, k, "float32") for call, k in ((0, 16), (2, 16), (2, 1)))
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    fresh = lambda: 3 * torch.randn((T, V), generator=gen, device="cuda")  # noqa: E731
+    s, te = fresh(), fresh()
+    adv, y = torch.randn(T, generator=gen, device="cuda"), torch.randint(0, V, (T,), generator=gen, device="cuda").int()
+
+    def step():
+        ids, logp, tail = opd_top_logits(te, 16)
+        return (ids, logp, tail) + opd_distill(s, ids, logp, tail, labels=y, grad=True)
+
+    def policy():
+        loss, logp, _, g = opd_policy(s, y, adv, grad=True)
+        return opd_top_logits(s, 5) + (loss, logp, g)
+
+    side = torch.cuda.Stream()
+    want = [t.clone() for t in step() + policy()]
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = step() + policy()
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    graphs, outs = [], []
+    for fn in (step, policy):
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(fn())
+        graphs.append(g)
+    for i in range(4):
+        s.copy_(fresh())
+        te.copy_(fresh())
+        for g in graphs if i % 2 else graphs[::-1]:
+            g.replay()
+        want = step() + policy()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs[0] + outs[1], want)), i
