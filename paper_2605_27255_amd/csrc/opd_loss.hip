@@ -248,7 +248,7 @@ __device__ __forceinline__ void put_constant(const LossParams<L> &p, int t, floa
 
 // A piece of a row (or segment) into a sum, without its listed elements.
 template <typename L>
-__device__ __forceinline__ void add_piece(MaxSum &a, u32x4 w, int i, const uint32_t *bits, ExpScale c) {
+__device__ __forceinline__ void add_piece(MaxSum<double> &a, u32x4 w, int i, const uint32_t *bits, ExpScale c) {
     constexpr int N = Piece<L>::N;
     const uint32_t b = listed_bits<N>(bits, i);
     float v[N];
@@ -262,7 +262,7 @@ __device__ __forceinline__ void add_piece(MaxSum &a, u32x4 w, int i, const uint3
 }
 // The sum of a row (or segment) of far values, by differences from its maximum m.
 template <typename L, int NT>
-__device__ __forceinline__ double sum_far(const Span<const L> &row, const uint32_t *bits, float m, ExpScale c, float *s_w) {
+__device__ __forceinline__ double sum_far(const Span<const L> &row, const uint32_t *bits, float m, ExpScale c, double *s_w) {
     constexpr int N = Piece<L>::N;
     float s = 0.f;
     each_piece<NT, 1>(row, (int)threadIdx.x, [&](u32x4 w, int i) {
@@ -306,7 +306,7 @@ __device__ __forceinline__ void put_far(L *out, const Span<const L> &row, float 
 }
 
 // A thread's sum of 2^(z c - B), and its largest piece's share and slab.
-struct PieceSum { float s, most; int slab; };
+struct PieceSum { double s; float most; int slab; };
 // Adds a piece, unless it holds a listed element.
 template <typename L> __device__ __forceinline__ void sum_piece(PieceSum &a, u32x4 w, int slab, uint32_t listed, float B, ExpScale c) {
     constexpr int N = Piece<L>::N;
@@ -339,13 +339,13 @@ template <typename L> __device__ __forceinline__ void max_piece(float &m, u32x4 
 // (max, sum) of the unlisted elements of a row where the reference of the fast
 // pass did not fit, from two passes of their own.
 template <typename L, int NT>
-__device__ __forceinline__ RowSum sum_slowly(const Span<const L> &row, const uint32_t *bits, ExpScale c, float (*red)[NT / 64]) {
-    MaxSum own{-INFINITY, 0.f};
+__device__ __forceinline__ RowSum sum_slowly(const Span<const L> &row, const uint32_t *bits, ExpScale c, Reduce<NT> &red) {
+    MaxSum<double> own{-INFINITY, 0.};
     each_piece<NT, 1>(row, (int)threadIdx.x, [&](u32x4 w, int i) { add_piece<L>(own, w, i, bits, c); });
     __syncthreads();
     RowSum a = block_merge<NT>(own, c, red);
     __syncthreads();
-    if (is_far(a.m, c)) a.s = sum_far<L, NT>(row, bits, a.m, c, red[0]);
+    if (is_far(a.m, c)) a.s = sum_far<L, NT>(row, bits, a.m, c, red.sum[1]);
     __syncthreads();
     return a;
 }
@@ -375,7 +375,7 @@ __global__ __launch_bounds__(NT, waves_of(NT, NV, GRAD)) void k_opd_loss(LossPar
     constexpr int AHEAD = NV < 12 ? NV : 12, N = Piece<L>::N;
     extern __shared__ uint32_t bits[];
     __shared__ LossShared sh;
-    __shared__ float red[3][NT / 64];
+    __shared__ Reduce<NT> red;
     const int tid = threadIdx.x, V = p.V;
     const int held = min(NV, p.pieces / NT), lower = DEEP ? held + p.spill : held;
     u32x4 *more = (u32x4 *)(bits + bitmap_words<L>(V));
@@ -417,7 +417,7 @@ __global__ __launch_bounds__(NT, waves_of(NT, NV, GRAD)) void k_opd_loss(LossPar
         if (scored) {
             // this thread's entry: its logit and, if it is the first listed one of its piece, the piece's others
             float zj = 0.f;
-            PieceSum sum{0.f, 8.f, -1};
+            PieceSum sum{0., 8.f, -1};
             u32x4 shared_piece;
             uint32_t others = 0;
             if (id >= 0) {
@@ -436,9 +436,9 @@ __global__ __launch_bounds__(NT, waves_of(NT, NV, GRAD)) void k_opd_loss(LossPar
                 __builtin_amdgcn_sched_barrier(0);
             }
             if (NV <= STEP && held == 0) each_piece<NT, 1>(row, tid, [&](u32x4 w, int i) { max_piece<L>(m, w, listed_bits<N>(bits, i)); });
-            m = block_max<NT>(m, red[0]);
+            m = block_max<NT>(m, red.max[0]);
             const bool borrowed = !(m * p.c.hi > -kFar);
-            if (borrowed) m = block_max<NT>(id >= 0 ? zj : -INFINITY, red[2]);
+            if (borrowed) m = block_max<NT>(id >= 0 ? zj : -INFINITY, red.max[1]);
             const float B = ref_of(m, p.c);
             off = (tid + NT * AHEAD) * 16;
 #pragma unroll
@@ -455,10 +455,10 @@ __global__ __launch_bounds__(NT, waves_of(NT, NV, GRAD)) void k_opd_loss(LossPar
             whole_pieces<NT, 4, GRAD>(row.body, tid + NT * lower, row.whole, [&](u32x4 w, int i) {
                 sum_piece<L>(sum, w, i / NT, listed_bits<N>(bits, i), B, p.c);
             });
-            float s = sum.s;
+            double s = sum.s;
             if (sum.slab >= 0) s += rounding_of<L>(load_piece(row.body, tid + NT * sum.slab), B, p.c);
             edges<NT>(row, [&](u32x4 w, int i) {
-                PieceSum edge{0.f, 8.f, -1};
+                PieceSum edge{0., 8.f, -1};
                 sum_piece<L>(edge, w, 0, listed_bits<N>(bits, i), B, p.c);
                 s += edge.s;
             });
@@ -468,7 +468,7 @@ __global__ __launch_bounds__(NT, waves_of(NT, NV, GRAD)) void k_opd_loss(LossPar
                     if (others >> e & 1u) s += exp_at(Piece<L>::get(shared_piece, e), B, p.c);
             }
             if (tid < p.k) sh.z[tid] = zj;
-            a = RowSum{m, B, block_sum<NT>(s, red[1])};
+            a = RowSum{m, B, block_sum<NT>(s, red.sum[0])};
             if (!(a.s < INFINITY) || is_far(m, p.c) || (borrowed && (a.s < 1e-30 || m == -INFINITY))) a = sum_slowly<L, NT>(row, bits, p.c, red);
             far = is_far(a.m, p.c);
             if (id >= 0) bits[(id - row.head + N) >> 5] = 0;     // every wave is past its sums: ready for the next position
@@ -534,7 +534,7 @@ template <typename L> __global__ __launch_bounds__(kPartThreads) void k_opd_part
     constexpr int NT = kPartThreads;
     extern __shared__ uint32_t bits[];
     __shared__ LossShared sh;
-    __shared__ float red[3][NT / 64];
+    __shared__ Reduce<NT> red;
     const int t = blockIdx.x / q.S, seg = blockIdx.x % q.S, tid = threadIdx.x;
     const int lo = seg * q.seg, len = min(q.seg, p.V - lo);
     const Position x = read_position(p, t);
@@ -548,10 +548,10 @@ template <typename L> __global__ __launch_bounds__(kPartThreads) void k_opd_part
     mark_entry(id, tq, p.k, p.V, lo, row, sh, bits);
     __syncthreads();
     if (id >= lo && id < lo + len) q.z[(int64_t)t * p.k + tid] = Piece<L>::one(row.body + (id - lo - row.head));
-    MaxSum own{-INFINITY, 0.f};
+    MaxSum<double> own{-INFINITY, 0.};
     each_piece<NT, 4, true>(row, tid, [&](u32x4 w, int i) { add_piece<L>(own, w, i, bits, p.c); });
     RowSum a = block_merge<NT>(own, p.c, red);
-    if (is_far(a.m, p.c)) a.s = sum_far<L, NT>(row, bits, a.m, p.c, red[2]);
+    if (is_far(a.m, p.c)) a.s = sum_far<L, NT>(row, bits, a.m, p.c, red.sum[1]);
     if (tid == 0) q.part[(int64_t)t * q.S + seg] = Part{a.m, a.B, a.s, sh.bad, 0};
 }
 

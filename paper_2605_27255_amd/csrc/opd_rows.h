@@ -179,8 +179,9 @@ __device__ __forceinline__ float exp_diff(float a, float b, ExpScale c) {
 }
 
 // ---- (max, sum of 2^(z c - ref_of(max))) ----------------------------------------------
-struct MaxSum { float m, s; };
-template <int N> __device__ __forceinline__ void add_values(MaxSum &a, const float *v, ExpScale c) {
+// (S: float, or double where the registers allow it)
+template <typename S> struct MaxSum { float m; S s; };
+template <int N, typename S> __device__ __forceinline__ void add_values(MaxSum<S> &a, const float *v, ExpScale c) {
     float m = v[0];
 #pragma unroll
     for (int e = 1; e < N; ++e) m = fmaxf(m, v[e]);
@@ -238,13 +239,13 @@ template <int NT> __device__ __forceinline__ float block_max(float v, float *s_w
     for (int w = 1; w < NT / 64; ++w) v = fmaxf(v, s_w[w]);
     return v;
 }
-template <int NT> __device__ __forceinline__ double block_sum(float v, float *s_w) {
-    v = wave_sum_dpp(v);
+template <int NT> __device__ __forceinline__ double block_sum(double v, double *s_w) {
+    v = wave_sum_f64(v);
     if ((threadIdx.x & 63) == 0) s_w[threadIdx.x >> 6] = v;
     __syncthreads();
     double r = 0.;
 #pragma unroll
-    for (int w = 0; w < NT / 64; ++w) r += (double)s_w[w];
+    for (int w = 0; w < NT / 64; ++w) r += s_w[w];
     return r;
 }
 // A row's unlisted values: their sum in multiples of 2^B (where m is far, of
@@ -255,11 +256,13 @@ __device__ __forceinline__ double log_unit(float m, float B, double at, ExpScale
     return is_far(m, c) ? ((double)m - at) * c.inv : (double)B * kLn2 - at * c.inv;
 }
 
-// The threads' (max, sum) as one: the sum in 64 bits across waves.  s_w: NT / 64 each for the maxima and the sums.
-template <int NT> __device__ __forceinline__ RowSum block_merge(MaxSum a, ExpScale c, float (*s_w)[NT / 64]) {
-    const float m = block_max<NT>(a.m, s_w[0]);
-    const float B = ref_of(m, c), s = a.s * __builtin_amdgcn_exp2f(ref_of(a.m, c) - B);
-    return RowSum{m, B, block_sum<NT>(s, s_w[1])};
+// What a workgroup's maxima and sums of a value per wave pass through.
+template <int NT> struct Reduce { float max[2][NT / 64]; double sum[2][NT / 64]; };
+// The threads' (max, sum) as one.
+template <int NT> __device__ __forceinline__ RowSum block_merge(MaxSum<double> a, ExpScale c, Reduce<NT> &red) {
+    const float m = block_max<NT>(a.m, red.max[0]);
+    const float B = ref_of(m, c);
+    return RowSum{m, B, block_sum<NT>(a.s * __builtin_amdgcn_exp2f(ref_of(a.m, c) - B), red.sum[0])};
 }
 
 // A row's segments as one (max, sum), in every lane.

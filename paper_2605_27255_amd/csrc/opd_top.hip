@@ -57,7 +57,7 @@ template <int NT, int H> struct TopShared {
     uint32_t umax[NT * H];          // each unit's largest value key, 0: no pieces
     uint64_t cand[kTopCand];
     uint64_t sorted[kTopCand];
-    float red[3][NT / 64];
+    Reduce<NT> red;
     uint32_t wmin[NT / 64];
     int count[2][NT / 64], wcount[NT / 64];
     int hist[256];
@@ -145,7 +145,7 @@ __device__ __forceinline__ void put_top(const TopParams<L> &p, int t, const uint
 constexpr double kThin = 1e-25;
 // The sum of a row's values whose keys are below `last`, over a reference of their own.
 template <typename L, int NT>
-__device__ __forceinline__ RowSum sum_below(const Span<const L> &row, uint64_t last, ExpScale c, float (*red)[NT / 64]) {
+__device__ __forceinline__ RowSum sum_below(const Span<const L> &row, uint64_t last, ExpScale c, Reduce<NT> &red) {
     constexpr int N = Piece<L>::N;
     float m = -INFINITY, s = 0.f;
     auto below = [&](float v, int i, int e) { return row.has(i, e) && pair_key(value_key(v), row.head + i * N + e) < last; };
@@ -157,7 +157,7 @@ __device__ __forceinline__ RowSum sum_below(const Span<const L> &row, uint64_t l
         }
     });
     __syncthreads();
-    m = block_max<NT>(m, red[0]);
+    m = block_max<NT>(m, red.max[0]);
     const bool far = is_far(m, c);
     const float B = ref_of(m, c);
     if (m != -INFINITY) {
@@ -169,7 +169,7 @@ __device__ __forceinline__ RowSum sum_below(const Span<const L> &row, uint64_t l
             }
         });
     }
-    return RowSum{m, B, block_sum<NT>(s, red[1])};
+    return RowSum{m, B, block_sum<NT>(s, red.sum[1])};
 }
 
 // One workgroup per row, or (SPLIT) per segment of one.
@@ -185,10 +185,10 @@ __global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
 
     // unit h NT + tid: the pieces tid + NT j for j from h per on, per of them
     const int per = (n + NT * H - 1) / (NT * H);
-    MaxSum unit[H];
+    MaxSum<float> unit[H];
 #pragma unroll
     for (int h = 0; h < H; ++h) {
-        unit[h] = MaxSum{-INFINITY, 0.f};
+        unit[h] = MaxSum<float>{-INFINITY, 0.f};
         const int first = tid + h * per * NT, end = (h + 1) * per * NT;
         auto add = [&](u32x4 w, int) {
             float v[N];
@@ -214,7 +214,7 @@ __global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
     const float least_w = -wave_max_dpp(-least_own);
     if (lane == 0) sh.wmin[wave] = value_key(least_w);
     if (tid == 0) sh.n = 0;
-    const float m = block_max<NT>(most_own, sh.red[0]);     // its barrier: umax, wmin and n are set
+    const float m = block_max<NT>(most_own, sh.red.max[0]);     // its barrier: umax, wmin and n are set
     const bool far = is_far(m, p.c);
     const float B = ref_of(m, p.c);
     auto term = [&](float v) { return far ? exp_diff(v, m, p.c) : exp_at(v, B, p.c); };
@@ -337,7 +337,7 @@ __global__ __launch_bounds__(NT, 8) void k_opd_top(TopParams<L> p) {
     }
     sort_candidates(sh, nc);
     for (int j = k + tid; j < nc; j += NT) rest += term(key_value((uint32_t)(sh.sorted[j] >> 32)));
-    RowSum out{m, B, block_sum<NT>(rest, sh.red[2])};
+    RowSum out{m, B, block_sum<NT>(rest, sh.red.sum[0])};
     if (out.s < kThin) {
         const uint64_t last = sh.sorted[k - 1];     // (below a last one of -inf, or where all are on the list, there is nothing)
         if (k < V && (uint32_t)(last >> 32) > value_key(-INFINITY)) out = sum_below<L, NT>(row, last, p.c, sh.red);
@@ -383,9 +383,9 @@ template <typename L> __global__ __launch_bounds__(kJoinThreads) void k_opd_top_
     // the lists' other keys and the segments' other values, over the largest of them
     const bool other = mine && mine < sh.sorted[k - 1];
     const float v = key_value((uint32_t)(mine >> 32));
-    const float m = fmaxf(block_max<NT>(other ? v : -INFINITY, sh.red[0]), rests.m), B = ref_of(m, p.c);
+    const float m = fmaxf(block_max<NT>(other ? v : -INFINITY, sh.red.max[0]), rests.m), B = ref_of(m, p.c);
     const float term = !other ? 0.f : is_far(m, p.c) ? exp_diff(v, m, p.c) : exp_at(v, B, p.c);
-    RowSum out{m, B, block_sum<NT>(term, sh.red[1])};
+    RowSum out{m, B, block_sum<NT>(term, sh.red.sum[0])};
     const double f = exp(log_unit(rests.m, rests.B, m, p.c) - (is_far(m, p.c) ? 0. : log_unit(m, B, m, p.c)));
     out.s += rests.m == -INFINITY || rests.m == m ? rests.s : rests.s * f;
     if (tid < 64) put_top(p, t, sh.sorted, key_value((uint32_t)(sh.sorted[0] >> 32)), out);
