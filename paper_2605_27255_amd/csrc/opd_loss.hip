@@ -367,8 +367,8 @@ __device__ __forceinline__ RowSum sum_slowly(const Span<const L> &row, const uin
 template <int NT, int NV> constexpr bool kTakesSeveral = NT == 512 && NV >= 12;    // one workgroup fills a compute unit
 template <int NT, int NV> constexpr bool kSpills = NV >= (NT == 512 ? 33 : 44);     // the longest rows' variants
 // Waves of a SIMD that the registers leave room for: short rows live by their number (16384 x 8192 bf16 with the gradient
-// from five 108 us, from six 99).
-constexpr int waves_of(int nt, int nv, bool grad) { return !grad ? 8 : nv <= 2 ? 7 : nv <= 4 ? 6 : nv <= 8 ? 5 : nt / 256; }
+// from five 108 us, from six 99).  Workgroups of sixteen waves have a compute unit to themselves.
+constexpr int waves_of(int nt, int nv, bool grad) { return !grad ? (nt == 1024 ? 4 : 8) : nv <= 2 ? 7 : nv <= 4 ? 6 : nv <= 8 ? 5 : nt / 256; }
 template <typename L, int NT, int NV, int STEP, bool GRAD>
 __global__ __launch_bounds__(NT, waves_of(NT, NV, GRAD)) void k_opd_loss(LossParams<L> p) {
     constexpr bool LOOP = kTakesSeveral<NT, NV>, DEEP = kSpills<NT, NV>;
