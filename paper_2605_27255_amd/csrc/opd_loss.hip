@@ -365,7 +365,7 @@ __device__ __forceinline__ RowSum sum_slowly(const Span<const L> &row, const uin
 // AHEAD slabs before their sum, so that neither loads nor sums wait for all of
 // the other.
 template <int NT, int NV> constexpr bool kTakesSeveral = NT == 512 && NV >= 12;    // one workgroup fills a compute unit
-template <int NT, int NV> constexpr bool kSpills = NV >= (NT == 512 ? 33 : 44);     // the longest rows' variants
+template <int NT, int NV> constexpr bool kSpills = NV >= (NT == 512 ? 32 : 44);     // the longest rows' variants
 // Waves of a SIMD that the registers leave room for: short rows live by their number (16384 x 8192 bf16 with the gradient
 // from five 108 us, from six 99).  Workgroups of sixteen waves have a compute unit to themselves.
 constexpr int waves_of(int nt, int nv, bool grad) { return !grad ? (nt == 1024 ? 4 : 8) : nv <= 2 ? 7 : nv <= 4 ? 6 : nv <= 8 ? 5 : nt / 256; }
@@ -680,7 +680,7 @@ template <typename L> static int launch_loss(LossParams<L> p, void *work, hipStr
     if (n < 256 * 35) return launch_rows<L, 256, 34, 5, true>(p, s);
     if (n < 256 * 40) return launch_rows<L, 256, 39, 5, true>(p, s);
     if (n < 256 * 82) return launch_rows<L, 256, 44, 5, true>(p, s);
-    return launch_rows<L, 512, sizeof(L) == 4 ? 33 : 35, 4, true>(p, s);    // (slabs that fit beside the other values)
+    return launch_rows<L, 512, sizeof(L) == 4 ? 32 : 34, 4, true>(p, s);    // (slabs that fit beside the other values)
 }
 
 // ---- checks ---------------------------------------------------------------------
