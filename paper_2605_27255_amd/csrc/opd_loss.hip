@@ -207,10 +207,12 @@ __device__ __forceinline__ void finish_row(const LossParams<L> &p, int t, const 
             a_rest = readlane_f64(a_rest, p.k & 63);
             if (!(lse == lse)) f = lse;
             if (lane == 0 && first) p.loss[t] = (float)f;
-            for (int j = lane; j < p.k; j += 64)
-                if (sh.id[j] >= 0) sh.patch[j] = (float)(g * (sh.a[j] - sh.p[j] * A));
+            if (p.grad) {
+                for (int j = lane; j < p.k; j += 64)
+                    if (sh.id[j] >= 0) sh.patch[j] = (float)(g * (sh.a[j] - sh.p[j] * A));
+            }
         }
-        if (lane == 0) {
+        if (lane == 0 && p.grad) {
             const double unit_p = rest_at * exp(-lse);      // the probability of one of the rest's units
             if (p.kind == kPolicy) sh.patch[0] = (float)(g * A * (rest.s * unit_p));    // (1 - p of the label without cancellation)
             // with no mass outside the list there is nothing to spread there

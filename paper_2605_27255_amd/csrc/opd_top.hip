@@ -380,15 +380,19 @@ template <typename L> __global__ __launch_bounds__(kJoinThreads) void k_opd_top_
     if (mine && (uint32_t)(mine >> 32) >= bound) sh.cand[atomicAdd(&sh.n, 1)] = mine;
     __syncthreads();
     sort_candidates(sh, sh.n);
-    // the lists' other keys and the segments' other values, over the largest of them
+    // the lists' other keys and the segments' other values, over the row's largest value, or where that is thin over their own
+    const float top = key_value((uint32_t)(sh.sorted[0] >> 32)), v = key_value((uint32_t)(mine >> 32));
     const bool other = mine && mine < sh.sorted[k - 1];
-    const float v = key_value((uint32_t)(mine >> 32));
-    const float m = fmaxf(block_max<NT>(other ? v : -INFINITY, sh.red.max[0]), rests.m), B = ref_of(m, p.c);
-    const float term = !other ? 0.f : is_far(m, p.c) ? exp_diff(v, m, p.c) : exp_at(v, B, p.c);
-    RowSum out{m, B, block_sum<NT>(term, sh.red.sum[0])};
-    const double f = exp(log_unit(rests.m, rests.B, m, p.c) - (is_far(m, p.c) ? 0. : log_unit(m, B, m, p.c)));
-    out.s += rests.m == -INFINITY || rests.m == m ? rests.s : rests.s * f;
-    if (tid < 64) put_top(p, t, sh.sorted, key_value((uint32_t)(sh.sorted[0] >> 32)), out);
+    auto sum_over = [&](float m, double *s_w) {
+        const bool far = is_far(m, p.c);
+        const float B = ref_of(m, p.c), term = !other ? 0.f : far ? exp_diff(v, m, p.c) : exp_at(v, B, p.c);
+        double f = 1.;      // the segments' unit over this one: as a rule the same
+        if (rests.m != m && rests.m != -INFINITY) f = exp(log_unit(rests.m, rests.B, m, p.c) - (far ? 0. : log_unit(m, B, m, p.c)));
+        return RowSum{m, B, block_sum<NT>(term, s_w) + rests.s * f};
+    };
+    RowSum out = sum_over(top, sh.red.sum[0]);
+    if (out.s < kThin) out = sum_over(fmaxf(block_max<NT>(other ? v : -INFINITY, sh.red.max[0]), rests.m), sh.red.sum[1]);
+    if (tid < 64) put_top(p, t, sh.sorted, top, out);
 }
 
 // Segments of each row: about two workgroups a compute unit in all, at least
