@@ -245,7 +245,7 @@ int pipo_opd_targets_bf16(int32_t T, int32_t V, const uint16_t *d_logits_s, cons
  * beyond their element's), V from 1 to 524288.  x = z / temperature (1e-5 to
  * 1e5), p = softmax(x).  All sums are fp32 or wider, the arithmetic on single
  * entries is fp64.  T = 0 is allowed (the arrays may then be NULL).  Logits may
- * be -inf or the type's lowest value (masked tokens); a row without any token
+ * be finite of any magnitude, or -inf (masked tokens); a row without any token
  * of positive probability, or with a NaN or +inf, gives NaN results (ids
  * stay in range).  Outputs must not overlap inputs or each other, except that
  * a gradient may be written over the logits themselves (same address and ld).
@@ -285,8 +285,10 @@ int pipo_opd_targets_bf16(int32_t T, int32_t V, const uint16_t *d_logits_s, cons
  *   loss = -min(A rho, A clip(rho, 1 - clip_low, 1 + clip_high)) + kl_coef * kl
  *   kl   = exp(u) - u - 1,  u = d_ref_logp[t] - logp
  * with 0 <= clip_low <= 1, clip_high >= 0.  Without d_ref_logp kl_coef must be
- * 0 and d_kl NULL.  d_logp and d_kl ([T]) may be NULL.  Positions with y < 0
- * are not scored (all outputs 0), y >= V gets NaN.
+ * 0 and d_kl NULL.  d_logp and d_kl ([T]) may be NULL.  A label of probability 0
+ * has logp -inf, rho 0 (without d_old_logp 1, as everywhere) and, where its
+ * d_ref_logp is finite, kl +inf.  Positions with y < 0 are not scored (all outputs
+ * 0), y >= V gets NaN.
  *
  * Both losses: d_loss [T]; with d_grad non-NULL its row t (stride ld_grad >= V,
  * the logits' type) = d_scale[t] (NULL: 1) times the gradient of loss t with

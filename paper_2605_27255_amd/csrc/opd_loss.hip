@@ -14,8 +14,9 @@
 // second pass, from registers and LDS as far as the row fits, writes the
 // gradient, and the listed entries are written over it.
 // HBM-bound: V logits read, V gradients written.  2048 x 151936 with the
-// gradient: bf16 248 us, 5.0 TB/s (a copy of as many bytes: 236 us), fp32 485 us,
-// 5.1 TB/s; without it bf16 100 us, 6.2 TB/s, fp32 190 us, 6.5 TB/s.
+// gradient, a tenth of the positions not scored and only written: bf16 248 us, 4.8
+// TB/s (a copy of as many bytes: 224 us), fp32 488 us, 4.8 TB/s (478 us); without
+// the gradient bf16 99 us, 6.3 TB/s, fp32 184 us, 6.8 TB/s.
 //
 // Where there are too few rows for the chip, each is split over several
 // workgroups: k_opd_part sums a segment and gathers the listed logits,
@@ -599,9 +600,9 @@ __global__ __launch_bounds__(kPartThreads) void k_opd_apply(LossParams<L> p, Spl
 // Segments of each row: about two workgroups a compute unit in all, at least
 // 4096 elements each.  The second launch takes 4 us of the host's time, so a row
 // is split only where one workgroup would take longer than that over it: with
-// the gradient (bf16, us for split / whole) 8 x 65536 15.5 / 13.5, 8 x 151936
-// 15.6 / 20, 64 x 151936 16 / 22, 128 x 151936 27 / 25; without it 8 x 151936
-// bf16 14.5 / 12.6.
+// the gradient (bf16, us for split / whole) 8 x 65536 16.8 / 14.7, 8 x 151936
+// 17.2 / 28.2, 64 x 151936 17.9 / 30.1, 128 x 151936 29.9 / 30.3; without it 8 x
+// 151936 bf16 15.1 / 15.9, fp32 15.0 / 17.7.
 static void split_of(int T, int V, int es, bool grad, int &S, int &seg) {
     S = 512 / (T > 0 ? T : 1);
     if (S > kMaxParts) S = kMaxParts;
@@ -668,8 +669,8 @@ template <typename L> static int launch_loss(LossParams<L> p, void *work, hipStr
     // Workgroups of four waves, as many to a compute unit as their registers allow (two with 44 slabs): while one sums
     // or finishes a row, others load and write.  Only rows of which two leave most to be read again go to one workgroup
     // of eight waves a compute unit, which holds twice as much.  With the gradient, two of four waves / one of eight,
-    // logits from memory, in us: bf16 2048 x 151936 255 / 256, 2048 x 168000 283 / 283, 1187 x 262144 287 / 275; fp32
-    // 1944 x 80000 254 / 253, 2048 x 100000 336 / 322, 2048 x 151936 538 / 519: the same up to some 80 slabs.
+    // logits from memory, in us: bf16 2048 x 151936 248 / 253, 2048 x 168000 279 / 281, 1187 x 262144 272 / 263; fp32
+    // 1944 x 80000 247 / 248, 2048 x 100000 327 / 312, 2048 x 151936 525 / 512: the same up to some 80 slabs.
     if (n < 256 * 3) return launch_rows<L, 256, 2, 2, true>(p, s);
     if (n < 256 * 5) return launch_rows<L, 256, 4, 2, true>(p, s);
     if (n < 256 * 7) return launch_rows<L, 256, 6, 2, true>(p, s);

@@ -398,8 +398,8 @@ template <typename L> __global__ __launch_bounds__(kJoinThreads) void k_opd_top_
 // Segments of each row: about two workgroups a compute unit in all, at least
 // 4096 elements each, and no more keys than the joining workgroup has threads.
 // Two launches pay for few long rows (bf16, top 20, us for split / whole): 8 x
-// 65536 15.1 / 11.6, 8 x 151936 15.1 / 17.4, 64 x 151936 18 / 22, 128 x 151936
-// 23 / 22.
+// 65536 16.7 / 13.0, 8 x 151936 17.0 / 21.1, 64 x 151936 19.8 / 23.0, 128 x
+// 151936 24.1 / 23.7.
 static void top_split(int T, int V, int k, int es, int &S, int &seg) {
     S = 512 / T;
     if (S > kMaxParts) S = kMaxParts;
