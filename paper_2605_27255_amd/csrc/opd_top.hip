@@ -129,17 +129,18 @@ template <int NT, int H> __device__ __forceinline__ void sort_candidates(TopShar
 template <typename L>
 __device__ __forceinline__ void put_top(const TopParams<L> &p, int t, const uint64_t *sorted, float m, RowSum out) {
     const int lane = threadIdx.x;
+    const bool none = out.m == -INFINITY;
+    const double unit = none ? 0. : log_unit(out.m, out.B, m, p.c), mass = out.s * exp(unit);
     double sum = 0.;
     for (int j = lane; j < p.k; j += 64)
         sum += exp(((double)key_value((uint32_t)(sorted[j] >> 32)) - (double)m) * p.c.inv);
-    const double unit = log_unit(out.m, out.B, m, p.c);
-    const double lse = log(wave_sum_f64(sum) + (out.m == -INFINITY ? out.s : out.s * exp(unit)));   // of x - m / temperature
+    const double lse = log(wave_sum_f64(sum) + mass);   // of x - m / temperature
     for (int j = lane; j < p.k; j += 64) {
         const uint64_t key = sorted[j];
         p.ids[(int64_t)t * p.k + j] = key_id(key);
         p.logp[(int64_t)t * p.k + j] = (float)(((double)key_value((uint32_t)(key >> 32)) - (double)m) * p.c.inv - lse);
     }
-    if (lane == 0 && p.tail) p.tail[t] = (float)(!(lse == lse) ? lse : out.s == 0. ? -INFINITY : unit + log(out.s) - lse);
+    if (lane == 0 && p.tail) p.tail[t] = (float)(log(out.s) + unit - lse);
 }
 // A sum of exponentials under this share of its reference may have lost some that no float holds (2^-126, of 2^19 at most).
 constexpr double kThin = 1e-25;
