@@ -8,6 +8,7 @@ from __future__ import annotations
 import concurrent.futures as cf
 import glob
 import os
+import re
 import subprocess
 import sys
 
@@ -27,7 +28,14 @@ FLAGS = [
 
 # k_opd_loss keeps a row of logits in registers across a loop: the constants of
 # its few 64-bit exponentials must not be hoisted in front of it (47 registers spilled).
-FILE_FLAGS = {"opd_loss.hip": ["-mllvm", "-disable-machine-licm"]}
+# The compiler reports what its kernels use, and a build in which they spill again says so.
+FILE_FLAGS = {"opd_loss.hip": ["-mllvm", "-disable-machine-licm", "-Rpass-analysis=kernel-resource-usage"]}
+SPILL_LIMIT = 64        # bytes a thread (the longest bf16 rows' kernel: 20)
+
+
+def spilled(remarks: str) -> int:
+    """The most scratch bytes a thread that the compiler reports for a kernel."""
+    return max((int(n) for n in re.findall(r"ScratchSize \[bytes/lane\]: (\d+)", remarks)), default=0)
 
 
 def _compile(src: str) -> str:
@@ -36,6 +44,8 @@ def _compile(src: str) -> str:
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"hipcc failed for {src}:\n{r.stdout}\n{r.stderr}")
+    if spilled(r.stderr) > SPILL_LIMIT:
+        print(f"{os.path.basename(src)}: a kernel spills {spilled(r.stderr)} bytes a thread; it will be slow", file=sys.stderr)
     return obj
 
 

@@ -186,3 +186,10 @@ def test_empty_calls_with_empty_lists(lib):
         assert _distill(lib, dt, Tt=-1, **nothing) == PIPO_EINVAL
         assert _distill(lib, dt, Tt=0, k=0, **nothing) == PIPO_EINVAL
         assert _distill(lib, dt, Tt=0) == PIPO_EINVAL
+
+
+def test_build_reads_the_compilers_report_of_spills():
+    from paper_2605_27255_amd import build
+    report = ("a.hip:1:1: remark:     ScratchSize [bytes/lane]: 0 [-Rpass-analysis=kernel-resource-usage]\n"
+              "a.hip:9:1: remark:     ScratchSize [bytes/lane]: 188 [-Rpass-analysis=kernel-resource-usage]\n")
+    assert build.spilled(report) == 188 > build.SPILL_LIMIT and build.spilled("") == 0
