@@ -1096,3 +1096,55 @@ def test_split_streams_and_graphs(torch):
         want = step() + policy()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs[0] + outs[1], want)), i
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("level", [0.0, -2907280.0, -2907200.0, -1e9])
+@pytest.mark.parametrize("mask", [-float("inf"), -3e38])
+@pytest.mark.parametrize("T,V", [(100, 40001), (3, 3001), (3, 110001)])
+def test_rows_whose_beginning_and_list_are_masked(torch, T, V, mask, level, dtype):
+    """No reference for the sum at the row's beginning nor on its list, and
+    tokens at any level behind them (exponents on both sides of 2^22)."""
+    d, _ = _rows(torch, 3, V, "float32", seed=V, pad=-V % 8)
+    d += level
+    d = d.to(getattr(torch, dtype))
+    listed = torch.arange(0, 90, 10).int().cuda().repeat(3, 1)
+    d[:, : V - 300] = mask
+    z = d.double().cpu().numpy()
+    logp, tail = torch.full((3, 9), -4.0).cuda(), torch.full((3,), -0.2).cuda()
+    many = lambda a: a.repeat((T + 2) // 3, *[1] * (a.dim() - 1))[:T]  # noqa: E731
+    zz = np.tile(z, ((T + 2) // 3, 1))[:T]
+    for kind in ("reverse", "jsd"):
+        for grad in (True, None):
+            loss, g = _check_distill(torch, many(d), zz, many(listed), many(logp), many(tail), kind=kind, grad=grad)
+            assert loss.isfinite().all()
+    y = torch.tensor([V - 1, V - 300, V - 7], dtype=torch.int32).cuda()
+    loss, _, _, g = _check_policy(torch, many(d), zz, many(y), torch.linspace(0.5, 1.5, T).cuda())
+    assert loss.isfinite().all() and g.isfinite().all()
+
+
+def test_split_calls_on_two_streams_at_once(torch):
+    """Calls that overlap on two streams work in arrays of their own."""
+    from paper_2605_27255_amd import opd_distill, opd_policy, opd_top_logits
+    T, V = 8, 151936
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    sets = []
+    for _ in range(2):
+        z = 3 * torch.randn((T, V), generator=gen, device="cuda")
+        sets.append((z, torch.randint(0, V, (T,), generator=gen, device="cuda").int(), torch.randn(T, generator=gen, device="cuda")))
+
+    def chain(z, y, adv):
+        ids, logp, tail = opd_top_logits(z, 20)
+        return (ids, logp, tail) + opd_distill(z, ids, logp, tail, kind="jsd", grad=True) + opd_policy(z, y, adv, grad=True)[:2]
+
+    want = [[t.clone() for t in chain(*s)] for s in sets]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in sets], [[], []]
+    for _ in range(10):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[i].append(chain(*sets[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for outs in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(outs, want[i]))
