@@ -326,6 +326,117 @@ int pipo_opd_policy_bf16(int32_t T, int32_t V, const uint16_t *d_logits, int64_t
                          float *d_logp, float *d_kl, uint16_t *d_grad, int64_t ld_grad, void *d_work,
                          int64_t work_bytes, void *stream);
 
+/* ---- Serving operators: drafted tokens verified over a paged 8-bit cache (no context needed) ----
+ * What a target model's step needs around its matrices when drafts are verified
+ * without loss (the comparison systems of Sec. 4.3; the acceptance probability
+ * min(p_t/p_s, 1) is App. C's): blocks and slots for the step's tokens, keys and
+ * values into the cache, attention over it, and the drafts accepted or replaced.
+ *
+ * The cache is `blocks` blocks of `block` tokens (32, 64, 128 or 256), each of
+ * n_kv heads (1 to 256) x head_dim (64 or 128).  A byte u stands for (u - 128) s, with one
+ * scale s for each block, head, and keys (scales[0]) or values (scales[1]).
+ * Token t, dimension e of a block's keys and values lie at byte
+ *   keys    ((t/16 * head_dim/64 + e/64) * 64 + 16 (e%64/16) + t%16) * 16 + e%16
+ *   values  ((t/32 * head_dim/32 + e/32) * 64 + 16 (t%16/4) + e%16) * 16
+ *           + 8 (e%32/16) + 4 (t%32/16) + t%4
+ * of its block and head.  Slot number i is token i % block of block i / block;
+ * blocks * block < 2^31.  A request's block table (a row of d_tables) holds the blocks of its
+ * tokens in order.  A block belongs to one request.
+ * All sizes are host values, lengths and tables are read on the device: a call
+ * can be captured and replayed with other contents.  Entries that a kernel finds
+ * out of range there (a block or slot that the cache does not have, a length
+ * beyond the table) are left out, never followed.  Work arrays and errors as for
+ * the OPD losses.
+ *
+ * pipo_kv8_plan: the blocks and slots of a step that adds d_new[r] tokens to the
+ * d_lens[r] that request r (of R, 1 to 2^20) has.  d_free is a stack of d_n_free[0] free blocks
+ * (room for `blocks`), d_held[r] how many blocks row r of d_tables ([R][width])
+ * holds.  First the blocks of requests that ended (d_new[r] < 0) go back, the
+ * first of them on top, and their rows become -1.  Then, request by request, those
+ * who need blocks for d_lens[r] + d_new[r] tokens take them from the top; from
+ * the first that does not find enough on, none that needs any gets some.  Blocks
+ * that a request holds beyond its need (drafts were rejected) stay with it.
+ * d_starts [R+1] counts the new tokens before each request (cut off at `rows`, up to 2^20),
+ * d_total [R] = d_lens + d_new, 0 for a request that ended, has a negative
+ * length, more tokens than its table's width holds or than d_slots has room for,
+ * or found no blocks (whose d_held and table stay as they were).  d_slots and d_positions [rows]: slot and position of each new
+ * token, -1 for tokens of a request with total 0 and behind the last one.
+ *
+ * pipo_kv8_append: rows i of d_k and d_v ([n_kv][head_dim] each, fp32 or bf16, row
+ * stride ld elements) into slot d_slots[i] (negative: not at all; of rows with one slot
+ * the last counts).  Rows of one block have to be consecutive.  A block whose first slot
+ * is written begins anew with s = max|x| / 127 of its written rows; else s only grows,
+ * to the larger of it and that.  u = 128 + x / s rounded to nearest even; where s
+ * grows, what the block holds besides is rounded to the new s.  A scale below 2^-126
+ * is 0; NaN and infinities make it NaN, and with it every value of the block and
+ * head, until the block begins anew.
+ *
+ * pipo_kv8_read: the values of the slots d_slots[i] as rows i of d_k and d_v
+ * ([rows][n_kv][head_dim], fp32 or bf16); zeros where there is no such slot.
+ *
+ * pipo_kv8_attention: rows d_starts[r] .. d_starts[r+1]-1 of d_q ([n_q][head_dim], row stride
+ * ld_q; n_q / n_kv whole, up to 16) are the last tokens of request r's d_total[r]: row i sees the
+ * keys up to its own position d_total[r] - d_starts[r+1] + i, query head h those
+ * of KV head h * n_kv / n_q.  d_out row i = sum softmax(scale q.k) v, rounded once
+ * to the type of q; zeros for a row that sees no key; rows outside
+ * [d_starts[0], d_starts[R]) are not written.  No request may have more than max_len tokens (up to
+ * width * block; what is behind max_len is not seen).  d_work as for the OPD losses
+ * (pipo_kv8_attention_work_bytes); with NULL each row's keys are not split over
+ * workgroups, which is slower for few long requests.
+ *
+ * pipo_verify_drafts: request r (of R) has up to K drafted tokens d_drafts[r] ([R][K],
+ * the first negative one ends them) and the target's logits of the positions that
+ * they and the token behind them stand at: rows d_starts[r] .. d_starts[r+1]-1
+ * of the `rows` of d_logits (NULL: r (K+1) .. r (K+1) + K), fp32 or bf16, row
+ * stride ld.  d_draft_logits: the logits that draft i was drawn from, at (r ld_request + i ld_draft)
+ * elements; NULL: drafts were not drawn (probability 1).  With p, q =
+ * softmax(logits / temperature) and random numbers d_u [R][K+1] in [0, 1):
+ * draft i is accepted while d_u[r][i] q_i < p_i; the token behind the accepted
+ * ones is the first, by id, at which the running sum of max(p - q, 0) (of p, where all
+ * drafts were accepted or where p is nowhere above q) exceeds d_u[r][K] of
+ * its total.  Every token is then distributed as p alone would draw it.
+ * temperature <= 0: a draft is accepted where it is the target's largest logit (equal
+ * ones: the lowest id), and the token behind is that.  d_tokens [R][K+1]: the
+ * accepted drafts, the token behind them, then -1; d_accepted [R] their number.
+ * A row with a NaN or +inf, or without any token of positive probability, accepts no draft, and gives
+ * the token -1; a request without rows has 0 and only -1.  A draft without a row of its own and one behind it is not looked at.
+ * R up to 65535, K from 0 to 63, V and ld as for the OPD losses. */
+typedef struct {
+    uint8_t *keys, *values;         /* device [blocks][n_kv][block * head_dim], 16-byte aligned */
+    float *scales;                  /* device [blocks][n_kv][2], 8-byte aligned                 */
+    int32_t blocks, n_kv, head_dim, block;
+} pipo_kv8;
+
+int pipo_kv8_plan(int32_t R, int32_t width, int32_t block, int32_t blocks, const int32_t *d_lens, const int32_t *d_new,
+                  int32_t *d_tables, int32_t *d_held, int32_t *d_free, int32_t *d_n_free, int32_t rows,
+                  int32_t *d_starts, int32_t *d_total, int32_t *d_slots, int32_t *d_positions, void *stream);
+int pipo_kv8_append(const pipo_kv8 *cache, int32_t rows, const float *d_k, int64_t ld_k, const float *d_v,
+                    int64_t ld_v, const int32_t *d_slots, void *stream);
+int pipo_kv8_append_bf16(const pipo_kv8 *cache, int32_t rows, const uint16_t *d_k, int64_t ld_k, const uint16_t *d_v,
+                         int64_t ld_v, const int32_t *d_slots, void *stream);
+int pipo_kv8_read(const pipo_kv8 *cache, int32_t rows, const int32_t *d_slots, float *d_k, float *d_v, void *stream);
+int pipo_kv8_read_bf16(const pipo_kv8 *cache, int32_t rows, const int32_t *d_slots, uint16_t *d_k, uint16_t *d_v,
+                       void *stream);
+int64_t pipo_kv8_attention_work_bytes(const pipo_kv8 *cache, int32_t R, int32_t rows, int32_t n_q, int32_t max_len,
+                                      int32_t bf16);
+int pipo_kv8_attention(const pipo_kv8 *cache, int32_t R, int32_t rows, int32_t n_q, const float *d_q, int64_t ld_q,
+                       const int32_t *d_tables, int32_t width, const int32_t *d_starts, const int32_t *d_total,
+                       int32_t max_len, double scale, float *d_out, int64_t ld_out, void *d_work, int64_t work_bytes,
+                       void *stream);
+int pipo_kv8_attention_bf16(const pipo_kv8 *cache, int32_t R, int32_t rows, int32_t n_q, const uint16_t *d_q,
+                            int64_t ld_q, const int32_t *d_tables, int32_t width, const int32_t *d_starts,
+                            const int32_t *d_total, int32_t max_len, double scale, uint16_t *d_out, int64_t ld_out,
+                            void *d_work, int64_t work_bytes, void *stream);
+int64_t pipo_verify_work_bytes(int32_t R, int32_t K, int32_t V);
+int pipo_verify_drafts(int32_t R, int32_t K, int32_t V, int32_t rows, const float *d_logits, int64_t ld,
+                       const int32_t *d_starts, const int32_t *d_drafts, const float *d_draft_logits,
+                       int64_t ld_request, int64_t ld_draft, const float *d_u, double temperature, int32_t *d_tokens,
+                       int32_t *d_accepted, void *d_work, int64_t work_bytes, void *stream);
+int pipo_verify_drafts_bf16(int32_t R, int32_t K, int32_t V, int32_t rows, const uint16_t *d_logits, int64_t ld,
+                            const int32_t *d_starts, const int32_t *d_drafts, const uint16_t *d_draft_logits,
+                            int64_t ld_request, int64_t ld_draft, const float *d_u, double temperature,
+                            int32_t *d_tokens, int32_t *d_accepted, void *d_work, int64_t work_bytes, void *stream);
+
 /* Release a context made by pipo_init_weights and all its device memory.
  * NULL is a no-op (returns 0). */
 int pipo_free(pipo_ctx *ctx);

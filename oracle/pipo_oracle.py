@@ -775,3 +775,191 @@ class RegularOracle:
             self.step_idx[i] += 1
             self.next_tok[i] = rec["tok"]
         return out
+
+
+# ---- drafted tokens verified over a paged 8-bit cache ----------------------------------------
+
+def kv8_place(block, D, values):
+    """Byte of token t, dimension e in a block and head's tiles: an index array [block, D]."""
+    t, e = np.arange(block)[:, None], np.arange(D)[None, :]
+    if not values:
+        return ((t // 16 * (D // 64) + e // 64) * 64 + 16 * (e % 64 // 16) + t % 16) * 16 + e % 16
+    return (((t // 32 * (D // 32) + e // 32) * 64 + 16 * (t % 16 // 4) + e % 16) * 16 + 8 * (e % 32 // 16)
+            + 4 * (t % 32 // 16) + t % 4)
+
+
+class Kv8Oracle:
+    """The cache as codes [2, blocks, n_kv, block, D] (keys, values; uint8) and scales [blocks, n_kv, 2] (float32)."""
+
+    def __init__(self, codes, scales):
+        self.codes, self.scales = codes, scales
+        _, self.blocks, self.n_kv, self.block, self.D = codes.shape
+
+    def append(self, k, v, slots):
+        slots = np.asarray(slots)
+        blk = np.where((slots >= 0) & (slots < self.blocks * self.block), slots // self.block, -1)
+        i = 0
+        while i < len(slots):
+            j = i + 1
+            while j < len(slots) and blk[j] == blk[i]:
+                j += 1
+            if blk[i] >= 0:
+                row = {int(slots[n]) % self.block: n for n in range(i, j)}       # the last row of a slot counts
+                for w, x in enumerate((k, v)):
+                    self._into(w, int(blk[i]), sorted(row), x[[row[o] for o in sorted(row)]])
+            i = j
+
+    def _into(self, w, b, offs, x):
+        for h in range(self.n_kv):
+            top = np.float32(np.abs(x[:, h]).max()) if np.isfinite(x[:, h]).all() else np.float32(np.nan)
+            old = np.float32(0) if offs[0] == 0 else self.scales[b, h, w]
+            s = np.maximum(old, np.float32(top / np.float32(127)))               # (a NaN stays one)
+            if s < 2.0 ** -126:
+                s = np.float32(0)
+            c = self.codes[w, b, h]
+            if offs[0] != 0 and not s == old:
+                rest = [o for o in range(self.block) if o not in set(offs)]
+                c[rest] = 128 + _kv8_round((c[rest].astype(np.float64) - 128) * float(old), s)
+            c[offs] = 128 + _kv8_round(x[:, h].astype(np.float64), s)
+            self.scales[b, h, w] = s
+
+    def rows(self, w, slots):
+        """The values of these slots in float64 [n, n_kv, D]; zeros where there is no such slot."""
+        slots = np.asarray(slots)
+        ok = (slots >= 0) & (slots < self.blocks * self.block)
+        b, t = np.where(ok, slots // self.block, 0), np.where(ok, slots % self.block, 0)
+        x = (self.codes[w, b, :, t].astype(np.float64) - 128) * self.scales[b, :, w].astype(np.float64)[:, :, None]
+        return np.where(ok[:, None, None], x, 0.0)
+
+
+def _kv8_round(x, s):
+    if not s > 0:                       # 0 or NaN
+        return np.zeros(x.shape, dtype=np.uint8)
+    return np.clip(np.rint(x / float(s)), -127, 127).astype(np.int64).astype(np.uint8)
+
+
+def kv8_plan(lens, new, tables, held, free, n_free, rows, block):
+    """One request after the other; returns the new (tables, held, free stack, starts, total, slots, positions)."""
+    tables, held, stack = np.array(tables), np.array(held), list(free[:n_free])
+    R, W = tables.shape
+    back = [b for r in range(R) if new[r] < 0 for b in tables[r, :held[r]]]
+    stack += back[::-1]                 # the first of them on top
+    starts, total, short = [0], [], False
+    slots, positions = np.full(rows, -1), np.full(rows, -1)
+    over = 0
+    for r in range(R):
+        n = max(int(new[r]), 0)
+        if new[r] < 0:
+            tables[r, :held[r]], held[r] = -1, 0
+            total.append(0)
+            starts.append(min(over, rows))
+            continue
+        want = -(-(int(lens[r]) + n) // block)
+        ok = lens[r] >= 0 and want <= W
+        need = max(want - int(held[r]), 0) if ok else 0
+        if need > 0 and (short or need > len(stack)):
+            ok, short = False, True
+        at, over = over, over + n
+        if over > rows:
+            ok, short = False, short or need > 0
+        if ok:
+            for i in range(need):
+                tables[r, held[r] + i] = stack.pop()
+            held[r] += need
+            for i in range(n):
+                pos = int(lens[r]) + i
+                slots[at + i], positions[at + i] = tables[r, pos // block] * block + pos % block, pos
+        total.append(int(lens[r]) + n if ok else 0)
+        starts.append(min(over, rows))
+    return tables, held, stack, np.array(starts), np.array(total), slots, positions
+
+
+def kv8_attention(q, cache, tables, starts, total, scale=None, max_len=None):
+    """float64 [rows, n_q, D] and, for tolerances, of each row and head the largest sum |q k| scale and |v| that it sees."""
+    rows, n_q, D = q.shape
+    G, B, W = n_q // cache.n_kv, cache.block, tables.shape[1]
+    scale, most = D ** -0.5 if scale is None else scale, W * B if max_len is None else max_len
+    out, size, top = np.zeros((rows, n_q, D)), np.zeros((rows, n_q)), np.zeros((rows, n_q))
+    for r in range(len(total)):
+        n = starts[r + 1] - starts[r]
+        L = min(max(int(total[r]), 0), most)
+        pos = np.arange(L)
+        blk = tables[r, pos // B]
+        here = (blk >= 0) & (blk < cache.blocks)
+        slots = np.where(here, blk * B + pos % B, -1)
+        k, v = cache.rows(0, slots), cache.rows(1, slots)
+        for i in range(n):
+            sees = here & (pos < total[r] - n + i + 1)
+            if not sees.any():
+                continue
+            for h in range(n_q):
+                kk, vv, x = k[sees, h // G], v[sees, h // G], q[starts[r] + i, h].astype(np.float64)
+                s = kk @ x * scale
+                p = np.exp(s - s.max())
+                out[starts[r] + i, h] = p @ vv / p.sum()
+                size[starts[r] + i, h] = (np.abs(kk) @ np.abs(x)).max() * abs(scale)
+                top[starts[r] + i, h] = np.abs(vv).max()
+    return out, size, top
+
+
+def verify_drafts(logits, drafts, u, draft_logits=None, starts=None, temperature=1.0):
+    """(tokens, accepted, margin): margin [R], how near the nearest decision was to going the other way (in units of
+    probability for accepted drafts, of the drawn total for the token behind)."""
+    R, K = drafts.shape
+    tokens, accepted, margin = np.full((R, K + 1), -1), np.zeros(R, dtype=int), np.full(R, np.inf)
+    for r in range(R):
+        first, end = (r * (K + 1), (r + 1) * (K + 1)) if starts is None else (starts[r], starts[r + 1])
+        n = min(end - first - 1, K)
+        if n < 0:
+            continue
+        ends = np.flatnonzero(drafts[r, :n] < 0)
+        n = int(ends[0]) if len(ends) else n
+        dist = lambda row: _verify_softmax(row, temperature)  # noqa: E731
+        j, q = 0, None
+        while j < n:
+            p, y, q = dist(logits[first + j]), drafts[r, j], None
+            if temperature <= 0:
+                if p is None or y != np.argmax(logits[first + j]):
+                    break
+            else:
+                q = dist(draft_logits[r, j]) if draft_logits is not None else np.ones(len(logits[0]))
+                if p is None or q is None or y >= len(p):
+                    break
+                if p[y] > 0 or q[y] > 0:        # (0 < 0 is no close decision)
+                    margin[r] = min(margin[r], abs(u[r, j] * q[y] - p[y]))
+                if not u[r, j] * q[y] < p[y]:
+                    break
+            j += 1
+        accepted[r] = j
+        tokens[r, :j] = drafts[r, :j]
+        p = dist(logits[first + j])
+        if p is None or (j < n and draft_logits is not None and temperature > 0 and dist(draft_logits[r, j]) is None):
+            continue
+        if temperature <= 0:
+            tokens[r, j] = int(np.argmax(logits[first + j]))
+            continue
+        mass = p
+        if j < n:
+            if draft_logits is not None:
+                mass = np.maximum(p - dist(draft_logits[r, j]), 0)
+            elif drafts[r, j] < len(p):
+                mass = p.copy()
+                mass[drafts[r, j]] = 0
+            if not mass.sum() > 0:
+                mass = p
+        cum = np.cumsum(mass)
+        over = np.flatnonzero((cum > u[r, K] * cum[-1]) & (mass > 0))
+        at = int(over[0]) if len(over) else int(np.flatnonzero(mass)[-1])
+        tokens[r, j] = at
+        margin[r] = min(margin[r], min(abs(cum[at] - u[r, K] * cum[-1]), abs(cum[at] - mass[at] - u[r, K] * cum[-1])) / cum[-1])
+    return tokens, accepted, margin
+
+
+def _verify_softmax(row, temperature):
+    """None for a row with a NaN or +inf, or without any token."""
+    x = np.asarray(row, dtype=np.float64)
+    if np.isnan(x).any() or np.isposinf(x).any() or not (x > -np.inf).any():
+        return None
+    x = x / (temperature if temperature > 0 else 1.0)
+    e = np.exp(x - x.max())
+    return e / e.sum()

@@ -1,0 +1,456 @@
+// The paged 8-bit cache: blocks and slots of a step's tokens, keys and values into
+// the cache, and back.
+#include "kv8.h"
+
+namespace pipo {
+
+bool kv8_ok(const pipo_kv8 *c) {
+    return c && kv8_aligned(c->keys, 16) && kv8_aligned(c->values, 16) && kv8_aligned(c->scales, 8) && c->blocks >= 1 &&
+           c->n_kv >= 1 && c->n_kv <= 256 && (c->head_dim == 64 || c->head_dim == 128) &&
+           (c->block == 32 || c->block == 64 || c->block == 128 || c->block == 256) &&
+           (int64_t)c->blocks * c->block < (int64_t)1 << 31;
+}
+
+// ---- blocks and slots --------------------------------------------------------------
+struct PlanParams {
+    int R, W, block, blocks;
+    const int32_t *lens, *add;
+    int32_t *tables, *held, *stack, *n_free;
+    int rows;
+    int32_t *starts, *total, *slots, *positions;
+    int fill;                       // the rows are written by the planning workgroup itself
+};
+
+// Exclusive sums of a and b over the workgroup's threads; A and B get the totals.
+template <int NT> __device__ __forceinline__ void scan2(int &a, int &b, int &A, int &B, int (*s_w)[NT / 64]) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int x = a, y = b;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(x, o), v = __shfl_up(y, o);
+        if (lane >= o) { x += u; y += v; }
+    }
+    __syncthreads();
+    if (lane == 63) { s_w[0][wave] = x; s_w[1][wave] = y; }
+    __syncthreads();
+    int p = 0, q = 0;
+    A = B = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+        const int u = s_w[0][w], v = s_w[1][w];
+        if (w < wave) { p += u; q += v; }
+        A += u;
+        B += v;
+    }
+    a = p + x - a;
+    b = q + y - b;
+}
+
+__device__ __forceinline__ void put_row(const PlanParams &p, int row, int r, int from, int to, int total, int last) {
+    int slot = -1, pos = -1;
+    if (row < last && total > 0) {
+        pos = total - (to - row);
+        const int at = p.tables[(int64_t)r * p.W + pos / p.block];
+        if ((unsigned)at < (unsigned)p.blocks) slot = at * p.block + pos % p.block; else pos = -1;
+    }
+    p.slots[row] = slot;
+    p.positions[row] = pos;
+}
+
+// One workgroup, a request a thread (NT at a time), then a block a thread: sums over
+// the requests give each its place in the stack and its rows.  Latency-bound: three
+// dependent rounds of loads (lengths, stack, table) and the sums' barriers.
+template <int NT> __global__ __launch_bounds__(NT) void k_kv8_plan(PlanParams p) {
+    __shared__ int s_w[2][NT / 64], s_pref[NT + 1], s_held[NT], s_start[NT + 1], s_total[NT], s_take;
+    const int tid = threadIdx.x;
+    auto held_of = [&](int r) { return r < p.R ? min(max(p.held[r], 0), p.W) : 0; };
+    auto find = [&](int n, int e) {     // the last of n requests whose sum before it is at most e
+        int lo = 0, hi = n;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (s_pref[mid] <= e) lo = mid; else hi = mid;
+        }
+        return lo;
+    };
+    int64_t avail = min(max(p.n_free[0], 0), p.blocks);
+    // what the requests that ended give back
+    int64_t back_all = 0;
+    for (int c0 = 0; c0 < p.R; c0 += NT) {
+        const int r = c0 + tid;
+        int back = r < p.R && p.add[r] < 0 ? held_of(r) : 0, none = 0, all, z;
+        scan2<NT>(back, none, all, z, s_w);
+        back_all += all;
+    }
+    if (back_all > 0) {
+        int64_t before = 0;
+        for (int c0 = 0; c0 < p.R; c0 += NT) {
+            const int r = c0 + tid;
+            int back = r < p.R && p.add[r] < 0 ? held_of(r) : 0, none = 0, all, z;
+            scan2<NT>(back, none, all, z, s_w);
+            s_pref[tid] = back;
+            __syncthreads();
+            for (int e = tid; e < all; e += NT) {
+                const int i = find(NT, e);
+                int32_t *entry = p.tables + (int64_t)(c0 + i) * p.W + (e - s_pref[i]);
+                const int64_t to = avail + back_all - 1 - (before + e);
+                if (to < p.blocks) p.stack[to] = *entry;    // (more than there are: the caller's counts are wrong)
+                *entry = -1;
+            }
+            before += all;
+            __syncthreads();
+        }
+        avail = avail + back_all < p.blocks ? avail + back_all : p.blocks;
+    }
+    // blocks for the others
+    int64_t taken = 0, wanted = 0;
+    int rows_before = 0;
+    for (int c0 = 0; c0 < p.R; c0 += NT) {
+        const int r = c0 + tid;
+        const int add = r < p.R ? p.add[r] : -1, len = r < p.R ? p.lens[r] : 0, h = add < 0 ? 0 : held_of(r);
+        const int n = min(max(add, 0), kKv8MaxRows + 1);
+        const int64_t want = ((int64_t)len + max(add, 0) + p.block - 1) / p.block;
+        const bool valid = add >= 0 && len >= 0 && want <= p.W;
+        const int need = valid ? max((int)want - h, 0) : 0;
+        int nb = need, nr = n, all_b, all_r;
+        scan2<NT>(nb, nr, all_b, all_r, s_w);
+        const int64_t from = (int64_t)rows_before + nr;     // (a sum of at most NT (2^20 + 1) and 2^20 + 1)
+        const bool fits = valid && (need == 0 || wanted + nb + need <= avail) && from + n <= p.rows;
+        if (tid == 0) s_take = 0;
+        s_pref[tid] = nb;
+        s_held[tid] = h;
+        __syncthreads();
+        if (fits && need > 0) atomicMax(&s_take, nb + need);    // (behind the first that finds none, none takes any)
+        const int start = (int)(from < p.rows ? from : p.rows), total = fits ? len + add : 0;
+        if (r < p.R) {
+            p.starts[r] = start;
+            p.total[r] = total;
+            if (add < 0 || fits) p.held[r] = h + (fits ? need : 0);
+        }
+        s_start[tid] = start;
+        s_total[tid] = total;
+        __syncthreads();
+        const int take = s_take;
+        for (int e = tid; e < take; e += NT) {
+            const int i = find(NT, e);
+            p.tables[(int64_t)(c0 + i) * p.W + s_held[i] + (e - s_pref[i])] = p.stack[avail - 1 - (wanted + e)];
+        }
+        taken += take;
+        wanted += all_b;
+        rows_before = (int)min((int64_t)rows_before + all_r, (int64_t)kKv8MaxRows + 1);
+    }
+    const int last = min(rows_before, p.rows);
+    if (tid == 0) {
+        p.starts[p.R] = last;
+        p.n_free[0] = (int)(avail - taken);
+        s_start[min(p.R, NT)] = last;
+    }
+    if (!p.fill) return;
+    __syncthreads();
+    for (int row = tid; row < p.rows; row += NT) {      // (R <= NT)
+        const int r = request_of(s_start, p.R, row);
+        put_row(p, row, r, s_start[r], s_start[r + 1], s_total[r], last);
+    }
+}
+// The rows of a step of many tokens.
+__global__ __launch_bounds__(256) void k_kv8_rows(PlanParams p) {
+    constexpr int kInLds = 4096;
+    __shared__ int s_start[kInLds + 1];
+    const int row = blockIdx.x * 256 + threadIdx.x;
+    const int32_t *starts = p.starts;
+    if (p.R <= kInLds) {
+        for (int i = threadIdx.x; i <= p.R; i += 256) s_start[i] = p.starts[i];
+        __syncthreads();
+        starts = s_start;
+    }
+    if (row >= p.rows) return;
+    const int r = request_of(starts, p.R, row);
+    put_row(p, row, r, starts[r], starts[r + 1], p.total[r], starts[p.R]);
+}
+
+// ---- keys and values into the cache ---------------------------------------------------
+template <typename L> struct AppendParams {
+    const L *x[2]; int64_t ld[2];   // keys, values
+    uint8_t *store[2];
+    float *scales;
+    const int32_t *slots;
+    int rows, chunk, blocks, n_kv, D, shift;    // block = 1 << shift
+};
+
+// x / s rounded to nearest even, from the product with 1 / s and what it leaves,
+// which one fma gives exactly.
+__device__ __forceinline__ float round_to(float x, float s, float inv) {
+    float q = rintf(x * inv);
+    const float e = fmaf(-q, s, x), a = fabsf(e), h = 0.5f * s;
+    if (a > h || (a == h && ((int)q & 1))) q += copysignf(1.f, e);
+    return fminf(fmaxf(q, -127.f), 127.f);
+}
+// q old / s likewise, in 64 bits: the product has more digits than a float.
+__device__ __forceinline__ int round_again(int u, double old, double s, double inv) {
+    const double x = (double)(u - 128) * old;
+    double q = rint(x * inv);
+    const double e = fma(-q, s, x), a = fabs(e), h = 0.5 * s;
+    if (a > h || (a == h && ((int)q & 1))) q += copysign(1., e);
+    return 128 + (int)q;
+}
+
+// A workgroup takes the blocks whose first row is among `chunk` rows, of one head, keys
+// or values: the block's rows by token (the last row of a token counts), their
+// largest magnitude, the scale, and the tiles with new bytes.  A thread holds 16
+// dimensions of IT tokens.  Bound by latency at a step's single tokens, by what it
+// reads and writes at a prompt's.
+template <typename L, int NT, int IT> __global__ __launch_bounds__(NT) void k_kv8_append(AppendParams<L> p) {
+    extern __shared__ uint8_t s_stage[];        // values: [block][D + 16] bytes
+    __shared__ int s_row[256], s_end;
+    __shared__ uint32_t s_top[NT / 64];
+    const int tid = threadIdx.x, head = blockIdx.y, which = blockIdx.z;
+    const int B = 1 << p.shift, D = p.D, E = D >> 4;
+    const L *x = p.x[which] + (int64_t)head * D;
+    const int64_t ld = p.ld[which];
+    const int from = blockIdx.x * p.chunk, upto = min(from + p.chunk, p.rows);
+    auto block_of = [&](int i) {
+        const int s = p.slots[i];
+        return s >= 0 && (s >> p.shift) < p.blocks ? s >> p.shift : -1;
+    };
+    // the rows that begin a block's run, one a lane
+    const int lane = tid & 63, own = from + lane < upto ? block_of(from + lane) : -1;
+    const int before = own >= 0 && from + lane > 0 ? block_of(from + lane - 1) : -1;
+    for (uint64_t runs = __ballot(own >= 0 && own != before); runs; runs &= runs - 1) {
+        const int at = __builtin_ctzll(runs), first = from + at, blk = __builtin_amdgcn_readlane(own, at);
+        // the run's rows by token
+        for (int i = tid; i < B; i += NT) s_row[i] = -1;
+        if (tid == 0) s_end = p.rows;
+        __syncthreads();
+        for (int i0 = first;; i0 += NT) {
+            const int i = i0 + tid;
+            const bool mine = i < p.rows && block_of(i) == blk;
+            if (i < p.rows && !mine) atomicMin(&s_end, i);
+            __syncthreads();
+            const int end = s_end;
+            if (mine && i < end) atomicMax(&s_row[p.slots[i] & (B - 1)], i);
+            if (end <= i0 + NT) break;
+            __syncthreads();
+        }
+        __syncthreads();
+        float *scale = p.scales + ((int64_t)blk * p.n_kv + head) * 2 + which;
+        const float held = s_row[0] >= 0 ? 0.f : *scale;
+        uint8_t *store = p.store[which] + ((int64_t)blk * p.n_kv + head) * B * D;
+        // item: a token's 16 dimensions; tokens fastest within 16, as the key tiles have them
+        auto token = [&](int it) { const int i = tid + it * NT; return i / (E * 16) * 16 + (i & 15); };
+        auto group = [&](int it) { return (tid + it * NT) / 16 % E; };
+        float v[IT][16];
+        uint32_t top = 0;
+#pragma unroll
+        for (int it = 0; it < IT; ++it) {
+            const int row = s_row[token(it)];
+            if (row < 0) continue;
+            const L *at = x + row * ld + group(it) * 16;
+            constexpr int N = Piece<L>::N;
+#pragma unroll
+            for (int e = 0; e < 16 / N; ++e) {
+                const u32x4 w = *(const typename Piece<L>::raw_t *)(at + e * N);
+#pragma unroll
+                for (int f = 0; f < N; ++f) {
+                    v[it][e * N + f] = Piece<L>::get(w, f);
+                    top = max(top, __float_as_uint(v[it][e * N + f]) & 0x7FFFFFFFu);    // (NaN above infinity above all)
+                }
+            }
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
+        if ((tid & 63) == 0) s_top[tid >> 6] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < NT / 64; ++w) top = max(top, s_top[w]);
+        const float mine = top >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : __uint_as_float(top) / 127.f;
+        float s = __uint_as_float(max(__float_as_uint(mine), __float_as_uint(held) & 0x7FFFFFFFu));
+        if (s < 0x1p-126f) s = 0.f;
+        const bool finite = __float_as_uint(s) < 0x7F800000u;
+        const float inv = finite && s > 0.f ? 1.f / s : 0.f;
+        const bool grown = s_row[0] < 0 && !(s == held);
+        const double inv64 = grown && inv > 0.f ? 1. / (double)s : 0.;
+        if (tid == 0) *scale = s;
+        auto codes = [&](const float *f) {
+            u32x4 w;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                w[k] = 0;
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+                    w[k] |= (uint32_t)(128 + (inv > 0.f ? (int)round_to(f[4 * k + b], s, inv) : 0)) << 8 * b;
+            }
+            return w;
+        };
+        auto again = [&](u32x4 w) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                uint32_t r = 0;
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+                    r |= (uint32_t)(inv64 > 0. ? round_again((w[k] >> 8 * b) & 255, held, s, inv64) : 128) << 8 * b;
+                w[k] = r;
+            }
+            return w;
+        };
+        if (which == 0) {
+#pragma unroll
+            for (int it = 0; it < IT; ++it) {
+                const int t = token(it);
+                u32x4 *at = (u32x4 *)store + key_piece(t, group(it), D);
+                if (s_row[t] >= 0) *at = codes(v[it]);
+                else if (grown) *at = again(*at);
+            }
+        } else {
+            const int pitch = D + 16;
+#pragma unroll
+            for (int it = 0; it < IT; ++it)
+                if (s_row[token(it)] >= 0) *(u32x4 *)(s_stage + token(it) * pitch + group(it) * 16) = codes(v[it]);
+            __syncthreads();
+#pragma unroll
+            for (int it = 0; it < IT; ++it) {
+                const int i = tid + it * NT, tile = i >> 6;     // piece i: dimensions e and e + 16, tokens t + v and t + 16 + v
+                const int t = tile / (D >> 5) * 32 + ((i & 63) >> 4) * 4, e = tile % (D >> 5) * 32 + (i & 15);
+                uint32_t fresh = 0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) fresh |= (uint32_t)(s_row[t + (k >> 2) * 16 + (k & 3)] >= 0) << k;
+                if (!fresh && !grown) continue;
+                u32x4 *at = (u32x4 *)store + i;
+                u32x4 w{};
+                if (fresh != 255) {
+                    w = *at;
+                    if (grown) w = again(w);
+                }
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    if (!(fresh >> (k & 7) & 1)) continue;
+                    const uint32_t b = s_stage[(t + ((k >> 2) & 1) * 16 + (k & 3)) * pitch + e + (k >> 3) * 16];
+                    w[k >> 2] = (w[k >> 2] & ~(255u << 8 * (k & 3))) | b << 8 * (k & 3);
+                }
+                *at = w;
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// ---- and back ------------------------------------------------------------------------
+template <typename L> struct ReadParams {
+    const uint8_t *keys, *values;
+    const float *scales;
+    const int32_t *slots;
+    L *k, *v;
+    int rows, blocks, n_kv, D, shift;
+};
+
+// A thread reads 16 dimensions of a row and head.
+template <typename L> __global__ __launch_bounds__(256) void k_kv8_read(ReadParams<L> p) {
+    const int E = p.D >> 4;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)p.rows * p.n_kv * E;
+    if (i >= all) return;
+    const int e = (int)(i % E), head = (int)(i / E % p.n_kv), row = (int)(i / E / p.n_kv);
+    const int slot = p.slots[row], blk = slot >> p.shift, t = slot & ((1 << p.shift) - 1);
+    float k[16], v[16];
+    if (slot >= 0 && blk < p.blocks) {
+        const int64_t at = (int64_t)blk * p.n_kv + head;
+        const float2 s = *(const float2 *)(p.scales + at * 2);
+        const uint8_t *ks = p.keys + (at << p.shift) * p.D, *vs = p.values + (at << p.shift) * p.D;
+        const u32x4 w = ((const u32x4 *)ks)[key_piece(t, e, p.D)];
+#pragma unroll
+        for (int d = 0; d < 16; ++d) {
+            k[d] = (float)((int)(w[d >> 2] >> 8 * (d & 3) & 255) - 128) * s.x;
+            v[d] = (float)((int)vs[value_byte(t, e * 16 + d, p.D)] - 128) * s.y;
+        }
+    } else {
+#pragma unroll
+        for (int d = 0; d < 16; ++d) k[d] = v[d] = 0.f;
+    }
+    constexpr int N = Piece<L>::N;
+#pragma unroll
+    for (int d = 0; d < 16; d += N) {
+        *(u32x4 *)(p.k + i * 16 + d) = Piece<L>::pack(k + d);
+        *(u32x4 *)(p.v + i * 16 + d) = Piece<L>::pack(v + d);
+    }
+}
+
+static int log2_of(int n) { return __builtin_ctz((unsigned)n); }
+
+template <typename L, int NT, int IT> static bool launch_append(const AppendParams<L> &p, hipStream_t s) {
+    const size_t lds = (size_t)(1 << p.shift) * (p.D + 16);
+    void *ptrs[] = {(void *)&p};
+    return hipLaunchKernel((const void *)k_kv8_append<L, NT, IT>, dim3((p.rows + p.chunk - 1) / p.chunk, p.n_kv, 2),
+                           dim3(NT), ptrs, lds, s) == hipSuccess;
+}
+
+template <typename L>
+static int append(const pipo_kv8 *c, int32_t rows, const L *k, int64_t ld_k, const L *v, int64_t ld_v,
+                  const int32_t *d_slots, void *stream) {
+    if (!kv8_ok(c) || rows < 0 || rows > kKv8MaxRows) return PIPO_EINVAL;
+    if (rows == 0) return PIPO_OK;
+    const int64_t least = (int64_t)c->n_kv * c->head_dim;
+    if (!kv8_aligned(k, sizeof(L)) || !kv8_aligned(v, sizeof(L)) || !kv8_aligned(d_slots, 4)) return PIPO_EINVAL;
+    if (rows > 1 && (ld_k < least || ld_v < least || ld_k > (int64_t)1 << 31 || ld_v > (int64_t)1 << 31)) return PIPO_EINVAL;
+    AppendParams<L> p{{k, v}, {ld_k, ld_v}, {c->keys, c->values}, c->scales, d_slots, rows, 1, c->blocks, c->n_kv,
+                      c->head_dim, log2_of(c->block)};
+    // a workgroup's rows: single tokens of many requests one by one, prompts' rows by the block
+    p.chunk = rows <= 256 ? 1 : rows >= 64 * 256 ? 64 : (rows + 255) / 256;
+    const int items = c->block * c->head_dim / 16;
+    hipStream_t s = (hipStream_t)stream;
+    const bool ok = items == 128   ? launch_append<L, 128, 1>(p, s)
+                    : items == 256 ? launch_append<L, 256, 1>(p, s)
+                    : items == 512 ? launch_append<L, 512, 1>(p, s)
+                    : items == 1024 ? launch_append<L, 512, 2>(p, s)
+                                    : launch_append<L, 512, 4>(p, s);
+    return ok ? PIPO_OK : PIPO_EHIP;
+}
+
+template <typename L>
+static int read_rows(const pipo_kv8 *c, int32_t rows, const int32_t *d_slots, L *k, L *v, void *stream) {
+    if (!kv8_ok(c) || rows < 0 || rows > 64 * kKv8MaxRows) return PIPO_EINVAL;
+    if (rows == 0) return PIPO_OK;
+    if (!kv8_aligned(d_slots, 4) || !kv8_aligned(k, 16) || !kv8_aligned(v, 16)) return PIPO_EINVAL;
+    ReadParams<L> p{c->keys, c->values, c->scales, d_slots, k, v, rows, c->blocks, c->n_kv, c->head_dim, log2_of(c->block)};
+    const int64_t all = (int64_t)rows * c->n_kv * (c->head_dim / 16);
+    if (all > (int64_t)256 * 0x7FFFFFFF) return PIPO_EINVAL;
+    return launch(k_kv8_read<L>, (unsigned)((all + 255) / 256), 256, 0, (hipStream_t)stream, p) ? PIPO_OK : PIPO_EHIP;
+}
+
+}  // namespace pipo
+
+using namespace pipo;
+
+extern "C" int pipo_kv8_plan(int32_t R, int32_t width, int32_t block, int32_t blocks, const int32_t *d_lens,
+                             const int32_t *d_new, int32_t *d_tables, int32_t *d_held, int32_t *d_free,
+                             int32_t *d_n_free, int32_t rows, int32_t *d_starts, int32_t *d_total, int32_t *d_slots,
+                             int32_t *d_positions, void *stream) {
+    if (R < 1 || R > kKv8MaxRows || width < 1 || width > 1 << 20 || blocks < 1 || rows < 0 || rows > kKv8MaxRows) return PIPO_EINVAL;
+    if (block != 32 && block != 64 && block != 128 && block != 256) return PIPO_EINVAL;
+    if ((int64_t)width * block >= (int64_t)1 << 31 || (int64_t)blocks * block >= (int64_t)1 << 31) return PIPO_EINVAL;
+    for (const void *a : {(const void *)d_lens, (const void *)d_new, (const void *)d_tables, (const void *)d_held,
+                          (const void *)d_free, (const void *)d_n_free, (const void *)d_starts, (const void *)d_total})
+        if (!kv8_aligned(a, 4)) return PIPO_EINVAL;
+    if (rows > 0 && (!kv8_aligned(d_slots, 4) || !kv8_aligned(d_positions, 4))) return PIPO_EINVAL;
+    PlanParams p{R, width, block, blocks, d_lens, d_new, d_tables, d_held, d_free, d_n_free,
+                 rows, d_starts, d_total, d_slots, d_positions, 0};
+    hipStream_t s = (hipStream_t)stream;
+    p.fill = R <= 1024 && rows <= 4096;
+    const bool ok = R <= 256 && rows <= 1024 ? launch(k_kv8_plan<256>, 1, 256, 0, s, p) : launch(k_kv8_plan<1024>, 1, 1024, 0, s, p);
+    if (!ok) return PIPO_EHIP;
+    if (!p.fill && rows > 0 && !launch(k_kv8_rows, (unsigned)((rows + 255) / 256), 256, 0, s, p)) return PIPO_EHIP;
+    return PIPO_OK;
+}
+
+extern "C" int pipo_kv8_append(const pipo_kv8 *cache, int32_t rows, const float *d_k, int64_t ld_k, const float *d_v,
+                               int64_t ld_v, const int32_t *d_slots, void *stream) {
+    return append<float>(cache, rows, d_k, ld_k, d_v, ld_v, d_slots, stream);
+}
+extern "C" int pipo_kv8_append_bf16(const pipo_kv8 *cache, int32_t rows, const uint16_t *d_k, int64_t ld_k,
+                                    const uint16_t *d_v, int64_t ld_v, const int32_t *d_slots, void *stream) {
+    return append<uint16_t>(cache, rows, d_k, ld_k, d_v, ld_v, d_slots, stream);
+}
+extern "C" int pipo_kv8_read(const pipo_kv8 *cache, int32_t rows, const int32_t *d_slots, float *d_k, float *d_v,
+                             void *stream) {
+    return read_rows<float>(cache, rows, d_slots, d_k, d_v, stream);
+}
+extern "C" int pipo_kv8_read_bf16(const pipo_kv8 *cache, int32_t rows, const int32_t *d_slots, uint16_t *d_k,
+                                  uint16_t *d_v, void *stream) {
+    return read_rows<uint16_t>(cache, rows, d_slots, d_k, d_v, stream);
+}

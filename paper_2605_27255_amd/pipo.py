@@ -20,6 +20,9 @@ EXPORTED = ("pipo_init_weights", "pipo_prefill", "pipo_prefill_ragged", "pipo_de
             "pipo_opd_teacher_rows", "pipo_opd_targets", "pipo_opd_targets_bf16",
             "pipo_opd_work_bytes", "pipo_opd_top_logits", "pipo_opd_top_logits_bf16", "pipo_opd_distill",
             "pipo_opd_distill_bf16", "pipo_opd_policy", "pipo_opd_policy_bf16",
+            "pipo_kv8_plan", "pipo_kv8_append", "pipo_kv8_append_bf16", "pipo_kv8_read", "pipo_kv8_read_bf16",
+            "pipo_kv8_attention_work_bytes", "pipo_kv8_attention", "pipo_kv8_attention_bf16",
+            "pipo_verify_work_bytes", "pipo_verify_drafts", "pipo_verify_drafts_bf16",
             "pipo_calibrate_stream", "pipo_calibrate_mfma")
 #: kernel classes of the profiling counters (PIPO_K_* in include/pipo.h)
 KERNEL_CLASSES = ("gemv_layer", "gemv_lmhead", "gemv_small", "attn_decode", "sample", "gate",
@@ -49,6 +52,12 @@ class PipoSampling(ctypes.Structure):
 class PipoPair(ctypes.Structure):
     _fields_ = [("tok_b", ctypes.c_int32), ("tok_d", ctypes.c_int32), ("conf", ctypes.c_float),
                 ("accept", ctypes.c_int32)]
+
+
+class PipoKv8(ctypes.Structure):
+    _fields_ = [("keys", ctypes.c_void_p), ("values", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("blocks", ctypes.c_int32), ("n_kv", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("block", ctypes.c_int32)]
 
 
 _lib = None
@@ -91,6 +100,18 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                                                           f64, vp, vp, vp, i64, vp, i64, vp]
         getattr(lib, "pipo_opd_policy" + dt).argtypes = [i32, i32, vp, i64, vp, vp, vp, vp, f64, f64, f64, f64, vp,
                                                          vp, vp, vp, vp, i64, vp, i64, vp]
+    kv = ctypes.POINTER(PipoKv8)
+    lib.pipo_kv8_plan.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp]
+    lib.pipo_kv8_attention_work_bytes.argtypes = [kv, i32, i32, i32, i32, i32]
+    lib.pipo_verify_work_bytes.argtypes = [i32, i32, i32]
+    lib.pipo_kv8_attention_work_bytes.restype = lib.pipo_verify_work_bytes.restype = i64
+    for dt in ("", "_bf16"):
+        getattr(lib, "pipo_kv8_append" + dt).argtypes = [kv, i32, vp, i64, vp, i64, vp, vp]
+        getattr(lib, "pipo_kv8_read" + dt).argtypes = [kv, i32, vp, vp, vp, vp]
+        getattr(lib, "pipo_kv8_attention" + dt).argtypes = [kv, i32, i32, i32, vp, i64, vp, i32, vp, vp, i32, f64, vp,
+                                                            i64, vp, i64, vp]
+        getattr(lib, "pipo_verify_drafts" + dt).argtypes = [i32, i32, i32, i32, vp, i64, vp, vp, vp, i64, i64, vp, f64,
+                                                            vp, vp, vp, i64, vp]
     lib.pipo_calibrate_stream.argtypes = [vp, i64, i64, i32, ctypes.POINTER(ctypes.c_double), vp]
     lib.pipo_calibrate_mfma.argtypes = [vp, i32, i32, i32, ctypes.POINTER(ctypes.c_double), vp]
     for fn in ("pipo_init_weights", "pipo_prefill", "pipo_prefill_ragged", "pipo_decode_step",
@@ -99,6 +120,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                "pipo_profile_enable", "pipo_profile_read", "pipo_opd_teacher_rows", "pipo_opd_targets",
                "pipo_opd_targets_bf16", "pipo_opd_top_logits", "pipo_opd_top_logits_bf16", "pipo_opd_distill",
                "pipo_opd_distill_bf16", "pipo_opd_policy", "pipo_opd_policy_bf16",
+               "pipo_kv8_plan", "pipo_kv8_append", "pipo_kv8_append_bf16", "pipo_kv8_read", "pipo_kv8_read_bf16",
+               "pipo_kv8_attention", "pipo_kv8_attention_bf16", "pipo_verify_drafts", "pipo_verify_drafts_bf16",
                "pipo_calibrate_stream", "pipo_calibrate_mfma"):
         getattr(lib, fn).restype = ctypes.c_int
     _lib = lib
@@ -486,6 +509,233 @@ def opd_policy(logits, labels, advantages, old_logp=None, ref_logp=None, clip=(0
     if grad is not None and wanted is not True:
         _opd_written(grad)
     return loss, logp, kl, grad
+
+
+# ---- drafted tokens verified over a paged 8-bit cache -----------------------------------------------------------------
+
+def _serve_call(name, dt, device, *args):
+    """Calls a serving entry on the current stream of `device`, which is the current one."""
+    import torch
+    lib = _lib or load_library()
+    rc = getattr(lib, name + dt)(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    if rc != PIPO_OK:
+        raise PipoError(rc, f"{name}{dt}: " + ("sizes, strides or values outside the documented ranges"
+                                               if rc == PIPO_EINVAL else "launch failure"))
+
+
+def _int32(x, name, device, shape):
+    """The address of a contiguous int32 tensor of that shape on that device."""
+    import torch
+    if (getattr(x, "dtype", None) is not torch.int32 or x.shape != shape or x.device != device or not x.is_contiguous()):
+        _refuse(f"{name}: a contiguous int32 tensor of shape {tuple(shape)} on {device}")
+    return x.data_ptr()
+
+
+def _head_rows(x, name, heads, D, device, dtype=None):
+    """The row stride of a [rows, heads, D] tensor of fp32 or bf16 whose rows are contiguous, and the library's suffix."""
+    import torch
+    dt = x.dtype if isinstance(x, torch.Tensor) else None
+    if (dt is not torch.float32 and dt is not torch.bfloat16) or x.dim() != 3 or x.device != device or (dtype and dt is not dtype):
+        _refuse(f"{name}: a tensor [rows, heads, {D}] of {dtype or 'float32 or bfloat16'} on {device}, not {dt}")
+    n, h, d = x.shape
+    ld, sh, sd = x.stride()
+    if d != D or (heads and h != heads) or h < 1 or sd != 1 or (h > 1 and sh != D) or (n > 1 and ld < h * D):
+        _refuse(f"{name}: rows of {heads or 'n'} x {D} consecutive elements that do not overlap, not {tuple(x.shape)} "
+                f"with strides {(ld, sh, sd)}")
+    return ld if n > 1 else h * D, "" if dt is torch.float32 else "_bf16"
+
+
+class Kv8Cache:
+    """Keys and values in 8 bits, in blocks of tokens with a scale for each block and head.
+
+    keys [blocks, n_kv, block/16, head_dim/64, 64, 16] and values [blocks, n_kv,
+    block/32, head_dim/32, 64, 16] uint8 (tiles, see include/pipo.h), scales
+    [blocks, n_kv, 2] float32: the tensors that a program keeps.  ``Kv8Cache.new``
+    makes them."""
+
+    def __init__(self, keys, values, scales):
+        import torch
+        ok = all(isinstance(x, torch.Tensor) and x.is_cuda and x.is_contiguous() for x in (keys, values, scales))
+        if not ok or keys.dim() != 6 or keys.dtype is not torch.uint8 or values.dtype is not torch.uint8:
+            _refuse("keys, values: contiguous uint8 CUDA tensors of six dimensions, scales float32")
+        P, H, T, C = keys.shape[:4]
+        if (keys.shape[4:] != (64, 16) or values.shape != (P, H, T // 2, 2 * C, 64, 16) or scales.shape != (P, H, 2)
+                or scales.dtype is not torch.float32 or values.device != keys.device or scales.device != keys.device
+                or 16 * T not in (32, 64, 128, 256) or C not in (1, 2) or P < 1 or not 1 <= H <= 256 or P * T * 16 >= 2 ** 31
+                or (keys.data_ptr() | values.data_ptr()) & 15 or scales.data_ptr() & 7):
+            _refuse(f"a cache's tensors do not fit together: {tuple(keys.shape)}, {tuple(values.shape)}, {tuple(scales.shape)}")
+        self.keys, self.values, self.scales, self.device = keys, values, scales, keys.device
+        self.blocks, self.n_kv, self.block, self.head_dim = P, H, 16 * T, 64 * C
+        self.c = PipoKv8(keys.data_ptr(), values.data_ptr(), scales.data_ptr(), P, H, 64 * C, 16 * T)
+
+    @classmethod
+    def new(cls, blocks: int, n_kv: int, head_dim: int, block: int = 64, device="cuda"):
+        """A cache of that many blocks; nothing in it counts before it is appended."""
+        import torch
+        if block not in (32, 64, 128, 256) or head_dim not in (64, 128):
+            _refuse(f"block: 32, 64, 128 or 256, head_dim: 64 or 128, not {block} and {head_dim}")
+        u8 = dict(dtype=torch.uint8, device=device)
+        return cls(torch.zeros((blocks, n_kv, block // 16, head_dim // 64, 64, 16), **u8),
+                   torch.zeros((blocks, n_kv, block // 32, head_dim // 32, 64, 16), **u8),
+                   torch.zeros((blocks, n_kv, 2), dtype=torch.float32, device=device))
+
+
+def _cache(cache):
+    if not isinstance(cache, Kv8Cache):
+        _refuse("cache: a Kv8Cache")
+    return cache.device
+
+
+def kv8_plan(lens, new, tables, held, free, n_free, rows: int, block: int):
+    """Blocks, slots and positions of a step that adds new[r] tokens to the lens[r]
+    that request r has (int32 CUDA [R]; new[r] < 0: it has ended, its blocks go
+    back).  tables [R, width], held [R] (blocks in each row), free [blocks] (a
+    stack) and n_free [1] are the int32 state that the call updates; rows: room
+    for the step's tokens.  Returns (starts [R + 1], total [R], slots [rows],
+    positions [rows]) int32: the rows of request r, the tokens it has then (0: none
+    could be placed), and -1 where a row has none."""
+    import torch
+    if _elsewhere(lens):
+        with torch.cuda.device(lens.device):
+            return kv8_plan(lens, new, tables, held, free, n_free, rows, block)
+    if not getattr(lens, "is_cuda", False) or lens.dim() != 1 or getattr(tables, "ndim", 0) != 2 or getattr(free, "ndim", 0) != 1:
+        _refuse("lens, tables, free: int32 CUDA tensors of one, two and one dimensions")
+    dev, R, W, P = lens.device, lens.shape[0], tables.shape[1], free.shape[0]
+    if not 0 <= rows <= 1 << 20:
+        _refuse(f"rows: from 0 to {1 << 20}, not {rows}")
+    one = (R,)
+    ins = (_int32(lens, "lens", dev, one), _int32(new, "new", dev, one), _int32(tables, "tables", dev, (R, W)),
+           _int32(held, "held", dev, one), _int32(free, "free", dev, (P,)), _int32(n_free, "n_free", dev, (1,)))
+    out = torch.empty(2 * (R + rows) + 1, dtype=torch.int32, device=dev)
+    starts, total, slots, positions = out[:R + 1], out[R + 1:2 * R + 1], out[2 * R + 1:2 * R + 1 + rows], out[2 * R + 1 + rows:]
+    _serve_call("pipo_kv8_plan", "", dev, R, W, block, P, *ins, rows, starts.data_ptr(), total.data_ptr(),
+                slots.data_ptr(), positions.data_ptr())
+    return starts, total, slots, positions
+
+
+def kv8_append(cache, k, v, slots):
+    """Keys and values (fp32 or bf16 CUDA [rows, n_kv, head_dim], any row stride) into
+    the cache's slots (int32 [rows], negative: not at all).  Rows of one block are
+    consecutive; one at a block's first slot begins the block anew, otherwise its
+    scale only grows."""
+    import torch
+    dev = _cache(cache)
+    if _elsewhere(cache.keys):
+        with torch.cuda.device(dev):
+            return kv8_append(cache, k, v, slots)
+    ld_k, dt = _head_rows(k, "k", cache.n_kv, cache.head_dim, dev)
+    ld_v, _ = _head_rows(v, "v", cache.n_kv, cache.head_dim, dev, k.dtype)
+    if v.shape[0] != k.shape[0]:
+        _refuse("k and v: as many rows")
+    _serve_call("pipo_kv8_append", dt, dev, ctypes.byref(cache.c), k.shape[0], k.data_ptr(), ld_k, v.data_ptr(), ld_v,
+                _int32(slots, "slots", dev, (k.shape[0],)))
+
+
+def kv8_read(cache, slots, dtype=None):
+    """The keys and values that the cache holds in these slots (int32 [rows]), as
+    [rows, n_kv, head_dim] tensors of float32 (None) or bfloat16; zeros where
+    there is no such slot."""
+    import torch
+    dev = _cache(cache)
+    if _elsewhere(cache.keys):
+        with torch.cuda.device(dev):
+            return kv8_read(cache, slots, dtype)
+    dtype = dtype or torch.float32
+    if dtype is not torch.float32 and dtype is not torch.bfloat16:
+        _refuse(f"dtype: float32 or bfloat16, not {dtype}")
+    n = slots.numel() if isinstance(slots, torch.Tensor) else 0
+    at = _int32(slots, "slots", dev, (n,))
+    k = torch.empty((n, cache.n_kv, cache.head_dim), dtype=dtype, device=dev)
+    v = torch.empty_like(k)
+    _serve_call("pipo_kv8_read", "" if dtype is torch.float32 else "_bf16", dev, ctypes.byref(cache.c), n, at,
+                k.data_ptr(), v.data_ptr())
+    return k, v
+
+
+def kv8_attention(q, cache, tables, starts, total, scale=None, max_len=None, out=None):
+    """Attention of each request's last tokens over what the cache holds of it.
+    q: fp32 or bf16 CUDA [rows, n_q, head_dim], any row stride; rows starts[r] ..
+    starts[r + 1] - 1 are request r's, its tokens total[r] lie in the blocks of
+    tables[r] (int32 [R + 1], [R], [R, width], as kv8_plan gives them); each row
+    sees the tokens up to its own.  scale: of the scores (None: 1 /
+    sqrt(head_dim)); max_len: no request has more tokens (None: the tables'
+    width), fewer make better use of the GPU; out: where to write (None: a new
+    tensor; rows that belong to no request are not written).  Returns out."""
+    import torch
+    dev = _cache(cache)
+    if _elsewhere(cache.keys):
+        with torch.cuda.device(dev):
+            return kv8_attention(q, cache, tables, starts, total, scale, max_len, out)
+    D = cache.head_dim
+    ld, dt = _head_rows(q, "q", 0, D, dev)
+    rows, n_q = q.shape[:2]
+    if n_q % cache.n_kv or n_q // cache.n_kv > 16:
+        _refuse(f"q: 1 to 16 query heads for each of {cache.n_kv} heads of the cache, not {n_q} in all")
+    if getattr(tables, "ndim", 0) != 2 or tables.shape[0] < 1 or tables.shape[1] < 1:
+        _refuse("tables: an int32 tensor [R, width]")
+    R, W = tables.shape
+    ptrs = _int32(tables, "tables", dev, (R, W)), W, _int32(starts, "starts", dev, (R + 1,)), _int32(total, "total", dev, (R,))
+    most = W * cache.block if max_len is None else int(max_len)
+    if not 1 <= most <= W * cache.block or W * cache.block >= 2 ** 31:
+        _refuse(f"max_len: from 1 to {W * cache.block}, not {most}")
+    if out is None:
+        out = torch.empty((rows, n_q, D), dtype=q.dtype, device=dev)
+    ld_out, _ = _head_rows(out, "out", n_q, D, dev, q.dtype)
+    if out.shape != q.shape:
+        _refuse("out: a tensor of q's shape")
+    lib, work = _lib or load_library(), None
+    n = lib.pipo_kv8_attention_work_bytes(ctypes.byref(cache.c), R, rows, n_q, most, bool(dt))
+    if n:
+        work = torch.empty(n, dtype=torch.uint8, device=dev)
+    _serve_call("pipo_kv8_attention", dt, dev, ctypes.byref(cache.c), R, rows, n_q, q.data_ptr(), ld, *ptrs, most,
+                D ** -0.5 if scale is None else scale, out.data_ptr(), ld_out, work.data_ptr() if n else None, n)
+    return out
+
+
+def verify_drafts(logits, drafts, u, draft_logits=None, starts=None, temperature: float = 1.0):
+    """Accepts drafted tokens, and draws the one behind them, so that every token is
+    distributed as the target alone would draw it.  logits: the target's, fp32 or bf16 CUDA
+    [rows, V], any row stride: request r's positions are rows starts[r] ..
+    starts[r + 1] - 1 (int32 [R + 1]; None: K + 1 rows each); drafts: int32 [R,
+    K], a negative one ends a request's; u: float32 [R, K + 1] random numbers in
+    [0, 1), the last for the token behind; draft_logits: [R, K, V] of the logits'
+    type, what the drafts were drawn from (None: they were not drawn); temperature:
+    of both, 0: greedy.  Returns (tokens [R, K + 1] int32, -1 behind the last,
+    accepted [R] int32)."""
+    import torch
+    if _elsewhere(logits):
+        with torch.cuda.device(logits.device):
+            return verify_drafts(logits, drafts, u, draft_logits, starts, temperature)
+    rows, V, ld, dt = _opd_rows(logits)
+    dev = logits.device
+    if getattr(drafts, "ndim", 0) != 2 or drafts.shape[1] > 63:
+        _refuse("drafts: an int32 tensor [R, K], K up to 63")
+    R, K = drafts.shape
+    at = _int32(drafts, "drafts", dev, (R, K))
+    _, u_at = _opd_args(dev, (None, "", None, None), (u, "u", torch.float32, (R, K + 1)))
+    starts_at = None
+    if starts is not None:
+        starts_at = _int32(starts, "starts", dev, (R + 1,))
+    elif rows != R * (K + 1):
+        _refuse(f"logits: {R * (K + 1)} rows, or starts")
+    if u is None:
+        _refuse(f"u: a contiguous torch.float32 tensor of shape {(R, K + 1)} on {dev}")
+    d_at, lr, ln = None, 0, 0
+    if draft_logits is not None:
+        d = draft_logits
+        if not isinstance(d, torch.Tensor) or d.dtype is not logits.dtype or d.shape != (R, K, V) or d.device != dev:
+            _refuse(f"draft_logits: a tensor of shape {(R, K, V)} of the logits' type and device")
+        lr, ln, step = d.stride()
+        if (V > 1 and step != 1) or (K > 1 and ln < V) or (R > 1 and lr < V):
+            _refuse(f"draft_logits: rows of consecutive elements that do not overlap, not strides {d.stride()}")
+        d_at = d.data_ptr() if K else None
+    tokens = torch.empty((R, K + 1), dtype=torch.int32, device=dev)
+    accepted = torch.empty(R, dtype=torch.int32, device=dev)
+    n = (_lib or load_library()).pipo_verify_work_bytes(R, K, V)
+    work = torch.empty(n, dtype=torch.uint8, device=dev)
+    _serve_call("pipo_verify_drafts", dt, dev, R, K, V, rows, logits.data_ptr(), ld, starts_at, at, d_at, lr, ln, u_at,
+                temperature, tokens.data_ptr(), accepted.data_ptr(), work.data_ptr(), n)
+    return tokens, accepted
 
 
 def calibrate_stream(buf, nbytes: int, reps: int = 20) -> float:
