@@ -13,6 +13,7 @@
 // queries, and their probabilities, go in as hi + lo fp16 pairs (2^-22), two MFMAs each.
 #include "kv8.h"
 #include <math.h>
+#include <type_traits>
 
 namespace pipo {
 
@@ -32,6 +33,10 @@ struct Kv8Attn {
 __device__ __forceinline__ f32x4 mfma16_f16(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
+// The largest of three, a NaN if there is one (which costs one instruction; fmaxf would first quiet each operand).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+}
 // Eight bytes u as fp16 u - 128: 0x6400 | u is 1024 + u.
 __device__ __forceinline__ u32x4 widen8(uint32_t a, uint32_t b) {
     const f16x2_t off = {(_Float16)1152.f, (_Float16)1152.f};
@@ -41,6 +46,12 @@ __device__ __forceinline__ u32x4 widen8(uint32_t a, uint32_t b) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) r[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2_t, w[i]) - off);
     return r;
+}
+// Eight bytes u as the fp16 numbers u 2^-24, which have the bytes themselves for bits
+// (the products take fp16's smallest numbers as they are).
+__device__ __forceinline__ u32x4 tiny8(uint32_t a, uint32_t b) {
+    return u32x4{__builtin_amdgcn_perm(0u, a, 0x0C010C00u), __builtin_amdgcn_perm(0u, a, 0x0C030C02u),
+                 __builtin_amdgcn_perm(0u, b, 0x0C010C00u), __builtin_amdgcn_perm(0u, b, 0x0C030C02u)};
 }
 __device__ __forceinline__ float f16_lo(uint32_t w) { return (float)__builtin_bit_cast(f16x2_t, w)[0]; }
 __device__ __forceinline__ float f16_hi(uint32_t w) { return (float)__builtin_bit_cast(f16x2_t, w)[1]; }
@@ -55,18 +66,31 @@ template <bool PAIR> __device__ __forceinline__ void fp16_8(const float *v, u32x
 // Where a row group lies: request r's groups are numbered from start(r) * qpg / (16 NCT) + r
 // on, which leaves room for the part-filled last one of every request before it.
 struct RowGroup { int r, row0, n, first, last; };   // rows row0 .. of the request's n * qpg; last: its total, cut off
-template <int ROWS> __device__ __forceinline__ bool find_group(const Kv8Attn &p, int f, RowGroup &g) {
-    auto at = [&](int r) { return (int)(((int64_t)max(p.starts[r], 0) * p.qpg) / ROWS) + r; };
-    int lo = 0, hi = p.R;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (at(mid) <= f) lo = mid; else hi = mid;
+template <int ROWS> __device__ __forceinline__ bool find_group(const Kv8Attn &p, int f, RowGroup &g, int &total) {
+    // 64 requests at a time, a lane each: the last whose groups begin at or before f
+    const int lane = threadIdx.x & 63;
+    int lo = 0, width = p.R;
+    int64_t start = 0;
+    for (;;) {
+        const int step = (width + 63) >> 6, r = lo + lane * step;
+        const bool in = lane * step < width;
+        start = in ? max(p.starts[r], 0) : 0;
+        total = in && step == 1 ? p.total[r] : 0;       // (asked for together: one round trip)
+        const int next = in && step == 1 ? p.starts[r + 1] : 0;
+        const uint64_t upto = __ballot(in && (int)(start * p.qpg / ROWS) + r <= f);
+        const int at = 63 - __builtin_clzll(upto | 1);
+        lo += at * step;
+        width = min(step, width - at * step);
+        if (step == 1) {
+            g.first = __builtin_amdgcn_readlane((int)start, at);
+            total = __builtin_amdgcn_readlane(total, at);
+            g.n = min(__builtin_amdgcn_readlane(next, at), p.rows) - g.first;
+            break;
+        }
     }
     g.r = lo;
-    g.first = max(p.starts[lo], 0);
-    g.n = min(p.starts[lo + 1], p.rows) - g.first;
-    g.row0 = (f - at(lo)) * ROWS;
-    g.last = min(max(p.total[lo], 0), p.max_len);
+    g.row0 = (f - (int)((int64_t)g.first * p.qpg / ROWS) - lo) * ROWS;
+    g.last = min(max(total, 0), p.max_len);
     return g.row0 >= 0 && g.row0 < g.n * p.qpg;
 }
 // Tiles that the rows of a group see: up to its last token's position.
@@ -79,25 +103,27 @@ template <int ROWS> __device__ __forceinline__ int tiles_of(const Kv8Attn &p, co
 // (SPLIT), or take a row group each.
 template <typename L, int D, int NCT, bool SPLIT>
 __global__ __launch_bounds__(256, (NCT > 2 || (NCT > 1 && sizeof(L) == 4)) ? 1 : 2) void k_kv8_attn(Kv8Attn p) {
-    constexpr bool PAIR = sizeof(L) == 4;
+    constexpr bool PAIR = sizeof(L) == 4, DEEP = NCT == 1;
     constexpr int ROWS = 16 * NCT, NC = D / 64, NT = D / 16, NV = D / 32;
     const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     int x = blockIdx.x;
     const int head = x % p.n_kv;
     x /= p.n_kv;
-    const int split = x % p.S, f = x / p.S * (SPLIT ? 1 : 4) + (SPLIT ? 0 : wave);
-    RowGroup rg;
-    bool live = f < p.groups && find_group<ROWS>(p, f, rg);
-    if (!live) {
-        if (SPLIT) return;
-        rg = RowGroup{0, 0, 0, 0, 0};
+    const int split = SPLIT ? x % p.S : 0;
+    int f = x / p.S;
+    if (!SPLIT) {
+        // A prompt's later rows see more tokens and go first; where every workgroup is resident at once (two a compute
+        // unit), the second half goes the other way round, so that a unit has long and short ones.
+        const int n = (p.groups + 3) >> 2, half = (n + 1) >> 1;
+        f = (n * p.n_kv <= 512 + p.n_kv && f >= half ? f - half : n - 1 - f) * 4 + wave;
     }
-    const int total = live ? p.total[rg.r] : 0;
-    const int tiles = live ? tiles_of<ROWS>(p, rg, total) : 0;
+    RowGroup rg;
+    int total;
+    if (f >= p.groups || !find_group<ROWS>(p, f, rg, total)) return;
+    const int tiles = tiles_of<ROWS>(p, rg, total);
     const int t_lo = split * p.chunk, t_hi = min(t_lo + p.chunk, tiles);
-    if (SPLIT ? t_lo >= t_hi && split > 0 : false) return;
-    if (!SPLIT && (!live || (t_lo >= t_hi && split > 0))) return;
+    if (t_lo >= t_hi && split > 0) return;
     const int n_split = tiles > 0 ? (tiles + p.chunk - 1) / p.chunk : 1;
     int ta = t_lo, tb = max(t_hi, t_lo);
     if (SPLIT) {
@@ -105,19 +131,61 @@ __global__ __launch_bounds__(256, (NCT > 2 || (NCT > 1 && sizeof(L) == 4)) ? 1 :
         ta = t_lo + (n * wave >> 2);
         tb = t_lo + (n * (wave + 1) >> 2);
     }
+    // A lane holds the number and scales of one of 64 blocks from blk0 on.
+    const int sh = p.shift - 5;     // tiles of a block: 1 << sh
+    int blk0 = 0, id = -1;
+    float2 sc = make_float2(0.f, 0.f);
+    auto load_ids = [&](int b0) {
+        blk0 = b0;
+        const int at = b0 + lane;
+        id = at < p.W ? p.tables[(int64_t)rg.r * p.W + at] : -1;
+        if ((unsigned)id >= (unsigned)p.blocks) id = -1;
+        sc = id >= 0 ? *(const float2 *)(p.scales + ((int64_t)id * p.n_kv + head) * 2) : make_float2(0.f, 0.f);
+    };
+    struct Tile { u32x4 k[2][NC], v[NV]; float sk, sv; bool there; };
+    Tile buf[DEEP ? 2 : 1];
+    int64_t off = 0;                // of the tile that load_keys was called for last
+    auto load_keys = [&](Tile &to, int t) {
+        const int tc = min(t, tb - 1), b = tc >> sh;
+        if (b - blk0 >= 64) load_ids(b);
+        const int bi = b - blk0, bid = __builtin_amdgcn_readlane(id, bi);
+        off = ((((int64_t)max(bid, 0) * p.n_kv + head) << p.shift) + ((tc & ((1 << sh) - 1)) << 5)) * D;
+        const u32x4 *k = (const u32x4 *)(p.keys + off) + lane;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) to.k[u][c] = SPLIT ? __builtin_nontemporal_load(k + (u * NC + c) * 64) : k[(u * NC + c) * 64];
+        return bi;
+    };
+    auto load_values = [&](Tile &to) {
+        const u32x4 *v = (const u32x4 *)(p.values + off) + lane;
+#pragma unroll
+        for (int c = 0; c < NV; ++c) to.v[c] = SPLIT ? __builtin_nontemporal_load(v + c * 64) : v[c * 64];
+    };
+    auto load_scales = [&](Tile &to, int bi) {
+        __builtin_amdgcn_sched_barrier(0);      // (they may still be on their way when the tile is asked for)
+        to.there = __builtin_amdgcn_readlane(id, bi) >= 0;
+        to.sk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc.x), bi));
+        to.sv = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc.y), bi));
+    };
+    auto load_tile = [&](Tile &to, int t) {
+        const int bi = load_keys(to, t);
+        load_values(to);
+        load_scales(to, bi);
+    };
+    if (ta < tb) load_ids(ta >> sh);
     // this lane's query rows
     u32x4 qh[NCT][NC][2], ql[NCT][NC][2];
-    float fq[NCT];                  // the row's factor of the scores
-    int seen[NCT], row_at[NCT], head_at[NCT];   // tokens it sees; its output row (-1: none) and head
+    float fq[NCT], cq[NCT];         // a product's score is product * fq + cq, both times the tile's scale
+    int seen[NCT];                  // tokens it sees
+    const float sign = p.scale < 0.f ? -1.f : 1.f;
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct) {
         const int rr = rg.row0 + 16 * ct + j, i = rr / p.qpg, h = head * p.qpg + rr - i * p.qpg;
         const bool is = i < rg.n;
-        row_at[ct] = is ? rg.first + i : -1;
-        head_at[ct] = h;
         seen[ct] = is ? max(min(total - rg.n + i + 1, rg.last), 0) : 0x7FFFFFFF;    // (what is no row is not written)
         float v[NC][16];
-        const L *q = (const L *)p.q + (is ? row_at[ct] * p.ld_q + (int64_t)h * D + 16 * g : 0);
+        const L *q = (const L *)p.q + (is ? (rg.first + i) * p.ld_q + (int64_t)h * D + 16 * g : 0);
         float top = 0.f;
 #pragma unroll
         for (int c = 0; c < NC; ++c)
@@ -134,14 +202,27 @@ __global__ __launch_bounds__(256, (NCT > 2 || (NCT > 1 && sizeof(L) == 4)) ? 1 :
         top = col_max(top);
         // the power of two that brings the largest to [2^14, 2^15)
         const int ex = top > 0.f && top < INFINITY ? 14 - ilogbf(top) : 0;
-        fq[ct] = ldexpf(p.scale, -ex);
+        fq[ct] = ldexpf(fabsf(p.scale), -ex);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) v[c][e] = ldexpf(v[c][e], ex);
+            for (int e = 0; e < 16; ++e) v[c][e] = ldexpf(v[c][e], ex) * sign;
             fp16_8<PAIR>(v[c], qh[ct][c][0], ql[ct][c][0]);
             fp16_8<PAIR>(v[c] + 8, qh[ct][c][1], ql[ct][c][1]);
         }
+        cq[ct] = 0.f;
+        if (!PAIR) {                // the keys go in as u 2^-24, not u - 128
+            float sum = 0.f;
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) sum += f16_lo(qh[ct][c][e][k]) + f16_hi(qh[ct][c][e][k]);
+            cq[ct] = -128.f * col_sum(sum) * fq[ct];
+            fq[ct] *= 0x1p24f;
+        }
+        __builtin_amdgcn_sched_barrier(0);      // (one after the other, or their floats do not fit)
     }
     int all_see = 0x7FFFFFFF;       // tokens that every row sees
 #pragma unroll
@@ -150,8 +231,13 @@ __global__ __launch_bounds__(256, (NCT > 2 || (NCT > 1 && sizeof(L) == 4)) ? 1 :
     for (int o = 8; o > 0; o >>= 1) all_see = min(all_see, __shfl_xor(all_see, o));
     all_see = __builtin_amdgcn_readfirstlane(all_see);
 
+    // O in units of a value scale U; probabilities as 2^8 exp2(s - m), where m, a row's reference, follows its
+    // maximum only when that is more than 6 above it: O is seldom rescaled, and 2^15 at most goes into fp16.  Pairs
+    // take 2^14 and the maximum itself: the lower half of a small probability has fp16's smallest step (errors of the
+    // whole, 8 x 16384 tokens: 3.9e-6 with 2^8, 5e-7).
+    constexpr float kUp = PAIR ? 14.f : 8.f, kSlack = PAIR ? 0.f : 6.f;
     f32x4 o[NCT][NT];
-    float m_run[NCT], l_run[NCT];
+    float m_run[NCT], l_run[NCT], U = PAIR ? 1.f : 0.f;
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct) {
         m_run[ct] = -INFINITY;
@@ -159,39 +245,8 @@ __global__ __launch_bounds__(256, (NCT > 2 || (NCT > 1 && sizeof(L) == 4)) ? 1 :
 #pragma unroll
         for (int t = 0; t < NT; ++t) o[ct][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    // A lane holds the number and scales of one of 64 blocks from blk0 on.
-    const int sh = p.shift - 5;     // tiles of a block: 1 << sh
-    int blk0 = 0, id = -1;
-    float2 sc = make_float2(0.f, 0.f);
-    auto load_ids = [&](int b0) {
-        blk0 = b0;
-        const int at = b0 + lane;
-        id = at < p.W ? p.tables[(int64_t)rg.r * p.W + at] : -1;
-        if ((unsigned)id >= (unsigned)p.blocks) id = -1;
-        sc = id >= 0 ? *(const float2 *)(p.scales + ((int64_t)id * p.n_kv + head) * 2) : make_float2(0.f, 0.f);
-    };
-    u32x4 kf[2][2][NC], vf[2][NV];
-    int at_id[2];
-    float at_k[2], at_v[2];
-    auto load_tile = [&](int buf, int t) {
-        const int tc = min(t, tb - 1), b = tc >> sh;
-        if (b - blk0 >= 64) load_ids(b);
-        const int bi = b - blk0, bid = __builtin_amdgcn_readlane(id, bi);
-        at_id[buf] = bid;
-        at_k[buf] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc.x), bi));
-        at_v[buf] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sc.y), bi));
-        const int64_t off = ((((int64_t)max(bid, 0) * p.n_kv + head) << p.shift) + ((tc & ((1 << sh) - 1)) << 5)) * D;
-        const u32x4 *k = (const u32x4 *)(p.keys + off) + lane, *v = (const u32x4 *)(p.values + off) + lane;
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int c = 0; c < NC; ++c) kf[buf][u][c] = SPLIT ? __builtin_nontemporal_load(k + (u * NC + c) * 64) : k[(u * NC + c) * 64];
-#pragma unroll
-        for (int c = 0; c < NV; ++c) vf[buf][c] = SPLIT ? __builtin_nontemporal_load(v + c * 64) : v[c * 64];
-    };
-    auto tile = [&](int buf, int t) {
-        if (at_id[buf] < 0) return;         // no such block: its tokens are not there
-        f32x4 st[NCT][2];
+    typedef f32x4 Scores[NCT][2];
+    auto score = [&](const Tile &b, Scores &st) {
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
@@ -202,90 +257,170 @@ __global__ __launch_bounds__(256, (NCT > 2 || (NCT > 1 && sizeof(L) == 4)) ? 1 :
             for (int c = 0; c < NC; ++c)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const u32x4 a = widen8(kf[buf][u][c][2 * e], kf[buf][u][c][2 * e + 1]);
+                    const u32x4 a = PAIR ? widen8(b.k[u][c][2 * e], b.k[u][c][2 * e + 1]) : tiny8(b.k[u][c][2 * e], b.k[u][c][2 * e + 1]);
 #pragma unroll
                     for (int ct = 0; ct < NCT; ++ct) {
                         st[ct][u] = mfma16_f16(a, qh[ct][c][e], st[ct][u]);
                         if (PAIR) st[ct][u] = mfma16_f16(a, ql[ct][c][e], st[ct][u]);
                     }
                 }
-        const int t0 = t * 32;
-        const bool whole = t0 + 32 <= all_see;
-        u32x4 ph[NCT], pl[NCT];
-        float al[NCT], sv[NCT];
+    };
+    // A tile's probabilities, and what they add to l and O.
+    auto tile_as = [&](const Tile &b, int t0, const Scores &st, auto all) {
+        constexpr bool whole = decltype(all)::value;    // every row sees all of it
+        if (!b.there) return;       // no such block: its tokens are not there
+        float s[NCT][8], mx[NCT], fk[NCT], ck[NCT];
+        bool rise = false;
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct) {
-            const float fk = fq[ct] * at_k[buf];
-            float mx = -INFINITY, pf[8];
+            fk[ct] = fq[ct] * b.sk;
+            ck[ct] = cq[ct] * b.sk;
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int k = 0; k < 8; ++k) s[ct][k] = st[ct][k >> 2][k & 3];
+        }
+        auto hidden = [&](int ct, int k) { return t0 + 16 * (k >> 2) + 4 * g + (k & 3) >= seen[ct]; };
+        auto max8 = [](const float *v) { return max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), max3(v[6], v[7], v[7])); };
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    float s = st[ct][u][v] * fk;
-                    if (!whole && t0 + 16 * u + 4 * g + v >= seen[ct]) s = -INFINITY;
-                    pf[4 * u + v] = s;
-                    mx = fmaxf(mx, s);
-                }
-            const float m_new = fmaxf(m_run[ct], col_max(mx));
-            const float ref = m_new == -INFINITY ? 0.f : m_new;
-            al[ct] = __builtin_amdgcn_exp2f(m_run[ct] - ref);
-            m_run[ct] = m_new;
-            float sum = 0.f;
+        for (int ct = 0; ct < NCT; ++ct) {
+            if (whole) {
+                mx[ct] = fmaf(max8(s[ct]), fk[ct], ck[ct]);
+            } else {
+                float v[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                pf[k] = __builtin_amdgcn_exp2f(pf[k] - ref + 14.f);
-                sum += pf[k];
+                for (int k = 0; k < 8; ++k) v[k] = hidden(ct, k) ? -INFINITY : s[ct][k];
+                mx[ct] = max8(v);
+                mx[ct] = mx[ct] == -INFINITY ? mx[ct] : fmaf(mx[ct], fk[ct], ck[ct]);   // (a scale of 0 times it is no number)
             }
-            l_run[ct] = l_run[ct] * al[ct] + sum;
-            fp16_8<PAIR>(pf, ph[ct], pl[ct]);
-            sv[ct] = t0 < seen[ct] ? at_v[buf] : 0.f;   // (a row that sees nothing of the tile gets nothing of its scale)
+            rise |= mx[ct] > m_run[ct] + kSlack;
+        }
+        if (__builtin_amdgcn_ballot_w64(rise)) {
+#pragma unroll
+            for (int ct = 0; ct < NCT; ++ct) {
+                const float m = fmaxf(m_run[ct], col_max(mx[ct]));
+                const float al = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[ct] - m);
+                m_run[ct] = m;
+                l_run[ct] *= al;
+#pragma unroll
+                for (int d = 0; d < NT; ++d) o[ct][d] *= al;
+            }
+        }
+        // The tile's scale, over U, goes into its probabilities; where that is not near 1, U follows.  Below 2^-64 U (or 0)
+        // it adds nothing to O.  (Pairs: into what the tile adds, by an fma, which rounds to nearest.)
+        bool none = false;
+        float up = 0.f, back = 1.f;
+        if constexpr (!PAIR) {
+            none = b.sv < 0x1p-64f * U || b.sv == 0.f;
+            if (!none && (b.sv > 2.f * U || b.sv < 0.125f * U)) {       // (never with a NaN)
+                const float k = U / b.sv;
+                U = b.sv;
+#pragma unroll
+                for (int ct = 0; ct < NCT; ++ct)
+#pragma unroll
+                    for (int d = 0; d < NT; ++d) o[ct][d] *= k;
+            }
+            if (!none) {
+                up = __builtin_amdgcn_logf(b.sv) - __builtin_amdgcn_logf(U > 0.f ? U : 1.f);
+                back = b.sv > 0.f ? __builtin_amdgcn_exp2f(-up) : 1.f;
+            }
+        }
+        u32x4 ph[NCT], pl[NCT];
+        f32x4 w[NCT];
+#pragma unroll
+        for (int ct = 0; ct < NCT; ++ct) {
+            const float c = ck[ct] - (m_run[ct] == -INFINITY ? -kUp : m_run[ct] - kUp) + up;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s[ct][k] = __builtin_amdgcn_exp2f(fmaf(s[ct][k], fk[ct], c));
+            if (!whole) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) s[ct][k] = hidden(ct, k) ? 0.f : s[ct][k];
+            }
+            fp16_8<PAIR>(s[ct], ph[ct], pl[ct]);
+            // their sum, over the tile's tokens: from the matrix cores, where they have been rounded
+            const u32x4 ones{0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u};
+            w[ct] = mfma16_f16(ones, ph[ct], f32x4{0.f, 0.f, 0.f, 0.f});
+            if (PAIR) w[ct] = mfma16_f16(ones, pl[ct], w[ct]);
+            if (none) ph[ct] = u32x4{0u, 0u, 0u, 0u};
         }
 #pragma unroll
-        for (int c = 0; c < NV; ++c)
+        for (int d = 0; d < NT; ++d) {
+            const u32x4 a = widen8(b.v[d >> 1][2 * (d & 1)], b.v[d >> 1][2 * (d & 1) + 1]);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const u32x4 a = widen8(vf[buf][c][2 * e], vf[buf][c][2 * e + 1]);
+            for (int ct = 0; ct < NCT; ++ct) {
+                if constexpr (PAIR) {
+                    f32x4 x = mfma16_f16(a, ph[ct], f32x4{0.f, 0.f, 0.f, 0.f});
+                    x = mfma16_f16(a, pl[ct], x);
+                    const float k = t0 < seen[ct] ? b.sv : 0.f;    // (a row that sees nothing of the tile gets no NaN from it)
 #pragma unroll
-                for (int ct = 0; ct < NCT; ++ct) {
-                    f32x4 w = mfma16_f16(a, ph[ct], f32x4{0.f, 0.f, 0.f, 0.f});
-                    if (PAIR) w = mfma16_f16(a, pl[ct], w);
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) o[ct][2 * c + e][v] = fmaf(w[v], sv[ct], o[ct][2 * c + e][v] * al[ct]);
+                    for (int v = 0; v < 4; ++v) o[ct][d][v] = fmaf(x[v], k, o[ct][d][v]);
+                } else {
+                    o[ct][d] = mfma16_f16(a, ph[ct], o[ct][d]);
                 }
             }
+        }
+#pragma unroll
+        for (int ct = 0; ct < NCT; ++ct) l_run[ct] = fmaf(w[ct][0], back, l_run[ct]);
     };
     if (ta < tb) {
-        load_ids(ta >> sh);
-        load_tile(0, ta);
-        load_tile(1, ta + 1);
+        Scores st;
         int t = ta;
-        for (; t + 2 < tb; t += 2) {
-            tile(0, t);
-            load_tile(0, t + 2);
-            tile(1, t + 1);
-            load_tile(1, t + 3);
+        const int tw = all_see >> 5;            // tiles before this one are seen whole
+        load_tile(buf[0], ta);
+        if constexpr (DEEP) {       // two tiles on their way
+            load_tile(buf[1], ta + 1);
+            auto two = [&](auto all) {
+                score(buf[0], st);
+                tile_as(buf[0], t * 32, st, all);
+                load_tile(buf[0], t + 2);
+                score(buf[1], st);
+                tile_as(buf[1], t * 32 + 32, st, all);
+                load_tile(buf[1], t + 3);
+                t += 2;
+            };
+            while (t + 2 < min(tb, tw + 1)) two(std::true_type{});
+            while (t + 2 < tb) two(std::false_type{});
+            score(buf[0], st);
+            tile_as(buf[0], t * 32, st, std::false_type{});
+            if (t + 1 < tb) {
+                score(buf[1], st);
+                tile_as(buf[1], t * 32 + 32, st, std::false_type{});
+            }
+        } else {                    // the next tile's keys while this one's values are used, its values while its keys are
+            auto one = [&](auto all) {
+                score(buf[0], st);
+                const int bi = load_keys(buf[0], t + 1);
+                tile_as(buf[0], t * 32, st, all);
+                load_values(buf[0]);
+                load_scales(buf[0], bi);
+                ++t;
+            };
+            while (t < min(tb, tw)) one(std::true_type{});
+            while (t < tb) one(std::false_type{});
         }
-        tile(0, t);
-        if (t + 1 < tb) tile(1, t + 1);
     }
+    constexpr float kDown = PAIR ? 0x1p-14f : 0x1p-8f;
+    // (both without their power of two)
 #pragma unroll
-    for (int ct = 0; ct < NCT; ++ct) l_run[ct] = col_sum(l_run[ct]);
-
-    // to the output, or as a record for the others of the row's key ranges
-    auto finish = [&](int ct, int rr, int row, int h, int d, float a, float b, float c, float e, float m, float l, bool stat) {
-        if (row < 0) return;
+    for (int ct = 0; ct < NCT; ++ct) {
+        l_run[ct] *= kDown;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) o[ct][t] *= U * kDown;
+    }
+    // row rr of the group: to the output, or as a record for the others of its key ranges
+    auto finish = [&](int rr, int d, float a, float b, float c, float e, float m, float l) {
+        const int at = rg.row0 + rr, i = at / p.qpg;
+        if (i >= rg.n) return;
         if (n_split == 1) {
             const float inv = l == 0.f ? 0.f : 1.f / l;
-            L *to = (L *)p.out + row * p.ld_out + (int64_t)h * D + d;
+            L *to = (L *)p.out + (rg.first + i) * p.ld_out + (int64_t)(head * p.qpg + at - i * p.qpg) * D + d;
             Piece<L>::put(to, a * inv);
             Piece<L>::put(to + 1, b * inv);
             Piece<L>::put(to + 2, c * inv);
             Piece<L>::put(to + 3, e * inv);
         } else {
-            float *rec = p.part + ((((int64_t)f * p.n_kv + head) * p.S + split) * ROWS + 16 * ct + rr) * (D + 2);
+            float *rec = p.part + ((((int64_t)f * p.n_kv + head) * p.S + split) * ROWS + rr) * (D + 2);
             *(float2 *)(rec + d) = make_float2(a, b);
             *(float2 *)(rec + d + 2) = make_float2(c, e);
-            if (stat) *(float2 *)(rec + D) = make_float2(m, l);
+            if (d == 0) *(float2 *)(rec + D) = make_float2(m, l);
         }
     };
     if constexpr (!SPLIT) {
@@ -293,8 +428,7 @@ __global__ __launch_bounds__(256, (NCT > 2 || (NCT > 1 && sizeof(L) == 4)) ? 1 :
         for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
             for (int t = 0; t < NT; ++t)
-                finish(ct, j, row_at[ct], head_at[ct], 16 * t + 4 * g, o[ct][t][0], o[ct][t][1], o[ct][t][2], o[ct][t][3],
-                       m_run[ct], l_run[ct], t == 0 && g == 0);
+                finish(16 * ct + j, 16 * t + 4 * g, o[ct][t][0], o[ct][t][1], o[ct][t][2], o[ct][t][3], m_run[ct], l_run[ct]);
     } else {
         __shared__ float red[4][16][D + 2];
 #pragma unroll
@@ -308,8 +442,7 @@ __global__ __launch_bounds__(256, (NCT > 2 || (NCT > 1 && sizeof(L) == 4)) ? 1 :
             if (g == 0) *(float2 *)&red[wave][j][D] = make_float2(m_run[ct], l_run[ct]);
             __syncthreads();
             for (int e = threadIdx.x; e < 16 * D / 4; e += 256) {
-                const int rr = e / (D / 4), d = e % (D / 4) * 4, at = rg.row0 + 16 * ct + rr, i = at / p.qpg;
-                if (i >= rg.n) continue;
+                const int rr = e / (D / 4), d = e % (D / 4) * 4;
                 float M = -INFINITY, l = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int w = 0; w < 4; ++w) M = fmaxf(M, red[w][rr][D]);
@@ -321,20 +454,21 @@ __global__ __launch_bounds__(256, (NCT > 2 || (NCT > 1 && sizeof(L) == 4)) ? 1 :
 #pragma unroll
                     for (int v = 0; v < 4; ++v) a[v] += k * red[w][rr][d + v];
                 }
-                finish(ct, rr, rg.first + i, head * p.qpg + at - i * p.qpg, d, a[0], a[1], a[2], a[3], M, l, d == 0);
+                finish(16 * ct + rr, d, a[0], a[1], a[2], a[3], M, l);
             }
         }
     }
 }
 
-// The key ranges' records of a row as one: a wave a row, D / 64 dimensions a lane.
+// The key ranges' records of a row as one: a wave a row, D / 64 dimensions a lane; a lane has a range's weight.
 template <typename L, int D, int NCT> __global__ __launch_bounds__(256) void k_kv8_attn_join(Kv8Attn p) {
-    constexpr int ROWS = 16 * NCT, E = D / 64;
+    constexpr int ROWS = 16 * NCT, E = D / 64, U = 8;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int head = blockIdx.x % p.n_kv, f = blockIdx.x / p.n_kv;
     RowGroup rg;
-    if (!find_group<ROWS>(p, f, rg)) return;
-    const int tiles = tiles_of<ROWS>(p, rg, p.total[rg.r]);
+    int total;
+    if (!find_group<ROWS>(p, f, rg, total)) return;
+    const int tiles = tiles_of<ROWS>(p, rg, total);
     const int n = (tiles + p.chunk - 1) / p.chunk;
     if (n <= 1) return;             // the unit wrote it out itself
     for (int rr = wave; rr < ROWS && rg.row0 + rr < rg.n * p.qpg; rr += 4) {
@@ -343,13 +477,30 @@ template <typename L, int D, int NCT> __global__ __launch_bounds__(256) void k_k
         float M = -INFINITY, l = 0.f, a[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) a[e] = 0.f;
-        for (int s = 0; s < n; ++s) M = fmaxf(M, rec[s * step + D]);
-        const float ref = M == -INFINITY ? 0.f : M;
-        for (int s = 0; s < n; ++s) {
-            const float k = __builtin_amdgcn_exp2f(rec[s * step + D] - ref);
-            l += k * rec[s * step + D + 1];
+        for (int s0 = 0; s0 < n; s0 += 64) {
+            float2 ml = make_float2(-INFINITY, 0.f);
+            if (s0 + lane < n) ml = *(const float2 *)(rec + (s0 + lane) * step + D);
+            const float m = fmaxf(M, wave_max_dpp(ml.x)), ref = m == -INFINITY ? 0.f : m;
+            const float k = __builtin_amdgcn_exp2f(ml.x - ref), al = __builtin_amdgcn_exp2f(M - ref);
+            l = l * al + wave_sum_dpp(k * ml.y);
 #pragma unroll
-            for (int e = 0; e < E; ++e) a[e] += k * rec[s * step + lane * E + e];
+            for (int e = 0; e < E; ++e) a[e] *= al;
+            M = m;
+            const int cnt = min(n - s0, 64);
+            for (int s = 0; s < cnt; s += U) {
+                float v[U][E];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) v[u][e] = rec[(s0 + min(s + u, cnt - 1)) * step + lane * E + e];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(k), min(s + u, 63)));
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        if (s + u < cnt) a[e] += w * v[u][e];
+                }
+            }
         }
         const float inv = l == 0.f ? 0.f : 1.f / l;
         const int i = (rg.row0 + rr) / p.qpg, h = head * p.qpg + rg.row0 + rr - i * p.qpg;
@@ -363,7 +514,7 @@ template <typename L, int D, int NCT> __global__ __launch_bounds__(256) void k_k
 struct Kv8Shape { int nct, S, chunk, groups; bool split; int64_t part; };
 static Kv8Shape shape_of(int R, int rows, int n_q, int n_kv, int D, int max_len, int es, bool work) {
     Kv8Shape s{};
-    const int qpg = n_q / n_kv, most = es == 4 ? 2 : 4;
+    const int qpg = n_q / n_kv, most = 2;
     const int64_t per = ((int64_t)(rows + R - 1) / R) * qpg;        // query rows of a request and KV head, on average
     s.nct = per <= 16 ? 1 : per <= 32 || most == 2 ? 2 : 4;
     const int64_t tile_rows = 16 * s.nct;
@@ -384,12 +535,12 @@ static Kv8Shape shape_of(int R, int rows, int n_q, int n_kv, int D, int max_len,
 }
 
 template <typename L, int D, int NCT, bool SPLIT> static bool run_attn(const Kv8Attn &p, hipStream_t s) {
-    const int64_t grid = (int64_t)(SPLIT ? p.groups : (p.groups + 3) / 4) * p.S * p.n_kv;
+    const int64_t grid = (int64_t)(SPLIT ? p.groups * (int64_t)p.S : (p.groups + 3) / 4) * p.n_kv;     // (!SPLIT: S is 1)
     if (!launch(k_kv8_attn<L, D, NCT, SPLIT>, (unsigned)grid, 256, 0, s, p)) return false;
     return p.S == 1 || launch(k_kv8_attn_join<L, D, NCT>, (unsigned)(p.groups * p.n_kv), 256, 0, s, p);
 }
 template <typename L, int D> static bool run_attn_d(const Kv8Attn &p, const Kv8Shape &s, hipStream_t st) {
-    constexpr int most = sizeof(L) == 4 ? 2 : 4;
+    constexpr int most = 2;
     if (s.nct == 1) return run_attn<L, D, 1, true>(p, st);
     if (most == 4 && s.nct == 2) return run_attn<L, D, 2, true>(p, st);
     return s.split ? run_attn<L, D, most, true>(p, st) : run_attn<L, D, most, false>(p, st);
