@@ -460,11 +460,23 @@ __global__ __launch_bounds__(256, (NCT > 2 || (NCT > 1 && sizeof(L) == 4)) ? 1 :
     }
 }
 
-// The key ranges' records of a row as one: a wave a row, D / 64 dimensions a lane; a lane has a range's weight.
+// The key ranges' records of a row as one: a wave a row, D / 64 dimensions a lane, a lane a range's weight.  Where
+// a row's records lie does not hang on whose row it is: the first ones are asked for along with the lengths.
 template <typename L, int D, int NCT> __global__ __launch_bounds__(256) void k_kv8_attn_join(Kv8Attn p) {
     constexpr int ROWS = 16 * NCT, E = D / 64, U = 8;
+    typedef __attribute__((ext_vector_type(E))) float vec;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int head = blockIdx.x % p.n_kv, f = blockIdx.x / p.n_kv;
+    const float *records = p.part + ((int64_t)f * p.n_kv + head) * p.S * ROWS * (D + 2);
+    const int64_t step = (int64_t)ROWS * (D + 2);
+    auto stat = [&](int rr, int s) { return s < p.S ? *(const float2 *)(records + s * step + rr * (D + 2) + D) : make_float2(0.f, 0.f); };
+    auto ask = [&](vec (&v)[U], int rr, int s) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = *(const vec *)(records + min(s + u, p.S - 1) * step + rr * (D + 2) + lane * E);
+    };
+    vec v[U];
+    float2 ml = stat(wave, lane);
+    ask(v, wave, 0);
     RowGroup rg;
     int total;
     if (!find_group<ROWS>(p, f, rg, total)) return;
@@ -472,33 +484,27 @@ template <typename L, int D, int NCT> __global__ __launch_bounds__(256) void k_k
     const int n = (tiles + p.chunk - 1) / p.chunk;
     if (n <= 1) return;             // the unit wrote it out itself
     for (int rr = wave; rr < ROWS && rg.row0 + rr < rg.n * p.qpg; rr += 4) {
-        const float *rec = p.part + (((int64_t)f * p.n_kv + head) * p.S * ROWS + rr) * (D + 2);
-        const int64_t step = (int64_t)ROWS * (D + 2);
-        float M = -INFINITY, l = 0.f, a[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) a[e] = 0.f;
+        if (rr != wave) {
+            ml = stat(rr, lane);
+            ask(v, rr, 0);
+        }
+        float M = -INFINITY, l = 0.f;
+        vec a = 0.f;
         for (int s0 = 0; s0 < n; s0 += 64) {
-            float2 ml = make_float2(-INFINITY, 0.f);
-            if (s0 + lane < n) ml = *(const float2 *)(rec + (s0 + lane) * step + D);
-            const float m = fmaxf(M, wave_max_dpp(ml.x)), ref = m == -INFINITY ? 0.f : m;
-            const float k = __builtin_amdgcn_exp2f(ml.x - ref), al = __builtin_amdgcn_exp2f(M - ref);
-            l = l * al + wave_sum_dpp(k * ml.y);
-#pragma unroll
-            for (int e = 0; e < E; ++e) a[e] *= al;
+            if (s0 > 0) ml = stat(rr, s0 + lane);
+            const float mine = s0 + lane < n ? ml.x : -INFINITY;
+            const float m = fmaxf(M, wave_max_dpp(mine)), ref = m == -INFINITY ? 0.f : m;
+            const float k = __builtin_amdgcn_exp2f(mine - ref), al = __builtin_amdgcn_exp2f(M - ref);
+            l = l * al + wave_sum_dpp(s0 + lane < n ? k * ml.y : 0.f);
+            a *= al;
             M = m;
             const int cnt = min(n - s0, 64);
             for (int s = 0; s < cnt; s += U) {
-                float v[U][E];
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-#pragma unroll
-                    for (int e = 0; e < E; ++e) v[u][e] = rec[(s0 + min(s + u, cnt - 1)) * step + lane * E + e];
+                if (s0 + s > 0) ask(v, rr, s0 + s);
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(k), min(s + u, 63)));
-#pragma unroll
-                    for (int e = 0; e < E; ++e)
-                        if (s + u < cnt) a[e] += w * v[u][e];
+                    if (s + u < cnt) a += w * v[u];
                 }
             }
         }
@@ -514,7 +520,8 @@ template <typename L, int D, int NCT> __global__ __launch_bounds__(256) void k_k
 struct Kv8Shape { int nct, S, chunk, groups; bool split; int64_t part; };
 static Kv8Shape shape_of(int R, int rows, int n_q, int n_kv, int D, int max_len, int es, bool work) {
     Kv8Shape s{};
-    const int qpg = n_q / n_kv, most = 2;
+    constexpr int most = 2;
+    const int qpg = n_q / n_kv;
     const int64_t per = ((int64_t)(rows + R - 1) / R) * qpg;        // query rows of a request and KV head, on average
     s.nct = per <= 16 ? 1 : per <= 32 || most == 2 ? 2 : 4;
     const int64_t tile_rows = 16 * s.nct;
@@ -522,11 +529,16 @@ static Kv8Shape shape_of(int R, int rows, int n_q, int n_kv, int D, int max_len,
     const int64_t units = (int64_t)R * ((per + tile_rows - 1) / tile_rows) * n_kv;
     const int tiles = (max_len + 31) / 32;
     s.split = s.nct < most || units < 1024;
+    // Key ranges: what fills the chip in whole rounds.  A unit takes its prologue (about as long as three tiles of a
+    // wave) and a quarter of its tiles, the joining launch two and what it reads.  (Workgroups that a compute unit holds
+    // by their registers; 32 x 8192 tokens, 256 units, in 3 / 4 / 8 / 12 ranges: 89 / 95 / 95 / 100 us.)
+    const int slots = 256 * (D == 64 ? (s.nct == 1 ? 4 : 3) : (s.nct == 1 ? 3 : 2));
     s.S = 1;
-    if (work && s.split && units < 1024) {
-        int64_t S = (1024 + units - 1) / units;
-        if (S > tiles / 8) S = tiles / 8;
-        s.S = S < 1 ? 1 : (int)S;
+    double best = 1e300;
+    for (int S = 1; work && s.split && S <= 64 && 4 * S <= tiles + 3; ++S) {
+        const int64_t rounds = (units * S + slots - 1) / slots;
+        const double t = (double)rounds * (((tiles + S - 1) / S + 3) / 4 + 3) + (S > 1 ? 2. + S / 16. : 0.);
+        if (t < best) { best = t; s.S = S; }
     }
     s.chunk = (tiles + s.S - 1) / s.S;
     s.S = (tiles + s.chunk - 1) / s.chunk;
