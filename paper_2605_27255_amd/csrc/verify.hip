@@ -2,12 +2,13 @@
 //
 // Draft i of a request is accepted while u_i q_i < p_i; the token behind the accepted ones
 // is drawn from max(p - q, 0), or p, by the inverse of its running sum over the ids.
-// Three launches: each segment of each row to its maximum and its sum of exponentials of
-// differences to it (every logit read once, from HBM: what bounds it); the accepted drafts
-// of a request from a few numbers a row, and the masses of the segments of the one or
-// two rows that the next token is drawn from (again from the caches); the segment
-// that holds the drawn mass, element by element.  Exponentials are fp32 of exact
-// differences, everything that a choice hangs on is added and compared in 64 bits.
+// Two launches: each segment of each row to its maximum and its sum of exponentials of
+// differences to it (every logit read once, from HBM: what bounds it); then for each request
+// the accepted drafts from a few numbers a row, the masses of the segments of the one or
+// two rows that the next token is drawn from (again from the caches), and by the
+// workgroup that finishes last the segment that holds the drawn mass, element by
+// element.  Exponentials are fp32 of exact differences (of the drafts' own 64-bit ones);
+// everything that a choice hangs on is added, in a fixed order, and compared in 64 bits.
 #include "kv8.h"
 
 namespace pipo {
@@ -29,326 +30,298 @@ template <typename L> struct VerifyParams {
     int32_t *tokens, *accepted;
     SegPart *part;                  // [target rows R (K + 1), then drafter rows R K][S]
     double *mass;                   // [R][S]
-    Verdict *verdict;               // [R]
+    int32_t *done;                  // [R] workgroups that have written their mass
 };
 
-// Rows of request r: the first, and the number of drafts that have one (-1: no rows at all).
+// Rows of request r: the first, and how many drafts have one (-1: no rows at all).
 template <typename L> __device__ __forceinline__ int rows_of(const VerifyParams<L> &p, int r, int &first) {
     int n = p.K + 1;
     first = r * (p.K + 1);
     if (p.starts) {
         first = max(p.starts[r], 0);
         n = min(p.starts[r + 1], p.rows) - first;
-    } else {
-        n = min(n, p.rows - first);
     }
-    n = min(n - 1, p.K);
-    if (n < 0) return -1;
-    // (up to 63 drafts: a lane each)
+    return max(min(n - 1, p.K), -1);
+}
+// ... of which so many come before the first negative one (up to 63: a lane each).
+template <typename L> __device__ __forceinline__ int drafts_of(const VerifyParams<L> &p, int r, int n) {
     const int lane = threadIdx.x & 63;
-    const uint64_t ends = __ballot(lane >= n || p.drafts[(int64_t)r * p.K + lane] < 0);
-    return __builtin_ctzll(ends);
+    return __builtin_ctzll(__ballot(lane >= n || p.drafts[(int64_t)r * p.K + lane] < 0));
 }
-// Logits [seg kSeg, ...) of a row, kSegEach a thread: thread t's are pieces t, t + kSegThreads, ...
-template <typename L, typename F> __device__ __forceinline__ void each_of(const L *row, int lo, int n, F f) {
-    constexpr int N = Piece<L>::N, P = kSegEach / N;
+// The logits of a segment that a thread has: whole pieces, kSegThreads apart, and one element of what is left behind
+// the last whole one.  Elements that are not there are -inf.
+template <typename L> struct SegRow {
+    static constexpr int N = Piece<L>::N, P = kSegEach / N;
     u32x4 w[P];
-    const L *at = row + lo;
+    float tail;
+    __device__ __forceinline__ void load(const L *row, int lo, int len) {
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-        const int e0 = ((int)threadIdx.x + i * kSegThreads) * N;
-        if (e0 + N <= n) w[i] = *(const typename Piece<L>::raw_t *)(at + e0);
-    }
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-        const int e0 = ((int)threadIdx.x + i * kSegThreads) * N;
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            float v = -INFINITY;
-            if (e0 + N <= n) v = Piece<L>::get(w[i], e);
-            else if (e0 + e < n) v = Piece<L>::one(at + e0 + e);
-            f(v, lo + e0 + e, i * N + e);
+        for (int k = 0; k < P; ++k) {
+            const int e0 = ((int)threadIdx.x + k * kSegThreads) * N;
+            w[k] = u32x4{Piece<L>::kNegInf, Piece<L>::kNegInf, Piece<L>::kNegInf, Piece<L>::kNegInf};
+            if (e0 + N <= len) w[k] = *(const typename Piece<L>::raw_t *)(row + lo + e0);
         }
+        tail = -INFINITY;
+        if (tail_at(len) < len) tail = Piece<L>::one(row + lo + tail_at(len));
     }
-}
+    static __device__ __forceinline__ int tail_at(int len) { return len / N * N + (int)threadIdx.x; }
+    static __device__ __forceinline__ int at(int k, int e) { return ((int)threadIdx.x + k * kSegThreads) * N + e; }
+    __device__ __forceinline__ float get(int k, int e) const { return Piece<L>::get(w[k], e); }
+};
 
 template <typename L> __global__ __launch_bounds__(kSegThreads) void k_verify_rows(VerifyParams<L> p) {
+    constexpr int N = Piece<L>::N, P = kSegEach / N;
     const int seg = blockIdx.x % p.S, line = blockIdx.x / p.S, targets = p.R * (p.K + 1);
-    const L *row;
-    int first, r, n;
-    if (line < targets) {
-        r = line / (p.K + 1);
-        const int i = line - r * (p.K + 1);
-        n = rows_of(p, r, first);
-        if (i > n) return;
-        row = p.z + (first + i) * p.ld;
-    } else {
-        r = (line - targets) / p.K;
-        const int i = line - targets - r * p.K;
-        n = rows_of(p, r, first);
-        if (i >= n) return;
-        row = p.d + r * p.ld_request + i * p.ld_draft;
-    }
+    const bool target = line < targets;
+    const int at = target ? line : line - targets, each = target ? p.K + 1 : p.K, r = at / each, i = at - r * each;
+    int first;
+    const int n = rows_of(p, r, first);
+    if (target && i == 0 && seg == 0 && threadIdx.x == 0) p.done[r] = 0;
+    if (target ? i > n : i >= n) return;
+    const L *row = target ? p.z + (first + i) * p.ld : p.d + r * p.ld_request + i * p.ld_draft;
     __shared__ float s_m[kSegThreads / 64];
     __shared__ double s_s[kSegThreads / 64];
     __shared__ int s_id[kSegThreads / 64];
     const int lo = seg * kSeg, len = min(kSeg, p.V - lo);
-    float v[kSegEach], m = -INFINITY;
-    each_of(row, lo, len, [&](float x, int, int k) { v[k] = x; m = fmaxf(m, x); });
+    SegRow<L> x;
+    x.load(row, lo, len);           // (before the drafts, which may say that nobody needs them)
+    if (i > drafts_of(p, r, n) - !target) return;
+    float m = x.tail;
+#pragma unroll
+    for (int k = 0; k < P; ++k)
+#pragma unroll
+        for (int e = 0; e < N; ++e) m = fmaxf(m, x.get(k, e));
     m = block_max<kSegThreads>(m, s_m);
-    float sum = 0.f;
-    if (m != -INFINITY) {
+    // (without any token only a NaN is left to be found)
+    auto term = [&](float v) { return m == -INFINITY ? v != v ? v : 0.f : exp_diff(v, m, p.c); };
+    float sum = term(x.tail);
 #pragma unroll
-        for (int k = 0; k < kSegEach; ++k) sum += exp_diff(v[k], m, p.c);
-    } else {
+    for (int k = 0; k < P; ++k)
 #pragma unroll
-        for (int k = 0; k < kSegEach; ++k) sum += v[k] != v[k] ? v[k] : 0.f;
-    }
+        for (int e = 0; e < N; ++e) sum += term(x.get(k, e));
     const double s = block_sum<kSegThreads>((double)sum, s_s);
     int id = p.V;
     if (p.greedy) {
-        constexpr int N = Piece<L>::N;
+        if (x.tail == m) id = lo + x.tail_at(len);
 #pragma unroll
-        for (int k = kSegEach - 1; k >= 0; --k)
-            if (v[k] == m) id = lo + ((int)threadIdx.x + k / N * kSegThreads) * N + k % N;
+        for (int k = P - 1; k >= 0; --k)
+#pragma unroll
+            for (int e = N - 1; e >= 0; --e)
+                if (x.get(k, e) == m) id = lo + x.at(k, e);
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) id = min(id, __shfl_xor(id, o));
         if ((threadIdx.x & 63) == 0) s_id[threadIdx.x >> 6] = id;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kSegThreads / 64; ++w) id = min(id, s_id[w]);
+        for (int k = 0; k < kSegThreads / 64; ++k) id = min(id, s_id[k]);
     }
     if (threadIdx.x == 0) p.part[(int64_t)line * p.S + seg] = SegPart{s, m, id};
 }
 
 // A row from its segments, in every lane of a wave: maximum, 1 / sum (0: the row is bad), its largest logit's id.
-struct RowStat { float m; double inv; int id; };
+struct RowStat { float m; int id; double inv; };
 __device__ __forceinline__ RowStat join_row(const SegPart *part, int S, ExpScale c) {
     const int lane = threadIdx.x & 63;
     SegPart x{0., -INFINITY, 0x7FFFFFFF};
     if (lane < S) x = part[lane];
     const float m = wave_max_dpp(x.m);
-    double s = 0.;
-    if (lane < S) s = x.m == -INFINITY ? x.s : x.s * exp(((double)x.m - (double)m) * c.inv);    // (a segment without any keeps its NaN)
-    s = wave_sum_f64(s);
+    // (a segment without any keeps its NaN)
+    const double s = wave_sum_f64(x.m == -INFINITY ? x.s : x.s * (double)exp_diff(x.m, m, c));
     int id = x.m == m ? x.id : 0x7FFFFFFF;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) id = min(id, __shfl_xor(id, o));
-    return RowStat{m, s > 0. && s < INFINITY && m < INFINITY ? 1. / s : 0., id};
+    return RowStat{m, id, s > 0. && s < INFINITY && m < INFINITY ? 1. / s : 0.};
 }
 
 // The accepted drafts of a request and where its next token comes from: each wave of a
-// workgroup takes every fourth draft.
+// workgroup takes every fourth draft, and the row behind them.
 template <typename L> __device__ __forceinline__ Verdict judge(const VerifyParams<L> &p, int r, int n, int first, int &accepted) {
     __shared__ int s_stop;
-    __shared__ Verdict s_v;
+    __shared__ RowStat s_p[64], s_q[64];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     if (threadIdx.x == 0) s_stop = n;
     __syncthreads();
-    const int targets = p.R * (p.K + 1);
-    for (int i = wave; i < n; i += kSegThreads / 64) {
-        const RowStat a = join_row(p.part + (int64_t)(r * (p.K + 1) + i) * p.S, p.S, p.c);
-        const int y = p.drafts[(int64_t)r * p.K + i];
-        bool yes = a.inv > 0. && y < p.V;
+    const SegPart *targets = p.part + (int64_t)r * (p.K + 1) * p.S, *drawn = p.part + ((int64_t)p.R * (p.K + 1) + r * p.K) * p.S;
+    for (int i = wave; i <= n; i += kSegThreads / 64) {
+        const int y = i < n ? p.drafts[(int64_t)r * p.K + i] : 0;
+        const bool in = i < n && y < p.V;
+        const float u = p.u[(int64_t)r * (p.K + 1) + i];
+        const double z = in && !p.greedy ? (double)Piece<L>::one(p.z + (first + i) * p.ld + y) : 0.;
+        const double zq = in && p.d ? (double)Piece<L>::one(p.d + r * p.ld_request + i * p.ld_draft + y) : 0.;
+        const RowStat a = join_row(targets + i * p.S, p.S, p.c);
+        RowStat b{0.f, 0, 0.};
+        if (p.d && i < n) b = join_row(drawn + i * p.S, p.S, p.c);
+        bool yes = in && a.inv > 0.;
         if (p.greedy) {
             yes = yes && y == a.id;
         } else if (yes) {
-            const double z = (double)Piece<L>::one(p.z + (first + i) * p.ld + y);
             const double pr = exp((z - (double)a.m) * p.c.inv) * a.inv;
-            double q = 1.;
-            if (p.d) {
-                const RowStat b = join_row(p.part + ((int64_t)targets + r * p.K + i) * p.S, p.S, p.c);
-                const double zq = (double)Piece<L>::one(p.d + r * p.ld_request + i * p.ld_draft + y);
-                q = exp((zq - (double)b.m) * p.c.inv) * b.inv;
-                yes = b.inv > 0.;
-            }
-            yes = yes && (double)p.u[(int64_t)r * (p.K + 1) + i] * q < pr;
+            const double q = p.d ? exp((zq - (double)b.m) * p.c.inv) * b.inv : 1.;
+            yes = (!p.d || b.inv > 0.) && (double)u * q < pr;
         }
-        if (!yes && lane == 0) atomicMin(&s_stop, i);
+        if (lane == 0) {
+            s_p[i] = a;
+            s_q[i] = b;
+            if (i < n && !yes) atomicMin(&s_stop, i);
+        }
     }
     __syncthreads();
     const int j = s_stop;
     accepted = j;
-    if (wave == 0) {
-        const RowStat a = join_row(p.part + (int64_t)(r * (p.K + 1) + j) * p.S, p.S, p.c);
-        Verdict v{a.inv, 0., a.m, 0.f, kFromP, first + j};
-        if (!(a.inv > 0.)) v.kind = kNone;
-        else if (p.greedy) { v.kind = kToken; v.row = a.id; }
-        else if (j < n && p.d) {
-            const RowStat b = join_row(p.part + ((int64_t)targets + r * p.K + j) * p.S, p.S, p.c);
-            v.kind = b.inv > 0. ? kFromRest : kNone;
-            v.q_inv = b.inv;
-            v.q_m = b.m;
-        } else if (j < n) {
-            v.kind = kWithout;
-        }
-        if (lane == 0) s_v = v;
-    }
-    __syncthreads();
-    return s_v;
+    const RowStat a = s_p[j], b = s_q[j];
+    Verdict v{a.inv, b.inv, a.m, b.m, kFromP, first + j};
+    if (!(a.inv > 0.)) v.kind = kNone;
+    else if (p.greedy) { v.kind = kToken; v.row = a.id; }
+    else if (j < n && p.d) v.kind = b.inv > 0. ? kFromRest : kNone;
+    else if (j < n) v.kind = kWithout;
+    return v;
 }
-// The mass that id has in what the next token is drawn from.
+template <typename L> __device__ __forceinline__ void put_tokens(const VerifyParams<L> &p, int r, int j, int token) {
+    const int i = threadIdx.x;
+    if (i == 0) p.accepted[r] = j;
+    if (i <= p.K) p.tokens[(int64_t)r * (p.K + 1) + i] = i < j ? p.drafts[(int64_t)r * p.K + i] : i == j ? token : -1;
+}
+// What the next token is drawn from: the masses of a thread's logits of a segment.
 template <typename L> struct Masses {
-    Verdict v; ExpScale c; int without;
-    const L *p, *q;
-    __device__ __forceinline__ double of(float zp, float zq, int id) const {
+    Verdict v; ExpScale c; int without, lo, len;
+    SegRow<L> p, q;
+    __device__ __forceinline__ Masses(const VerifyParams<L> &a, const Verdict &v_, int r, int j, int seg)
+        : v(v_), c(a.c), without(-1), lo(seg * kSeg), len(min(kSeg, a.V - seg * kSeg)) {
+        p.load(a.z + v.row * a.ld, lo, len);
+        if (v.kind == kFromRest) q.load(a.d + r * a.ld_request + j * a.ld_draft, lo, len);
+        if (v.kind == kWithout) without = a.drafts[(int64_t)r * a.K + j] - lo;
+    }
+    __device__ __forceinline__ double of(float zp, float zq, int at) const {
         double x = (double)exp_diff(zp, v.p_m, c) * v.p_inv;
         if (v.kind == kFromRest) {
             x -= (double)exp_diff(zq, v.q_m, c) * v.q_inv;
             x = x > 0. ? x : 0.;
-        } else if (v.kind == kWithout && id == without) {
+        } else if (at == without) {
             x = 0.;
         }
         return x;
     }
+    __device__ __forceinline__ double get(int k, int e) const { return of(p.get(k, e), q.get(k, e), p.at(k, e)); }
+    __device__ __forceinline__ double tail() const { return of(p.tail, q.tail, p.tail_at(len)); }
 };
-template <typename L> __device__ __forceinline__ Masses<L> masses_of(const VerifyParams<L> &p, const Verdict &v, int r, int j) {
-    Masses<L> a{v, p.c, -1, p.z + v.row * p.ld, nullptr};
-    if (v.kind == kFromRest) a.q = p.d + r * p.ld_request + j * p.ld_draft;
-    if (v.kind == kWithout) a.without = p.drafts[(int64_t)r * p.K + j];
-    return a;
-}
-// A thread's masses of its elements of a segment, in turn.
-template <typename L, typename F> __device__ __forceinline__ void each_mass(const Masses<L> &a, int lo, int n, F f) {
-    float z[kSegEach];
-    each_of(a.p, lo, n, [&](float x, int, int k) { z[k] = x; });
-    if (a.q) {
-        each_of(a.q, lo, n, [&](float x, int id, int k) { f(a.of(z[k], x, id), id, k); });
-    } else {
-        constexpr int N = Piece<L>::N;
-#pragma unroll
-        for (int k = 0; k < kSegEach; ++k) {
-            const int id = lo + ((int)threadIdx.x + k / N * kSegThreads) * N + k % N;
-            f(a.of(z[k], 0.f, id), id, k);
-        }
-    }
-}
 
-template <typename L> __global__ __launch_bounds__(kSegThreads) void k_verify_masses(VerifyParams<L> p) {
-    __shared__ double s_s[kSegThreads / 64];
-    const int seg = blockIdx.x % p.S, r = blockIdx.x / p.S;
-    int first, j;
-    const int n = rows_of(p, r, first);
-    if (n < 0) {
-        if (seg == 0 && threadIdx.x == 0) {
-            p.verdict[r] = Verdict{0., 0., 0.f, 0.f, kNone, 0};
-            p.accepted[r] = 0;
+// Of 64 masses in order, a lane each: the first at which the running sum from `from` on
+// exceeds t, or (rounding, or a number that is none) the last that is positive; `from`
+// becomes the sum before it.
+__device__ __forceinline__ int crossing(double mine, double t, double &from) {
+    const int lane = threadIdx.x & 63;
+    double run = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const double b = __shfl_up(run, o);
+        if (lane >= o) run += b;
+    }
+    const uint64_t some = __ballot(mine > 0.), over = __ballot(from + run > t && mine > 0.);
+    const int at = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some | 1);
+    from += readlane_f64(run, at) - readlane_f64(mine, at);
+    return at;
+}
+// The token at which the running sum of a request's masses exceeds its number's share.
+template <typename L> __device__ __forceinline__ int draw_token(const VerifyParams<L> &p, Verdict v, int r, int j) {
+    constexpr int W = kSegThreads / 64, N = Piece<L>::N, P = kSegEach / N;
+    static_assert((P + 1) * W <= 64, "a lane for each wave and round");
+    __shared__ double s_sum[(P + 1) * W];
+    __shared__ int s_token;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    double mine = 0.;
+    if (lane < p.S) mine = __hip_atomic_load(p.mass + (int64_t)r * p.S + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const double u = (double)p.u[(int64_t)r * (p.K + 1) + p.K];
+    double all = wave_sum_f64(mine);
+    if (!(all > 0.)) {              // p is nowhere above q
+        v.kind = kFromP;
+        const SegPart x = p.part[(int64_t)(r * (p.K + 1) + j) * p.S + min(lane, p.S - 1)];
+        mine = lane < p.S && x.m != -INFINITY ? x.s * (double)exp_diff(x.m, v.p_m, p.c) * v.p_inv : 0.;
+        all = wave_sum_f64(mine);
+    }
+    const double t = u * all;
+    double from = 0.;
+    const int seg = crossing(mine, t, from);
+    // its elements by rounds of the workgroup's threads (the last: what is left behind the whole pieces) and waves
+    const Masses<L> x(p, v, r, j, seg);
+    double in[P + 1];
+#pragma unroll
+    for (int i = 0; i <= P; ++i) {
+        in[i] = i == P ? x.tail() : 0.;
+        if (i < P) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) in[i] += x.get(i, k);
         }
-        return;
+        const double sum = wave_sum_f64(in[i]);
+        if (lane == 0) s_sum[i * W + wave] = sum;
     }
-    const Verdict v = judge(p, r, n, first, j);
-    if (seg == 0 && threadIdx.x == 0) {
-        p.verdict[r] = v;
-        p.accepted[r] = j;
+    __syncthreads();
+    const int part = crossing(lane < (P + 1) * W ? s_sum[lane] : 0., t, from);
+    if (part % W == wave) {         // this wave has it: its lanes, then the lane's elements
+        double e = 0.;
+#pragma unroll
+        for (int i = 0; i <= P; ++i) e = part / W == i ? in[i] : e;
+        const int l = crossing(e, t, from);
+        int id = p.V - 1;
+        if (lane == l) {
+            bool found = false;
+#pragma unroll
+            for (int i = 0; i <= P; ++i) {
+                if (part / W != i) continue;
+                auto next = [&](double m, int at) {
+                    from += m;
+                    if (m > 0. && !found) {
+                        id = x.lo + at;
+                        found = from > t;
+                    }
+                };
+                if (i == P) next(x.tail(), x.p.tail_at(x.len));
+                else {
+#pragma unroll
+                    for (int k = 0; k < N; ++k) next(x.get(i, k), x.p.at(i, k));
+                }
+            }
+            s_token = id;
+        }
     }
-    if (v.kind == kNone || v.kind == kToken) return;
-    const Masses<L> a = masses_of(p, v, r, j);
-    const int lo = seg * kSeg;
-    double s = 0.;
-    each_mass(a, lo, min(kSeg, p.V - lo), [&](double x, int, int) { s += x; });
-    s = block_sum<kSegThreads>(s, s_s);
-    if (threadIdx.x == 0) p.mass[(int64_t)r * p.S + seg] = s;
+    __syncthreads();
+    return s_token;
 }
 
 template <typename L> __global__ __launch_bounds__(kSegThreads) void k_verify_tokens(VerifyParams<L> p) {
-    constexpr int W = kSegThreads / 64, N = Piece<L>::N, P = kSegEach / N;
-    __shared__ double s_sum[P][W];
-    __shared__ int s_id, s_last;
-    const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const Verdict was = p.verdict[r];
-    const int j = p.accepted[r];
-    int token = -1;
-    if (was.kind == kToken) token = was.row;
-    else if (was.kind != kNone) {
-        Verdict v = was;
-        double mine = lane < p.S ? p.mass[(int64_t)r * p.S + lane] : 0.;
-        if (!(wave_sum_f64(mine) > 0.)) {       // p is nowhere above q
-            v.kind = kFromP;
-            const SegPart x = p.part[(int64_t)(r * (p.K + 1) + j) * p.S + min(lane, p.S - 1)];
-            mine = lane < p.S && x.m != -INFINITY ? x.s * exp(((double)x.m - (double)v.p_m) * p.c.inv) * v.p_inv : 0.;
-        }
-        // the segment at which the running sum exceeds the number's share
-        double run = mine;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const double b = __shfl_up(run, o);
-            if (lane >= o) run += b;
-        }
-        const double all = readlane_f64(run, 63), t = (double)p.u[(int64_t)r * (p.K + 1) + p.K] * all;
-        const uint64_t some = __ballot(mine > 0.), over = __ballot(run > t && mine > 0.);
-        const int seg = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(some | 1);
-        const double before = __shfl(run, seg) - __shfl(mine, seg);
-        // its elements: the sums of each round's waves, then of the lanes before this one
-        const Masses<L> a = masses_of(p, v, r, j);
-        const int lo = seg * kSeg, len = min(kSeg, p.V - lo);
-        double x[kSegEach];
-        each_mass(a, lo, len, [&](double e, int, int k) { x[k] = e; });
-        double in[P];
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            double e = 0.;
-#pragma unroll
-            for (int k = 0; k < N; ++k) e += x[i * N + k];
-            in[i] = e;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const double b = __shfl_up(in[i], o);
-                if (lane >= o) in[i] += b;
-            }
-            if (lane == 63) s_sum[i][wave] = in[i];
-            in[i] -= e;
-        }
-        if (tid == 0) { s_id = p.V; s_last = -1; }
-        __syncthreads();
-        double base = before;
-        int found = p.V, last = -1;
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            double at = base;
-#pragma unroll
-            for (int w = 0; w < W; ++w) {
-                if (w < wave) at += s_sum[i][w];
-                base += s_sum[i][w];
-            }
-            at += in[i];
-#pragma unroll
-            for (int k = 0; k < N; ++k) {
-                at += x[i * N + k];
-                const int id = lo + (tid + i * kSegThreads) * N + k;
-                if (x[i * N + k] > 0.) {
-                    last = id;
-                    if (at > t && id < found) found = id;
-                }
-            }
-        }
-        if (found < p.V) atomicMin(&s_id, found);
-        if (last >= 0) atomicMax(&s_last, last);
-        __syncthreads();
-        token = s_id < p.V ? s_id : s_last;     // (rounding may leave the last one's sum short of its share)
-    }
-    if (tid <= p.K) {
-        const int i = tid;
-        p.tokens[(int64_t)r * (p.K + 1) + i] = i < j ? p.drafts[(int64_t)r * p.K + i] : i == j ? token : -1;
-    }
-}
-// Greedy: no masses.
-template <typename L> __global__ __launch_bounds__(kSegThreads) void k_verify_greedy(VerifyParams<L> p) {
-    const int r = blockIdx.x;
-    int first, j = 0, token = -1;
+    __shared__ double s_s[kSegThreads / 64];
+    __shared__ int s_done;
+    const int seg = p.greedy ? 0 : blockIdx.x % p.S, r = p.greedy ? blockIdx.x : blockIdx.x / p.S;
+    int first, j = 0;
     const int n = rows_of(p, r, first);
-    if (n >= 0) {
-        const Verdict v = judge(p, r, n, first, j);
-        if (v.kind == kToken) token = v.row;
+    Verdict v{0., 0., 0.f, 0.f, kNone, 0};
+    if (n >= 0) v = judge(p, r, drafts_of(p, r, n), first, j);
+    if (v.kind == kNone || v.kind == kToken) {
+        if (seg == 0) put_tokens(p, r, j, v.kind == kToken ? v.row : -1);
+        return;
     }
-    const int i = threadIdx.x;
-    if (i == 0) p.accepted[r] = j;
-    if (i <= p.K) p.tokens[(int64_t)r * (p.K + 1) + i] = i < j ? p.drafts[(int64_t)r * p.K + i] : i == j ? token : -1;
+    const Masses<L> x(p, v, r, j, seg);
+    double s = x.tail();
+#pragma unroll
+    for (int k = 0; k < kSegEach / Piece<L>::N; ++k)
+#pragma unroll
+        for (int e = 0; e < Piece<L>::N; ++e) s += x.get(k, e);
+    s = block_sum<kSegThreads>(s, s_s);
+    // the last to have written its mass goes on (the first launch has cleared the count)
+    if (threadIdx.x == 0) {
+        __hip_atomic_store(p.mass + (int64_t)r * p.S + seg, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        // (both are agent-wide by themselves and the one is there before the other: no cache has to be written back)
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        s_done = __hip_atomic_fetch_add(p.done + r, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (s_done != p.S - 1) return;
+    put_tokens(p, r, j, draw_token(p, v, r, j));
 }
 
 static int segments(int V) { return (V + kSeg - 1) / kSeg; }
 static int64_t verify_bytes(int R, int K, int V) {
     const int64_t S = segments(V);
-    return (int64_t)R * (2 * K + 1) * S * (int64_t)sizeof(SegPart) + R * S * 8 + (int64_t)R * sizeof(Verdict);
+    return (int64_t)R * (2 * K + 1) * S * (int64_t)sizeof(SegPart) + R * S * 8 + (int64_t)R * 4;
 }
 static bool verify_sizes_ok(int R, int K, int V) {
     return R >= 0 && R <= 65535 && K >= 0 && K <= 63 && V >= 1 && V <= kOpdMaxVocab &&
@@ -374,13 +347,11 @@ static int verify(int32_t R, int32_t K, int32_t V, int32_t rows, const L *z, int
     VerifyParams<L> p{z, ld, d, ld_request, ld_draft, starts, drafts, u, R, K, V, rows, segments(V), greedy,
                       exp_scale(greedy ? 1. : temperature), tokens, accepted, (SegPart *)work, nullptr, nullptr};
     p.mass = (double *)(p.part + (int64_t)R * (2 * K + 1) * p.S);
-    p.verdict = (Verdict *)(p.mass + (int64_t)R * p.S);
+    p.done = (int32_t *)(p.mass + (int64_t)R * p.S);
     hipStream_t s = (hipStream_t)stream;
     const int64_t lines = (int64_t)R * (K + 1) + (d ? (int64_t)R * K : 0);
-    bool ok = launch(k_verify_rows<L>, (unsigned)(lines * p.S), kSegThreads, 0, s, p);
-    if (greedy) ok = ok && launch(k_verify_greedy<L>, (unsigned)R, kSegThreads, 0, s, p);
-    else ok = ok && launch(k_verify_masses<L>, (unsigned)(R * p.S), kSegThreads, 0, s, p) &&
-              launch(k_verify_tokens<L>, (unsigned)R, kSegThreads, 0, s, p);
+    const bool ok = launch(k_verify_rows<L>, (unsigned)(lines * p.S), kSegThreads, 0, s, p) &&
+                    launch(k_verify_tokens<L>, (unsigned)(greedy ? R : R * p.S), kSegThreads, 0, s, p);
     return ok ? PIPO_OK : PIPO_EHIP;
 }
 
