@@ -176,13 +176,28 @@ template <typename L> struct AppendParams {
     int rows, chunk, blocks, n_kv, D, shift;    // block = 1 << shift
 };
 
-// x / s rounded to nearest even, from the product with 1 / s and what it leaves,
-// which one fma gives exactly.
-__device__ __forceinline__ float round_to(float x, float s, float inv) {
-    float q = rintf(x * inv);
-    const float e = fmaf(-q, s, x), a = fabsf(e), h = 0.5f * s;
-    if (a > h || (a == h && ((int)q & 1))) q += copysignf(1.f, e);
-    return fminf(fmaxf(q, -127.f), 127.f);
+// Sixteen x / s rounded to nearest even, as bytes 128 + x / s: the product with 1 / s
+// rounded, unless what that leaves, which one fma gives exactly, is half a step or more.
+__device__ __forceinline__ u32x4 round16(const float *x, float s, float inv) {
+    float q[16];
+    const float h = 0.5f * s;
+    bool near = false;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        q[i] = rintf(x[i] * inv);
+        near |= fabsf(fmaf(-q[i], s, x[i])) >= h;
+    }
+    if (near) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float e = fmaf(-q[i], s, x[i]), a = fabsf(e);
+            if (a > h || (a == h && ((int)q[i] & 1))) q[i] += copysignf(1.f, e);
+        }
+    }
+    u32x4 w{0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) w[i >> 2] = __builtin_amdgcn_cvt_pk_u8_f32(q[i] + 128.f, i & 3, w[i >> 2]);
+    return w;
 }
 // q old / s likewise, in 64 bits: the product has more digits than a float.
 __device__ __forceinline__ int round_again(int u, double old, double s, double inv) {
@@ -194,45 +209,51 @@ __device__ __forceinline__ int round_again(int u, double old, double s, double i
 }
 
 // A workgroup takes the blocks whose first row is among `chunk` rows, of one head, keys
-// or values: the block's rows by token (the last row of a token counts), their
-// largest magnitude, the scale, and the tiles with new bytes.  A thread holds 16
-// dimensions of IT tokens.  Bound by latency at a step's single tokens, by what it
-// reads and writes at a prompt's.
+// or values: their largest magnitude, the scale, and the tiles with new bytes.  A thread
+// holds 16 dimensions of IT tokens.  Rows that follow one another as their slots do, as a
+// rule, are found by their number; others by a table of tokens (of rows with one slot the
+// last).  Bound by latency at a step's single tokens, by what it reads and writes at a
+// prompt's.
 template <typename L, int NT, int IT> __global__ __launch_bounds__(NT) void k_kv8_append(AppendParams<L> p) {
     extern __shared__ uint8_t s_stage[];        // values: [block][D + 16] bytes
-    __shared__ int s_row[256], s_end;
+    __shared__ int s_row[256];
     __shared__ uint32_t s_top[NT / 64];
-    const int tid = threadIdx.x, head = blockIdx.y, which = blockIdx.z;
+    const int tid = threadIdx.x, lane = tid & 63, head = blockIdx.y, which = blockIdx.z;
     const int B = 1 << p.shift, D = p.D, E = D >> 4;
     const L *x = p.x[which] + (int64_t)head * D;
     const int64_t ld = p.ld[which];
     const int from = blockIdx.x * p.chunk, upto = min(from + p.chunk, p.rows);
-    auto block_of = [&](int i) {
-        const int s = p.slots[i];
-        return s >= 0 && (s >> p.shift) < p.blocks ? s >> p.shift : -1;
-    };
+    auto slot_of = [&](int i) { return i >= 0 && i < p.rows ? p.slots[i] : -1; };
+    auto block_of = [&](int slot) { return slot >= 0 && (slot >> p.shift) < p.blocks ? slot >> p.shift : -1; };
     // the rows that begin a block's run, one a lane
-    const int lane = tid & 63, own = from + lane < upto ? block_of(from + lane) : -1;
-    const int before = own >= 0 && from + lane > 0 ? block_of(from + lane - 1) : -1;
-    for (uint64_t runs = __ballot(own >= 0 && own != before); runs; runs &= runs - 1) {
+    const int slot = slot_of(from + lane), own = block_of(slot), before = block_of(slot_of(from + lane - 1));
+    uint64_t runs = __ballot(from + lane < upto && own >= 0 && own != before);
+    while (runs) {
         const int at = __builtin_ctzll(runs), first = from + at, blk = __builtin_amdgcn_readlane(own, at);
-        // the run's rows by token
-        for (int i = tid; i < B; i += NT) s_row[i] = -1;
-        if (tid == 0) s_end = p.rows;
-        __syncthreads();
-        for (int i0 = first;; i0 += NT) {
-            const int i = i0 + tid;
-            const bool mine = i < p.rows && block_of(i) == blk;
-            if (i < p.rows && !mine) atomicMin(&s_end, i);
+        const int off0 = __builtin_amdgcn_readlane(slot, at) & (B - 1);
+        runs &= runs - 1;
+        float *scale = p.scales + ((int64_t)blk * p.n_kv + head) * 2 + which;
+        const float was = *scale;
+        // how far the run goes, and whether its slots count up
+        int n = 0;
+        bool straight = true;
+        for (;;) {
+            const int s = slot_of(first + n + lane);
+            const uint64_t in = __ballot(block_of(s) == blk);
+            const int k = in == ~0ull ? 64 : __builtin_ctzll(~in);
+            straight = straight && !__ballot(lane < k && (s & (B - 1)) != off0 + n + lane);
+            n += k;
+            if (k < 64) break;
+        }
+        if (!straight) {
+            for (int i = tid; i < B; i += NT) s_row[i] = -1;
             __syncthreads();
-            const int end = s_end;
-            if (mine && i < end) atomicMax(&s_row[p.slots[i] & (B - 1)], i);
-            if (end <= i0 + NT) break;
+            for (int i = tid; i < n; i += NT) atomicMax(&s_row[p.slots[first + i] & (B - 1)], first + i);
             __syncthreads();
         }
-        __syncthreads();
-        float *scale = p.scales + ((int64_t)blk * p.n_kv + head) * 2 + which;
-        const float held = s_row[0] >= 0 ? 0.f : *scale;
+        auto row_of = [&](int t) { return straight ? (t >= off0 && t < off0 + n ? first + t - off0 : -1) : s_row[t]; };
+        const bool anew = row_of(0) >= 0;
+        const float held = anew ? 0.f : was;
         uint8_t *store = p.store[which] + ((int64_t)blk * p.n_kv + head) * B * D;
         // item: a token's 16 dimensions; tokens fastest within 16, as the key tiles have them
         auto token = [&](int it) { const int i = tid + it * NT; return i / (E * 16) * 16 + (i & 15); };
@@ -241,7 +262,7 @@ template <typename L, int NT, int IT> __global__ __launch_bounds__(NT) void k_kv
         uint32_t top = 0;
 #pragma unroll
         for (int it = 0; it < IT; ++it) {
-            const int row = s_row[token(it)];
+            const int row = row_of(token(it));
             if (row < 0) continue;
             const L *at = x + row * ld + group(it) * 16;
             constexpr int N = Piece<L>::N;
@@ -266,28 +287,21 @@ template <typename L, int NT, int IT> __global__ __launch_bounds__(NT) void k_kv
         if (s < 0x1p-126f) s = 0.f;
         const bool finite = __float_as_uint(s) < 0x7F800000u;
         const float inv = finite && s > 0.f ? 1.f / s : 0.f;
-        const bool grown = s_row[0] < 0 && !(s == held);
+        const bool grown = !anew && !(s == held);
         const double inv64 = grown && inv > 0.f ? 1. / (double)s : 0.;
         if (tid == 0) *scale = s;
         auto codes = [&](const float *f) {
-            u32x4 w;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                w[k] = 0;
-#pragma unroll
-                for (int b = 0; b < 4; ++b)
-                    w[k] |= (uint32_t)(128 + (inv > 0.f ? (int)round_to(f[4 * k + b], s, inv) : 0)) << 8 * b;
-            }
-            return w;
+            const u32x4 zero{0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
+            return inv > 0.f ? round16(f, s, inv) : zero;
         };
         auto again = [&](u32x4 w) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
+#pragma unroll 1
+            for (int k = 0; k < 4; ++k) {       // (a word at a time, the words in turn: few registers for what is rare)
                 uint32_t r = 0;
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
-                    r |= (uint32_t)(inv64 > 0. ? round_again((w[k] >> 8 * b) & 255, held, s, inv64) : 128) << 8 * b;
-                w[k] = r;
+                    r |= (uint32_t)(inv64 > 0. ? round_again((w[0] >> 8 * b) & 255, held, s, inv64) : 128) << 8 * b;
+                w = u32x4{w[1], w[2], w[3], r};
             }
             return w;
         };
@@ -296,14 +310,14 @@ template <typename L, int NT, int IT> __global__ __launch_bounds__(NT) void k_kv
             for (int it = 0; it < IT; ++it) {
                 const int t = token(it);
                 u32x4 *at = (u32x4 *)store + key_piece(t, group(it), D);
-                if (s_row[t] >= 0) *at = codes(v[it]);
+                if (row_of(t) >= 0) *at = codes(v[it]);
                 else if (grown) *at = again(*at);
             }
         } else {
             const int pitch = D + 16;
 #pragma unroll
             for (int it = 0; it < IT; ++it)
-                if (s_row[token(it)] >= 0) *(u32x4 *)(s_stage + token(it) * pitch + group(it) * 16) = codes(v[it]);
+                if (row_of(token(it)) >= 0) *(u32x4 *)(s_stage + token(it) * pitch + group(it) * 16) = codes(v[it]);
             __syncthreads();
 #pragma unroll
             for (int it = 0; it < IT; ++it) {
@@ -311,7 +325,7 @@ template <typename L, int NT, int IT> __global__ __launch_bounds__(NT) void k_kv
                 const int t = tile / (D >> 5) * 32 + ((i & 63) >> 4) * 4, e = tile % (D >> 5) * 32 + (i & 15);
                 uint32_t fresh = 0;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) fresh |= (uint32_t)(s_row[t + (k >> 2) * 16 + (k & 3)] >= 0) << k;
+                for (int k = 0; k < 8; ++k) fresh |= (uint32_t)(row_of(t + (k >> 2) * 16 + (k & 3)) >= 0) << k;
                 if (!fresh && !grown) continue;
                 u32x4 *at = (u32x4 *)store + i;
                 u32x4 w{};
@@ -328,7 +342,7 @@ template <typename L, int NT, int IT> __global__ __launch_bounds__(NT) void k_kv
                 *at = w;
             }
         }
-        __syncthreads();
+        if (runs) __syncthreads();
     }
 }
 
@@ -391,7 +405,7 @@ static int append(const pipo_kv8 *c, int32_t rows, const L *k, int64_t ld_k, con
     AppendParams<L> p{{k, v}, {ld_k, ld_v}, {c->keys, c->values}, c->scales, d_slots, rows, 1, c->blocks, c->n_kv,
                       c->head_dim, log2_of(c->block)};
     // a workgroup's rows: single tokens of many requests one by one, prompts' rows by the block
-    p.chunk = rows <= 256 ? 1 : rows >= 64 * 256 ? 64 : (rows + 255) / 256;
+    p.chunk = rows <= 256 ? 1 : rows >= 32 * 128 ? 64 : (rows + 255) / 256;
     const int items = c->block * c->head_dim / 16;
     hipStream_t s = (hipStream_t)stream;
     const bool ok = items == 128   ? launch_append<L, 128, 1>(p, s)
