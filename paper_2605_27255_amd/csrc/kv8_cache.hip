@@ -355,33 +355,59 @@ template <typename L> struct ReadParams {
     int rows, blocks, n_kv, D, shift;
 };
 
-// A thread reads 16 dimensions of a row and head.
+// A wave reads eight rows of a head: a lane 16 dimensions of a row's keys, and of the
+// values, where a token's bytes lie 16 apart, 16 lanes a dimension each of four rows, whose
+// bytes are neighbours if their slots are.  Bound by HBM at many rows.
 template <typename L> __global__ __launch_bounds__(256) void k_kv8_read(ReadParams<L> p) {
-    const int E = p.D >> 4;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)p.rows * p.n_kv * E;
-    if (i >= all) return;
-    const int e = (int)(i % E), head = (int)(i / E % p.n_kv), row = (int)(i / E / p.n_kv);
-    const int slot = p.slots[row], blk = slot >> p.shift, t = slot & ((1 << p.shift) - 1);
-    float k[16], v[16];
-    if (slot >= 0 && blk < p.blocks) {
-        const int64_t at = (int64_t)blk * p.n_kv + head;
-        const float2 s = *(const float2 *)(p.scales + at * 2);
-        const uint8_t *ks = p.keys + (at << p.shift) * p.D, *vs = p.values + (at << p.shift) * p.D;
-        const u32x4 w = ((const u32x4 *)ks)[key_piece(t, e, p.D)];
-#pragma unroll
-        for (int d = 0; d < 16; ++d) {
-            k[d] = (float)((int)(w[d >> 2] >> 8 * (d & 3) & 255) - 128) * s.x;
-            v[d] = (float)((int)vs[value_byte(t, e * 16 + d, p.D)] - 128) * s.y;
-        }
-    } else {
-#pragma unroll
-        for (int d = 0; d < 16; ++d) k[d] = v[d] = 0.f;
-    }
     constexpr int N = Piece<L>::N;
+    const int lane = threadIdx.x & 63, head = blockIdx.y * 4 + (threadIdx.x >> 6), row0 = blockIdx.x * 8;
+    if (head >= p.n_kv) return;
+    const int B = 1 << p.shift, E = p.D >> 4;
+    const int slot = row0 + (lane & 7) < p.rows ? p.slots[row0 + (lane & 7)] : -1;      // (eight lanes a row's)
+    const bool there = slot >= 0 && (slot >> p.shift) < p.blocks;
+    const int at = there ? slot : 0;
+    const int64_t place = (int64_t)(at >> p.shift) * p.n_kv + head;
+    float2 scale = make_float2(0.f, 0.f);
+    if (there) scale = *(const float2 *)(p.scales + place * 2);
+    // keys
+    {
+        const int i = lane / E, e = lane % E;       // (D = 64: half of the lanes)
+        const int64_t b = (((int64_t)__shfl((int)(place >> 32), i & 7) << 32) | (uint32_t)__shfl((int)place, i & 7)) * B * p.D;
+        const int t = __shfl(at, i & 7) & (B - 1), ok = __shfl((int)there, i & 7);
+        const float s = __shfl(scale.x, i & 7);
+        if (i < 8 && row0 + i < p.rows) {
+            float k[16];
+            u32x4 w{};
+            if (ok) w = *((const u32x4 *)(p.keys + b) + key_piece(t, e, p.D));
 #pragma unroll
-    for (int d = 0; d < 16; d += N) {
-        *(u32x4 *)(p.k + i * 16 + d) = Piece<L>::pack(k + d);
-        *(u32x4 *)(p.v + i * 16 + d) = Piece<L>::pack(v + d);
+            for (int d = 0; d < 16; ++d) k[d] = ok ? (float)((int)(w[d >> 2] >> 8 * (d & 3) & 255) - 128) * s : 0.f;
+            L *to = p.k + (((int64_t)(row0 + i) * p.n_kv + head) * E + e) * 16;
+#pragma unroll
+            for (int d = 0; d < 16; d += N) *(u32x4 *)(to + d) = Piece<L>::pack(k + d);
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int i = 4 * h + (lane >> 4), d = lane & 15;
+        const int64_t b = (((int64_t)__shfl((int)(place >> 32), i) << 32) | (uint32_t)__shfl((int)place, i)) * B * p.D;
+        const int t = __shfl(at, i) & (B - 1), ok = __shfl((int)there, i);
+        const float s = __shfl(scale.y, i);
+        if (row0 + i >= p.rows) continue;
+        L *to = p.v + ((int64_t)(row0 + i) * p.n_kv + head) * p.D + d;
+        const uint8_t *from = p.values + b;
+        if (p.D == 128) {
+            uint8_t u[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[e] = ok ? from[value_byte(t, 16 * e + d, 128)] : 128;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) Piece<L>::put(to + 16 * e, ok ? (float)((int)u[e] - 128) * s : 0.f);
+        } else {
+            uint8_t u[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[e] = ok ? from[value_byte(t, 16 * e + d, 64)] : 128;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) Piece<L>::put(to + 16 * e, ok ? (float)((int)u[e] - 128) * s : 0.f);
+        }
     }
 }
 
@@ -422,9 +448,9 @@ static int read_rows(const pipo_kv8 *c, int32_t rows, const int32_t *d_slots, L 
     if (rows == 0) return PIPO_OK;
     if (!kv8_aligned(d_slots, 4) || !kv8_aligned(k, 16) || !kv8_aligned(v, 16)) return PIPO_EINVAL;
     ReadParams<L> p{c->keys, c->values, c->scales, d_slots, k, v, rows, c->blocks, c->n_kv, c->head_dim, log2_of(c->block)};
-    const int64_t all = (int64_t)rows * c->n_kv * (c->head_dim / 16);
-    if (all > (int64_t)256 * 0x7FFFFFFF) return PIPO_EINVAL;
-    return launch(k_kv8_read<L>, (unsigned)((all + 255) / 256), 256, 0, (hipStream_t)stream, p) ? PIPO_OK : PIPO_EHIP;
+    void *ptrs[] = {(void *)&p};
+    return hipLaunchKernel((const void *)k_kv8_read<L>, dim3((rows + 7) / 8, (c->n_kv + 3) / 4), dim3(256), ptrs, 0,
+                           (hipStream_t)stream) == hipSuccess ? PIPO_OK : PIPO_EHIP;
 }
 
 }  // namespace pipo
