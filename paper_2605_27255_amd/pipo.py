@@ -513,27 +513,25 @@ def opd_policy(logits, labels, advantages, old_logp=None, ref_logp=None, clip=(0
 
 # ---- drafted tokens verified over a paged 8-bit cache -----------------------------------------------------------------
 
-def _serve_call(name, dt, device, *args):
+# (torch is handed down: these calls take some 10 us of host time, an import statement 0.3 of them)
+
+def _serve_call(torch, name, device, *args):
     """Calls a serving entry on the current stream of `device`, which is the current one."""
-    import torch
-    lib = _lib or load_library()
-    rc = getattr(lib, name + dt)(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    rc = getattr(_lib or load_library(), name)(*args, torch._C._cuda_getCurrentRawStream(device.index))
     if rc != PIPO_OK:
-        raise PipoError(rc, f"{name}{dt}: " + ("sizes, strides or values outside the documented ranges"
-                                               if rc == PIPO_EINVAL else "launch failure"))
+        raise PipoError(rc, f"{name}: " + ("sizes, strides or values outside the documented ranges"
+                                           if rc == PIPO_EINVAL else "launch failure"))
 
 
-def _int32(x, name, device, shape):
+def _int32(torch, x, name, device, shape):
     """The address of a contiguous int32 tensor of that shape on that device."""
-    import torch
     if (getattr(x, "dtype", None) is not torch.int32 or x.shape != shape or x.device != device or not x.is_contiguous()):
         _refuse(f"{name}: a contiguous int32 tensor of shape {tuple(shape)} on {device}")
     return x.data_ptr()
 
 
-def _head_rows(x, name, heads, D, device, dtype=None):
+def _head_rows(torch, x, name, heads, D, device, dtype=None):
     """The row stride of a [rows, heads, D] tensor of fp32 or bf16 whose rows are contiguous, and the library's suffix."""
-    import torch
     dt = x.dtype if isinstance(x, torch.Tensor) else None
     if (dt is not torch.float32 and dt is not torch.bfloat16) or x.dim() != 3 or x.device != device or (dtype and dt is not dtype):
         _refuse(f"{name}: a tensor [rows, heads, {D}] of {dtype or 'float32 or bfloat16'} on {device}, not {dt}")
@@ -555,18 +553,20 @@ class Kv8Cache:
 
     def __init__(self, keys, values, scales):
         import torch
-        ok = all(isinstance(x, torch.Tensor) and x.is_cuda and x.is_contiguous() for x in (keys, values, scales))
-        if not ok or keys.dim() != 6 or keys.dtype is not torch.uint8 or values.dtype is not torch.uint8:
-            _refuse("keys, values: contiguous uint8 CUDA tensors of six dimensions, scales float32")
-        P, H, T, C = keys.shape[:4]
-        if (keys.shape[4:] != (64, 16) or values.shape != (P, H, T // 2, 2 * C, 64, 16) or scales.shape != (P, H, 2)
-                or scales.dtype is not torch.float32 or values.device != keys.device or scales.device != keys.device
-                or 16 * T not in (32, 64, 128, 256) or C not in (1, 2) or P < 1 or not 1 <= H <= 256 or P * T * 16 >= 2 ** 31
-                or (keys.data_ptr() | values.data_ptr()) & 15 or scales.data_ptr() & 7):
+        for x in (keys, values, scales):
+            if not isinstance(x, torch.Tensor) or not x.is_cuda or not x.is_contiguous():
+                _refuse("keys, values, scales: contiguous CUDA tensors")
+        if keys.dim() != 6 or keys.dtype is not torch.uint8 or values.dtype is not torch.uint8 or scales.dtype is not torch.float32:
+            _refuse("keys, values: uint8 tensors of six dimensions, scales float32")
+        P, H, T, C, lanes, piece = keys.shape
+        dev, k, v, s = keys.device, keys.data_ptr(), values.data_ptr(), scales.data_ptr()
+        if (lanes != 64 or piece != 16 or values.shape != (P, H, T // 2, 2 * C, 64, 16) or scales.shape != (P, H, 2)
+                or values.device != dev or scales.device != dev or T not in (2, 4, 8, 16) or C not in (1, 2) or P < 1
+                or not 1 <= H <= 256 or P * T * 16 >= 2 ** 31 or (k | v) & 15 or s & 7):
             _refuse(f"a cache's tensors do not fit together: {tuple(keys.shape)}, {tuple(values.shape)}, {tuple(scales.shape)}")
-        self.keys, self.values, self.scales, self.device = keys, values, scales, keys.device
+        self.keys, self.values, self.scales, self.device = keys, values, scales, dev
         self.blocks, self.n_kv, self.block, self.head_dim = P, H, 16 * T, 64 * C
-        self.c = PipoKv8(keys.data_ptr(), values.data_ptr(), scales.data_ptr(), P, H, 64 * C, 16 * T)
+        self.c = PipoKv8(k, v, s, P, H, 64 * C, 16 * T)
 
     @classmethod
     def new(cls, blocks: int, n_kv: int, head_dim: int, block: int = 64, device="cuda"):
@@ -604,13 +604,13 @@ def kv8_plan(lens, new, tables, held, free, n_free, rows: int, block: int):
     if not 0 <= rows <= 1 << 20:
         _refuse(f"rows: from 0 to {1 << 20}, not {rows}")
     one = (R,)
-    ins = (_int32(lens, "lens", dev, one), _int32(new, "new", dev, one), _int32(tables, "tables", dev, (R, W)),
-           _int32(held, "held", dev, one), _int32(free, "free", dev, (P,)), _int32(n_free, "n_free", dev, (1,)))
-    out = torch.empty(2 * (R + rows) + 1, dtype=torch.int32, device=dev)
-    starts, total, slots, positions = out[:R + 1], out[R + 1:2 * R + 1], out[2 * R + 1:2 * R + 1 + rows], out[2 * R + 1 + rows:]
-    _serve_call("pipo_kv8_plan", "", dev, R, W, block, P, *ins, rows, starts.data_ptr(), total.data_ptr(),
+    ins = (_int32(torch, lens, "lens", dev, one), _int32(torch, new, "new", dev, one), _int32(torch, tables, "tables", dev, (R, W)),
+           _int32(torch, held, "held", dev, one), _int32(torch, free, "free", dev, (P,)), _int32(torch, n_free, "n_free", dev, (1,)))
+    out = torch.empty(2 * (R + rows) + 1, dtype=torch.int32, device=dev).split_with_sizes((R + 1, R, rows, rows))
+    starts, total, slots, positions = out = tuple(out)
+    _serve_call(torch, "pipo_kv8_plan", dev, R, W, block, P, *ins, rows, starts.data_ptr(), total.data_ptr(),
                 slots.data_ptr(), positions.data_ptr())
-    return starts, total, slots, positions
+    return out
 
 
 def kv8_append(cache, k, v, slots):
@@ -623,12 +623,12 @@ def kv8_append(cache, k, v, slots):
     if _elsewhere(cache.keys):
         with torch.cuda.device(dev):
             return kv8_append(cache, k, v, slots)
-    ld_k, dt = _head_rows(k, "k", cache.n_kv, cache.head_dim, dev)
-    ld_v, _ = _head_rows(v, "v", cache.n_kv, cache.head_dim, dev, k.dtype)
+    ld_k, dt = _head_rows(torch, k, "k", cache.n_kv, cache.head_dim, dev)
+    ld_v, _ = _head_rows(torch, v, "v", cache.n_kv, cache.head_dim, dev, k.dtype)
     if v.shape[0] != k.shape[0]:
         _refuse("k and v: as many rows")
-    _serve_call("pipo_kv8_append", dt, dev, ctypes.byref(cache.c), k.shape[0], k.data_ptr(), ld_k, v.data_ptr(), ld_v,
-                _int32(slots, "slots", dev, (k.shape[0],)))
+    _serve_call(torch, "pipo_kv8_append" + dt, dev, ctypes.byref(cache.c), k.shape[0], k.data_ptr(), ld_k, v.data_ptr(), ld_v,
+                _int32(torch, slots, "slots", dev, (k.shape[0],)))
 
 
 def kv8_read(cache, slots, dtype=None):
@@ -644,10 +644,10 @@ def kv8_read(cache, slots, dtype=None):
     if dtype is not torch.float32 and dtype is not torch.bfloat16:
         _refuse(f"dtype: float32 or bfloat16, not {dtype}")
     n = slots.numel() if isinstance(slots, torch.Tensor) else 0
-    at = _int32(slots, "slots", dev, (n,))
+    at = _int32(torch, slots, "slots", dev, (n,))
     k = torch.empty((n, cache.n_kv, cache.head_dim), dtype=dtype, device=dev)
     v = torch.empty_like(k)
-    _serve_call("pipo_kv8_read", "" if dtype is torch.float32 else "_bf16", dev, ctypes.byref(cache.c), n, at,
+    _serve_call(torch, "pipo_kv8_read" if dtype is torch.float32 else "pipo_kv8_read_bf16", dev, ctypes.byref(cache.c), n, at,
                 k.data_ptr(), v.data_ptr())
     return k, v
 
@@ -667,27 +667,28 @@ def kv8_attention(q, cache, tables, starts, total, scale=None, max_len=None, out
         with torch.cuda.device(dev):
             return kv8_attention(q, cache, tables, starts, total, scale, max_len, out)
     D = cache.head_dim
-    ld, dt = _head_rows(q, "q", 0, D, dev)
+    ld, dt = _head_rows(torch, q, "q", 0, D, dev)
     rows, n_q = q.shape[:2]
     if n_q % cache.n_kv or n_q // cache.n_kv > 16:
         _refuse(f"q: 1 to 16 query heads for each of {cache.n_kv} heads of the cache, not {n_q} in all")
     if getattr(tables, "ndim", 0) != 2 or tables.shape[0] < 1 or tables.shape[1] < 1:
         _refuse("tables: an int32 tensor [R, width]")
     R, W = tables.shape
-    ptrs = _int32(tables, "tables", dev, (R, W)), W, _int32(starts, "starts", dev, (R + 1,)), _int32(total, "total", dev, (R,))
+    ptrs = _int32(torch, tables, "tables", dev, (R, W)), W, _int32(torch, starts, "starts", dev, (R + 1,)), _int32(torch, total, "total", dev, (R,))
     most = W * cache.block if max_len is None else int(max_len)
     if not 1 <= most <= W * cache.block or W * cache.block >= 2 ** 31:
         _refuse(f"max_len: from 1 to {W * cache.block}, not {most}")
     if out is None:
-        out = torch.empty((rows, n_q, D), dtype=q.dtype, device=dev)
-    ld_out, _ = _head_rows(out, "out", n_q, D, dev, q.dtype)
-    if out.shape != q.shape:
-        _refuse("out: a tensor of q's shape")
+        out, ld_out = torch.empty((rows, n_q, D), dtype=q.dtype, device=dev), n_q * D
+    else:
+        ld_out, _ = _head_rows(torch, out, "out", n_q, D, dev, q.dtype)
+        if out.shape != q.shape:
+            _refuse("out: a tensor of q's shape")
     lib, work = _lib or load_library(), None
     n = lib.pipo_kv8_attention_work_bytes(ctypes.byref(cache.c), R, rows, n_q, most, bool(dt))
     if n:
         work = torch.empty(n, dtype=torch.uint8, device=dev)
-    _serve_call("pipo_kv8_attention", dt, dev, ctypes.byref(cache.c), R, rows, n_q, q.data_ptr(), ld, *ptrs, most,
+    _serve_call(torch, "pipo_kv8_attention" + dt, dev, ctypes.byref(cache.c), R, rows, n_q, q.data_ptr(), ld, *ptrs, most,
                 D ** -0.5 if scale is None else scale, out.data_ptr(), ld_out, work.data_ptr() if n else None, n)
     return out
 
@@ -711,11 +712,11 @@ def verify_drafts(logits, drafts, u, draft_logits=None, starts=None, temperature
     if getattr(drafts, "ndim", 0) != 2 or drafts.shape[1] > 63:
         _refuse("drafts: an int32 tensor [R, K], K up to 63")
     R, K = drafts.shape
-    at = _int32(drafts, "drafts", dev, (R, K))
+    at = _int32(torch, drafts, "drafts", dev, (R, K))
     _, u_at = _opd_args(dev, (None, "", None, None), (u, "u", torch.float32, (R, K + 1)))
     starts_at = None
     if starts is not None:
-        starts_at = _int32(starts, "starts", dev, (R + 1,))
+        starts_at = _int32(torch, starts, "starts", dev, (R + 1,))
     elif rows != R * (K + 1):
         _refuse(f"logits: {R * (K + 1)} rows, or starts")
     if u is None:
@@ -733,7 +734,7 @@ def verify_drafts(logits, drafts, u, draft_logits=None, starts=None, temperature
     accepted = torch.empty(R, dtype=torch.int32, device=dev)
     n = (_lib or load_library()).pipo_verify_work_bytes(R, K, V)
     work = torch.empty(n, dtype=torch.uint8, device=dev)
-    _serve_call("pipo_verify_drafts", dt, dev, R, K, V, rows, logits.data_ptr(), ld, starts_at, at, d_at, lr, ln, u_at,
+    _serve_call(torch, "pipo_verify_drafts" + dt, dev, R, K, V, rows, logits.data_ptr(), ld, starts_at, at, d_at, lr, ln, u_at,
                 temperature, tokens.data_ptr(), accepted.data_ptr(), work.data_ptr(), n)
     return tokens, accepted
 
