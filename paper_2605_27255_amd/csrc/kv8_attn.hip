@@ -530,14 +530,14 @@ static Kv8Shape shape_of(int R, int rows, int n_q, int n_kv, int D, int max_len,
     const int tiles = (max_len + 31) / 32;
     s.split = s.nct < most || units < 1024;
     // Key ranges: what fills the chip in whole rounds.  A unit takes its prologue (about as long as three tiles of a
-    // wave) and a quarter of its tiles, the joining launch two and what it reads.  (Workgroups that a compute unit holds
+    // wave) and a quarter of its tiles, the joining launch eight (its launch) and what it reads.  (Workgroups that a compute unit holds
     // by their registers; 32 x 8192 tokens, 256 units, in 3 / 4 / 8 / 12 ranges: 89 / 95 / 95 / 100 us.)
     const int slots = 256 * (D == 64 ? (s.nct == 1 ? 4 : 3) : (s.nct == 1 ? 3 : 2));
     s.S = 1;
     double best = 1e300;
     for (int S = 1; work && s.split && S <= 64 && 4 * S <= tiles + 3; ++S) {
         const int64_t rounds = (units * S + slots - 1) / slots;
-        const double t = (double)rounds * (((tiles + S - 1) / S + 3) / 4 + 3) + (S > 1 ? 2. + S / 16. : 0.);
+        const double t = (double)rounds * (((tiles + S - 1) / S + 3) / 4 + 3) + (S > 1 ? 8. + S / 16. : 0.);
         if (t < best) { best = t; s.S = S; }
     }
     s.chunk = (tiles + s.S - 1) / s.S;

@@ -294,24 +294,28 @@ template <typename L, int NT, int IT> __global__ __launch_bounds__(NT) void k_kv
             const u32x4 zero{0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
             return inv > 0.f ? round16(f, s, inv) : zero;
         };
-        auto again = [&](u32x4 w) {
+        if (grown) {                // what the block holds, to the new scale
 #pragma unroll 1
-            for (int k = 0; k < 4; ++k) {       // (a word at a time, the words in turn: few registers for what is rare)
-                uint32_t r = 0;
+            for (int i = tid; i < B * E; i += NT) {
+                u32x4 w = ((u32x4 *)store)[i];
+#pragma unroll 1
+                for (int k = 0; k < 4; ++k) {       // (a word at a time, the words in turn: few registers for what is rare)
+                    uint32_t r = 0;
 #pragma unroll
-                for (int b = 0; b < 4; ++b)
-                    r |= (uint32_t)(inv64 > 0. ? round_again((w[0] >> 8 * b) & 255, held, s, inv64) : 128) << 8 * b;
-                w = u32x4{w[1], w[2], w[3], r};
+                    for (int b = 0; b < 4; ++b)
+                        r |= (uint32_t)(inv64 > 0. ? round_again((w[0] >> 8 * b) & 255, held, s, inv64) : 128) << 8 * b;
+                    w = u32x4{w[1], w[2], w[3], r};
+                }
+                ((u32x4 *)store)[i] = w;
             }
-            return w;
-        };
+            __syncthreads();
+        }
         if (which == 0) {
 #pragma unroll
             for (int it = 0; it < IT; ++it) {
                 const int t = token(it);
                 u32x4 *at = (u32x4 *)store + key_piece(t, group(it), D);
                 if (row_of(t) >= 0) *at = codes(v[it]);
-                else if (grown) *at = again(*at);
             }
         } else {
             const int pitch = D + 16;
@@ -326,13 +330,10 @@ template <typename L, int NT, int IT> __global__ __launch_bounds__(NT) void k_kv
                 uint32_t fresh = 0;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) fresh |= (uint32_t)(row_of(t + (k >> 2) * 16 + (k & 3)) >= 0) << k;
-                if (!fresh && !grown) continue;
+                if (!fresh) continue;
                 u32x4 *at = (u32x4 *)store + i;
                 u32x4 w{};
-                if (fresh != 255) {
-                    w = *at;
-                    if (grown) w = again(w);
-                }
+                if (fresh != 255) w = *at;
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
                     if (!(fresh >> (k & 7) & 1)) continue;
