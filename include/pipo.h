@@ -362,7 +362,7 @@ int pipo_opd_policy_bf16(int32_t T, int32_t V, const uint16_t *d_logits, int64_t
  * or found no blocks (whose d_held and table stay as they were).  d_slots and d_positions [rows]: slot and position of each new
  * token, -1 for tokens of a request with total 0 and behind the last one.
  *
- * pipo_kv8_append: rows i of d_k and d_v ([n_kv][head_dim] each, fp32 or bf16, row
+ * pipo_kv8_append: rows i (up to 2^20) of d_k and d_v ([n_kv][head_dim] each, fp32 or bf16, row
  * stride ld elements) into slot d_slots[i] (negative: not at all; of rows with one slot
  * the last counts).  Rows of one block have to be consecutive.  A block whose first slot
  * is written begins anew with s = max|x| / 127 of its written rows; else s only grows,
@@ -372,14 +372,16 @@ int pipo_opd_policy_bf16(int32_t T, int32_t V, const uint16_t *d_logits, int64_t
  * head, until the block begins anew.
  *
  * pipo_kv8_read: the values of the slots d_slots[i] as rows i of d_k and d_v
- * ([rows][n_kv][head_dim], fp32 or bf16); zeros where there is no such slot.
+ * ([rows][n_kv][head_dim], fp32 or bf16, 16-byte aligned; up to 2^26 rows); zeros where
+ * there is no such slot.
  *
  * pipo_kv8_attention: rows d_starts[r] .. d_starts[r+1]-1 of d_q ([n_q][head_dim], row stride
  * ld_q; n_q / n_kv whole, up to 16) are the last tokens of request r's d_total[r]: row i sees the
  * keys up to its own position d_total[r] - d_starts[r+1] + i, query head h those
  * of KV head h * n_kv / n_q.  d_out row i = sum softmax(scale q.k) v, rounded once
  * to the type of q; zeros for a row that sees no key; rows outside
- * [d_starts[0], d_starts[R]) are not written.  No request may have more than max_len tokens (up to
+ * [d_starts[0], d_starts[R]) are not written.  (rows n_q / n_kv / 16 + R) n_kv < 2^24; d_out
+ * must not overlap d_q.  No request may have more than max_len tokens (up to
  * width * block; what is behind max_len is not seen).  d_work as for the OPD losses
  * (pipo_kv8_attention_work_bytes); with NULL each row's keys are not split over
  * workgroups, which is slower for few long requests.
@@ -400,7 +402,8 @@ int pipo_opd_policy_bf16(int32_t T, int32_t V, const uint16_t *d_logits, int64_t
  * accepted drafts, the token behind them, then -1; d_accepted [R] their number.
  * A row with a NaN or +inf, or without any token of positive probability, accepts no draft, and gives
  * the token -1; a request without rows has 0 and only -1.  A draft without a row of its own and one behind it is not looked at.
- * R up to 65535, K from 0 to 63, V and ld as for the OPD losses. */
+ * K from 0 to 63, V and ld as for the OPD losses, R up to 65535 and R (2 K + 1) ceil(V / 8192) < 2^24.
+ * d_work is needed here. */
 typedef struct {
     uint8_t *keys, *values;         /* device [blocks][n_kv][block * head_dim], 16-byte aligned */
     float *scales;                  /* device [blocks][n_kv][2], 8-byte aligned                 */

@@ -335,7 +335,7 @@ static int64_t verify_bytes(int R, int K, int V) {
 }
 static bool verify_sizes_ok(int R, int K, int V) {
     return R >= 0 && R <= 65535 && K >= 0 && K <= 63 && V >= 1 && V <= kOpdMaxVocab &&
-           (int64_t)R * (2 * K + 1) * segments(V) < (int64_t)1 << 31;
+           (int64_t)R * (2 * K + 1) * segments(V) < (int64_t)1 << 24;      // (a launch's threads are counted in 32 bits)
 }
 
 template <typename L>

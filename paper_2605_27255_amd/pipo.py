@@ -660,7 +660,8 @@ def kv8_attention(q, cache, tables, starts, total, scale=None, max_len=None, out
     sees the tokens up to its own.  scale: of the scores (None: 1 /
     sqrt(head_dim)); max_len: no request has more tokens (None: the tables'
     width), fewer make better use of the GPU; out: where to write (None: a new
-    tensor; rows that belong to no request are not written).  Returns out."""
+    tensor; rows that belong to no request are not written).  Returns out (autograd
+    does not follow it)."""
     import torch
     dev = _cache(cache)
     if _elsewhere(cache.keys):
@@ -678,18 +679,23 @@ def kv8_attention(q, cache, tables, starts, total, scale=None, max_len=None, out
     most = W * cache.block if max_len is None else int(max_len)
     if not 1 <= most <= W * cache.block or W * cache.block >= 2 ** 31:
         _refuse(f"max_len: from 1 to {W * cache.block}, not {most}")
+    wanted = out
     if out is None:
         out, ld_out = torch.empty((rows, n_q, D), dtype=q.dtype, device=dev), n_q * D
     else:
         ld_out, _ = _head_rows(torch, out, "out", n_q, D, dev, q.dtype)
         if out.shape != q.shape:
             _refuse("out: a tensor of q's shape")
+        if torch.is_grad_enabled() and out.requires_grad:
+            _refuse("out: a tensor that requires no gradient (but under torch.no_grad())")
     lib, work = _lib or load_library(), None
     n = lib.pipo_kv8_attention_work_bytes(ctypes.byref(cache.c), R, rows, n_q, most, bool(dt))
     if n:
         work = torch.empty(n, dtype=torch.uint8, device=dev)
     _serve_call(torch, "pipo_kv8_attention" + dt, dev, ctypes.byref(cache.c), R, rows, n_q, q.data_ptr(), ld, *ptrs, most,
                 D ** -0.5 if scale is None else scale, out.data_ptr(), ld_out, work.data_ptr() if n else None, n)
+    if wanted is not None:
+        _opd_written(out)
     return out
 
 

@@ -423,7 +423,7 @@ def test_attention_a_bad_block_spoils_only_who_sees_it(dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("q_size,scale", [(1e-30, 1e28), (3e4, 1e-5), (1e30, 1e-31), (0.0, None), (1.0, -0.125), (40.0, None)])
+@pytest.mark.parametrize("q_size,scale", [(1e-30, 1e28), (3e4, 1e-5), (1e30, 1e-31), (0.0, None), (1.0, 0.0), (1.0, -0.125), (40.0, None)])
 def test_attention_scales(dtype, q_size, scale):
     rng = np.random.default_rng(13)
     c, tables = _paged(rng, [300], 1, 64, 128)
@@ -488,6 +488,84 @@ def test_attention_without_a_work_array_and_with_a_small_one():
         assert call(w, b) == pipo.PIPO_OK
         torch.cuda.synchronize()
         assert (np.abs(out.double().cpu().numpy() - want) <= _tolerance(want, size, top, 64, 3008, torch.float32)).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shift", [1, 3, 5])
+def test_rows_at_any_element(dtype, shift):
+    """Keys, values, queries and outputs that begin off the 16-byte grid, in rows of odd stride."""
+    rng = np.random.default_rng(20)
+    total, new, D = [70, 45], [3, 2], 64
+    c, tables = _paged(rng, total, 2, 32, D)
+    k, v = _kv(rng, 5, 2, D, dtype)
+    q = _bits(rng.standard_normal((5, 4, D)), dtype)
+    slots = np.array([tables[0, t // 32] * 32 + t % 32 for t in (67, 68, 69)] + [tables[1, t // 32] * 32 + t % 32 for t in (43, 44)])
+
+    def at(x):
+        n, h, _ = x.shape
+        ld = h * D + 7
+        flat = torch.full((n * ld + 16,), 7.0, dtype=dtype, device="cuda")
+        y = flat.as_strided((n, h, D), (ld, D, 1), shift)
+        y.copy_(torch.tensor(x).to(dtype))
+        return y
+
+    cache = to_gpu(c)
+    _api().kv8_append(cache, at(k), at(v), _i32(slots))
+    c.append(k, v, slots)
+    assert_same_cache(cache, c)
+    out = at(np.zeros_like(q))
+    _api().kv8_attention(at(q), cache, _i32(tables), _i32([0, 3, 5]), _i32(total), out=out)
+    want, size, top = O.kv8_attention(q, c, tables, np.array([0, 3, 5]), np.array(total))
+    assert (np.abs(out.double().cpu().numpy() - want) <= _tolerance(want, size, top, D, 96, dtype)).all()
+    assert (out._base.as_strided((4, 7), (4 * D + 7, 1), shift + 4 * D) == 7.0).all()      # nothing between the rows
+
+
+def test_appends_on_two_streams_to_different_blocks():
+    rng = np.random.default_rng(21)
+    c = random_cache(rng, 40, 2, 64, 128)
+    cache = to_gpu(c)
+    parts = []
+    for i in range(2):
+        slots = np.concatenate([np.arange(64 * b, 64 * b + 64) for b in range(20 * i, 20 * i + 20)])
+        parts.append((slots, *_kv(rng, len(slots), 2, 128, torch.bfloat16)))
+    gpu = [(_i32(s), torch.tensor(k).bfloat16().cuda(), torch.tensor(v).bfloat16().cuda()) for s, k, v in parts]
+    torch.cuda.synchronize()
+    for i in range(2):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            _api().kv8_append(cache, gpu[i][1], gpu[i][2], gpu[i][0])
+    for s, k, v in parts:
+        c.append(k, v, s)
+    assert_same_cache(cache, c)
+
+
+def test_python_calls_refuse_what_does_not_fit():
+    A = _api()
+    cache = A.Kv8Cache.new(4, 2, 64)
+    assert (cache.blocks, cache.n_kv, cache.block, cache.head_dim) == (4, 2, 64, 64)
+    x = torch.zeros((3, 2, 64), device="cuda")
+    q, i = torch.zeros((3, 4, 64), device="cuda"), lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")
+    t, s, n = i(1, 2), i(2), i(1)
+    bad = [lambda: A.Kv8Cache(cache.keys, cache.values[:3], cache.scales), lambda: A.Kv8Cache(cache.keys[:, :, ::2], cache.values, cache.scales),
+           lambda: A.Kv8Cache(cache.keys.char(), cache.values, cache.scales), lambda: A.Kv8Cache(cache.keys.cpu(), cache.values, cache.scales),
+           lambda: A.kv8_append(cache, x, x[:2], i(3)), lambda: A.kv8_append(cache, x, x.bfloat16(), i(3)),
+           lambda: A.kv8_append(cache, x.half(), x.half(), i(3)), lambda: A.kv8_append(cache, x, x, i(4)),
+           lambda: A.kv8_append(cache, x, x, i(3).long()), lambda: A.kv8_append(cache, x[:, :1], x[:, :1], i(3)),
+           lambda: A.kv8_append(cache, x.transpose(1, 2), x, i(3)), lambda: A.kv8_append(cache, x[:1].expand(3, 2, 64), x, i(3)),
+           lambda: A.kv8_read(cache, i(3), dtype=torch.float16), lambda: A.kv8_read(cache, i(3).cpu()),
+           lambda: A.kv8_attention(q[:, :3], cache, t, s, n), lambda: A.kv8_attention(q.half(), cache, t, s, n),
+           lambda: A.kv8_attention(q, cache, t, i(3), n), lambda: A.kv8_attention(q, cache, t, s, i(2)),
+           lambda: A.kv8_attention(q, cache, t, s, n, max_len=129), lambda: A.kv8_attention(q, cache, t, s, n, max_len=0),
+           lambda: A.kv8_attention(q, cache, t, s, n, scale=float("nan")), lambda: A.kv8_attention(q, cache, t, s, n, out=q[:2]),
+           lambda: A.kv8_attention(q, cache, t, s, n, out=q.bfloat16()),
+           lambda: A.kv8_attention(q, cache, t, s, n, out=torch.zeros_like(q, requires_grad=True)),
+           lambda: A.kv8_plan(i(2), i(2), i(2, 3), i(2), i(5), i(1), rows=4, block=48), lambda: A.kv8_plan(i(2), i(3), i(2, 3), i(2), i(5), i(1), rows=4, block=32),
+           lambda: A.kv8_plan(i(2), i(2), i(2, 3), i(2), i(5), i(1), rows=-1, block=32)]
+    for call in bad:
+        with pytest.raises(A.PipoError):
+            call()
+    # nothing to do is no error
+    A.kv8_append(cache, x[:0], x[:0], i(0))
+    assert A.kv8_read(cache, i(0))[0].shape == (0, 2, 64) and A.kv8_attention(q[:0], cache, t, s, n).shape == (0, 4, 64)
 
 
 def test_attention_same_bits_every_time():

@@ -233,3 +233,21 @@ def test_verify_captured_into_a_graph_and_on_two_streams():
         for x in got[i]:
             for y, z in zip(x, want[i]):
                 np.testing.assert_array_equal(y.cpu().numpy(), z)
+
+
+def test_python_calls_refuse_what_does_not_fit():
+    A = _api()
+    z, d, u = torch.zeros((8, 50), device="cuda"), torch.zeros((2, 3), dtype=torch.int32, device="cuda"), torch.zeros((2, 4), device="cuda")
+    q = torch.zeros((2, 3, 50), device="cuda")
+    bad = [lambda: A.verify_drafts(z[:7], d, u), lambda: A.verify_drafts(z, d.long(), u), lambda: A.verify_drafts(z, d, u[:, :3]),
+           lambda: A.verify_drafts(z, d, None), lambda: A.verify_drafts(z, d, u.double()), lambda: A.verify_drafts(z, d, u, q[:, :2]),
+           lambda: A.verify_drafts(z, d, u, q.bfloat16()), lambda: A.verify_drafts(z, d, u, q[:, :1].expand(2, 3, 50)),
+           lambda: A.verify_drafts(z, d, u, starts=d[0, :2]), lambda: A.verify_drafts(z, d, u, temperature=float("nan")),
+           lambda: A.verify_drafts(z, d, u, temperature=1e-7), lambda: A.verify_drafts(z.half(), d, u),
+           lambda: A.verify_drafts(torch.zeros((130, 5), device="cuda"), torch.zeros((2, 64), dtype=torch.int32, device="cuda"),
+                                   torch.zeros((2, 65), device="cuda"))]
+    for call in bad:
+        with pytest.raises(A.PipoError):
+            call()
+    t, a = A.verify_drafts(z[:0], d[:0], u[:0])
+    assert t.shape == (0, 4) and a.shape == (0,)

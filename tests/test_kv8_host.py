@@ -177,6 +177,7 @@ def test_attention_refusals(lib, dt):
 def test_verify_refusals(lib, dt):
     from paper_2605_27255_amd import PIPO_EINVAL, PIPO_OK
     need = lib.pipo_verify_work_bytes(2, 3, 50)
+    assert lib.pipo_verify_work_bytes(65535, 63, 1 << 19) == 0     # more workgroups than a launch has
     assert need > 0 and lib.pipo_verify_work_bytes(2, 64, 50) == 0 and lib.pipo_verify_work_bytes(-1, 3, 50) == 0
     base = dict(R=2, K=3, V=50, rows=8, z=A, ld=50, starts=None, drafts=A, d=A, lr=150, ln=50, u=A, t=1.0, tokens=A, accepted=A,
                 work=A, bytes=need, stream=None)
