@@ -100,11 +100,12 @@ template <int ROWS> __device__ __forceinline__ int tiles_of(const Kv8Attn &p, co
 }
 
 // The four waves of a workgroup share a row group and cut its key range into four
-// (SPLIT), or take a row group each.
+// (SPLIT), or take a quarter of a group of four times the rows each, and share the tiles: each
+// wave makes a quarter of a tile's bytes to operands, which all of them read from LDS.
 template <typename L, int D, int NCT, bool SPLIT>
 __global__ __launch_bounds__(256, (NCT > 2 || (NCT > 1 && sizeof(L) == 4)) ? 1 : 2) void k_kv8_attn(Kv8Attn p) {
     constexpr bool PAIR = sizeof(L) == 4, DEEP = NCT == 1;
-    constexpr int ROWS = 16 * NCT, NC = D / 64, NT = D / 16, NV = D / 32;
+    constexpr int ROWS = 16 * NCT, GROUP = SPLIT ? ROWS : 4 * ROWS, NC = D / 64, NT = D / 16, NV = D / 32;
     const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     int x = blockIdx.x;
@@ -115,13 +116,14 @@ __global__ __launch_bounds__(256, (NCT > 2 || (NCT > 1 && sizeof(L) == 4)) ? 1 :
     if (!SPLIT) {
         // A prompt's later rows see more tokens and go first; where every workgroup is resident at once (two a compute
         // unit), the second half goes the other way round, so that a unit has long and short ones.
-        const int n = (p.groups + 3) >> 2, half = (n + 1) >> 1;
-        f = (n * p.n_kv <= 512 + p.n_kv && f >= half ? f - half : n - 1 - f) * 4 + wave;
+        const int n = p.groups, half = (n + 1) >> 1;
+        f = n * p.n_kv <= 512 + p.n_kv && f >= half ? f - half : n - 1 - f;
     }
     RowGroup rg;
     int total;
-    if (f >= p.groups || !find_group<ROWS>(p, f, rg, total)) return;
-    const int tiles = tiles_of<ROWS>(p, rg, total);
+    if (f >= p.groups || !find_group<GROUP>(p, f, rg, total)) return;
+    const int tiles = tiles_of<GROUP>(p, rg, total);
+    if (!SPLIT) rg.row0 += wave * ROWS;
     const int t_lo = split * p.chunk, t_hi = min(t_lo + p.chunk, tiles);
     if (t_lo >= t_hi && split > 0) return;
     const int n_split = tiles > 0 ? (tiles + p.chunk - 1) / p.chunk : 1;
@@ -172,6 +174,32 @@ __global__ __launch_bounds__(256, (NCT > 2 || (NCT > 1 && sizeof(L) == 4)) ? 1 :
         const int bi = load_keys(to, t);
         load_values(to);
         load_scales(to, bi);
+    };
+    // !SPLIT: this wave's pieces of the next tile, and the operands of two tiles (keys, then values)
+    constexpr int OPS = 4 * NC + NT, OWN = (2 * NC + NV) / 4;
+    __shared__ u32x4 s_op[SPLIT ? 1 : 2][SPLIT ? 1 : OPS][64];
+    u32x4 raw[OWN];
+    auto load_share = [&](int t) {
+        const int tc = min(t, tb - 1), b = tc >> sh;
+        if (b - blk0 >= 64) load_ids(b);
+        const int bi = b - blk0, bid = __builtin_amdgcn_readlane(id, bi);
+        off = ((((int64_t)max(bid, 0) * p.n_kv + head) << p.shift) + ((tc & ((1 << sh) - 1)) << 5)) * D;
+#pragma unroll
+        for (int u = 0; u < OWN; ++u) {
+            const int piece = wave + 4 * u;
+            raw[u] = *((const u32x4 *)((piece < 2 * NC ? p.keys : p.values) + off) + (piece < 2 * NC ? piece : piece - 2 * NC) * 64 + lane);
+        }
+        return bi;
+    };
+    auto put_share = [&](int at) {
+#pragma unroll
+        for (int u = 0; u < OWN; ++u) {
+            const int piece = wave + 4 * u;
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                s_op[SPLIT ? 0 : at][SPLIT ? 0 : 2 * piece + e][lane] =
+                    piece < 2 * NC && !PAIR ? tiny8(raw[u][2 * e], raw[u][2 * e + 1]) : widen8(raw[u][2 * e], raw[u][2 * e + 1]);
+        }
     };
     if (ta < tb) load_ids(ta >> sh);
     // this lane's query rows
@@ -246,7 +274,13 @@ __global__ __launch_bounds__(256, (NCT > 2 || (NCT > 1 && sizeof(L) == 4)) ? 1 :
         for (int t = 0; t < NT; ++t) o[ct][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     typedef f32x4 Scores[NCT][2];
-    auto score = [&](const Tile &b, Scores &st) {
+    auto score = [&](const Tile &b, Scores &st, int share) {
+        u32x4 ka[SPLIT ? 1 : 4 * NC];
+        if constexpr (!SPLIT) {
+#pragma unroll
+            for (int i = 0; i < 4 * NC; ++i) ka[i] = s_op[share][i][lane];
+            __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct)
 #pragma unroll
@@ -257,7 +291,9 @@ __global__ __launch_bounds__(256, (NCT > 2 || (NCT > 1 && sizeof(L) == 4)) ? 1 :
             for (int c = 0; c < NC; ++c)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const u32x4 a = PAIR ? widen8(b.k[u][c][2 * e], b.k[u][c][2 * e + 1]) : tiny8(b.k[u][c][2 * e], b.k[u][c][2 * e + 1]);
+                    const u32x4 a = !SPLIT ? ka[SPLIT ? 0 : (u * NC + c) * 2 + e]
+                                    : PAIR ? widen8(b.k[u][c][2 * e], b.k[u][c][2 * e + 1])
+                                           : tiny8(b.k[u][c][2 * e], b.k[u][c][2 * e + 1]);
 #pragma unroll
                     for (int ct = 0; ct < NCT; ++ct) {
                         st[ct][u] = mfma16_f16(a, qh[ct][c][e], st[ct][u]);
@@ -266,9 +302,15 @@ __global__ __launch_bounds__(256, (NCT > 2 || (NCT > 1 && sizeof(L) == 4)) ? 1 :
                 }
     };
     // A tile's probabilities, and what they add to l and O.
-    auto tile_as = [&](const Tile &b, int t0, const Scores &st, auto all) {
+    auto tile_as = [&](const Tile &b, int t0, const Scores &st, int share, auto all) {
         constexpr bool whole = decltype(all)::value;    // every row sees all of it
         if (!b.there) return;       // no such block: its tokens are not there
+        u32x4 va[SPLIT ? 1 : NT];
+        if constexpr (!SPLIT) {     // asked for before the exponentials
+#pragma unroll
+            for (int d = 0; d < NT; ++d) va[d] = s_op[share][4 * NC + d][lane];
+            __builtin_amdgcn_sched_barrier(0);
+        }
         float s[NCT][8], mx[NCT], fk[NCT], ck[NCT];
         bool rise = false;
 #pragma unroll
@@ -343,7 +385,7 @@ __global__ __launch_bounds__(256, (NCT > 2 || (NCT > 1 && sizeof(L) == 4)) ? 1 :
         }
 #pragma unroll
         for (int d = 0; d < NT; ++d) {
-            const u32x4 a = widen8(b.v[d >> 1][2 * (d & 1)], b.v[d >> 1][2 * (d & 1) + 1]);
+            const u32x4 a = !SPLIT ? va[SPLIT ? 0 : d] : widen8(b.v[d >> 1][2 * (d & 1)], b.v[d >> 1][2 * (d & 1) + 1]);
 #pragma unroll
             for (int ct = 0; ct < NCT; ++ct) {
                 if constexpr (PAIR) {
@@ -364,31 +406,56 @@ __global__ __launch_bounds__(256, (NCT > 2 || (NCT > 1 && sizeof(L) == 4)) ? 1 :
         Scores st;
         int t = ta;
         const int tw = all_see >> 5;            // tiles before this one are seen whole
-        load_tile(buf[0], ta);
-        if constexpr (DEEP) {       // two tiles on their way
+        if constexpr (!SPLIT) {
+            Tile &now = buf[0], next{};
+            int bi = load_share(t);
+            load_scales(now, bi);
+            put_share(0);
+            bi = load_share(t + 1);
+            load_scales(next, bi);
+            __syncthreads();
+            int at = 0;
+            auto one = [&](auto all) {
+                score(now, st, at);
+                put_share(at ^ 1);              // (nobody reads it since the last barrier)
+                bi = load_share(t + 2);
+                tile_as(now, t * 32, st, at, all);
+                now.there = next.there;
+                now.sk = next.sk;
+                now.sv = next.sv;
+                load_scales(next, bi);
+                __syncthreads();
+                at ^= 1;
+                ++t;
+            };
+            while (t < min(tb, tw)) one(std::true_type{});
+            while (t < tb) one(std::false_type{});
+        } else if constexpr (DEEP) {            // two tiles on their way
+            load_tile(buf[0], ta);
             load_tile(buf[1], ta + 1);
             auto two = [&](auto all) {
-                score(buf[0], st);
-                tile_as(buf[0], t * 32, st, all);
+                score(buf[0], st, 0);
+                tile_as(buf[0], t * 32, st, 0, all);
                 load_tile(buf[0], t + 2);
-                score(buf[1], st);
-                tile_as(buf[1], t * 32 + 32, st, all);
+                score(buf[1], st, 0);
+                tile_as(buf[1], t * 32 + 32, st, 0, all);
                 load_tile(buf[1], t + 3);
                 t += 2;
             };
             while (t + 2 < min(tb, tw + 1)) two(std::true_type{});
             while (t + 2 < tb) two(std::false_type{});
-            score(buf[0], st);
-            tile_as(buf[0], t * 32, st, std::false_type{});
+            score(buf[0], st, 0);
+            tile_as(buf[0], t * 32, st, 0, std::false_type{});
             if (t + 1 < tb) {
-                score(buf[1], st);
-                tile_as(buf[1], t * 32 + 32, st, std::false_type{});
+                score(buf[1], st, 0);
+                tile_as(buf[1], t * 32 + 32, st, 0, std::false_type{});
             }
         } else {                    // the next tile's keys while this one's values are used, its values while its keys are
+            load_tile(buf[0], ta);
             auto one = [&](auto all) {
-                score(buf[0], st);
+                score(buf[0], st, 0);
                 const int bi = load_keys(buf[0], t + 1);
-                tile_as(buf[0], t * 32, st, all);
+                tile_as(buf[0], t * 32, st, 0, all);
                 load_values(buf[0]);
                 load_scales(buf[0], bi);
                 ++t;
@@ -525,10 +592,10 @@ static Kv8Shape shape_of(int R, int rows, int n_q, int n_kv, int D, int max_len,
     const int64_t per = ((int64_t)(rows + R - 1) / R) * qpg;        // query rows of a request and KV head, on average
     s.nct = per <= 16 ? 1 : per <= 32 || most == 2 ? 2 : 4;
     const int64_t tile_rows = 16 * s.nct;
-    s.groups = (int)((int64_t)rows * qpg / tile_rows) + R;
     const int64_t units = (int64_t)R * ((per + tile_rows - 1) / tile_rows) * n_kv;
     const int tiles = (max_len + 31) / 32;
     s.split = s.nct < most || units < 1024;
+    s.groups = (int)((int64_t)rows * qpg / (s.split ? tile_rows : 4 * tile_rows)) + R;
     // Key ranges: what fills the chip in whole rounds.  A unit takes its prologue (about as long as three tiles of a
     // wave) and a quarter of its tiles, the joining launch eight (its launch) and what it reads.  (Workgroups that a compute unit holds
     // by their registers; 32 x 8192 tokens, 256 units, in 3 / 4 / 8 / 12 ranges: 89 / 95 / 95 / 100 us.)
@@ -547,7 +614,7 @@ static Kv8Shape shape_of(int R, int rows, int n_q, int n_kv, int D, int max_len,
 }
 
 template <typename L, int D, int NCT, bool SPLIT> static bool run_attn(const Kv8Attn &p, hipStream_t s) {
-    const int64_t grid = (int64_t)(SPLIT ? p.groups * (int64_t)p.S : (p.groups + 3) / 4) * p.n_kv;     // (!SPLIT: S is 1)
+    const int64_t grid = (int64_t)p.groups * p.S * p.n_kv;
     if (!launch(k_kv8_attn<L, D, NCT, SPLIT>, (unsigned)grid, 256, 0, s, p)) return false;
     return p.S == 1 || launch(k_kv8_attn_join<L, D, NCT>, (unsigned)(p.groups * p.n_kv), 256, 0, s, p);
 }
