@@ -4,13 +4,24 @@
 // and a range of 32-token tiles.  Scores are computed transposed, S^T[token][row] =
 // K Q^T, so that a lane's accumulators belong to one row, and the probabilities
 // are already the B operand of O^T[dim][row] += V^T P^T in the value tiles' token
-// order.  The bytes become fp16 exactly (1024 + u by a byte permutation, less
-// 1152), the scales go into the scores and into what each tile adds to O.  Queries
-// are brought to magnitudes below 2^15 by a power of two for each row, and probabilities are
-// kept as 2^14 times themselves, so that fp16's exponents hold them; bf16 queries
-// are then fp16 numbers (parts below 2^-38 of the row's largest are lost), and probabilities
-// lose 2^-12 of themselves, an eighth of what the output's rounding to bf16 costs.  fp32
-// queries, and their probabilities, go in as hi + lo fp16 pairs (2^-22), two MFMAs each.
+// order.  Value bytes become fp16 exactly (1024 + u by a byte permutation, less
+// 1152); key bytes go in as fp16's smallest numbers, u 2^-24, for bf16 queries, whose
+// scores are then less 128 times the query's sum, and like the values for fp32 ones.
+// Scales go into the scores and into the probabilities (fp32: into what a tile adds to
+// O).  Queries are brought to magnitudes below 2^15 by a power of two for each row, and
+// probabilities are kept as a power of two times themselves, so that fp16's exponents hold
+// them: bf16 queries are then fp16 numbers (parts below 2^-38 of the row's largest are
+// lost), and probabilities lose 2^-12 of themselves, an eighth of what the output's rounding
+// to bf16 costs.  fp32 queries, and their probabilities, go in as hi + lo fp16
+// pairs (2^-22), two MFMAs each.
+// Few rows: HBM-bound, a key range a workgroup, its waves a quarter each, whose (m, l, o)
+// meet in LDS and, of several ranges, in a second launch.  32 requests x 8192 tokens, 32/8
+// heads of 128: 83-86 us for 537 MB, 6.3 TB/s, and 4 us for the second launch; 8 x 16384 x 3
+// queries in fp32 49 us, 5.4 TB/s (a third of it the two prologues' and the last
+// workgroups' time).  Many rows (a prompt): bound by the waves' instructions, exponentials
+// and conversions (about 720 cycles a tile of 32 rows) beside the matrix cores'
+// (544), two waves a SIMD: 2048 queries on 6144 tokens 272 us, 880 TFLOP/s; each
+// wave converting its own tiles 281, 64 rows a wave 525, a rescaled O every tile 1169.
 #include "kv8.h"
 #include <math.h>
 #include <type_traits>

@@ -10,6 +10,9 @@
 // element.  Exponentials are fp32 of exact differences, masses fp32 products of them
 // (added eight, or in fp32 rows four, at a time); sums are added, in a fixed order, and
 // compared in 64 bits.
+// 64 requests of four drafts over 151936 bf16 logits: 30 us (5.9 TB/s of row bytes) and 20
+// (judging 5, two rows a request from the memory-side cache, the draw 5); one request of
+// one draft 4 and 9, latency.  Segments of 16384 in the second launch: 22.
 #include "kv8.h"
 
 namespace pipo {
