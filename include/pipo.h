@@ -334,7 +334,7 @@ int pipo_opd_policy_bf16(int32_t T, int32_t V, const uint16_t *d_logits, int64_t
  *
  * The cache is `blocks` blocks of `block` tokens (32, 64, 128 or 256), each of
  * n_kv heads (1 to 256) x head_dim (64 or 128).  A byte u stands for (u - 128) s, with one
- * scale s for each block, head, and keys (scales[0]) or values (scales[1]).
+ * scale s >= 0 for each block, head, and keys (scales[0]) or values (scales[1]).
  * Token t, dimension e of a block's keys and values lie at byte
  *   keys    ((t/16 * head_dim/64 + e/64) * 64 + 16 (e%64/16) + t%16) * 16 + e%16
  *   values  ((t/32 * head_dim/32 + e/32) * 64 + 16 (t%16/4) + e%16) * 16

@@ -541,7 +541,7 @@ __global__ __launch_bounds__(256, (NCT > 2 || (NCT > 1 && sizeof(L) == 4)) ? 1 :
 // The key ranges' records of a row as one: a wave a row, D / 64 dimensions a lane, a lane a range's weight.  Where
 // a row's records lie does not hang on whose row it is: the first ones are asked for along with the lengths.
 template <typename L, int D, int NCT> __global__ __launch_bounds__(256) void k_kv8_attn_join(Kv8Attn p) {
-    constexpr int ROWS = 16 * NCT, E = D / 64, U = 8;
+    constexpr int ROWS = 16 * NCT, E = D / 64, U = 16;
     typedef __attribute__((ext_vector_type(E))) float vec;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int head = blockIdx.x % p.n_kv, f = blockIdx.x / p.n_kv;

@@ -146,6 +146,14 @@ def test_plan_refuses_requests_one_by_one(R):
     check_plan(lens, new, (tables, held, free, 0), 4 * R, block)
 
 
+def test_plan_of_more_requests_than_lds_holds():
+    rng = np.random.default_rng(7)
+    R = 5000
+    lens, new = rng.integers(0, 90, R), rng.integers(0, 4, R)
+    new[rng.random(R) < 0.1] = -1
+    check_plan(lens, new, _state(rng, lens, 32, 4, R), int(np.maximum(new, 0).sum()) + 1, 32)
+
+
 def test_plan_long_prompts():
     rng = np.random.default_rng(6)
     lens, new = np.array([0, 100, 4096, 7]), np.array([70001, 1, 30000, 0])
@@ -327,7 +335,7 @@ PATTERNS = {
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("pattern", sorted(PATTERNS))
-@pytest.mark.parametrize("heads", [(2, 2), (4, 1), (14, 2), (16, 1)])
+@pytest.mark.parametrize("heads", [(2, 2), (4, 1), (15, 3), (14, 2), (16, 1)])
 def test_attention(dtype, D, pattern, heads):
     n_q, n_kv = heads
     total, new = PATTERNS[pattern]
@@ -383,6 +391,18 @@ def test_attention_rows_that_see_nothing_and_blocks_that_are_not_there(dtype):
     check_attention(q, c, tables, starts, np.array(total), dtype, max_len=70)
     tables[:] = -1
     assert (check_attention(q, c, tables, starts, np.array(total), dtype)[:10] == 0).all()
+
+
+@pytest.mark.parametrize("R", [63, 64, 65, 300, 4097, 5000])
+def test_attention_of_many_requests(R):
+    """A lane looks at one request, or at the first of several: both sides of 64 and of 64 x 64."""
+    rng = np.random.default_rng(R)
+    total, new = rng.integers(0, 5, R), rng.integers(0, 3, R)
+    total[R // 2], new[R // 2], new[0] = 90, 7, 1
+    c, tables = _paged(rng, total, 1, 32, 64)
+    starts = np.concatenate([[0], np.cumsum(new)])
+    q = _bits(rng.standard_normal((starts[-1], 2, 64)), torch.bfloat16)
+    check_attention(q, c, tables, starts, total, torch.bfloat16)
 
 
 def test_attention_starts_that_leave_rows_out():
