@@ -37,6 +37,7 @@ struct Kv8Attn {
     int R, rows, W, blocks, n_kv, n_q, qpg, shift, max_len;     // block = 1 << shift
     int S, chunk;                   // key ranges of `chunk` tiles
     int groups;                     // row groups of all requests, counted from above
+    int few;                        // 0, or: requests of up to so many rows are the other launch's; that one has a group a request
     float scale;                    // of the scores, times log2(e)
     float *part;                    // [groups][n_kv][S][16 NCT][D + 2]
 };
@@ -104,6 +105,19 @@ template <int ROWS> __device__ __forceinline__ bool find_group(const Kv8Attn &p,
     g.last = min(max(total, 0), p.max_len);
     return g.row0 >= 0 && g.row0 < g.n * p.qpg;
 }
+// The same for either launch of a call: whether this one has the group.
+template <int ROWS, bool SPLIT> __device__ __forceinline__ bool own_group(const Kv8Attn &p, int f, RowGroup &g, int &total) {
+    if (SPLIT && p.few) {           // group f is request f
+        g.r = f;
+        g.first = max(p.starts[f], 0);
+        g.n = min(p.starts[f + 1], p.rows) - g.first;
+        total = p.total[f];
+        g.row0 = 0;
+        g.last = min(max(total, 0), p.max_len);
+        return g.n > 0 && g.n * p.qpg <= p.few;
+    }
+    return find_group<ROWS>(p, f, g, total) && (SPLIT || g.n * p.qpg > p.few);
+}
 // Tiles that the rows of a group see: up to its last token's position.
 template <int ROWS> __device__ __forceinline__ int tiles_of(const Kv8Attn &p, const RowGroup &g, int total) {
     const int i = min(g.row0 + ROWS, g.n * p.qpg) - 1, seen = min(total - g.n + i / p.qpg + 1, g.last);
@@ -114,7 +128,7 @@ template <int ROWS> __device__ __forceinline__ int tiles_of(const Kv8Attn &p, co
 // (SPLIT), or take a quarter of a group of four times the rows each, and share the tiles: each
 // wave makes a quarter of a tile's bytes to operands, which all of them read from LDS.
 template <typename L, int D, int NCT, bool SPLIT>
-__global__ __launch_bounds__(256, (NCT > 2 || (NCT > 1 && sizeof(L) == 4)) ? 1 : 2) void k_kv8_attn(Kv8Attn p) {
+__global__ __launch_bounds__(256, NCT > 1 && sizeof(L) == 4 ? 1 : 2) void k_kv8_attn(Kv8Attn p) {
     constexpr bool PAIR = sizeof(L) == 4, DEEP = NCT == 1;
     constexpr int ROWS = 16 * NCT, GROUP = SPLIT ? ROWS : 4 * ROWS, NC = D / 64, NT = D / 16, NV = D / 32;
     const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
@@ -132,7 +146,7 @@ __global__ __launch_bounds__(256, (NCT > 2 || (NCT > 1 && sizeof(L) == 4)) ? 1 :
     }
     RowGroup rg;
     int total;
-    if (f >= p.groups || !find_group<GROUP>(p, f, rg, total)) return;
+    if (f >= p.groups || !own_group<GROUP, SPLIT>(p, f, rg, total)) return;
     const int tiles = tiles_of<GROUP>(p, rg, total);
     if (!SPLIT) rg.row0 += wave * ROWS;
     const int t_lo = split * p.chunk, t_hi = min(t_lo + p.chunk, tiles);
@@ -557,7 +571,7 @@ template <typename L, int D, int NCT> __global__ __launch_bounds__(256) void k_k
     ask(v, wave, 0);
     RowGroup rg;
     int total;
-    if (!find_group<ROWS>(p, f, rg, total)) return;
+    if (!own_group<ROWS, true>(p, f, rg, total)) return;
     const int tiles = tiles_of<ROWS>(p, rg, total);
     const int n = (tiles + p.chunk - 1) / p.chunk;
     if (n <= 1) return;             // the unit wrote it out itself
@@ -595,45 +609,60 @@ template <typename L, int D, int NCT> __global__ __launch_bounds__(256) void k_k
 }
 
 // ---- shapes of a launch ----------------------------------------------------------------
-struct Kv8Shape { int nct, S, chunk, groups; bool split; int64_t part; };
-static Kv8Shape shape_of(int R, int rows, int n_q, int n_kv, int D, int max_len, int es, bool work) {
-    Kv8Shape s{};
-    constexpr int most = 2;
-    const int qpg = n_q / n_kv;
-    const int64_t per = ((int64_t)(rows + R - 1) / R) * qpg;        // query rows of a request and KV head, on average
-    s.nct = per <= 16 ? 1 : per <= 32 || most == 2 ? 2 : 4;
-    const int64_t tile_rows = 16 * s.nct;
-    const int64_t units = (int64_t)R * ((per + tile_rows - 1) / tile_rows) * n_kv;
-    const int tiles = (max_len + 31) / 32;
-    s.split = s.nct < most || units < 1024;
-    s.groups = (int)((int64_t)rows * qpg / (s.split ? tile_rows : 4 * tile_rows)) + R;
-    // Key ranges: what fills the chip in whole rounds.  A unit takes its prologue (about as long as three tiles of a
-    // wave) and a quarter of its tiles, the joining launch eight (its launch) and what it reads.  (Workgroups that a compute unit holds
-    // by their registers; 32 x 8192 tokens, 256 units, in 3 / 4 / 8 / 12 ranges: 89 / 95 / 95 / 100 us.)
-    const int slots = 256 * (D == 64 ? (s.nct == 1 ? 4 : 3) : (s.nct == 1 ? 3 : 2));
-    s.S = 1;
+// Tiles of rows a wave (nct), key ranges or shared tiles (split), row groups; S ranges of `chunk` tiles: of the launch
+// or, beside one of shared tiles, of the second one for requests of few rows.
+constexpr int kFewRows = 32;
+struct Kv8Shape { int nct, groups, S, chunk; bool split, second; int64_t part; };
+
+// Key ranges that fill the chip in whole rounds.  A unit takes its prologue (about as long as three tiles of a wave) and
+// a quarter of its tiles, a joining launch eight and what it reads.  slots: workgroups that the compute units hold by their
+// registers.  (32 x 8192 tokens, 256 units, 768 slots, in 3 / 4 / 8 / 12 ranges: 89 / 95 / 95 / 100 us.)
+static int key_ranges(int64_t units, int tiles, int slots) {
+    int best_S = 1;
     double best = 1e300;
-    for (int S = 1; work && s.split && S <= 64 && 4 * S <= tiles + 3; ++S) {
+    for (int S = 1; S <= 64 && 4 * S <= tiles + 3; ++S) {
         const int64_t rounds = (units * S + slots - 1) / slots;
         const double t = (double)rounds * (((tiles + S - 1) / S + 3) / 4 + 3) + (S > 1 ? 8. + S / 16. : 0.);
-        if (t < best) { best = t; s.S = S; }
+        if (t < best) { best = t; best_S = S; }
     }
+    return best_S;
+}
+static Kv8Shape shape_of(int R, int rows, int n_q, int n_kv, int D, int max_len, bool work) {
+    Kv8Shape s{};
+    const int qpg = n_q / n_kv, tiles = (max_len + 31) / 32;
+    const int64_t per = ((int64_t)(rows + R - 1) / R) * qpg;        // query rows of a request and KV head, on average
+    s.nct = per <= 16 ? 1 : 2;
+    const int64_t tile_rows = 16 * s.nct;
+    int64_t units = (int64_t)R * ((per + tile_rows - 1) / tile_rows) * n_kv;
+    // Tiles are shared by waves of different rows where there are rows for two waves at least and units for every SIMD.
+    // A batch may still hold requests of a few rows and many tokens (decoding ones beside prompts), whose tokens one
+    // workgroup would take one after the other: they get key ranges, in a launch of their own.
+    s.split = per < 64 || units < 1024;
+    s.second = !s.split && R > 1;
+    s.groups = (int)((int64_t)rows * qpg / (s.split ? tile_rows : 4 * tile_rows)) + R;
+    if (s.second) units = (int64_t)R * n_kv;
+    s.S = work && (s.split || s.second) ? key_ranges(units, tiles, 256 * (D == 64 ? (s.nct == 1 ? 4 : 3) : (s.nct == 1 ? 3 : 2))) : 1;
     s.chunk = (tiles + s.S - 1) / s.S;
     s.S = (tiles + s.chunk - 1) / s.chunk;
-    s.part = s.S > 1 ? (int64_t)s.groups * n_kv * s.S * tile_rows * (D + 2) * 4 : 0;
+    s.part = s.S > 1 ? (int64_t)(s.second ? R : s.groups) * n_kv * s.S * tile_rows * (D + 2) * 4 : 0;
     return s;
 }
 
-template <typename L, int D, int NCT, bool SPLIT> static bool run_attn(const Kv8Attn &p, hipStream_t s) {
-    const int64_t grid = (int64_t)p.groups * p.S * p.n_kv;
-    if (!launch(k_kv8_attn<L, D, NCT, SPLIT>, (unsigned)grid, 256, 0, s, p)) return false;
-    return p.S == 1 || launch(k_kv8_attn_join<L, D, NCT>, (unsigned)(p.groups * p.n_kv), 256, 0, s, p);
+template <typename L, int D, int NCT> static bool run_split(const Kv8Attn &p, hipStream_t s) {
+    return launch(k_kv8_attn<L, D, NCT, true>, (unsigned)((int64_t)p.groups * p.S * p.n_kv), 256, 0, s, p) &&
+           (p.S == 1 || launch(k_kv8_attn_join<L, D, NCT>, (unsigned)(p.groups * p.n_kv), 256, 0, s, p));
 }
-template <typename L, int D> static bool run_attn_d(const Kv8Attn &p, const Kv8Shape &s, hipStream_t st) {
-    constexpr int most = 2;
-    if (s.nct == 1) return run_attn<L, D, 1, true>(p, st);
-    if (most == 4 && s.nct == 2) return run_attn<L, D, 2, true>(p, st);
-    return s.split ? run_attn<L, D, most, true>(p, st) : run_attn<L, D, most, false>(p, st);
+template <typename L, int D> static bool run_attn(const Kv8Attn &p, const Kv8Shape &s, hipStream_t st) {
+    if (s.split) return s.nct == 1 ? run_split<L, D, 1>(p, st) : run_split<L, D, 2>(p, st);
+    Kv8Attn rows = p;               // (all of a row's tokens: one range)
+    rows.S = 1;
+    rows.chunk = (p.max_len + 31) / 32;
+    rows.few = s.second ? kFewRows : 0;
+    if (!launch(k_kv8_attn<L, D, 2, false>, (unsigned)(p.groups * p.n_kv), 256, 0, st, rows)) return false;
+    Kv8Attn ranges = p;
+    ranges.groups = p.R;
+    ranges.few = kFewRows;
+    return !s.second || run_split<L, D, 2>(ranges, st);
 }
 
 static bool attn_sizes_ok(const pipo_kv8 *c, int32_t R, int32_t rows, int32_t n_q, int32_t max_len) {
@@ -654,13 +683,13 @@ static int attention(const pipo_kv8 *c, int32_t R, int32_t rows, int32_t n_q, co
         !kv8_aligned(total, 4))
         return PIPO_EINVAL;
     if (rows > 1 && (ld_q < least || ld_out < least || ld_q > (int64_t)1 << 31 || ld_out > (int64_t)1 << 31)) return PIPO_EINVAL;
-    const Kv8Shape s = shape_of(R, rows, n_q, c->n_kv, c->head_dim, max_len, sizeof(L), work != nullptr);
+    const Kv8Shape s = shape_of(R, rows, n_q, c->n_kv, c->head_dim, max_len, work != nullptr);
     if (work && s.part > 0 && (!kv8_aligned(work, 16) || work_bytes < s.part)) return PIPO_EINVAL;
     Kv8Attn p{c->keys, c->values, c->scales, tables, starts, total, q, out, ld_q, ld_out, R, rows, width, c->blocks,
-              c->n_kv, n_q, n_q / c->n_kv, __builtin_ctz((unsigned)c->block), max_len, s.S, s.chunk, s.groups,
+              c->n_kv, n_q, n_q / c->n_kv, __builtin_ctz((unsigned)c->block), max_len, s.S, s.chunk, s.groups, 0,
               (float)(scale * 1.4426950408889634074), (float *)work};
     hipStream_t st = (hipStream_t)stream;
-    return (c->head_dim == 128 ? run_attn_d<L, 128>(p, s, st) : run_attn_d<L, 64>(p, s, st)) ? PIPO_OK : PIPO_EHIP;
+    return (c->head_dim == 128 ? run_attn<L, 128>(p, s, st) : run_attn<L, 64>(p, s, st)) ? PIPO_OK : PIPO_EHIP;
 }
 
 }  // namespace pipo
@@ -670,7 +699,7 @@ using namespace pipo;
 extern "C" int64_t pipo_kv8_attention_work_bytes(const pipo_kv8 *c, int32_t R, int32_t rows, int32_t n_q, int32_t max_len,
                                                  int32_t bf16) {
     if (!attn_sizes_ok(c, R, rows, n_q, max_len) || rows == 0) return 0;
-    return shape_of(R, rows, n_q, c->n_kv, c->head_dim, max_len, bf16 ? 2 : 4, true).part;
+    return shape_of(R, rows, n_q, c->n_kv, c->head_dim, max_len, true).part;
 }
 
 extern "C" int pipo_kv8_attention(const pipo_kv8 *cache, int32_t R, int32_t rows, int32_t n_q, const float *d_q,
