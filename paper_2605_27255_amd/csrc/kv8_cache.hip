@@ -210,19 +210,19 @@ __device__ __forceinline__ int round_again(int u, double old, double s, double i
 }
 
 // A workgroup takes the blocks whose first row is among `chunk` rows, of one head, keys
-// or values: their largest magnitude, the scale, and the tiles with new bytes.  A thread
-// holds 16 dimensions of IT tokens.  Rows that follow one another as their slots do, as a
+// or values: their largest magnitude, the scale, and the tiles with new bytes.  An item
+// is 16 dimensions of a token.  Rows that follow one another as their slots do, as a
 // rule, are found by their number; others by a table of tokens (of rows with one slot the
 // last).  Bound by latency at a step's single tokens (32 in 7 us: slots, rows and scale,
 // the old tile, one after the other), at a prompt's by how many workgroups a compute unit
-// holds (8192 tokens of 8 heads x 128: 22 us, 2.3 TB/s in and out; two
-// workgroups of 85 registers 27).
-template <typename L, int NT, int IT> __global__ __launch_bounds__(NT) void k_kv8_append(AppendParams<L> p) {
-    extern __shared__ uint8_t s_stage[];        // values: [block][D + 16] bytes
+// holds (8192 tokens of 8 heads x 128: 23 us, 2.2 TB/s in and out).
+template <typename L, int NT> __global__ __launch_bounds__(NT) void k_kv8_append(AppendParams<L> p) {
+    constexpr int N = Piece<L>::N, KEEP = 2;    // items of a thread that stay in registers
+    extern __shared__ uint8_t s_stage[];        // values: [token][D + 16] bytes
     __shared__ int s_row[256];
     __shared__ uint32_t s_top[NT / 64];
     const int tid = threadIdx.x, lane = tid & 63, head = blockIdx.y, which = blockIdx.z;
-    const int B = 1 << p.shift, D = p.D, E = D >> 4;
+    const int B = 1 << p.shift, D = p.D, E = D >> 4, pitch = D + 16;
     const L *x = p.x[which] + (int64_t)head * D;
     const int64_t ld = p.ld[which];
     const int from = blockIdx.x * p.chunk, upto = min(from + p.chunk, p.rows);
@@ -254,34 +254,47 @@ template <typename L, int NT, int IT> __global__ __launch_bounds__(NT) void k_kv
             for (int i = tid; i < n; i += NT) atomicMax(&s_row[p.slots[first + i] & (B - 1)], first + i);
             __syncthreads();
         }
-        auto row_of = [&](int t) { return straight ? (t >= off0 && t < off0 + n ? first + t - off0 : -1) : s_row[t]; };
+        // the tokens that may have rows: m of them from t0 on
+        const int t0 = straight ? off0 : 0, m = straight ? n : B;
+        auto row_of = [&](int t) { return (unsigned)(t - t0) >= (unsigned)m ? -1 : straight ? first + t - off0 : s_row[t]; };
         const bool anew = row_of(0) >= 0;
         const float held = anew ? 0.f : was;
         uint8_t *store = p.store[which] + ((int64_t)blk * p.n_kv + head) * B * D;
-        // item: a token's 16 dimensions; tokens fastest within 16, as the key tiles have them
-        auto token = [&](int it) { const int i = tid + it * NT; return i / (E * 16) * 16 + (i & 15); };
-        auto group = [&](int it) { return (tid + it * NT) / 16 % E; };
-        float v[IT][16];
-        uint32_t top = 0;
-#pragma unroll
-        for (int it = 0; it < IT; ++it) {
-            const int row = row_of(token(it));
-            if (row < 0) continue;
-            const L *at = x + row * ld + group(it) * 16;
-            constexpr int N = Piece<L>::N;
+        // item i: of few tokens one after the other, of more sixteen side by side, as the key tiles have them
+        const int items = m < 16 ? m * E : (m + 15) / 16 * 16 * E;
+        auto token = [&](int i) { return t0 + (m < 16 ? i / E : i / (E * 16) * 16 + (i & 15)); };
+        auto group = [&](int i) { return m < 16 ? i % E : i / 16 % E; };
+        auto load = [&](int i, float (&v)[16]) {
+            const int row = i < items ? row_of(token(i)) : -1;
+            if (row < 0) return false;
+            const L *from_ = x + row * ld + group(i) * 16;
 #pragma unroll
             for (int e = 0; e < 16 / N; ++e) {
-                const u32x4 w = *(const typename Piece<L>::raw_t *)(at + e * N);
+                const u32x4 w = *(const typename Piece<L>::raw_t *)(from_ + e * N);
 #pragma unroll
-                for (int f = 0; f < N; ++f) {
-                    v[it][e * N + f] = Piece<L>::get(w, f);
-                    top = max(top, __float_as_uint(v[it][e * N + f]) & 0x7FFFFFFFu);    // (NaN above infinity above all)
-                }
+                for (int f = 0; f < N; ++f) v[e * N + f] = Piece<L>::get(w, f);
             }
+            return true;
+        };
+        float kept[KEEP][16];
+        bool has[KEEP];
+        uint32_t top = 0;
+        auto largest = [&](const float (&v)[16]) {     // (NaN above infinity above all)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+        };
+#pragma unroll
+        for (int k = 0; k < KEEP; ++k) has[k] = load(tid + k * NT, kept[k]);
+#pragma unroll
+        for (int k = 0; k < KEEP; ++k)
+            if (has[k]) largest(kept[k]);
+        for (int i = tid + KEEP * NT; i < items; i += NT) {
+            float v[16];
+            if (load(i, v)) largest(v);
         }
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
-        if ((tid & 63) == 0) s_top[tid >> 6] = top;
+        if (lane == 0) s_top[tid >> 6] = top;
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < NT / 64; ++w) top = max(top, s_top[w]);
@@ -290,14 +303,9 @@ template <typename L, int NT, int IT> __global__ __launch_bounds__(NT) void k_kv
         if (s < 0x1p-126f) s = 0.f;
         const bool finite = __float_as_uint(s) < 0x7F800000u;
         const float inv = finite && s > 0.f ? 1.f / s : 0.f;
-        const bool grown = !anew && !(s == held);
-        const double inv64 = grown && inv > 0.f ? 1. / (double)s : 0.;
         if (tid == 0) *scale = s;
-        auto codes = [&](const float *f) {
-            const u32x4 zero{0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
-            return inv > 0.f ? round16(f, s, inv) : zero;
-        };
-        if (grown) {                // what the block holds, to the new scale
+        if (!anew && !(s == held)) {            // what the block holds, to the new scale
+            const double inv64 = inv > 0.f ? 1. / (double)s : 0.;
 #pragma unroll 1
             for (int i = tid; i < B * E; i += NT) {
                 u32x4 w = ((u32x4 *)store)[i];
@@ -313,37 +321,39 @@ template <typename L, int NT, int IT> __global__ __launch_bounds__(NT) void k_kv
             }
             __syncthreads();
         }
-        if (which == 0) {
+        auto put = [&](int i, const float (&v)[16]) {
+            const u32x4 zero{0x80808080u, 0x80808080u, 0x80808080u, 0x80808080u};
+            const u32x4 w = inv > 0.f ? round16(v, s, inv) : zero;
+            const int t = token(i);
+            if (which == 0) ((u32x4 *)store)[key_piece(t, group(i), D)] = w;
+            else *(u32x4 *)(s_stage + (t - t0) * pitch + group(i) * 16) = w;
+        };
 #pragma unroll
-            for (int it = 0; it < IT; ++it) {
-                const int t = token(it);
-                u32x4 *at = (u32x4 *)store + key_piece(t, group(it), D);
-                if (row_of(t) >= 0) *at = codes(v[it]);
-            }
-        } else {
-            const int pitch = D + 16;
-#pragma unroll
-            for (int it = 0; it < IT; ++it)
-                if (row_of(token(it)) >= 0) *(u32x4 *)(s_stage + token(it) * pitch + group(it) * 16) = codes(v[it]);
+        for (int k = 0; k < KEEP; ++k)
+            if (has[k]) put(tid + k * NT, kept[k]);
+        for (int i = tid + KEEP * NT; i < items; i += NT) {
+            float v[16];
+            if (load(i, v)) put(i, v);
+        }
+        if (which == 1) {
             __syncthreads();
-#pragma unroll
-            for (int it = 0; it < IT; ++it) {
-                const int i = tid + it * NT, tile = i >> 6;     // piece i: dimensions e and e + 16, tokens t + v and t + 16 + v
-                const int t = tile / (D >> 5) * 32 + ((i & 63) >> 4) * 4, e = tile % (D >> 5) * 32 + (i & 15);
+            // the tiles of these tokens; piece i: dimensions e and e + 16, tokens t + v and t + 16 + v
+            const int last = (t0 + m - 1) >> 5, pieces = (D >> 5) * 64;
+            for (int i = (t0 >> 5) * pieces + tid; i < (last + 1) * pieces; i += NT) {
+                const int tile = i >> 6, t = tile / (D >> 5) * 32 + ((i & 63) >> 4) * 4, e = tile % (D >> 5) * 32 + (i & 15);
                 uint32_t fresh = 0;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) fresh |= (uint32_t)(row_of(t + (k >> 2) * 16 + (k & 3)) >= 0) << k;
                 if (!fresh) continue;
-                u32x4 *at = (u32x4 *)store + i;
                 u32x4 w{};
-                if (fresh != 255) w = *at;
+                if (fresh != 255) w = ((u32x4 *)store)[i];
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
                     if (!(fresh >> (k & 7) & 1)) continue;
-                    const uint32_t b = s_stage[(t + ((k >> 2) & 1) * 16 + (k & 3)) * pitch + e + (k >> 3) * 16];
+                    const uint32_t b = s_stage[(t - t0 + ((k >> 2) & 1) * 16 + (k & 3)) * pitch + e + (k >> 3) * 16];
                     w[k >> 2] = (w[k >> 2] & ~(255u << 8 * (k & 3))) | b << 8 * (k & 3);
                 }
-                *at = w;
+                ((u32x4 *)store)[i] = w;
             }
         }
         if (runs) __syncthreads();
@@ -418,11 +428,11 @@ template <typename L> __global__ __launch_bounds__(256) void k_kv8_read(ReadPara
 
 static int log2_of(int n) { return __builtin_ctz((unsigned)n); }
 
-template <typename L, int NT, int IT> static bool launch_append(const AppendParams<L> &p, hipStream_t s) {
+template <typename L, int NT> static bool launch_append(const AppendParams<L> &p, hipStream_t s) {
     const size_t lds = (size_t)(1 << p.shift) * (p.D + 16);
     void *ptrs[] = {(void *)&p};
-    return hipLaunchKernel((const void *)k_kv8_append<L, NT, IT>, dim3((p.rows + p.chunk - 1) / p.chunk, p.n_kv, 2),
-                           dim3(NT), ptrs, lds, s) == hipSuccess;
+    return hipLaunchKernel((const void *)k_kv8_append<L, NT>, dim3((p.rows + p.chunk - 1) / p.chunk, p.n_kv, 2), dim3(NT),
+                           ptrs, lds, s) == hipSuccess;
 }
 
 template <typename L>
@@ -435,15 +445,15 @@ static int append(const pipo_kv8 *c, int32_t rows, const L *k, int64_t ld_k, con
     if (rows > 1 && (ld_k < least || ld_v < least || ld_k > (int64_t)1 << 31 || ld_v > (int64_t)1 << 31)) return PIPO_EINVAL;
     AppendParams<L> p{{k, v}, {ld_k, ld_v}, {c->keys, c->values}, c->scales, d_slots, rows, 1, c->blocks, c->n_kv,
                       c->head_dim, log2_of(c->block)};
-    // a workgroup's rows: single tokens of many requests one by one, prompts' rows by the block
-    p.chunk = rows <= 256 ? 1 : rows >= 32 * 128 ? 64 : (rows + 255) / 256;
-    const int items = c->block * c->head_dim / 16;
+    // Rows and threads of a workgroup.  One costs 3 ns whether it finds a block's first row or not, and the runs of one
+    // are taken in turn: single tokens want one row a workgroup, prompts a block's.  How long the runs are is not known
+    // here.  8 heads x 128, us with 1 / 4 / 16 / 64 rows: 256 single tokens 14 / 19 / 55 / 206 (128 threads; 256: 18 / 17 / 44 /
+    // 162), 1024 37 / 40 / 67 / 216, 1000 requests of 5 55 / 43 / 46 / 70, a prompt of 2048 106 / 59 / 22 / 25 (256: 115 /
+    // 59 / 20 / 15), of 8192 397 / 202 / 62 / 36 (256: 444 / 218 / 62 / 26; 512: 30).
+    const int64_t single = (int64_t)rows * c->n_kv * 2;     // workgroups of one row
+    p.chunk = single <= 4096 ? 1 : single >= 64 * 2048 ? 64 : (int)((single + 2047) / 2048);
     hipStream_t s = (hipStream_t)stream;
-    const bool ok = items == 128   ? launch_append<L, 128, 1>(p, s)
-                    : items == 256 ? launch_append<L, 256, 1>(p, s)
-                    : items == 512 ? launch_append<L, 512, 1>(p, s)
-                    : items == 1024 ? launch_append<L, 512, 2>(p, s)
-                                    : launch_append<L, 512, 4>(p, s);
+    const bool ok = single > 1024 && single <= 16384 ? launch_append<L, 128>(p, s) : launch_append<L, 256>(p, s);
     return ok ? PIPO_OK : PIPO_EHIP;
 }
 

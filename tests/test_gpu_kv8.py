@@ -205,7 +205,7 @@ def test_append_prompts_and_tokens(dtype, D, block):
         assert torch.equal(got[w].cpu(), want)
 
 
-@pytest.mark.parametrize("rows", [1, 2, 255, 256, 257, 700, 5000])
+@pytest.mark.parametrize("rows", [1, 2, 64, 65, 255, 256, 257, 700, 1024, 1025, 4095, 4096, 5000])
 def test_append_many_rows(rows):
     """Row counts on both sides of where a workgroup takes several rows, single tokens and prompts among them."""
     rng = np.random.default_rng(rows)
