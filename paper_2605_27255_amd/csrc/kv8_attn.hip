@@ -20,7 +20,7 @@
 // queries in fp32 49 us, 5.4 TB/s (a third of it the two prologues' and the last
 // workgroups' time).  Many rows (a prompt): bound by the waves' instructions, exponentials
 // and conversions (about 720 cycles a tile of 32 rows) beside the matrix cores'
-// (544), two waves a SIMD: 2048 queries on 6144 tokens 272 us, 880 TFLOP/s; each
+// (544), two waves a SIMD: 2048 queries on 6144 tokens 274 us, 880 TFLOP/s; each
 // wave converting its own tiles 281, 64 rows a wave 525, a rescaled O every tile 1169.
 #include "kv8.h"
 #include <math.h>
