@@ -7,7 +7,6 @@
 namespace pipo {
 
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
-typedef __attribute__((ext_vector_type(16))) uint8_t u8x16;
 
 constexpr int kKv8MaxRows = 1 << 20;
 // (checks on the host)

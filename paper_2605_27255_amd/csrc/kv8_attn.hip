@@ -34,7 +34,7 @@ struct Kv8Attn {
     const int32_t *tables, *starts, *total;
     const void *q; void *out;
     int64_t ld_q, ld_out;
-    int R, rows, W, blocks, n_kv, n_q, qpg, shift, max_len;     // block = 1 << shift
+    int R, rows, W, blocks, n_kv, qpg, shift, max_len;     // block = 1 << shift
     int S, chunk;                   // key ranges of `chunk` tiles
     int groups;                     // row groups of all requests, counted from above
     int few;                        // 0, or: requests of up to so many rows are the other launch's; that one has a group a request
@@ -686,7 +686,7 @@ static int attention(const pipo_kv8 *c, int32_t R, int32_t rows, int32_t n_q, co
     const Kv8Shape s = shape_of(R, rows, n_q, c->n_kv, c->head_dim, max_len, work != nullptr);
     if (work && s.part > 0 && (!kv8_aligned(work, 16) || work_bytes < s.part)) return PIPO_EINVAL;
     Kv8Attn p{c->keys, c->values, c->scales, tables, starts, total, q, out, ld_q, ld_out, R, rows, width, c->blocks,
-              c->n_kv, n_q, n_q / c->n_kv, __builtin_ctz((unsigned)c->block), max_len, s.S, s.chunk, s.groups, 0,
+              c->n_kv, n_q / c->n_kv, __builtin_ctz((unsigned)c->block), max_len, s.S, s.chunk, s.groups, 0,
               (float)(scale * 1.4426950408889634074), (float *)work};
     hipStream_t st = (hipStream_t)stream;
     return (c->head_dim == 128 ? run_attn<L, 128>(p, s, st) : run_attn<L, 64>(p, s, st)) ? PIPO_OK : PIPO_EHIP;
