@@ -683,6 +683,9 @@ static int attention(const pipo_kv8 *c, int32_t R, int32_t rows, int32_t n_q, co
         !kv8_aligned(total, 4))
         return PIPO_EINVAL;
     if (rows > 1 && (ld_q < least || ld_out < least || ld_q > (int64_t)1 << 31 || ld_out > (int64_t)1 << 31)) return PIPO_EINVAL;
+    // The output may take the queries' place: a row's heads are read by the workgroup that writes them, before it does, or
+    // by those that leave them to the joining launch.
+    if (!same_or_apart(q, ld_q, out, ld_out, rows, least, sizeof(L))) return PIPO_EINVAL;
     const Kv8Shape s = shape_of(R, rows, n_q, c->n_kv, c->head_dim, max_len, work != nullptr);
     if (work && s.part > 0 && (!kv8_aligned(work, 16) || work_bytes < s.part)) return PIPO_EINVAL;
     Kv8Attn p{c->keys, c->values, c->scales, tables, starts, total, q, out, ld_q, ld_out, R, rows, width, c->blocks,

@@ -690,7 +690,7 @@ template <typename L> static int launch_loss(LossParams<L> p, void *work, hipStr
 static bool aligned(const void *p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 // Rows of V elements at stride ld (elements of es bytes) starting at a and at
 // b, T of each: the same rows, or no element in common.
-static bool same_or_apart(const void *a, int64_t lda, const void *b, int64_t ldb, int64_t T, int64_t V, int64_t es) {
+bool same_or_apart(const void *a, int64_t lda, const void *b, int64_t ldb, int64_t T, int64_t V, int64_t es) {
     const int64_t x = (int64_t)(uintptr_t)a, y = (int64_t)(uintptr_t)b;
     if (x == y && (lda == ldb || T == 1)) return true;
     if (x + ((T - 1) * lda + V) * es <= y || y + ((T - 1) * ldb + V) * es <= x) return true;

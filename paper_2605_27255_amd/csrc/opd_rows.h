@@ -21,6 +21,7 @@ inline bool launch(void (*kernel)(A...), unsigned grid, unsigned block, size_t l
 }
 bool opd_rows_ok(int32_t T, int32_t V, const void *z, int64_t ld, double temperature, size_t es);
 bool opd_work_ok(const void *work, int64_t work_bytes, int64_t need);
+bool same_or_apart(const void *a, int64_t lda, const void *b, int64_t ldb, int64_t T, int64_t V, int64_t es);
 int64_t opd_loss_work_bytes(int T, int V, int k, int es, bool grad);
 
 // ---- pieces of 16 bytes of a row ------------------------------------------------

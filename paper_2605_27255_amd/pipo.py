@@ -659,9 +659,9 @@ def kv8_attention(q, cache, tables, starts, total, scale=None, max_len=None, out
     tables[r] (int32 [R + 1], [R], [R, width], as kv8_plan gives them); each row
     sees the tokens up to its own.  scale: of the scores (None: 1 /
     sqrt(head_dim)); max_len: no request has more tokens (None: the tables'
-    width), fewer make better use of the GPU; out: where to write (None: a new
-    tensor; rows that belong to no request are not written).  Returns out (autograd
-    does not follow it)."""
+    width), fewer make better use of the GPU; out: where to write (q itself, or
+    apart from it; None: a new tensor; rows that belong to no request are not
+    written).  Returns out (autograd does not follow it)."""
     import torch
     dev = _cache(cache)
     if _elsewhere(cache.keys):

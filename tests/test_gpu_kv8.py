@@ -593,6 +593,21 @@ def test_python_calls_refuse_what_does_not_fit():
     assert A.kv8_read(cache, i(0))[0].shape == (0, 2, 64) and A.kv8_attention(q[:0], cache, t, s, n).shape == (0, 4, 64)
 
 
+@pytest.mark.parametrize("total,new", [([3000, 40], [3, 1]), ([2200, 700], [2200, 600])])
+def test_attention_over_its_own_queries(total, new):
+    """Short and split rows, and a prompt's: the output in place of the queries, in a wider tensor."""
+    rng = np.random.default_rng(19)
+    c, tables = _paged(rng, total, 8, 64, 64)
+    cache, args = to_gpu(c), (_i32(tables), _i32(np.concatenate([[0], np.cumsum(new)])), _i32(total))
+    x = torch.tensor(rng.standard_normal((sum(new), 70, 64))).bfloat16().cuda()
+    want = _api().kv8_attention(x[:, 3:67], cache, *args)
+    rest = x[:, 67:].clone(), x[:, :3].clone()
+    _api().kv8_attention(x[:, 3:67], cache, *args, out=x[:, 3:67])
+    assert torch.equal(x[:, 3:67], want) and torch.equal(x[:, 67:], rest[0]) and torch.equal(x[:, :3], rest[1])
+    with pytest.raises(_api().PipoError):
+        _api().kv8_attention(x[:, 3:67], cache, *args, out=x[:, 4:68])
+
+
 def test_attention_same_bits_every_time():
     rng = np.random.default_rng(17)
     total, new = [3000, 700, 45], [3, 1, 2]

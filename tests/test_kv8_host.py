@@ -158,11 +158,12 @@ def test_cache_refusals(lib, dt):
 def test_attention_refusals(lib, dt):
     from paper_2605_27255_amd import PIPO_EINVAL, PIPO_OK
     base = dict(cache={}, R=2, rows=3, n_q=8, q=A, ld=512, tables=A, width=2, starts=A, total=A, max_len=128, scale=0.125,
-                out=A, ldo=512, work=None, bytes=0, stream=None)
+                out=2 * A, ldo=512, work=None, bytes=0, stream=None)
     for kw in [dict(cache=c) for c in CACHES] + [
             dict(cache=None), dict(R=0), dict(rows=-1), dict(n_q=0), dict(n_q=7), dict(n_q=34), dict(q=None), dict(q=A + 1),
             dict(ld=511), dict(ldo=511), dict(tables=None), dict(width=0), dict(starts=None), dict(total=None), dict(max_len=0),
-            dict(max_len=129), dict(scale=float("nan")), dict(scale=1e300), dict(out=None), dict(rows=(1 << 20) + 1)]:
+            dict(max_len=129), dict(out=A + 64), dict(out=A, ldo=513), dict(scale=float("nan")), dict(scale=1e300),
+            dict(out=None), dict(rows=(1 << 20) + 1)]:
         assert _call(lib, "pipo_kv8_attention" + dt, base, kw) == PIPO_EINVAL, kw
     long = dict(width=200, max_len=200 * 64)
     need = lib.pipo_kv8_attention_work_bytes(ctypes.byref(_kv8()), 2, 3, 8, 200 * 64, dt != "")
