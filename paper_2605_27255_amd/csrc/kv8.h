@@ -27,6 +27,14 @@ __device__ __forceinline__ int value_byte(int t, int e, int D) {
            ((t & 16) >> 2) + (t & 3);
 }
 
+// A request's rows first .. first + n - 1 from the two starts around them, whatever these hold: both are cut off to
+// the call's rows before anything is computed with them, so that no difference or product passes 32 bits.
+struct RequestRows { int first, n; };
+__host__ __device__ __forceinline__ RequestRows request_rows(int32_t from, int32_t to, int32_t rows) {
+    const int a = from < 0 ? 0 : from < rows ? from : rows, b = to < rows ? to : rows;
+    return RequestRows{a, b > a ? b - a : 0};
+}
+
 // Request of a row: the last r with starts[r] <= row (0 <= r < R), the row not before starts[0].
 __device__ __forceinline__ int request_of(const int32_t *starts, int R, int row) {
     int lo = 0, hi = R;

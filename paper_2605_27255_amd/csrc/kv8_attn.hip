@@ -86,7 +86,7 @@ template <int ROWS> __device__ __forceinline__ bool find_group(const Kv8Attn &p,
     for (;;) {
         const int step = (width + 63) >> 6, r = lo + lane * step;
         const bool in = lane * step < width;
-        start = in ? max(p.starts[r], 0) : 0;
+        start = in ? min(max(p.starts[r], 0), p.rows) : 0;
         total = in && step == 1 ? p.total[r] : 0;       // (asked for together: one round trip)
         const int next = in && step == 1 ? p.starts[r + 1] : 0;
         const uint64_t upto = __ballot(in && (int)(start * p.qpg / ROWS) + r <= f);
@@ -94,26 +94,28 @@ template <int ROWS> __device__ __forceinline__ bool find_group(const Kv8Attn &p,
         lo += at * step;
         width = min(step, width - at * step);
         if (step == 1) {
-            g.first = __builtin_amdgcn_readlane((int)start, at);
-            total = __builtin_amdgcn_readlane(total, at);
-            g.n = min(__builtin_amdgcn_readlane(next, at), p.rows) - g.first;
+            const RequestRows rr = request_rows(__builtin_amdgcn_readlane((int)start, at), __builtin_amdgcn_readlane(next, at), p.rows);
+            g.first = rr.first;
+            g.n = rr.n;
+            total = max(__builtin_amdgcn_readlane(total, at), 0);
             break;
         }
     }
     g.r = lo;
     g.row0 = (f - (int)((int64_t)g.first * p.qpg / ROWS) - lo) * ROWS;
-    g.last = min(max(total, 0), p.max_len);
+    g.last = min(total, p.max_len);
     return g.row0 >= 0 && g.row0 < g.n * p.qpg;
 }
 // The same for either launch of a call: whether this one has the group.
 template <int ROWS, bool SPLIT> __device__ __forceinline__ bool own_group(const Kv8Attn &p, int f, RowGroup &g, int &total) {
     if (SPLIT && p.few) {           // group f is request f
         g.r = f;
-        g.first = max(p.starts[f], 0);
-        g.n = min(p.starts[f + 1], p.rows) - g.first;
-        total = p.total[f];
+        const RequestRows rr = request_rows(p.starts[f], p.starts[f + 1], p.rows);
+        g.first = rr.first;
+        g.n = rr.n;
+        total = max(p.total[f], 0);
         g.row0 = 0;
-        g.last = min(max(total, 0), p.max_len);
+        g.last = min(total, p.max_len);
         return g.n > 0 && g.n * p.qpg <= p.few;
     }
     return find_group<ROWS>(p, f, g, total) && (SPLIT || g.n * p.qpg > p.few);

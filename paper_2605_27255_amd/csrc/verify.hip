@@ -41,13 +41,10 @@ template <typename L> struct VerifyParams {
 
 // Rows of request r: the first, and how many drafts have one (-1: no rows at all).
 template <typename L> __device__ __forceinline__ int rows_of(const VerifyParams<L> &p, int r, int &first) {
-    int n = p.K + 1;
-    first = r * (p.K + 1);
-    if (p.starts) {
-        first = max(p.starts[r], 0);
-        n = min(p.starts[r + 1], p.rows) - first;
-    }
-    return max(min(n - 1, p.K), -1);
+    RequestRows rr{r * (p.K + 1), p.K + 1};
+    if (p.starts) rr = request_rows(p.starts[r], p.starts[r + 1], p.rows);
+    first = rr.first;
+    return min(rr.n - 1, p.K);
 }
 // ... of which so many come before the first negative one (up to 63: a lane each).
 template <typename L> __device__ __forceinline__ int drafts_of(const VerifyParams<L> &p, int r, int n) {
