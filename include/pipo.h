@@ -364,7 +364,8 @@ int pipo_opd_policy_bf16(int32_t T, int32_t V, const uint16_t *d_logits, int64_t
  *
  * pipo_kv8_append: rows i (up to 2^20) of d_k and d_v ([n_kv][head_dim] each, fp32 or bf16, row
  * stride ld elements) into slot d_slots[i] (negative: not at all; of rows with one slot
- * the last counts).  Rows of one block have to be consecutive.  A block whose first slot
+ * the last counts).  Rows of one block have to be consecutive, but for rows without a slot among
+ * them (two workgroups would take one block at once otherwise).  A block whose first slot
  * is written begins anew with s = max|x| / 127 of its written rows; else s only grows,
  * to the larger of it and that.  u = 128 + x / s rounded to nearest even; where s
  * grows, what the block holds besides is rounded to the new s.  A scale below 2^-126

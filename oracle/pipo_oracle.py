@@ -801,10 +801,10 @@ class Kv8Oracle:
         i = 0
         while i < len(slots):
             j = i + 1
-            while j < len(slots) and blk[j] == blk[i]:
+            while j < len(slots) and blk[i] >= 0 and blk[j] in (blk[i], -1):     # (rows without a slot do not end a run)
                 j += 1
             if blk[i] >= 0:
-                row = {int(slots[n]) % self.block: n for n in range(i, j)}       # the last row of a slot counts
+                row = {int(slots[n]) % self.block: n for n in range(i, j) if blk[n] >= 0}   # the last row of a slot counts
                 for w, x in enumerate((k, v)):
                     self._into(w, int(blk[i]), sorted(row), x[[row[o] for o in sorted(row)]])
             i = j

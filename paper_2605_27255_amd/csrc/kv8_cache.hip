@@ -228,30 +228,64 @@ template <typename L, int NT> __global__ __launch_bounds__(NT) void k_kv8_append
     const int from = blockIdx.x * p.chunk, upto = min(from + p.chunk, p.rows);
     auto slot_of = [&](int i) { return i >= 0 && i < p.rows ? p.slots[i] : -1; };
     auto block_of = [&](int slot) { return slot >= 0 && (slot >> p.shift) < p.blocks ? slot >> p.shift : -1; };
-    // the rows that begin a block's run, one a lane
-    const int slot = slot_of(from + lane), own = block_of(slot), before = block_of(slot_of(from + lane - 1));
-    uint64_t runs = __ballot(from + lane < upto && own >= 0 && own != before);
+    // the nearest row from `at` on (up: +1, down: -1) that has a slot: its block (-1: there is none)
+    auto seek = [&](int at, int up, int &row) {
+        for (; at >= 0 && at < p.rows; at += up * 1024) {       // (a step's padding may be long: 16 loads on their way)
+            int b[16];
+#pragma unroll
+            for (int u = 0; u < 16; ++u) b[u] = block_of(slot_of(at + up * (u * 64 + lane)));
+#pragma unroll
+            for (int u = 0; u < 16; ++u) {
+                const uint64_t in = __ballot(b[u] >= 0);
+                if (!in) continue;
+                row = at + up * (u * 64 + (int)__builtin_ctzll(in));
+                return __builtin_amdgcn_readlane(b[u], __builtin_ctzll(in));
+            }
+        }
+        row = -1;
+        return -1;
+    };
+    // the rows that begin a block's run, one a lane: the row before them that has a slot is of another block
+    const int slot = slot_of(from + lane), own = block_of(slot), back = block_of(slot_of(from - 1 - lane));
+    const uint64_t there = __ballot(from + lane < upto && own >= 0), behind = __ballot(back >= 0);
+    if (!there) return;
+    int at_row, carry = behind ? __builtin_amdgcn_readlane(back, __builtin_ctzll(behind)) : seek(from - 65, -1, at_row);
+    const uint64_t lower = there & ((1ull << lane) - 1);
+    const int near = __shfl(own, lower ? 63 - __builtin_clzll(lower) : 0), before = lower ? near : carry;
+    uint64_t runs = __ballot((there >> lane & 1) && own != before);
     while (runs) {
         const int at = __builtin_ctzll(runs), first = from + at, blk = __builtin_amdgcn_readlane(own, at);
         const int off0 = __builtin_amdgcn_readlane(slot, at) & (B - 1);
         runs &= runs - 1;
         float *scale = p.scales + ((int64_t)blk * p.n_kv + head) * 2 + which;
         const float was = *scale;
-        // how far the run goes, and whether its slots count up
+        // How far the run goes (rows without a slot do not end it: a second workgroup would take the same block), and
+        // whether it is one row after the other and their slots count up.
         int n = 0;
         bool straight = true;
-        for (;;) {
-            const int s = slot_of(first + n + lane);
-            const uint64_t in = __ballot(block_of(s) == blk);
-            const int k = in == ~0ull ? 64 : __builtin_ctzll(~in);
-            straight = straight && !__ballot(lane < k && (s & (B - 1)) != off0 + n + lane);
-            n += k;
-            if (k < 64) break;
+        for (int at = 0; first + at < p.rows;) {
+            const int s = slot_of(first + at + lane), b = block_of(s);
+            const uint64_t other = __ballot(b >= 0 && b != blk), ends = other & -other;
+            const uint64_t in = __ballot(b == blk) & (ends - 1);     // (no other one: all of them)
+            if (in) {
+                const int top = 63 - __builtin_clzll(in);
+                straight = straight && n == at && in == ~0ull >> (63 - top) &&
+                           !__ballot(lane <= top && (s & (B - 1)) != off0 + at + lane);
+                n = at + top + 1;
+            }
+            if (other) break;
+            at += 64;
+            int row = first + at;
+            if (n < at && seek(row, 1, row) != blk) break;
+            at = row - first;
         }
         if (!straight) {
             for (int i = tid; i < B; i += NT) s_row[i] = -1;
             __syncthreads();
-            for (int i = tid; i < n; i += NT) atomicMax(&s_row[p.slots[first + i] & (B - 1)], first + i);
+            for (int i = tid; i < n; i += NT) {
+                const int s = p.slots[first + i];
+                if (block_of(s) == blk) atomicMax(&s_row[s & (B - 1)], first + i);
+            }
             __syncthreads();
         }
         // the tokens that may have rows: m of them from t0 on

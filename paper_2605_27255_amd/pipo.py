@@ -615,9 +615,9 @@ def kv8_plan(lens, new, tables, held, free, n_free, rows: int, block: int):
 
 def kv8_append(cache, k, v, slots):
     """Keys and values (fp32 or bf16 CUDA [rows, n_kv, head_dim], any row stride) into
-    the cache's slots (int32 [rows], negative: not at all).  Rows of one block are
-    consecutive; one at a block's first slot begins the block anew, otherwise its
-    scale only grows."""
+    the cache's slots (int32 [rows], negative: not at all).  Rows of one block have to
+    be consecutive, but for rows without a slot among them; one at a block's first
+    slot begins the block anew, otherwise its scale only grows."""
     import torch
     dev = _cache(cache)
     if _elsewhere(cache.keys):

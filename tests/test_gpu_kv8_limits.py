@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 
 from oracle import pipo_oracle as O
-from test_gpu_kv8 import (_api, _bits, _i32, _paged, to_gpu)
+from test_gpu_kv8 import _api, _append_both, _i32, _kv, _paged, assert_same_cache, random_cache, to_gpu
 import test_gpu_verify as verify
 
 pytestmark = pytest.mark.gpu
@@ -59,3 +59,49 @@ def test_verify_starts_whose_difference_wraps(starts):
                                                  np.array([mine[0], mine[-1] + 1]))
         if margin[0] > 4e-5:
             assert a[r] == accepted[0] and (t[r] == want[0]).all()
+
+
+# ---- rows without a slot inside a block's run ---------------------------------------------------------------------------
+
+def _with_holes(rng, slots, gaps):
+    """The slots with runs of rows without one among them, of lengths drawn from `gaps`."""
+    out = []
+    for s in slots:
+        out.append(int(s))
+        if rng.random() < 0.4:
+            hole = [-1, -2 ** 31, 2 ** 31 - 1][rng.integers(3)]
+            out += [hole] * int(rng.choice(gaps))
+    return np.array(out)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("slots,D", [([64, -1, 65], 64), ([64, -1, -1, 66, 65], 128), ([-1, 97, -1, 98, 96], 64),
+                                     ([-1] * 70 + [40] + [-1] * 70 + [41, 42] + [-1] * 70, 64),
+                                     ([33, 34] + [-1] * 61 + [35] + [-1] * 2000 + [36, 64] + [-1] * 1100 + [65], 128)])
+def test_append_holes_inside_a_block(dtype, slots, D):
+    rng = np.random.default_rng(len(slots))
+    c = random_cache(rng, 4, 2, 32, D)
+    k, v = _kv(rng, len(slots), 2, D, dtype, size=3.0)
+    assert_same_cache(_append_both(c, k, v, np.array(slots), dtype), c)
+
+
+@pytest.mark.parametrize("tokens,n_kv", [(40, 1), (300, 2), (3000, 2), (2500, 8)])     # (one to 64 rows a workgroup)
+@pytest.mark.parametrize("gaps", [[1], [1, 3, 62, 63, 64, 65], [1, 1, 1, 1, 1500]])
+def test_append_holes_anywhere(tokens, n_kv, gaps):
+    rng = np.random.default_rng([tokens, n_kv, len(gaps)])
+    block, D = 64, 64
+    if len(gaps) == 5:
+        tokens //= 8
+    blocks = rng.permutation(tokens)
+    slots, b = [], 0
+    while len(slots) < tokens:          # runs from anywhere in a block, some backwards or with a slot twice
+        at = int(rng.integers(0, block))
+        run = list(range(at, int(rng.integers(at, block)) + 1))
+        if rng.random() < 0.2:
+            run = run[::-1] + run[:1]
+        slots += [int(blocks[b]) * block + t for t in run]
+        b += 1
+    slots = _with_holes(rng, slots, gaps)
+    c = random_cache(rng, tokens, n_kv, block, D)
+    k, v = _kv(rng, len(slots), n_kv, D, torch.bfloat16)
+    assert_same_cache(_append_both(c, k, v, slots, torch.bfloat16), c)

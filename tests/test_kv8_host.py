@@ -201,3 +201,14 @@ def test_python_calls_refuse_host_tensors(lib):
                  lambda: kv8_plan(i, i, i[:, None], i, i, i, 4, 64)):
         with pytest.raises(PipoError):
             call()
+
+
+def test_oracle_append_runs_go_over_rows_without_a_slot():
+    x = np.zeros((4, 1, 64))
+    x[:, 0, 0] = 127.0, 1e6, 254.0, 508.0
+    a, b = (O.Kv8Oracle(np.full((2, 3, 1, 32, 64), 128, np.uint8), np.ones((3, 1, 2), np.float32)) for _ in "ab")
+    a.append(x, x, [33, -1, 34, 35])
+    b.append(x[[0, 2, 3]], x[[0, 2, 3]], [33, 34, 35])
+    np.testing.assert_array_equal(a.codes, b.codes)
+    np.testing.assert_array_equal(a.scales, b.scales)
+    assert a.scales[1, 0, 0] == 4.0 and list(a.codes[0, 1, 0, 1:4, 0]) == [160, 192, 255]       # 31.75 to the nearest
