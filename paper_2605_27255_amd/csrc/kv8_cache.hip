@@ -218,7 +218,7 @@ __device__ __forceinline__ int round_again(int u, double old, double s, double i
 // holds (8192 tokens of 8 heads x 128: 22 us, 2.3 TB/s in and out).
 template <typename L, int NT> __global__ __launch_bounds__(NT) void k_kv8_append(AppendParams<L> p) {
     constexpr int N = Piece<L>::N, KEEP = 2;    // items of a thread that stay in registers
-    extern __shared__ uint8_t s_stage[];        // values: [token][D + 16] bytes
+    extern __shared__ __align__(16) uint8_t s_stage[];      // values: [token][D + 16] bytes, in pieces of 16
     __shared__ int s_row[256];
     __shared__ uint32_t s_top[NT / 64];
     const int tid = threadIdx.x, lane = tid & 63, head = blockIdx.y, which = blockIdx.z;
