@@ -216,10 +216,10 @@ __device__ __forceinline__ int round_again(int u, double old, double s, double i
 // last).  Bound by latency at a step's single tokens (32 in 6.4 us: slots, rows and scale,
 // the old tile, one after the other), at a prompt's by how many workgroups a compute unit
 // holds (8192 tokens of 8 heads x 128: 22 us, 2.3 TB/s in and out).
-template <typename L, int NT> __global__ __launch_bounds__(NT) void k_kv8_append(AppendParams<L> p) {
+template <typename L, int NT> __global__ __launch_bounds__(NT, 4) void k_kv8_append(AppendParams<L> p) {
     constexpr int N = Piece<L>::N, KEEP = 2;    // items of a thread that stay in registers
     extern __shared__ __align__(16) uint8_t s_stage[];      // values: [token][D + 16] bytes, in pieces of 16
-    __shared__ int s_row[256];
+    __shared__ int s_row[256], s_near[2];
     __shared__ uint32_t s_top[NT / 64];
     const int tid = threadIdx.x, lane = tid & 63, head = blockIdx.y, which = blockIdx.z;
     const int B = 1 << p.shift, D = p.D, E = D >> 4, pitch = D + 16;
@@ -228,18 +228,27 @@ template <typename L, int NT> __global__ __launch_bounds__(NT) void k_kv8_append
     const int from = blockIdx.x * p.chunk, upto = min(from + p.chunk, p.rows);
     auto slot_of = [&](int i) { return i >= 0 && i < p.rows ? p.slots[i] : -1; };
     auto block_of = [&](int slot) { return slot >= 0 && (slot >> p.shift) < p.blocks ? slot >> p.shift : -1; };
-    // the nearest row from `at` on (up: +1, down: -1) that has a slot: its block (-1: there is none)
+    // The nearest row from `at` on (up: 1, down: -1) that has a slot, and its block (-1: there is none), by the whole
+    // workgroup, all of whose waves see the same slots and call this together: a step's padding may be long (32 tokens
+    // and 65504 rows without a slot: 114 us a call, of them 94 for the launch; where each wave searches alone, 188).
     auto seek = [&](int at, int up, int &row) {
-        for (; at >= 0 && at < p.rows; at += up * 1024) {       // (a step's padding may be long: 16 loads on their way)
-            int b[16];
+        constexpr int U = 16, NONE = 0x7FFFFFFF;
+        __syncthreads();
+        if (tid < 2) s_near[tid] = NONE;
+        __syncthreads();
+#pragma unroll 1
+        for (int step = 0; at >= 0 && at < p.rows; ++step, at += up * U * NT) {
+            int s[U], near = NONE;
 #pragma unroll
-            for (int u = 0; u < 16; ++u) b[u] = block_of(slot_of(at + up * (u * 64 + lane)));
+            for (int u = 0; u < U; ++u) s[u] = slot_of(at + up * (u * NT + tid));
 #pragma unroll
-            for (int u = 0; u < 16; ++u) {
-                const uint64_t in = __ballot(b[u] >= 0);
-                if (!in) continue;
-                row = at + up * (u * 64 + (int)__builtin_ctzll(in));
-                return __builtin_amdgcn_readlane(b[u], __builtin_ctzll(in));
+            for (int u = U - 1; u >= 0; --u) near = block_of(s[u]) >= 0 ? u * NT + tid : near;
+            if (near != NONE) atomicMin(&s_near[step & 1], near);       // (a wave may be a step ahead of another's reading)
+            __syncthreads();
+            const int found = __builtin_amdgcn_readfirstlane(s_near[step & 1]);
+            if (found != NONE) {
+                row = at + up * found;
+                return block_of(p.slots[row]);
             }
         }
         row = -1;
