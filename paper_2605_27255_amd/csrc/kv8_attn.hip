@@ -75,6 +75,12 @@ template <bool PAIR> __device__ __forceinline__ void fp16_8(const float *v, u32x
     }
 }
 
+// log2 of a scale, the smallest ones too (the hardware's takes what is below 2^-126 as 0); -inf of 0.
+__device__ __forceinline__ float log2_any(float x) {
+    const bool tiny = x < 0x1p-64f;
+    return __builtin_amdgcn_logf(tiny ? x * 0x1p64f : x) - (tiny ? 64.f : 0.f);
+}
+
 // Where a row group lies: request r's groups are numbered from start(r) * qpg / (16 NCT) + r
 // on, which leaves room for the part-filled last one of every request before it.
 struct RowGroup { int r, row0, n, first, last; };   // rows row0 .. of the request's n * qpg; last: its total, cut off
@@ -130,7 +136,7 @@ template <int ROWS> __device__ __forceinline__ int tiles_of(const Kv8Attn &p, co
 // (SPLIT), or take a quarter of a group of four times the rows each, and share the tiles: each
 // wave makes a quarter of a tile's bytes to operands, which all of them read from LDS.
 template <typename L, int D, int NCT, bool SPLIT>
-__global__ __launch_bounds__(256, NCT > 1 && sizeof(L) == 4 ? 1 : 2) void k_kv8_attn(Kv8Attn p) {
+__global__ __launch_bounds__(256, SPLIT && NCT == 2 && D == 64 && sizeof(L) == 2 ? 4 : 2) void k_kv8_attn(Kv8Attn p) {
     constexpr bool PAIR = sizeof(L) == 4, DEEP = NCT == 1;
     constexpr int ROWS = 16 * NCT, GROUP = SPLIT ? ROWS : 4 * ROWS, NC = D / 64, NT = D / 16, NV = D / 32;
     const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
@@ -170,8 +176,9 @@ __global__ __launch_bounds__(256, NCT > 1 && sizeof(L) == 4 ? 1 : 2) void k_kv8_
         id = at < p.W ? p.tables[(int64_t)rg.r * p.W + at] : -1;
         if ((unsigned)id >= (unsigned)p.blocks) id = -1;
         sc = id >= 0 ? *(const float2 *)(p.scales + ((int64_t)id * p.n_kv + head) * 2) : make_float2(0.f, 0.f);
+        if (!PAIR) sc.y = log2_any(sc.y);
     };
-    struct Tile { u32x4 k[2][NC], v[NV]; float sk, sv; bool there; };
+    struct Tile { u32x4 k[2][NC], v[NV]; float sk, sv; bool there; };      // (sv: for bf16 queries the scale's log2)
     Tile buf[DEEP ? 2 : 1];
     int64_t off = 0;                // of the tile that load_keys was called for last
     auto load_keys = [&](Tile &to, int t) {
@@ -286,17 +293,20 @@ __global__ __launch_bounds__(256, NCT > 1 && sizeof(L) == 4 ? 1 : 2) void k_kv8_
     for (int o = 8; o > 0; o >>= 1) all_see = min(all_see, __shfl_xor(all_see, o));
     all_see = __builtin_amdgcn_readfirstlane(all_see);
 
-    // O in units of a value scale U; probabilities as 2^8 exp2(s - m), where m, a row's reference, follows its
+    // A row's O is in units of 2^unit; probabilities as 2^8 exp2(s - m), where m, a row's reference, follows its
     // maximum only when that is more than 6 above it: O is seldom rescaled, and 2^15 at most goes into fp16.  Pairs
     // take 2^14 and the maximum itself: the lower half of a small probability has fp16's smallest step (errors of the
     // whole, 8 x 16384 tokens: 3.9e-6 with 2^8, 5e-7).
     constexpr float kUp = PAIR ? 14.f : 8.f, kSlack = PAIR ? 0.f : 6.f;
     f32x4 o[NCT][NT];
-    float m_run[NCT], l_run[NCT], U = PAIR ? 1.f : 0.f;
+    float m_run[NCT], l_run[NCT], unit[NCT];
+    float unit0 = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(sc.y)));     // the first block's value scale, or any
+    unit0 = floorf(PAIR ? log2_any(unit0) : unit0) + 1.f;
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct) {
         m_run[ct] = -INFINITY;
         l_run[ct] = 0.f;
+        unit[ct] = fabsf(unit0) < 200.f ? unit0 : 0.f;
 #pragma unroll
         for (int t = 0; t < NT; ++t) o[ct][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -328,8 +338,49 @@ __global__ __launch_bounds__(256, NCT > 1 && sizeof(L) == 4 ? 1 : 2) void k_kv8_
                     }
                 }
     };
+    // A tile whose value scale is far from the rows' units: where it is to be seen in O beside what is there, the row's unit
+    // moves so that both can be held.  r: its largest score less the row's reference, in all of a row's lanes alike.
+    //   Up, where its probabilities times its scale would not go into fp16 (fp32: weigh more than 2^4), or what is there
+    // stays large enough (2^8) beside their smallest steps.  Down, as far as what is there keeps below 2^81 (more than
+    // that, and the tile is nothing beside it); what has lost its weight by its scores does not hold a unit up.
+    // fold: what the probabilities' exponents get; apart: they are too small then to be summed for l as well.
+    auto settle = [&](const Tile &b, const float (&mx)[NCT], float (&fold)[NCT], float (&kv)[NCT]) __attribute__((always_inline)) {
+        bool apart = false;
+        const float ls = PAIR ? log2_any(b.sv) : b.sv;
+#pragma unroll
+        for (int ct = 0; ct < NCT; ++ct) {
+            const float r = col_max(mx[ct]) - m_run[ct], d = ls - unit[ct], least = PAIR ? r + d : d;
+            float top = 0.f;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) top = fmaxf(top, fabsf(o[ct][t][v]));
+            top = col_max(top);
+            const float held = top > 0.f ? (float)ilogbf(top) : -1000.f;
+            float to = unit[ct];
+            if (r > -INFINITY) {        // (a row that sees nothing of it stays as it is, and so with a NaN)
+                if (r + d > (PAIR ? 4.f : 7.f)) to = fmaxf(to, floorf(ls + fminf(r, 0.f)) + 1.f);
+                else if (d > 1.f && held - d >= 8.f) to = floorf(ls) + 1.f;
+                else if (least < (PAIR ? -60.f : -3.f) && ls > -INFINITY)
+                    to = fminf(to, fmaxf(floorf(PAIR ? ls + r : ls) + 1.f, to + held - 80.f));
+            }
+            const int up = (int)(unit[ct] - to);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int v = 0; v < 4; ++v) o[ct][t][v] = ldexpf(o[ct][t][v], up);
+            unit[ct] = to;
+            fold[ct] = ls - to;
+            apart |= fold[ct] < -3.f && r > -INFINITY;
+            if (PAIR) {                 // (a tile of small weight and a large scale needs its probabilities' lower bits)
+                fold[ct] = r > -INFINITY ? fminf(ceilf(-r), 1000.f) : 0.f;
+                kv[ct] = ldexpf(b.sv, (int)(-to - fold[ct]));
+            }
+        }
+        return !PAIR && __builtin_amdgcn_ballot_w64(apart) != 0;
+    };
     // A tile's probabilities, and what they add to l and O.
-    auto tile_as = [&](const Tile &b, int t0, const Scores &st, int share, auto all) {
+    auto tile_as = [&](const Tile &b, int t0, const Scores &st, int share, auto all) __attribute__((always_inline)) {
         constexpr bool whole = decltype(all)::value;    // every row sees all of it
         if (!b.there) return;       // no such block: its tokens are not there
         u32x4 va[SPLIT ? 1 : NT];
@@ -373,30 +424,38 @@ __global__ __launch_bounds__(256, NCT > 1 && sizeof(L) == 4 ? 1 : 2) void k_kv8_
                 for (int d = 0; d < NT; ++d) o[ct][d] *= al;
             }
         }
-        // The tile's scale, over U, goes into its probabilities; where that is not near 1, U follows.  Below 2^-64 U (or 0)
-        // it adds nothing to O.  (Pairs: into what the tile adds, by an fma, which rounds to nearest.)
-        bool none = false;
-        float up = 0.f, back = 1.f;
-        if constexpr (!PAIR) {
-            none = b.sv < 0x1p-64f * U || b.sv == 0.f;
-            if (!none && (b.sv > 2.f * U || b.sv < 0.125f * U)) {       // (never with a NaN)
-                const float k = U / b.sv;
-                U = b.sv;
+        // The tile's scale, over the row's unit, goes into its probabilities.  (Pairs: into what the tile adds, by an fma,
+        // which rounds to nearest.)
+        float fold[NCT], kv[NCT];
+        bool odd = false, apart = false;
 #pragma unroll
-                for (int ct = 0; ct < NCT; ++ct)
-#pragma unroll
-                    for (int d = 0; d < NT; ++d) o[ct][d] *= k;
-            }
-            if (!none) {
-                up = __builtin_amdgcn_logf(b.sv) - __builtin_amdgcn_logf(U > 0.f ? U : 1.f);
-                back = b.sv > 0.f ? __builtin_amdgcn_exp2f(-up) : 1.f;
+        for (int ct = 0; ct < NCT; ++ct) {
+            if (PAIR) {
+                fold[ct] = 0.f;
+                kv[ct] = ldexpf(b.sv, -(int)unit[ct]);
+                odd |= kv[ct] < 0x1p-60f || kv[ct] > 0x1p8f;
+            } else {
+                fold[ct] = b.sv - unit[ct];
+                odd |= fabsf(fold[ct] + 1.f) > 2.f;
             }
         }
+        if (__builtin_amdgcn_ballot_w64(odd)) apart = settle(b, mx, fold, kv);
         u32x4 ph[NCT], pl[NCT];
         f32x4 w[NCT];
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct) {
-            const float c = ck[ct] - (m_run[ct] == -INFINITY ? -kUp : m_run[ct] - kUp) + up;
+            const float c0 = ck[ct] - (m_run[ct] == -INFINITY ? -kUp : m_run[ct] - kUp), c = c0 + fold[ct];
+            const u32x4 ones{0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u};
+            if (apart) {                // l from probabilities without the scale
+                float e[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    e[k] = __builtin_amdgcn_exp2f(fmaf(s[ct][k], fk[ct], c0));
+                    if (!whole && hidden(ct, k)) e[k] = 0.f;
+                }
+                fp16_8<false>(e, ph[ct], pl[ct]);
+                w[ct] = mfma16_f16(ones, ph[ct], f32x4{0.f, 0.f, 0.f, 0.f});
+            }
 #pragma unroll
             for (int k = 0; k < 8; ++k) s[ct][k] = __builtin_amdgcn_exp2f(fmaf(s[ct][k], fk[ct], c));
             if (!whole) {
@@ -405,10 +464,8 @@ __global__ __launch_bounds__(256, NCT > 1 && sizeof(L) == 4 ? 1 : 2) void k_kv8_
             }
             fp16_8<PAIR>(s[ct], ph[ct], pl[ct]);
             // their sum, over the tile's tokens: from the matrix cores, where they have been rounded
-            const u32x4 ones{0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u};
-            w[ct] = mfma16_f16(ones, ph[ct], f32x4{0.f, 0.f, 0.f, 0.f});
+            if (!apart) w[ct] = mfma16_f16(ones, ph[ct], f32x4{0.f, 0.f, 0.f, 0.f});
             if (PAIR) w[ct] = mfma16_f16(ones, pl[ct], w[ct]);
-            if (none) ph[ct] = u32x4{0u, 0u, 0u, 0u};
         }
 #pragma unroll
         for (int d = 0; d < NT; ++d) {
@@ -418,7 +475,7 @@ __global__ __launch_bounds__(256, NCT > 1 && sizeof(L) == 4 ? 1 : 2) void k_kv8_
                 if constexpr (PAIR) {
                     f32x4 x = mfma16_f16(a, ph[ct], f32x4{0.f, 0.f, 0.f, 0.f});
                     x = mfma16_f16(a, pl[ct], x);
-                    const float k = t0 < seen[ct] ? b.sv : 0.f;    // (a row that sees nothing of the tile gets no NaN from it)
+                    const float k = t0 < seen[ct] ? kv[ct] : 0.f;    // (a row that sees nothing of the tile gets no NaN from it)
 #pragma unroll
                     for (int v = 0; v < 4; ++v) o[ct][d][v] = fmaf(x[v], k, o[ct][d][v]);
                 } else {
@@ -427,7 +484,8 @@ __global__ __launch_bounds__(256, NCT > 1 && sizeof(L) == 4 ? 1 : 2) void k_kv8_
             }
         }
 #pragma unroll
-        for (int ct = 0; ct < NCT; ++ct) l_run[ct] = fmaf(w[ct][0], back, l_run[ct]);
+        for (int ct = 0; ct < NCT; ++ct)    // (finite whatever the scale: a row that sees nothing of the tile adds 0 times it)
+            l_run[ct] = fmaf(w[ct][0], apart ? 1.f : __builtin_amdgcn_exp2f(fminf(-fold[ct], 100.f)), l_run[ct]);
     };
     if (ta < tb) {
         Scores st;
@@ -491,25 +549,25 @@ __global__ __launch_bounds__(256, NCT > 1 && sizeof(L) == 4 ? 1 : 2) void k_kv8_
             while (t < tb) one(std::false_type{});
         }
     }
-    constexpr float kDown = PAIR ? 0x1p-14f : 0x1p-8f;
-    // (both without their power of two)
+    // O over l, so that no sum of values passes the largest of them
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct) {
-        l_run[ct] *= kDown;
+        const float inv = l_run[ct] == 0.f ? 0.f : 1.f / l_run[ct];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) o[ct][t] *= U * kDown;
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) o[ct][t][v] = ldexpf(o[ct][t][v] * inv, (int)unit[ct]);
     }
-    // row rr of the group: to the output, or as a record for the others of its key ranges
+    // row rr of the group: to the output, or as a record (average, m, l) for the others of its key ranges
     auto finish = [&](int rr, int d, float a, float b, float c, float e, float m, float l) {
         const int at = rg.row0 + rr, i = at / p.qpg;
         if (i >= rg.n) return;
         if (n_split == 1) {
-            const float inv = l == 0.f ? 0.f : 1.f / l;
             L *to = (L *)p.out + (rg.first + i) * p.ld_out + (int64_t)(head * p.qpg + at - i * p.qpg) * D + d;
-            Piece<L>::put(to, a * inv);
-            Piece<L>::put(to + 1, b * inv);
-            Piece<L>::put(to + 2, c * inv);
-            Piece<L>::put(to + 3, e * inv);
+            Piece<L>::put(to, a);
+            Piece<L>::put(to + 1, b);
+            Piece<L>::put(to + 2, c);
+            Piece<L>::put(to + 3, e);
         } else {
             float *rec = p.part + ((((int64_t)f * p.n_kv + head) * p.S + split) * ROWS + rr) * (D + 2);
             *(float2 *)(rec + d) = make_float2(a, b);
@@ -537,17 +595,20 @@ __global__ __launch_bounds__(256, NCT > 1 && sizeof(L) == 4 ? 1 : 2) void k_kv8_
             __syncthreads();
             for (int e = threadIdx.x; e < 16 * D / 4; e += 256) {
                 const int rr = e / (D / 4), d = e % (D / 4) * 4;
-                float M = -INFINITY, l = 0.f, a[4] = {0.f, 0.f, 0.f, 0.f};
+                float M = -INFINITY, l = 0.f, k[4], a[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int w = 0; w < 4; ++w) M = fmaxf(M, red[w][rr][D]);
                 const float ref = M == -INFINITY ? 0.f : M;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
-                    const float k = __builtin_amdgcn_exp2f(red[w][rr][D] - ref);
-                    l += k * red[w][rr][D + 1];
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) a[v] += k * red[w][rr][d + v];
+                    k[w] = __builtin_amdgcn_exp2f(red[w][rr][D] - ref) * red[w][rr][D + 1];
+                    l += k[w];
                 }
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) a[v] += k[w] * inv * red[w][rr][d + v];
                 finish(16 * ct + rr, d, a[0], a[1], a[2], a[3], M, l);
             }
         }
@@ -588,9 +649,12 @@ template <typename L, int D, int NCT> __global__ __launch_bounds__(256) void k_k
             if (s0 > 0) ml = stat(rr, s0 + lane);
             const float mine = s0 + lane < n ? ml.x : -INFINITY;
             const float m = fmaxf(M, wave_max_dpp(mine)), ref = m == -INFINITY ? 0.f : m;
-            const float k = __builtin_amdgcn_exp2f(mine - ref), al = __builtin_amdgcn_exp2f(M - ref);
-            l = l * al + wave_sum_dpp(s0 + lane < n ? k * ml.y : 0.f);
-            a *= al;
+            float k = s0 + lane < n ? __builtin_amdgcn_exp2f(mine - ref) * ml.y : 0.f;
+            const float before = l * __builtin_amdgcn_exp2f(M - ref);
+            l = before + wave_sum_dpp(k);
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            a *= before * inv;          // (averages, weighed by their part of l)
+            k *= inv;
             M = m;
             const int cnt = min(n - s0, 64);
             for (int s = 0; s < cnt; s += U) {
@@ -602,11 +666,10 @@ template <typename L, int D, int NCT> __global__ __launch_bounds__(256) void k_k
                 }
             }
         }
-        const float inv = l == 0.f ? 0.f : 1.f / l;
         const int i = (rg.row0 + rr) / p.qpg, h = head * p.qpg + rg.row0 + rr - i * p.qpg;
         L *to = (L *)p.out + (rg.first + i) * p.ld_out + (int64_t)h * D + lane * E;
 #pragma unroll
-        for (int e = 0; e < E; ++e) Piece<L>::put(to + e, a[e] * inv);
+        for (int e = 0; e < E; ++e) Piece<L>::put(to + e, a[e]);
     }
 }
 

@@ -105,3 +105,111 @@ def test_append_holes_anywhere(tokens, n_kv, gaps):
     c = random_cache(rng, tokens, n_kv, block, D)
     k, v = _kv(rng, len(slots), n_kv, D, torch.bfloat16)
     assert_same_cache(_append_both(c, k, v, slots, torch.bfloat16), c)
+
+
+# ---- scales, queries and scores of any magnitude ------------------------------------------------------------------------
+
+def _rows_in_64_bits(q, c, table, pos, scale):
+    """One request's rows q [n, n_q, D] (float64) at positions pos: output, sum p |v|, the largest p s and |score|s' size."""
+    n, n_q, D = q.shape
+    G = n_q // c.n_kv
+    L = int(max(pos)) + 1
+    at = np.arange(L)
+    blk, off = table[at // c.block], at % c.block
+    sc = c.scales.astype(np.float64)
+    out, size, most, reach = (np.zeros((n, n_q, D)), np.zeros((n, n_q, D)), np.zeros((n, n_q)), np.zeros((n, n_q)))
+    for h in range(n_q):
+        k = (c.codes[0, blk, h // G, off].astype(np.float64) - 128) * sc[blk, h // G, 0][:, None]
+        v = (c.codes[1, blk, h // G, off].astype(np.float64) - 128) * sc[blk, h // G, 1][:, None]
+        s = q[:, h] @ k.T * scale
+        s = np.where(at[None, :] <= np.asarray(pos)[:, None], s, -np.inf)
+        p = np.exp(s - s.max(1, keepdims=True))
+        p /= p.sum(1, keepdims=True)
+        out[:, h], size[:, h] = p @ v, p @ np.abs(v)
+        most[:, h] = (p * sc[blk, h // G, 1]).max(1)
+        reach[:, h] = (np.abs(q[:, h]) @ np.abs(k).T).max(1) * abs(scale)
+    return out, size, most, reach
+
+
+def _close(got, ref, n, D, dtype):
+    """Errors of a token's weight count by what it carries: the relative ones (test_gpu_kv8's, and 2^-17 for the log of a
+    scale up to 2^126) with sum p |v|; fp16's smallest step, 2^-25 in units of 2^5 at least a token's largest weight times
+    scale, with 128 of these for each of n tokens (bf16; the lower halves of fp32 probabilities: 2^-25 of 2^14)."""
+    out, size, most, reach = ref
+    e, half = 2.0 ** -24, dtype is torch.bfloat16
+    rel = (2 * reach * (D + 8) * e + 16 * e + n / 8 * e + (2.0 ** -11 + 2.0 ** -17 if half else 0))[:, :, None]
+    tol = rel * size + (n * 2.0 ** (-30 if half else -39) * 128 * most)[:, :, None]
+    tol = tol * (1 + 2.0 ** -8) + np.abs(out) * (2.0 ** -8 if half else e) + 2.0 ** (-133 if half else -149)
+    assert np.isfinite(got).all()
+    assert (np.abs(got - out) <= tol).all(), (np.abs(got - out) / tol).max()
+
+
+# one token; several heads' tokens (two tiles of rows a wave); a prompt's rows, whose waves share the tiles
+SHAPES = {"one": (1, 4, 1), "rows": (6, 8, 2), "prompt": (600, 64, 8)}
+
+
+def _attend(q, c, table, dtype, scale=None):
+    """The GPU's rows and those of 64 bits: the request's last tokens, all of them or (of a prompt) some."""
+    rows, n_q, D = q.shape
+    total = int(table.shape[0]) * c.block
+    x = torch.tensor(q).to(dtype)
+    got = _api().kv8_attention(x.cuda(), to_gpu(c), _i32(table[None]), _i32([0, rows]), _i32([total]), scale=scale)
+    some = np.arange(rows) if rows < 40 else np.concatenate([np.arange(0, rows, 71), [rows - 1]])
+    ref = _rows_in_64_bits(x.double().numpy()[some], c, table, some + total - rows, D ** -0.5 if scale is None else scale)
+    return got.double().cpu().numpy()[some], ref
+
+
+CHAINS = {"falling": [1e15, 1e-4, 1e-18], "falling far": [1e30, 1e12, 1e-6], "to nothing": [1.0, 1e-18, 1e-36],
+          "from above": [1e17, 1.0, 1e-18], "rising": [1e-18, 1e-4, 1e15], "rising far": [1e-36, 1e-18, 1.0, 1e18, 1e30],
+          "both": [1.0, 1e-30, 1.0, 1e30, 1e-30, 1e10], "again and again": [1e12, 1e-6] * 6, "near": [1.0, 0.3, 0.01, 3.0, 40.0, 0.2],
+          "zeros": [0.0, 1e-3, 0.0, 1e9, 0.0], "subnormal": [1e-40, 1e-44, 1e-39], "subnormal beside": [1e-3, 1e-40, 1e-3],
+          "largest": [2.6e36, 1e-37, 2.6e36]}
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", sorted(SHAPES))
+@pytest.mark.parametrize("chain", sorted(CHAINS))
+def test_attention_value_scales_in_steps(dtype, shape, chain):
+    """A wave that takes blocks whose value scales rise and fall by many powers of two (the quarters of a range alike)."""
+    rows, n_q, n_kv = SHAPES[shape]
+    rng = np.random.default_rng(len(chain))
+    steps = CHAINS[chain] * 4
+    c = random_cache(rng, max(len(steps), 19), n_kv, 32, 64)
+    table = rng.permutation(c.blocks)
+    for i, b in enumerate(table):
+        c.scales[b, :, 1] = steps[i % len(steps)]
+    got, ref = _attend(rng.standard_normal((rows, n_q, 64)), c, table, dtype)
+    _close(got, ref, len(table) * 32, 64, dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tiles", [13, 140])
+def test_attention_value_scales_at_random(dtype, tiles):
+    for seed in range(6):
+        rng = np.random.default_rng([seed, tiles])
+        c = random_cache(rng, tiles, 2, 32, 128)
+        c.scales[:, :, 1] = (10.0 ** rng.uniform(-30, 30, c.scales[:, :, 1].shape)).astype(np.float32)
+        got, ref = _attend(rng.standard_normal((2, 8, 128)), c, rng.permutation(tiles), dtype)
+        _close(got, ref, tiles * 32, 128, dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", sorted(SHAPES))
+@pytest.mark.parametrize("order", [[0, 1], [1, 0], [0, 1, 0], [0, 1, 2, 1, 0], [2, 0, 1], [0, 0, 2, 1, 1], [1, 2, 0]])
+def test_attention_large_values_that_weigh_nothing(dtype, shape, order):
+    """Blocks of huge values whose scores leave them no weight (e^-400), beside ones of small values: the output is
+    the small ones', to its own precision.  (0: huge, 1: small, 2: huge too, by another 2^60.)"""
+    rows, n_q, n_kv = SHAPES[shape]
+    rng = np.random.default_rng(5)
+    order = order * 4
+    c = random_cache(rng, max(len(order), 20), n_kv, 32, 64)
+    table = rng.permutation(c.blocks)
+    for i, b in enumerate(table):
+        kind = order[i % len(order)]
+        c.scales[b, :, 1] = [1e18, 1e-5, 1e-18][kind] if kind != 2 else 1e36
+        if kind != 1:
+            c.codes[0, b] = 28
+        c.scales[b, :, 0] = 0.5 if kind != 1 else 0.01
+    got, ref = _attend(np.full((rows, n_q, 64), 1.0) + 0.1 * rng.standard_normal((rows, n_q, 64)), c, table, dtype)
+    assert ref[1][-1].max() < 1e-2          # (a prompt's first rows may see huge ones only)
+    _close(got, ref, len(table) * 32, 64, dtype)
