@@ -38,7 +38,7 @@ struct Kv8Attn {
     int S, chunk;                   // key ranges of `chunk` tiles
     int groups;                     // row groups of all requests, counted from above
     int few;                        // 0, or: requests of up to so many rows are the other launch's; that one has a group a request
-    float scale;                    // of the scores, times log2(e)
+    float scale; int scale_e;       // of the scores, times log2(e): scale 2^scale_e
     float *part;                    // [groups][n_kv][S][16 NCT][D + 2]
 };
 
@@ -238,7 +238,10 @@ __global__ __launch_bounds__(256, SPLIT && NCT == 2 && D == 64 && sizeof(L) == 2
     if (ta < tb) load_ids(ta >> sh);
     // this lane's query rows
     u32x4 qh[NCT][NC][2], ql[NCT][NC][2];
-    float fq[NCT], cq[NCT];         // a product's score is product * fq + cq, both times the tile's scale
+    // A product's score is (product + cq) times the tile's scale, |p.scale| and 2^eq: powers of two are kept apart, so that
+    // no part of it passes what a float holds where the score does not.
+    int eq[NCT];
+    float cq[NCT];
     int seen[NCT];                  // tokens it sees
     const float sign = p.scale < 0.f ? -1.f : 1.f;
 #pragma unroll
@@ -264,7 +267,7 @@ __global__ __launch_bounds__(256, SPLIT && NCT == 2 && D == 64 && sizeof(L) == 2
         top = col_max(top);
         // the power of two that brings the largest to [2^14, 2^15)
         const int ex = top > 0.f && top < INFINITY ? 14 - ilogbf(top) : 0;
-        fq[ct] = ldexpf(fabsf(p.scale), -ex);
+        eq[ct] = p.scale_e - ex;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
 #pragma unroll
@@ -281,8 +284,8 @@ __global__ __launch_bounds__(256, SPLIT && NCT == 2 && D == 64 && sizeof(L) == 2
                 for (int e = 0; e < 2; ++e)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) sum += f16_lo(qh[ct][c][e][k]) + f16_hi(qh[ct][c][e][k]);
-            cq[ct] = -128.f * col_sum(sum) * fq[ct];
-            fq[ct] *= 0x1p24f;
+            cq[ct] = -0x1p-17f * col_sum(sum);
+            eq[ct] += 24;
         }
         __builtin_amdgcn_sched_barrier(0);      // (one after the other, or their floats do not fit)
     }
@@ -393,8 +396,8 @@ __global__ __launch_bounds__(256, SPLIT && NCT == 2 && D == 64 && sizeof(L) == 2
         bool rise = false;
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct) {
-            fk[ct] = fq[ct] * b.sk;
-            ck[ct] = cq[ct] * b.sk;
+            fk[ct] = ldexpf(b.sk, eq[ct]) * fabsf(p.scale);
+            ck[ct] = cq[ct] * fk[ct];
 #pragma unroll
             for (int k = 0; k < 8; ++k) s[ct][k] = st[ct][k >> 2][k & 3];
         }
@@ -753,9 +756,11 @@ static int attention(const pipo_kv8 *c, int32_t R, int32_t rows, int32_t n_q, co
     if (!same_or_apart(q, ld_q, out, ld_out, rows, least, sizeof(L))) return PIPO_EINVAL;
     const Kv8Shape s = shape_of(R, rows, n_q, c->n_kv, c->head_dim, max_len, work != nullptr);
     if (work && s.part > 0 && (!kv8_aligned(work, 16) || work_bytes < s.part)) return PIPO_EINVAL;
+    int scale_e;
+    const float scale_m = (float)frexp(scale * 1.4426950408889634074, &scale_e);
     Kv8Attn p{c->keys, c->values, c->scales, tables, starts, total, q, out, ld_q, ld_out, R, rows, width, c->blocks,
               c->n_kv, n_q / c->n_kv, __builtin_ctz((unsigned)c->block), max_len, s.S, s.chunk, s.groups, 0,
-              (float)(scale * 1.4426950408889634074), (float *)work};
+              scale_m, scale_e, (float *)work};
     hipStream_t st = (hipStream_t)stream;
     return (c->head_dim == 128 ? run_attn<L, 128>(p, s, st) : run_attn<L, 64>(p, s, st)) ? PIPO_OK : PIPO_EHIP;
 }

@@ -213,3 +213,23 @@ def test_attention_large_values_that_weigh_nothing(dtype, shape, order):
     got, ref = _attend(np.full((rows, n_q, 64), 1.0) + 0.1 * rng.standard_normal((rows, n_q, 64)), c, table, dtype)
     assert ref[1][-1].max() < 1e-2          # (a prompt's first rows may see huge ones only)
     _close(got, ref, len(table) * 32, 64, dtype)
+
+
+def _key_case(rng, n_kv, D, key_scale, blocks=20):
+    c = random_cache(rng, blocks, n_kv, 32, D)
+    c.scales[:, :, 0] = key_scale * (0.5 + rng.random((blocks, n_kv))).astype(np.float32)
+    return c, rng.permutation(blocks)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", sorted(SHAPES))
+@pytest.mark.parametrize("q_size,key_scale,scale", [(3e37, 1e-39, None), (1e37, 2e-37, 0.01), (2e35, 1e-36, None), (1e-38, 1e36, None),
+                                                    (1e-40, 1e36, 30.0), (1.0, 0.02, 1e-38), (1e-3, 1e-30, 1e33), (1e33, 1e3, 1e-36),
+                                                    (1e30, 1e-35, 3e5)])
+def test_attention_queries_and_keys_of_any_size(dtype, shape, q_size, key_scale, scale):
+    """Queries, key scales and the scale of the scores far from 1, whose product is not: no step between passes 32 bits."""
+    rows, n_q, n_kv = SHAPES[shape]
+    rng = np.random.default_rng(7)
+    c, table = _key_case(rng, n_kv, 64, key_scale)
+    got, ref = _attend(q_size * np.clip(rng.standard_normal((rows, n_q, 64)), -3, 3), c, table, dtype, scale)
+    _close(got, ref, len(table) * 32, 64, dtype)
