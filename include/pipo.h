@@ -381,7 +381,8 @@ int pipo_opd_policy_bf16(int32_t T, int32_t V, const uint16_t *d_logits, int64_t
  * keys up to its own position d_total[r] - d_starts[r+1] + i, query head h those
  * of KV head h * n_kv / n_q.  d_out row i = sum softmax(scale q.k) v, rounded once
  * to the type of q; zeros for a row that sees no key; rows outside
- * [d_starts[0], d_starts[R]) are not written.  (rows n_q / n_kv / 16 + R) n_kv < 2^24.
+ * [d_starts[0], d_starts[R]) are not written.  Scales, queries and scores may be of any size; a
+ * row with a score that no float holds is NaN.  (rows n_q / n_kv / 16 + R) n_kv < 2^24.
  * d_out may be d_q itself (same address and stride), and must not overlap it
  * otherwise.  No request may have more than max_len tokens (up to width * block;
  * what is behind max_len is not seen).  d_work as for the OPD losses

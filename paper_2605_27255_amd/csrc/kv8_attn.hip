@@ -13,7 +13,7 @@
 // them: bf16 queries are then fp16 numbers (parts below 2^-38 of the row's largest are
 // lost), and probabilities lose 2^-12 of themselves, an eighth of what the output's rounding
 // to bf16 costs.  fp32 queries, and their probabilities, go in as hi + lo fp16
-// pairs (2^-22), two MFMAs each.
+// pairs (2^-22), two MFMAs each.  Scores are sums in fp32; scores that no float holds make a row NaN.
 // Few rows: HBM-bound, a key range a workgroup, its waves a quarter each, whose (m, l, o)
 // meet in LDS and, of several ranges, in a second launch.  32 requests x 8192 tokens, 32/8
 // heads of 128: 83-86 us for 537 MB, 6.3 TB/s, and 4 us for the second launch; 8 x 16384 x 3
@@ -135,6 +135,8 @@ template <int ROWS> __device__ __forceinline__ int tiles_of(const Kv8Attn &p, co
 // The four waves of a workgroup share a row group and cut its key range into four
 // (SPLIT), or take a quarter of a group of four times the rows each, and share the tiles: each
 // wave makes a quarter of a tile's bytes to operands, which all of them read from LDS.
+// (Heads of 64 with two tiles of bf16 rows are held to four waves a SIMD, which costs 12 bytes of scratch: 32 requests x
+// 8192 tokens x 20 rows 65 us, with three waves 69.)
 template <typename L, int D, int NCT, bool SPLIT>
 __global__ __launch_bounds__(256, SPLIT && NCT == 2 && D == 64 && sizeof(L) == 2 ? 4 : 2) void k_kv8_attn(Kv8Attn p) {
     constexpr bool PAIR = sizeof(L) == 4, DEEP = NCT == 1;
@@ -241,7 +243,7 @@ __global__ __launch_bounds__(256, SPLIT && NCT == 2 && D == 64 && sizeof(L) == 2
     // A product's score is (product + cq) times the tile's scale, |p.scale| and 2^eq: powers of two are kept apart, so that
     // no part of it passes what a float holds where the score does not.
     int eq[NCT];
-    float cq[NCT];
+    float cq[NCT], far_sk = INFINITY;       // (the key scale above which a score may pass 2^22)
     int seen[NCT];                  // tokens it sees
     const float sign = p.scale < 0.f ? -1.f : 1.f;
 #pragma unroll
@@ -265,8 +267,8 @@ __global__ __launch_bounds__(256, SPLIT && NCT == 2 && D == 64 && sizeof(L) == 2
                 }
             }
         top = col_max(top);
-        // the power of two that brings the largest to [2^14, 2^15)
-        const int ex = top > 0.f && top < INFINITY ? 14 - ilogbf(top) : 0;
+        // the power of two that brings the largest to [2^14, 2^15) (of none: one with which no score is far)
+        const int ex = top > 0.f && top < INFINITY ? 14 - ilogbf(top) : 100;
         eq[ct] = p.scale_e - ex;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
@@ -287,8 +289,11 @@ __global__ __launch_bounds__(256, SPLIT && NCT == 2 && D == 64 && sizeof(L) == 2
             cq[ct] = -0x1p-17f * col_sum(sum);
             eq[ct] += 24;
         }
+        // (products and cq reach 2^22 D, and with keys as u 2^-24 D)
+        far_sk = fminf(far_sk, ldexpf((PAIR ? 1.f : 0x1p22f) / (D * fabsf(p.scale)), -eq[ct]));
         __builtin_amdgcn_sched_barrier(0);      // (one after the other, or their floats do not fit)
     }
+    far_sk = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(-wave_max_dpp(-far_sk))));
     int all_see = 0x7FFFFFFF;       // tokens that every row sees
 #pragma unroll
     for (int ct = 0; ct < NCT; ++ct) all_see = min(all_see, seen[ct]);
@@ -299,7 +304,8 @@ __global__ __launch_bounds__(256, SPLIT && NCT == 2 && D == 64 && sizeof(L) == 2
     // A row's O is in units of 2^unit; probabilities as 2^8 exp2(s - m), where m, a row's reference, follows its
     // maximum only when that is more than 6 above it: O is seldom rescaled, and 2^15 at most goes into fp16.  Pairs
     // take 2^14 and the maximum itself: the lower half of a small probability has fp16's smallest step (errors of the
-    // whole, 8 x 16384 tokens: 3.9e-6 with 2^8, 5e-7).
+    // whole, 8 x 16384 tokens: 3.9e-6 with 2^8, 5e-7).  So what is small beside the row's largest loses up to 2^-33 of
+    // that (pairs: 2^-39).
     constexpr float kUp = PAIR ? 14.f : 8.f, kSlack = PAIR ? 0.f : 6.f;
     f32x4 o[NCT][NT];
     float m_run[NCT], l_run[NCT], unit[NCT];
@@ -432,6 +438,8 @@ __global__ __launch_bounds__(256, SPLIT && NCT == 2 && D == 64 && sizeof(L) == 2
         float fold[NCT], kv[NCT];
         bool odd = false, apart = false;
 #pragma unroll
+        for (int ct = 0; ct < NCT; ++ct) ck[ct] -= m_run[ct] == -INFINITY ? -kUp : m_run[ct] - kUp;
+#pragma unroll
         for (int ct = 0; ct < NCT; ++ct) {
             if (PAIR) {
                 fold[ct] = 0.f;
@@ -442,18 +450,32 @@ __global__ __launch_bounds__(256, SPLIT && NCT == 2 && D == 64 && sizeof(L) == 2
                 odd |= fabsf(fold[ct] + 1.f) > 2.f;
             }
         }
-        if (__builtin_amdgcn_ballot_w64(odd)) apart = settle(b, mx, fold, kv);
+        if (__builtin_amdgcn_ballot_w64(odd || b.sk > far_sk)) {
+            apart = settle(b, mx, fold, kv);
+            // A score's exponent is one fma from the products on, s fk + (ck - m): exact where it counts, as long as the
+            // roundings of ck and m are small.  Where scores may pass 2^22 they are rounded by themselves, as m was, so
+            // that the largest is m and no exponent comes out far above it.
+            if (b.sk > far_sk) {
+#pragma unroll
+                for (int ct = 0; ct < NCT; ++ct) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) s[ct][k] = fmaf(s[ct][k], fk[ct], cq[ct] * fk[ct]) - (m_run[ct] == -INFINITY ? 0.f : m_run[ct]);
+                    fk[ct] = 1.f;
+                    ck[ct] = kUp;
+                }
+            }
+        }
         u32x4 ph[NCT], pl[NCT];
         f32x4 w[NCT];
 #pragma unroll
         for (int ct = 0; ct < NCT; ++ct) {
-            const float c0 = ck[ct] - (m_run[ct] == -INFINITY ? -kUp : m_run[ct] - kUp), c = c0 + fold[ct];
+            const float c = ck[ct] + fold[ct];
             const u32x4 ones{0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u};
             if (apart) {                // l from probabilities without the scale
                 float e[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    e[k] = __builtin_amdgcn_exp2f(fmaf(s[ct][k], fk[ct], c0));
+                    e[k] = __builtin_amdgcn_exp2f(fmaf(s[ct][k], fk[ct], ck[ct]));
                     if (!whole && hidden(ct, k)) e[k] = 0.f;
                 }
                 fp16_8<false>(e, ph[ct], pl[ct]);

@@ -233,3 +233,41 @@ def test_attention_queries_and_keys_of_any_size(dtype, shape, q_size, key_scale,
     c, table = _key_case(rng, n_kv, 64, key_scale)
     got, ref = _attend(q_size * np.clip(rng.standard_normal((rows, n_q, 64)), -3, 3), c, table, dtype, scale)
     _close(got, ref, len(table) * 32, 64, dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", sorted(SHAPES))
+@pytest.mark.parametrize("size", [1e6, 1e8, 1e9, 1e12, 1e20, 1e30])
+def test_attention_scores_far_above_a_float_s_unit(dtype, shape, size):
+    """Scores whose neighbours among floats are more than 1 apart: a token that is ahead by more than that takes all."""
+    rows, n_q, n_kv = SHAPES[shape]
+    rng = np.random.default_rng(9)
+    c, table = _key_case(rng, n_kv, 64, 0.02)
+    q = size * (1.0 + 0.1 * rng.standard_normal((rows, n_q, 64)))
+    c.codes[0] = np.clip(c.codes[0], 100, 156)
+    c.codes[0, table[0], :, 5] = 200            # its score is twice the others' in every row, and some are below 0
+    got, ref = _attend(q, c, table, dtype)
+    out, spread, most, _ = ref
+    want = (c.codes[1, table[0], :, 5].astype(np.float64) - 128) * c.scales[table[0], :, 1][:, None]
+    want = np.repeat(want, n_q // n_kv, 0)[None]
+    np.testing.assert_allclose(out, np.broadcast_to(want, out.shape), rtol=1e-12)
+    _close(got, (out, spread, most, np.zeros_like(most)), len(table) * 32, 64, dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_attention_codes_near_zero_beside_large_scales(dtype):
+    """A block whose scale goes by one large key that the query does not see (its dimension is 0 there): the others'
+    scores are 0, whatever cancels in them, and their average comes out to the roundings of 128 |q| scale."""
+    rng = np.random.default_rng(10)
+    for size in (1.0, 1e5, 1e9):
+        c, table = _key_case(rng, 1, 64, 0.02 * size)
+        c.codes[0] = 128
+        c.codes[0, :, :, 3, 0] = 255
+        q = rng.standard_normal((2, 4, 64))
+        q[:, :, 0] = 0.0
+        got, ref = _attend(q, c, table, dtype)
+        assert np.isfinite(got).all()
+        e = 2.0 ** -24 * 66 * 2 * 128 * 0.03 * size * np.abs(q).sum(2) / 8 if dtype is torch.bfloat16 else np.zeros((2, 4))
+        out, spread, most, _ = ref
+        tol = np.minimum(2 * np.expm1(np.minimum(e, 30.0)) + 2.0 ** -10, 2.0)[:, :, None] * np.maximum(spread, 4 * most[:, :, None] * 128)
+        assert (np.abs(got - out) <= tol).all()
