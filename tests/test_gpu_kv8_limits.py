@@ -271,3 +271,17 @@ def test_attention_codes_near_zero_beside_large_scales(dtype):
         out, spread, most, _ = ref
         tol = np.minimum(2 * np.expm1(np.minimum(e, 30.0)) + 2.0 ** -10, 2.0)[:, :, None] * np.maximum(spread, 4 * most[:, :, None] * 128)
         assert (np.abs(got - out) <= tol).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("total,new,n_q,n_kv", [([3000, 700, 45], [3, 1, 2], 8, 2), ([500, 400], [9, 3], 16, 2), ([900, 2300], [600, 1], 64, 8)])
+def test_attention_same_bits_of_every_form(dtype, total, new, n_q, n_kv):
+    """Key ranges and their join, several tiles of rows, prompts beside a request of few rows; scales that move units."""
+    rng = np.random.default_rng(17)
+    c, tables = _paged(rng, total, n_kv, 64, 128)
+    c.scales[::3, :, 1] *= 100.0
+    q = torch.tensor(rng.standard_normal((sum(new), n_q, 128))).to(dtype).cuda()
+    args = to_gpu(c), _i32(tables), _i32(np.concatenate([[0], np.cumsum(new)])), _i32(total)
+    first = _api().kv8_attention(q, *args)
+    for _ in range(5):
+        assert torch.equal(_api().kv8_attention(q, *args), first)
