@@ -382,17 +382,19 @@ int pipo_opd_policy_bf16(int32_t T, int32_t V, const uint16_t *d_logits, int64_t
  * of KV head h * n_kv / n_q.  d_out row i = sum softmax(scale q.k) v, rounded once
  * to the type of q; zeros for a row that sees no key; rows outside
  * [d_starts[0], d_starts[R]) are not written.  Scales, queries and scores may be of any size; a
- * row with a score that no float holds is NaN.  (rows n_q / n_kv / 16 + R) n_kv < 2^24.
+ * score above what a float holds makes its row NaN.  (rows n_q / n_kv / 16 + R) n_kv < 2^24.
  * d_out may be d_q itself (same address and stride), and must not overlap it
  * otherwise.  No request may have more than max_len tokens (up to width * block;
  * what is behind max_len is not seen).  d_work as for the OPD losses
- * (pipo_kv8_attention_work_bytes); with NULL each row's keys are not split over
- * workgroups, which is slower for few long requests.
+ * (pipo_kv8_attention_work_bytes; its bf16 argument is kept for later, the size
+ * does not go by it); with NULL each row's keys are not split over workgroups,
+ * which is slower for few long requests.
  *
  * pipo_verify_drafts: request r (of R) has up to K drafted tokens d_drafts[r] ([R][K],
  * the first negative one ends them) and the target's logits of the positions that
  * they and the token behind them stand at: rows d_starts[r] .. d_starts[r+1]-1
- * of the `rows` of d_logits (NULL: r (K+1) .. r (K+1) + K), fp32 or bf16, row
+ * (a request's first ones are taken, so one that feeds a prompt's end needs starts
+ * of its own) of the `rows` of d_logits (NULL: r (K+1) .. r (K+1) + K), fp32 or bf16, row
  * stride ld.  d_draft_logits: the logits that draft i was drawn from, at (r ld_request + i ld_draft)
  * elements; NULL: drafts were not drawn (probability 1).  With p, q =
  * softmax(logits / temperature) and random numbers d_u [R][K+1] in [0, 1):

@@ -11,17 +11,20 @@
 // O).  Queries are brought to magnitudes below 2^15 by a power of two for each row, and
 // probabilities are kept as a power of two times themselves, so that fp16's exponents hold
 // them: bf16 queries are then fp16 numbers (parts below 2^-38 of the row's largest are
-// lost), and probabilities lose 2^-12 of themselves, an eighth of what the output's rounding
+// lost), and probabilities lose up to 2^-11 of themselves, an eighth of what the output's rounding
 // to bf16 costs.  fp32 queries, and their probabilities, go in as hi + lo fp16
-// pairs (2^-22), two MFMAs each.  Scores are sums in fp32; scores that no float holds make a row NaN.
+// pairs (2^-22), two MFMAs each.  Scores are sums in fp32 (of bf16 queries of 128 |q| and less beside
+// the keys' part: 2^-24 of 128 sum |q| s, whatever the keys); one above what a float holds makes its row NaN.
 // Few rows: HBM-bound, a key range a workgroup, its waves a quarter each, whose (m, l, o)
 // meet in LDS and, of several ranges, in a second launch.  32 requests x 8192 tokens, 32/8
-// heads of 128: 83-86 us for 537 MB, 6.3 TB/s, and 4 us for the second launch; 8 x 16384 x 3
-// queries in fp32 49 us, 5.4 TB/s (a third of it the two prologues' and the last
-// workgroups' time).  Many rows (a prompt): bound by the waves' instructions, exponentials
-// and conversions (about 720 cycles a tile of 32 rows) beside the matrix cores'
-// (544), two waves a SIMD: 2048 queries on 6144 tokens 274 us, 880 TFLOP/s; each
-// wave converting its own tiles 281, 64 rows a wave 525, a rescaled O every tile 1169.
+// heads of 128: 83-86 us for 537 MB, 6.3 TB/s, and 5 us for the second launch; 8 x 16384 x 3
+// queries in fp32 50 us, 5.4 TB/s (a third of it the two prologues' and the last
+// workgroups' time).  Many rows (a prompt): a wave's products (545 cycles of the matrix cores a
+// tile of 32 rows) and its exponentials and conversions (660 cycles of vector instructions) follow
+// one another, and the two waves of a SIMD hide little of each other's: about 1390 cycles a tile, by
+// the counters.  2048 queries on 6144 tokens 276 us, 868 TFLOP/s (with one unit for all rows of a wave,
+// which some value scales made overflow, 270).  When that took 272: each wave converting its own tiles
+// 281, 64 rows a wave 525, a rescaled O every tile 1169.
 #include "kv8.h"
 #include <math.h>
 #include <type_traits>
@@ -726,7 +729,8 @@ static Kv8Shape shape_of(int R, int rows, int n_q, int n_kv, int D, int max_len,
     int64_t units = (int64_t)R * ((per + tile_rows - 1) / tile_rows) * n_kv;
     // Tiles are shared by waves of different rows where there are rows for two waves at least and units for every SIMD.
     // A batch may still hold requests of a few rows and many tokens (decoding ones beside prompts), whose tokens one
-    // workgroup would take one after the other: they get key ranges, in a launch of their own.
+    // workgroup would take one after the other: they get key ranges, in a launch of their own.  Few are as many rows as
+    // a unit of that launch holds (a number that comes from the kernel; requests of more rows have not been timed there).
     s.split = per < 64 || units < 1024;
     s.second = !s.split && R > 1;
     s.groups = (int)((int64_t)rows * qpg / (s.split ? tile_rows : 4 * tile_rows)) + R;

@@ -213,7 +213,7 @@ __device__ __forceinline__ int round_again(int u, double old, double s, double i
 // or values: their largest magnitude, the scale, and the tiles with new bytes.  An item
 // is 16 dimensions of a token.  Rows that follow one another as their slots do, as a
 // rule, are found by their number; others by a table of tokens (of rows with one slot the
-// last).  Bound by latency at a step's single tokens (32 in 6.4 us: slots, rows and scale,
+// last), and so are runs with rows among them that have no slot.  Bound by latency at a step's single tokens (32 in 6.8 us: slots, rows and scale,
 // the old tile, one after the other), at a prompt's by how many workgroups a compute unit
 // holds (8192 tokens of 8 heads x 128: 22 us, 2.3 TB/s in and out).
 template <typename L, int NT> __global__ __launch_bounds__(NT, 4) void k_kv8_append(AppendParams<L> p) {

@@ -660,8 +660,9 @@ def kv8_attention(q, cache, tables, starts, total, scale=None, max_len=None, out
     sees the tokens up to its own.  scale: of the scores (None: 1 /
     sqrt(head_dim)); max_len: no request has more tokens (None: the tables'
     width), fewer make better use of the GPU; out: where to write (q itself, or
-    apart from it; None: a new tensor; rows that belong to no request are not
-    written).  Returns out (autograd does not follow it)."""
+    apart from it; None: a new tensor).  Rows that belong to no request are not
+    written: in a new tensor they hold anything.  Returns out (autograd does not
+    follow it)."""
     import torch
     dev = _cache(cache)
     if _elsewhere(cache.keys):
@@ -703,7 +704,9 @@ def verify_drafts(logits, drafts, u, draft_logits=None, starts=None, temperature
     """Accepts drafted tokens, and draws the one behind them, so that every token is
     distributed as the target alone would draw it.  logits: the target's, fp32 or bf16 CUDA
     [rows, V], any row stride: request r's positions are rows starts[r] ..
-    starts[r + 1] - 1 (int32 [R + 1]; None: K + 1 rows each); drafts: int32 [R,
+    starts[r + 1] - 1 (int32 [R + 1]; None: K + 1 rows each), of which the first are
+    taken: after a step that also feeds prompts, their last rows need starts of
+    their own; drafts: int32 [R,
     K], a negative one ends a request's; u: float32 [R, K + 1] random numbers in
     [0, 1), the last for the token behind; draft_logits: [R, K, V] of the logits'
     type, what the drafts were drawn from (None: they were not drawn); temperature:
