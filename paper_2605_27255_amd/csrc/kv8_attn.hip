@@ -20,11 +20,11 @@
 // heads of 128: 83-86 us for 537 MB, 6.3 TB/s, and 5 us for the second launch; 8 x 16384 x 3
 // queries in fp32 50 us, 5.4 TB/s (a third of it the two prologues' and the last
 // workgroups' time).  Many rows (a prompt): a wave's products (545 cycles of the matrix cores a
-// tile of 32 rows) and its exponentials and conversions (660 cycles of vector instructions) follow
-// one another, and the two waves of a SIMD hide little of each other's: about 1390 cycles a tile, by
-// the counters.  2048 queries on 6144 tokens 276 us, 868 TFLOP/s (with one unit for all rows of a wave,
-// which some value scales made overflow, 270).  When that took 272: each wave converting its own tiles
-// 281, 64 rows a wave 525, a rescaled O every tile 1169.
+// tile of 32 rows) and its exponentials and conversions (650 cycles of vector instructions) follow
+// one another, and the two waves of a SIMD hide little of each other's: about 1360 cycles a tile, by
+// the counters.  2048 queries on 6144 tokens 272 us, 884 TFLOP/s; each wave converting its own tiles 281,
+// 64 rows a wave 525, a rescaled O every tile 1169.  Where value scales differ from block to block
+// by factors of 4 (the middle half of them) rows' units move more often: 294.
 #include "kv8.h"
 #include <math.h>
 #include <type_traits>
@@ -138,8 +138,8 @@ template <int ROWS> __device__ __forceinline__ int tiles_of(const Kv8Attn &p, co
 // The four waves of a workgroup share a row group and cut its key range into four
 // (SPLIT), or take a quarter of a group of four times the rows each, and share the tiles: each
 // wave makes a quarter of a tile's bytes to operands, which all of them read from LDS.
-// (Heads of 64 with two tiles of bf16 rows are held to four waves a SIMD, which costs 12 bytes of scratch: 32 requests x
-// 8192 tokens x 20 rows 65 us, with three waves 69.)
+// (Heads of 64 with two tiles of bf16 rows are held to four waves a SIMD, which costs 12 bytes of scratch where units
+// move: 32 requests x 8192 tokens x 20 rows 62 us, with three waves 69.)
 template <typename L, int D, int NCT, bool SPLIT>
 __global__ __launch_bounds__(256, SPLIT && NCT == 2 && D == 64 && sizeof(L) == 2 ? 4 : 2) void k_kv8_attn(Kv8Attn p) {
     constexpr bool PAIR = sizeof(L) == 4, DEEP = NCT == 1;
@@ -305,11 +305,11 @@ __global__ __launch_bounds__(256, SPLIT && NCT == 2 && D == 64 && sizeof(L) == 2
     all_see = __builtin_amdgcn_readfirstlane(all_see);
 
     // A row's O is in units of 2^unit; probabilities as 2^8 exp2(s - m), where m, a row's reference, follows its
-    // maximum only when that is more than 6 above it: O is seldom rescaled, and 2^15 at most goes into fp16.  Pairs
+    // maximum only when that is more than 4 above it: O is seldom rescaled, and 2^15 at most goes into fp16.  Pairs
     // take 2^14 and the maximum itself: the lower half of a small probability has fp16's smallest step (errors of the
     // whole, 8 x 16384 tokens: 3.9e-6 with 2^8, 5e-7).  So what is small beside the row's largest loses up to 2^-33 of
     // that (pairs: 2^-39).
-    constexpr float kUp = PAIR ? 14.f : 8.f, kSlack = PAIR ? 0.f : 6.f;
+    constexpr float kUp = PAIR ? 14.f : 8.f, kSlack = PAIR ? 0.f : 4.f, kMost = PAIR ? 1.f : 3.f;
     f32x4 o[NCT][NT];
     float m_run[NCT], l_run[NCT], unit[NCT];
     float unit0 = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(sc.y)));     // the first block's value scale, or any
@@ -371,10 +371,10 @@ __global__ __launch_bounds__(256, SPLIT && NCT == 2 && D == 64 && sizeof(L) == 2
             const float held = top > 0.f ? (float)ilogbf(top) : -1000.f;
             float to = unit[ct];
             if (r > -INFINITY) {        // (a row that sees nothing of it stays as it is, and so with a NaN)
-                if (r + d > (PAIR ? 4.f : 7.f)) to = fmaxf(to, floorf(ls + fminf(r, 0.f)) + 1.f);
-                else if (d > 1.f && held - d >= 8.f) to = floorf(ls) + 1.f;
+                if (r + d > (PAIR ? 4.f : 7.f)) to = fmaxf(to, ceilf(ls + fminf(r, 0.f) - kMost));
+                else if (d > kMost && held - d >= 8.f) to = ceilf(ls - kMost);
                 else if (least < (PAIR ? -60.f : -3.f) && ls > -INFINITY)
-                    to = fminf(to, fmaxf(floorf(PAIR ? ls + r : ls) + 1.f, to + held - 80.f));
+                    to = fminf(to, fmaxf(floorf(PAIR ? ls + r : ls + 3.f), to + held - 80.f));
             }
             const int up = (int)(unit[ct] - to);
 #pragma unroll
@@ -450,10 +450,11 @@ __global__ __launch_bounds__(256, SPLIT && NCT == 2 && D == 64 && sizeof(L) == 2
                 odd |= kv[ct] < 0x1p-60f || kv[ct] > 0x1p8f;
             } else {
                 fold[ct] = b.sv - unit[ct];
-                odd |= fabsf(fold[ct] + 1.f) > 2.f;
+                odd |= fabsf(fold[ct]) > 3.f;
             }
         }
-        if (__builtin_amdgcn_ballot_w64(odd || b.sk > far_sk)) {
+        // (said to be rare, so that its registers are not kept from the others': 2048 queries on 6144 tokens 272 us, else 280)
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd || b.sk > far_sk) != 0, 0)) {
             apart = settle(b, mx, fold, kv);
             // A score's exponent is one fma from the products on, s fk + (ck - m): exact where it counts, as long as the
             // roundings of ck and m are small.  Where scores may pass 2^22 they are rounded by themselves, as m was, so
@@ -474,7 +475,7 @@ __global__ __launch_bounds__(256, SPLIT && NCT == 2 && D == 64 && sizeof(L) == 2
         for (int ct = 0; ct < NCT; ++ct) {
             const float c = ck[ct] + fold[ct];
             const u32x4 ones{0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u};
-            if (apart) {                // l from probabilities without the scale
+            if (__builtin_expect(apart, 0)) {       // l from probabilities without the scale
                 float e[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
