@@ -23,8 +23,8 @@
 // tile of 32 rows) and its exponentials and conversions (650 cycles of vector instructions) follow
 // one another, and the two waves of a SIMD hide little of each other's: about 1360 cycles a tile, by
 // the counters.  2048 queries on 6144 tokens 272 us, 884 TFLOP/s; each wave converting its own tiles 281,
-// 64 rows a wave 525, a rescaled O every tile 1169.  Where value scales differ from block to block
-// by factors of 4 (the middle half of them) rows' units move more often: 294.
+// 64 rows a wave 525, a rescaled O every tile 1169.  Where value scales differ widely from block to
+// block rows' units move more often (factors of exp(1.5 N(0, 1)): 294 us).
 #include "kv8.h"
 #include <math.h>
 #include <type_traits>
